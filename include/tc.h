@@ -381,6 +381,52 @@ int32_t tc_broadcast_tensor(const tc_group* g, int32_t K, const void* src, void*
 int32_t easgd_pipeline_tensor(const tc_tensorlist* grads, const tc_tensorlist* params, void* g_tensor,
                               float* gbar, float* x, float* x_c, float eta, float rho, void* stream);
 
+/* ------------------------------------------------------------------------
+ * tc_layernorm: layer norm of K workers' rows, each worker with its own scale
+ * and shift (what makes the gradients of a group's vector tensors).  Worker k
+ * has rows[k] >= 0 rows of cols elements of dtype; with mu and var the mean
+ * and the variance of a row (the mean of (x - mu)^2), per row
+ *     rstd = 1 / sqrt(var + eps),   y = (x - mu) * rstd * weight + bias.
+ *
+ * rows: host array of K counts.  x, y: host arrays of K device pointers; a row
+ * starts every x_ld (y_ld) elements, at least cols, at any alignment of dtype.
+ * weight, bias: K device pointers to cols binary32 values, at any alignment of
+ * 4 bytes (pieces of a flat parameter buffer), which workers may share; NULL:
+ * ones, zeros.  mean, rstd: K device pointers to rows[k] binary32 values that
+ * receive mu and rstd for the backward pass; NULL: not written.  Statistics
+ * are summed in binary32, from the differences to mu; y is rounded once.  y[k]
+ * may be x[k] itself (with the same stride), and shares nothing else with any
+ * x or y; views of one wider buffer may interleave.  A worker without rows
+ * needs no pointers.  cols in [1, TC_MAX_NORM_COLS], eps >= 0.
+ * ---------------------------------------------------------------------- */
+#define TC_MAX_NORM_COLS (1 << 24)
+
+int32_t tc_layernorm(int32_t K, const int64_t* rows, int64_t cols, const void* const* x, int64_t x_ld,
+                     int32_t dtype, const float* const* weight, const float* const* bias, void* const* y,
+                     int64_t y_ld, float* const* mean, float* const* rstd, float eps, void* stream);
+
+/* Bytes of workspace that tc_layernorm_backward needs for these rows, of any
+ * type; -1 on bad arguments. */
+int64_t tc_layernorm_workspace(int32_t K, const int64_t* rows, int64_t cols);
+
+/* Gradients of tc_layernorm.  With xh = (x - mean) * rstd and h = dy * weight,
+ *     dx         = rstd * (h - avg(h) - xh * avg(h * xh))    (averages of a row)
+ *     dweight[k] = sum over worker k's rows of dy * xh,   dbias[k] = ... of dy
+ * (zeros for a worker without rows).  dy, x, dx: rows of dtype, as above; dx[k]
+ * may be dy[k] or x[k] itself.  mean, rstd: as tc_layernorm wrote them.
+ * weight: NULL for ones.  dweight, dbias: K device pointers to cols values of
+ * w_dtype (pieces of a flat gradient buffer, at any alignment of the type),
+ * all disjoint from each other and from the other buffers.  Sums are kept in
+ * binary32 and added in an order that only the shapes decide: the same inputs
+ * give the same bits.  workspace: at least tc_layernorm_workspace bytes of
+ * device memory, 16-byte aligned, that nothing else uses until the call's work
+ * is done. */
+int32_t tc_layernorm_backward(int32_t K, const int64_t* rows, int64_t cols, const void* const* dy, int64_t dy_ld,
+                              const void* const* x, int64_t x_ld, int32_t dtype, const float* const* weight,
+                              const float* const* mean, const float* const* rstd, void* const* dx, int64_t dx_ld,
+                              void* const* dweight, void* const* dbias, int32_t w_dtype, void* workspace,
+                              int64_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -103,6 +103,10 @@ def lib(path: str = LIBRARY) -> ctypes.CDLL:
         "tc_broadcast": (i32, [_VP, i32, _VP, _VPP, i32, _VP]),
         "tc_broadcast_tensor": (i32, [_VP, i32, _VP, _VP, i32, _VP]),
         "easgd_pipeline_tensor": (i32, [_VP, _VP, _VP, _VP, _VP, _VP, f32, f32, _VP]),
+        "tc_layernorm": (i32, [i32, ctypes.POINTER(i64), i64, _VPP, i64, i32, _VPP, _VPP, _VPP, i64, _VPP, _VPP, f32, _VP]),
+        "tc_layernorm_workspace": (i64, [i32, ctypes.POINTER(i64), i64]),
+        "tc_layernorm_backward": (i32, [i32, ctypes.POINTER(i64), i64, _VPP, i64, _VPP, i64, i32, _VPP, _VPP, _VPP, _VPP,
+                                        i64, _VPP, _VPP, i32, _VP, i64, _VP]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -452,3 +456,101 @@ def easgd_pipeline_tensor(grads: TensorList, params: TensorList, g_tensor: Optio
                                        _dev_ptr(x, n, (torch.float32,), "x"),
                                        _dev_ptr(xc, group.numel, (torch.float32,), "x_c"), float(eta), float(rho),
                                        _stream(stream)))
+
+
+# --------------------------------------------------------------- layer norm
+
+def _row_ptrs(ts, rows, cols: int, dtype: torch.dtype, what: str):
+    """(device pointers, row stride in elements) of the K workers' rows."""
+    if len(ts) != len(rows):
+        raise ValueError(f"need {len(rows)} tensors as {what}, got {len(ts)}")
+    ptrs, ld = [], None
+    for k, (t, r) in enumerate(zip(ts, rows)):
+        if not t.is_cuda:
+            raise ValueError(f"{what}[{k}] must be a GPU tensor")
+        if t.dtype != dtype:
+            raise TypeError(f"{what}[{k}] has dtype {t.dtype}, expected {dtype}")
+        if t.dim() != 2 or t.shape[0] != r or t.shape[1] != cols:
+            raise ValueError(f"{what}[{k}] has shape {tuple(t.shape)}, expected {(r, cols)}")
+        if r:
+            s0, s1 = t.stride()
+            if cols > 1 and s1 != 1:
+                raise ValueError(f"{what}[{k}]: a row's elements must be next to each other")
+            if r > 1:
+                if ld is not None and s0 != ld:
+                    raise ValueError(f"{what}[{k}] has a row stride of {s0}, the workers before it {ld}")
+                ld = s0
+        ptrs.append(t.data_ptr() if r else None)
+    return _ptr_array(ptrs), cols if ld is None else ld
+
+
+def _row_vectors(ts, sizes, dtypes, what: str):
+    if ts is None:
+        return None
+    if len(ts) != len(sizes):
+        raise ValueError(f"need {len(sizes)} tensors as {what}, got {len(ts)}")
+    return _ptr_array([_dev_ptr(t, n, dtypes, what) if n else None for t, n in zip(ts, sizes)])
+
+
+def _norm_rows(xs):
+    if not len(xs) or any(x.dim() != 2 for x in xs):
+        raise ValueError("need one [rows, columns] tensor per worker")
+    if xs[0].dtype not in _DTYPES:
+        raise TypeError(f"rows have dtype {xs[0].dtype}")
+    rows = [x.shape[0] for x in xs]
+    return (ctypes.c_int64 * len(rows))(*rows), rows, xs[0].shape[1], xs[0].dtype
+
+
+def layernorm(xs: Sequence[torch.Tensor], weights, biases, ys: Sequence[torch.Tensor], means=None, rstds=None,
+              eps: float = 1e-5, stream=None) -> None:
+    """ys[k] = layer norm of worker k's rows xs[k] ([rows_k, columns], row
+    stride free) with its own scale and shift (None: ones, zeros); means and
+    rstds receive each row's statistics for the backward pass (tc_layernorm)."""
+    arr, rows, cols, dt = _norm_rows(xs)
+    xp, x_ld = _row_ptrs(xs, rows, cols, dt, "x")
+    yp, y_ld = _row_ptrs(ys, rows, cols, dt, "y")
+    wide, f32 = [cols] * len(rows), (torch.float32,)
+    _check(lib().tc_layernorm(len(rows), arr, cols, xp, x_ld, _DTYPES[dt], _row_vectors(weights, wide, f32, "weight"),
+                              _row_vectors(biases, wide, f32, "bias"), yp, y_ld, _row_vectors(means, rows, f32, "mean"),
+                              _row_vectors(rstds, rows, f32, "rstd"), float(eps), _stream(stream)))
+
+
+def layernorm_workspace(rows: Sequence[int], cols: int) -> int:
+    """Bytes of workspace that layernorm_backward needs (tc_layernorm_workspace)."""
+    n = lib().tc_layernorm_workspace(len(rows), (ctypes.c_int64 * max(1, len(rows)))(*[int(r) for r in rows]), int(cols))
+    if n < 0:
+        raise TCError(TC_EINVAL, last_error())
+    return n
+
+
+def _scratch(workspace: Optional[torch.Tensor], need: int, device, stream) -> torch.Tensor:
+    """The caller's workspace, or one from torch's allocator that belongs to the stream the call runs on."""
+    if workspace is None:
+        if stream is None:
+            return torch.empty(max(16, need), dtype=torch.uint8, device=device)
+        s = stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=device)
+        with torch.cuda.stream(s):
+            return torch.empty(max(16, need), dtype=torch.uint8, device=device)
+    if not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("the workspace must be a contiguous GPU tensor")
+    return workspace
+
+
+def layernorm_backward(dys: Sequence[torch.Tensor], xs: Sequence[torch.Tensor], weights, means, rstds,
+                       dxs: Sequence[torch.Tensor], dweights, dbiases, workspace: Optional[torch.Tensor] = None,
+                       stream=None) -> None:
+    """The gradients of layernorm: dxs[k] of worker k's rows, and dweights[k],
+    dbiases[k] (binary32 or bfloat16) summed over them (tc_layernorm_backward)."""
+    arr, rows, cols, dt = _norm_rows(xs)
+    dyp, dy_ld = _row_ptrs(dys, rows, cols, dt, "dy")
+    xp, x_ld = _row_ptrs(xs, rows, cols, dt, "x")
+    dxp, dx_ld = _row_ptrs(dxs, rows, cols, dt, "dx")
+    wide, f32 = [cols] * len(rows), (torch.float32,)
+    wdt = _gdt(dweights)
+    need = lib().tc_layernorm_workspace(len(rows), arr, cols)
+    ws = _scratch(workspace, need, xs[0].device, stream)
+    _check(lib().tc_layernorm_backward(
+        len(rows), arr, cols, dyp, dy_ld, xp, x_ld, _DTYPES[dt], _row_vectors(weights, wide, f32, "weight"),
+        _row_vectors(means, rows, f32, "mean"), _row_vectors(rstds, rows, f32, "rstd"), dxp, dx_ld,
+        _row_vectors(dweights, wide, (wdt,), "dweight"), _row_vectors(dbiases, wide, (wdt,), "dbias"), _DTYPES[wdt],
+        ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream)))

@@ -643,3 +643,173 @@ TC_API int32_t easgd_pipeline_tensor(const tc_tensorlist* grads, const tc_tensor
                                            static_cast<hipStream_t>(stream)),
                     "easgd_pipeline_tensor launch");
 }
+
+// -------------------------------------------------------------- layer norm
+
+namespace {
+
+// K workers' rows of one buffer argument: `cols` elements every `ld`.
+struct Rows {
+    const void* const* p;
+    int64_t ld;
+    int es;
+    const char* name;
+};
+
+int64_t extent(const Rows& r, int64_t rows, int64_t cols) { return ((rows - 1) * r.ld + cols) * r.es; }
+
+// Rows of the two buffers share a byte.  Views of one wider buffer (equal
+// strides) may interleave without sharing any.
+bool rows_overlap(const Rows& a, const void* p, int64_t ra, const Rows& b, const void* q, int64_t rb, int64_t cols) {
+    if (ra == 0 || rb == 0 || !overlap(p, extent(a, ra, cols), q, extent(b, rb, cols))) return false;
+    const int64_t line = a.ld * a.es;
+    if (line != b.ld * b.es) return true;
+    int64_t at = static_cast<int64_t>(reinterpret_cast<uintptr_t>(q) - reinterpret_cast<uintptr_t>(p)) % line;
+    if (at < 0) at += line;
+    return at < cols * a.es || at + cols * b.es > line;
+}
+
+int32_t check_rows(int32_t K, const int64_t* rows, int64_t cols, const Rows& r) {
+    if (!r.p) { set_error("%s is NULL", r.name); return TC_EINVAL; }
+    int64_t most = 0;
+    for (int32_t k = 0; k < K; ++k) {
+        most = rows[k] > most ? rows[k] : most;
+        if (rows[k] == 0) continue;
+        if (!r.p[k]) { set_error("%s[%d] is NULL", r.name, k); return TC_EINVAL; }
+        if (!aligned(r.p[k], r.es)) { set_error("%s[%d] is not element-aligned", r.name, k); return TC_EINVAL; }
+    }
+    if (r.ld < cols) {
+        set_error("%s: a row stride of %lld is less than the %lld columns", r.name, (long long)r.ld, (long long)cols);
+        return TC_EINVAL;
+    }
+    if (most > 0 && r.ld > INT64_MAX / 8 / most) { set_error("%s is too large", r.name); return TC_EINVAL; }
+    return TC_OK;
+}
+
+// The rows written (out) share nothing with each other or with the rows read
+// (in), except that a worker's out may be its own in, element for element.
+int32_t check_written(int32_t K, const int64_t* rows, int64_t cols, const Rows& out, const Rows* in, int n) {
+    for (int32_t k = 0; k < K; ++k)
+        for (int32_t q = 0; q < K; ++q) {
+            if (q < k && rows_overlap(out, out.p[k], rows[k], out, out.p[q], rows[q], cols)) {
+                set_error("%s[%d] overlaps %s[%d]", out.name, k, out.name, q);
+                return TC_EINVAL;
+            }
+            for (int i = 0; i < n; ++i) {
+                if (!rows_overlap(out, out.p[k], rows[k], in[i], in[i].p[q], rows[q], cols)) continue;
+                if (q == k && out.p[k] == in[i].p[k] && (out.ld == in[i].ld || rows[k] == 1)) continue;
+                set_error("%s[%d] overlaps %s[%d]", out.name, k, in[i].name, q);
+                return TC_EINVAL;
+            }
+        }
+    return TC_OK;
+}
+
+// Optional per-worker arrays of `n` elements of es bytes each; `rows` given:
+// a worker without rows needs none.
+int32_t check_vectors(int32_t K, const int64_t* rows, const void* const* p, int es, const char* name) {
+    for (int32_t k = 0; k < K; ++k) {
+        if (rows && rows[k] == 0) continue;
+        if (!p[k]) { set_error("%s[%d] is NULL", name, k); return TC_EINVAL; }
+        if (!aligned(p[k], es)) { set_error("%s[%d] is not element-aligned", name, k); return TC_EINVAL; }
+    }
+    return TC_OK;
+}
+
+int32_t check_norm(int32_t K, const int64_t* rows, int64_t cols, int32_t dtype) {
+    if (K < 1 || K > TC_MAX_K) { set_error("K = %d outside [1, %d]", K, TC_MAX_K); return TC_EINVAL; }
+    if (!rows) return fail(TC_EINVAL, "rows is NULL");
+    if (cols < 1 || cols > TC_MAX_NORM_COLS) {
+        set_error("cols = %lld outside [1, %d]", (long long)cols, TC_MAX_NORM_COLS);
+        return TC_EINVAL;
+    }
+    for (int32_t k = 0; k < K; ++k)
+        if (rows[k] < 0) { set_error("rows[%d] = %lld is negative", k, (long long)rows[k]); return TC_EINVAL; }
+    if (!elem_size(dtype)) { set_error("unknown dtype %d", dtype); return TC_EINVAL; }
+    return TC_OK;
+}
+
+}  // namespace
+
+TC_API int32_t tc_layernorm(int32_t K, const int64_t* rows, int64_t cols, const void* const* x, int64_t x_ld,
+                            int32_t dtype, const float* const* weight, const float* const* bias, void* const* y,
+                            int64_t y_ld, float* const* mean, float* const* rstd, float eps, void* stream) {
+    clear_error();
+    if (int32_t r = check_norm(K, rows, cols, dtype)) return r;
+    if (!std::isfinite(eps) || eps < 0.0f) return fail(TC_EINVAL, "eps must be finite and not negative");
+    const int es = elem_size(dtype);
+    const Rows in{x, x_ld, es, "x"}, out{y, y_ld, es, "y"};
+    if (int32_t r = check_rows(K, rows, cols, in)) return r;
+    if (int32_t r = check_rows(K, rows, cols, out)) return r;
+    if (int32_t r = check_written(K, rows, cols, out, &in, 1)) return r;
+    const struct { const void* const* p; const char* name; } vectors[] = {
+        {reinterpret_cast<const void* const*>(weight), "weight"}, {reinterpret_cast<const void* const*>(bias), "bias"},
+        {reinterpret_cast<const void* const*>(mean), "mean"}, {reinterpret_cast<const void* const*>(rstd), "rstd"}};
+    for (auto& v : vectors)
+        if (v.p)
+            if (int32_t r = check_vectors(K, rows, v.p, 4, v.name)) return r;
+    hipError_t e = launch_layernorm(K, rows, cols, x, x_ld, dtype, weight, bias, y, y_ld, mean, rstd, eps,
+                                    static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "tc_layernorm launch");
+    return TC_OK;
+}
+
+TC_API int64_t tc_layernorm_workspace(int32_t K, const int64_t* rows, int64_t cols) {
+    clear_error();
+    if (check_norm(K, rows, cols, TC_F32) != TC_OK) return -1;
+    return layernorm_workspace(K, rows, cols);
+}
+
+TC_API int32_t tc_layernorm_backward(int32_t K, const int64_t* rows, int64_t cols, const void* const* dy, int64_t dy_ld,
+                                     const void* const* x, int64_t x_ld, int32_t dtype, const float* const* weight,
+                                     const float* const* mean, const float* const* rstd, void* const* dx, int64_t dx_ld,
+                                     void* const* dweight, void* const* dbias, int32_t w_dtype, void* workspace,
+                                     int64_t workspace_bytes, void* stream) {
+    clear_error();
+    if (int32_t r = check_norm(K, rows, cols, dtype)) return r;
+    const int es = elem_size(dtype), ws = elem_size(w_dtype);
+    if (!ws) { set_error("unknown dtype %d of dweight and dbias", w_dtype); return TC_EINVAL; }
+    const Rows in[2] = {{dy, dy_ld, es, "dy"}, {x, x_ld, es, "x"}}, out{dx, dx_ld, es, "dx"};
+    if (int32_t r = check_rows(K, rows, cols, in[0])) return r;
+    if (int32_t r = check_rows(K, rows, cols, in[1])) return r;
+    if (int32_t r = check_rows(K, rows, cols, out)) return r;
+    if (int32_t r = check_written(K, rows, cols, out, in, 2)) return r;
+    if (!mean || !rstd || !dweight || !dbias) return fail(TC_EINVAL, "mean, rstd, dweight or dbias is NULL");
+    if (weight)
+        if (int32_t r = check_vectors(K, rows, reinterpret_cast<const void* const*>(weight), 4, "weight")) return r;
+    if (int32_t r = check_vectors(K, rows, reinterpret_cast<const void* const*>(mean), 4, "mean")) return r;
+    if (int32_t r = check_vectors(K, rows, reinterpret_cast<const void* const*>(rstd), 4, "rstd")) return r;
+    if (int32_t r = check_vectors(K, nullptr, const_cast<const void* const*>(dweight), ws, "dweight")) return r;
+    if (int32_t r = check_vectors(K, nullptr, const_cast<const void* const*>(dbias), ws, "dbias")) return r;
+    // what is written as sums over rows shares nothing with what else is
+    // written, nor with what the rows' kernels read
+    const int64_t wb = cols * ws;
+    for (int32_t k = 0; k < K; ++k) {
+        for (int32_t q = 0; q < K; ++q) {
+            if ((q < k && (overlap(dweight[k], wb, dweight[q], wb) || overlap(dbias[k], wb, dbias[q], wb))) ||
+                overlap(dweight[k], wb, dbias[q], wb)) {
+                set_error("dweight or dbias of workers %d and %d overlap", k, q);
+                return TC_EINVAL;
+            }
+            for (const void* p : {const_cast<const void*>(dweight[k]), const_cast<const void*>(dbias[k])}) {
+                bool bad = weight && rows[q] > 0 && overlap(p, wb, weight[q], cols * 4);
+                for (const Rows* r : {&in[0], &in[1], &out})
+                    bad = bad || (rows[q] > 0 && overlap(p, wb, r->p[q], extent(*r, rows[q], cols)));
+                if (bad) {
+                    set_error("dweight[%d] or dbias[%d] overlaps a buffer of worker %d", k, k, q);
+                    return TC_EINVAL;
+                }
+            }
+        }
+    }
+    const int64_t need = layernorm_workspace(K, rows, cols);
+    if (!workspace || !aligned(workspace, 16)) return fail(TC_EINVAL, "workspace is NULL or not 16-byte aligned");
+    if (workspace_bytes < need) {
+        set_error("the workspace has %lld bytes, %lld are needed", (long long)workspace_bytes, (long long)need);
+        return TC_EINVAL;
+    }
+    hipError_t e = launch_layernorm_backward(K, rows, cols, dy, dy_ld, x, x_ld, dtype, weight, mean, rstd, dx, dx_ld,
+                                             dweight, dbias, w_dtype, workspace, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "tc_layernorm_backward launch");
+    return TC_OK;
+}

@@ -161,6 +161,17 @@ hipError_t launch_tensor_broadcast(int K, const void* src, void* dst, int es, in
 hipError_t launch_tensor_pipeline(const tc_tensorlist* grads, const tc_tensorlist* params, void* gt, float* gbar,
                                   float* x, float* xc, float eta, float rho, hipStream_t stream);
 
+// Layer norm of K workers' rows (row strides in elements); w, b, mean and rstd
+// of the forward pass may be null.
+hipError_t launch_layernorm(int K, const int64_t* rows, int64_t cols, const void* const* x, int64_t x_ld, int dtype,
+                            const float* const* w, const float* const* b, void* const* y, int64_t y_ld,
+                            float* const* mean, float* const* rstd, float eps, hipStream_t stream);
+int64_t layernorm_workspace(int K, const int64_t* rows, int64_t cols);
+hipError_t launch_layernorm_backward(int K, const int64_t* rows, int64_t cols, const void* const* dy, int64_t dy_ld,
+                                     const void* const* x, int64_t x_ld, int dtype, const float* const* w,
+                                     const float* const* mean, const float* const* rstd, void* const* dx, int64_t dx_ld,
+                                     void* const* dw, void* const* db, int w_dtype, void* workspace, hipStream_t stream);
+
 }  // namespace tc
 
 // One cut of the flat index space into chunks of `chunk` elements (the last

@@ -1,0 +1,688 @@
+// Layer norm of K workers' rows, and its backward pass.
+//
+// With mu and sigma^2 the mean and the variance of a row's C elements,
+// r = 1 / sqrt(sigma^2 + eps) and xh = (x - mu) r:
+//     y  = xh w + b
+//     h  = dy w;   dx = r (h - mean(h) - xh mean(h xh))
+//     dw = sum over rows of dy xh;   db = sum over rows of dy
+// Both passes are bound by memory: the forward reads x and writes y, the
+// backward reads dy and x and writes dx, each once.  A row is therefore held
+// in registers from its only read on, by a group of L lanes (8 to 64 lanes of
+// a wave, or a whole workgroup of 256 or 512) that takes NV vectors of 16
+// bytes a lane; the variance is summed from the differences to the mean, so it
+// loses nothing where the mean is large.  Workgroups stay on one worker and
+// take its rows in turn, the next row's loads under way while one is reduced:
+// the scale and shift stay in registers, and in the backward pass so do the
+// column sums of dw and db, in binary32, which are written once per workgroup
+// and added up by a second kernel in a fixed order (no atomics: the same
+// inputs give the same bits).
+//
+// Rows are at any alignment of their element: on gfx950 a 16-byte access at
+// any address is one instruction.
+#include "tc_internal.h"
+
+namespace tc {
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+// Elements of T in 16 bytes, and their conversions.
+template <typename T>
+struct Lane;
+template <>
+struct Lane<float> {
+    static constexpr int kVec = 4;
+    static __device__ __forceinline__ void widen(u32x4 v, float* f) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) f[i] = __uint_as_float(v[i]);
+    }
+    static __device__ __forceinline__ u32x4 narrow(const float* f) {
+        u32x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __float_as_uint(f[i]);
+        return v;
+    }
+    static __device__ __forceinline__ float get(uintptr_t a) { return gld<float>(a); }
+    static __device__ __forceinline__ void put(uintptr_t a, float f) { gst<float>(a, f); }
+};
+// bfloat16: widened exactly, rounded to nearest even once, where a result is
+// stored.
+template <>
+struct Lane<__bf16> {
+    static constexpr int kVec = 8;
+    static __device__ __forceinline__ void widen(u32x4 v, float* f) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[2 * i] = __uint_as_float(v[i] << 16);
+            f[2 * i + 1] = __uint_as_float(v[i] & 0xffff0000u);
+        }
+    }
+    static __device__ __forceinline__ u32x4 narrow(const float* f) {
+        typedef __bf16 bf2 __attribute__((ext_vector_type(2)));
+        u32x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            bf2 p = {static_cast<__bf16>(f[2 * i]), static_cast<__bf16>(f[2 * i + 1])};
+            v[i] = __builtin_bit_cast(uint32_t, p);
+        }
+        return v;
+    }
+    static __device__ __forceinline__ float get(uintptr_t a) {
+        return __uint_as_float(static_cast<uint32_t>(gld<uint16_t>(a)) << 16);
+    }
+    static __device__ __forceinline__ void put(uintptr_t a, float f) { gst<__bf16>(a, static_cast<__bf16>(f)); }
+};
+
+// Vector v of a row at address a: whole, or what the row has of it with zeros
+// after the row's end.
+template <typename T>
+__device__ __forceinline__ u32x4 load_vec(uintptr_t a, int v, int cols) {
+    constexpr int V = Lane<T>::kVec;
+    const int left = cols - v * V;
+    if (left >= V) return gld_u<u32x4>(a + static_cast<uintptr_t>(v) * 16);
+    u32x4 r = {0, 0, 0, 0};
+    if (left > 0) {
+        float f[V];
+#pragma unroll
+        for (int i = 0; i < V; ++i) f[i] = i < left ? Lane<T>::get(a + static_cast<uintptr_t>(v) * 16 + i * sizeof(T)) : 0.0f;
+        r = Lane<T>::narrow(f);
+    }
+    return r;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_vec(uintptr_t a, int v, int cols, const float* f) {
+    constexpr int V = Lane<T>::kVec;
+    const int left = cols - v * V;
+    if (left >= V) {
+        gst_u<u32x4>(a + static_cast<uintptr_t>(v) * 16, Lane<T>::narrow(f));
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < left) Lane<T>::put(a + static_cast<uintptr_t>(v) * 16 + i * sizeof(T), f[i]);
+    }
+}
+
+// V binary32 values (a scale, a shift) for the columns of vector v; `fill`
+// past the row's end and where there is no such buffer.
+template <int V>
+__device__ __forceinline__ void load_f32(const float* p, int v, int cols, float fill, float* f) {
+    const int left = cols - v * V;
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p) + static_cast<uintptr_t>(v) * V * 4;
+    if (p && left >= V) {
+#pragma unroll
+        for (int q = 0; q < V / 4; ++q) {
+            f32x4 t = gld_u<f32x4>(a + q * 16);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) f[q * 4 + i] = t[i];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i) f[i] = p && i < left ? gld<float>(a + i * 4) : fill;
+    }
+}
+
+// Sums of N values over the L lanes of a group, the same in every lane.  For
+// L over 64 the group is the workgroup, whose waves meet in LDS: `turn`
+// alternates between two halves of it, so one barrier a sum is enough.
+template <int L, int N>
+__device__ __forceinline__ void group_sum(float (&v)[N], float* lds, int& turn) {
+#pragma unroll
+    for (int m = (L < 64 ? L : 64) / 2; m > 0; m >>= 1)
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += __shfl_xor(v[i], m, 64);
+    if constexpr (L > 64) {
+        constexpr int W = L / 64;
+        float* half = lds + turn * (W * 2);
+        if (threadIdx.x % 64 == 0)
+#pragma unroll
+            for (int i = 0; i < N; ++i) half[i * W + threadIdx.x / 64] = v[i];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float s = half[i * W];
+#pragma unroll
+            for (int w = 1; w < W; ++w) s += half[i * W + w];
+            v[i] = s;
+        }
+        turn ^= 1;
+    }
+}
+
+// Pointers of the workers of one launch.
+constexpr int kWorkers = 32;
+
+struct NormArgs {
+    const void* x[kWorkers];
+    const float* w[kWorkers];
+    const float* b[kWorkers];
+    void* y[kWorkers];
+    float* mean[kWorkers];
+    float* rstd[kWorkers];
+    int64_t rows[kWorkers];
+    uint32_t wg[kWorkers + 1];  // first workgroup of each worker
+    int32_t K;
+    int32_t cols;
+    int64_t x_ld, y_ld;  // bytes from row to row
+    float eps;
+};
+
+struct NormGradArgs {
+    const void* dy[kWorkers];
+    const void* x[kWorkers];
+    const float* w[kWorkers];
+    const float* mean[kWorkers];
+    const float* rstd[kWorkers];
+    void* dx[kWorkers];
+    void* dw[kWorkers];
+    void* db[kWorkers];
+    int64_t rows[kWorkers];
+    uint32_t wg[kWorkers + 1];
+    int32_t K;
+    int32_t cols;
+    int64_t dy_ld, x_ld, dx_ld;  // bytes from row to row
+    float* part;                 // column sums of each workgroup: 2 * cols values
+    int32_t w_dtype;             // of dw and db
+    int32_t direct;              // one workgroup a worker: it writes dw and db itself
+};
+
+template <typename A>
+__device__ __forceinline__ int worker_of(const A& a, uint32_t b) {
+    int k = 0;
+    while (k + 1 < a.K && b >= a.wg[k + 1]) ++k;
+    return k;
+}
+
+template <typename T, int L, int NV>
+__global__ void __launch_bounds__(L > 256 ? L : 256) norm_kernel(const NormArgs a) {
+    constexpr int V = Lane<T>::kVec;
+    constexpr int kThreads = L > 256 ? L : 256;
+    constexpr int G = kThreads / L;  // rows at a time
+    __shared__ float lds[L > 64 ? 4 * (L / 64) : 1];
+    const int k = worker_of(a, blockIdx.x);
+    const int lane = threadIdx.x % L, cols = a.cols;
+    const int64_t step = static_cast<int64_t>(a.wg[k + 1] - a.wg[k]) * G;
+    int64_t row = static_cast<int64_t>(blockIdx.x - a.wg[k]) * G + threadIdx.x / L;
+    const int64_t rows = a.rows[k];
+    const uintptr_t x0 = reinterpret_cast<uintptr_t>(a.x[k]), y0 = reinterpret_cast<uintptr_t>(a.y[k]);
+    int turn = 0;
+    u32x4 next[NV];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) next[i] = row < rows ? load_vec<T>(x0 + row * a.x_ld, lane + i * L, cols) : u32x4{0, 0, 0, 0};
+    float w[NV][V], b[NV][V];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        load_f32<V>(a.w[k], lane + i * L, cols, 1.0f, w[i]);
+        load_f32<V>(a.b[k], lane + i * L, cols, 0.0f, b[i]);
+    }
+    // rows - (a row of the first group) is the same for all groups' loop ends
+    // when L > 64, where the barriers are; below that there are none
+    for (; row < rows; row += step) {
+        float x[NV][V];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) Lane<T>::widen(next[i], x[i]);
+        const int64_t then = row + step;
+        if (then < rows)
+#pragma unroll
+            for (int i = 0; i < NV; ++i) next[i] = load_vec<T>(x0 + then * a.x_ld, lane + i * L, cols);
+        float s[1] = {0.0f};
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e) s[0] += x[i][e];
+        group_sum<L, 1>(s, lds, turn);
+        const float mean = s[0] / static_cast<float>(cols);
+        float q[1] = {0.0f};
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int left = cols - (lane + i * L) * V;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                x[i][e] -= mean;
+                q[0] = e < left ? fmaf(x[i][e], x[i][e], q[0]) : q[0];
+            }
+        }
+        group_sum<L, 1>(q, lds, turn);
+        const float r = 1.0f / sqrtf(q[0] / static_cast<float>(cols) + a.eps);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) x[i][e] = fmaf(x[i][e] * r, w[i][e], b[i][e]);
+            store_vec<T>(y0 + row * a.y_ld, lane + i * L, cols, x[i]);
+        }
+        if (lane == 0) {
+            if (a.mean[k]) a.mean[k][row] = mean;
+            if (a.rstd[k]) a.rstd[k][row] = r;
+        }
+    }
+}
+
+__device__ __forceinline__ void put_weight(void* p, int dtype, int64_t c, float v) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+    if (dtype == TC_BF16)
+        Lane<__bf16>::put(a + c * 2, v);
+    else
+        Lane<float>::put(a + c * 4, v);
+}
+
+template <typename T, int L, int NV>
+__global__ void __launch_bounds__(L > 256 ? L : 256) norm_grad_kernel(const NormGradArgs a) {
+    constexpr int V = Lane<T>::kVec;
+    constexpr int kThreads = L > 256 ? L : 256;
+    constexpr int G = kThreads / L;
+    // the sums of a row's waves, and at the end the column sums of the groups
+    constexpr int kCols = L * NV * V;
+    __shared__ float lds[G > 1 ? G * kCols : 4 * (L / 64)];
+    const int k = worker_of(a, blockIdx.x);
+    const int lane = threadIdx.x % L, group = threadIdx.x / L, cols = a.cols;
+    const int64_t step = static_cast<int64_t>(a.wg[k + 1] - a.wg[k]) * G;
+    int64_t row = static_cast<int64_t>(blockIdx.x - a.wg[k]) * G + group;
+    const int64_t rows = a.rows[k];
+    const uintptr_t x0 = reinterpret_cast<uintptr_t>(a.x[k]), d0 = reinterpret_cast<uintptr_t>(a.dy[k]);
+    const uintptr_t o0 = reinterpret_cast<uintptr_t>(a.dx[k]);
+    const float* means = a.mean[k];
+    const float* rstds = a.rstd[k];
+    const float inv = 1.0f / static_cast<float>(cols);
+    int turn = 0;
+    u32x4 nx[NV], nd[NV];
+    float nm = 0.0f, nr = 0.0f;
+    auto fetch = [&](int64_t at) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            nx[i] = load_vec<T>(x0 + at * a.x_ld, lane + i * L, cols);
+            nd[i] = load_vec<T>(d0 + at * a.dy_ld, lane + i * L, cols);
+        }
+        nm = means[at];
+        nr = rstds[at];
+    };
+    if (row < rows) fetch(row);
+    float w[NV][V], dw[NV][V], db[NV][V];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        load_f32<V>(a.w[k], lane + i * L, cols, 1.0f, w[i]);
+#pragma unroll
+        for (int e = 0; e < V; ++e) dw[i][e] = db[i][e] = 0.0f;
+    }
+    for (; row < rows; row += step) {
+        float x[NV][V], d[NV][V];
+        const float mean = nm, r = nr;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            Lane<T>::widen(nx[i], x[i]);
+            Lane<T>::widen(nd[i], d[i]);
+        }
+        if (row + step < rows) fetch(row + step);
+        float s[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                // past the row's end dy is 0 and adds nothing, unless the mean
+                // or r is infinite: those columns are never stored, but they
+                // would put a NaN into the row's sums
+                const bool in = cols - (lane + i * L) * V > e;
+                x[i][e] = in ? (x[i][e] - mean) * r : 0.0f;
+                dw[i][e] = fmaf(d[i][e], x[i][e], dw[i][e]);
+                db[i][e] += d[i][e];
+                d[i][e] *= w[i][e];
+                s[0] += d[i][e];
+                s[1] = fmaf(d[i][e], x[i][e], s[1]);
+            }
+        group_sum<L, 2>(s, lds, turn);
+        const float c0 = s[0] * inv, c1 = s[1] * inv;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+#pragma unroll
+            for (int e = 0; e < V; ++e) x[i][e] = r * (d[i][e] - c0 - x[i][e] * c1);
+            store_vec<T>(o0 + row * a.dx_ld, lane + i * L, cols, x[i]);
+        }
+    }
+    // the workgroup's column sums
+    float* part = a.part + static_cast<int64_t>(blockIdx.x) * 2 * cols;
+    if constexpr (G == 1) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int c = (lane + i * L) * V;
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (c + e < cols) {
+                    if (a.direct) {
+                        put_weight(a.dw[k], a.w_dtype, c + e, dw[i][e]);
+                        put_weight(a.db[k], a.w_dtype, c + e, db[i][e]);
+                    } else {
+                        part[c + e] = dw[i][e];
+                        part[cols + c + e] = db[i][e];
+                    }
+                }
+        }
+    } else {
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    lds[group * kCols + (lane + i * L) * V + e] = which ? db[i][e] : dw[i][e];
+            __syncthreads();
+            for (int c = threadIdx.x; c < cols; c += kThreads) {
+                float t = lds[c];
+#pragma unroll 4
+                for (int g = 1; g < G; ++g) t += lds[g * kCols + c];
+                if (a.direct)
+                    put_weight(which ? a.db[k] : a.dw[k], a.w_dtype, c, t);
+                else
+                    part[which * cols + c] = t;
+            }
+        }
+    }
+}
+
+// Rows too long for the registers of a workgroup: three reads of the row,
+// the later ones from the caches.
+constexpr int kLong = 1024;
+
+template <typename T>
+__global__ void __launch_bounds__(kLong) norm_long_kernel(const NormArgs a) {
+    constexpr int V = Lane<T>::kVec;
+    __shared__ float lds[4 * (kLong / 64)];
+    const int k = worker_of(a, blockIdx.x);
+    const int cols = a.cols, nv = (cols + V - 1) / V;
+    const int64_t step = a.wg[k + 1] - a.wg[k];
+    int turn = 0;
+    for (int64_t row = blockIdx.x - a.wg[k]; row < a.rows[k]; row += step) {
+        const uintptr_t x = reinterpret_cast<uintptr_t>(a.x[k]) + row * a.x_ld;
+        const uintptr_t y = reinterpret_cast<uintptr_t>(a.y[k]) + row * a.y_ld;
+        float f[V], w[V], b[V], s[1] = {0.0f}, q[1] = {0.0f};
+        for (int v = threadIdx.x; v < nv; v += kLong) {
+            Lane<T>::widen(load_vec<T>(x, v, cols), f);
+#pragma unroll
+            for (int e = 0; e < V; ++e) s[0] += f[e];
+        }
+        group_sum<kLong, 1>(s, lds, turn);
+        const float mean = s[0] / static_cast<float>(cols);
+        for (int v = threadIdx.x; v < nv; v += kLong) {
+            Lane<T>::widen(load_vec<T>(x, v, cols), f);
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (v * V + e < cols) q[0] = fmaf(f[e] - mean, f[e] - mean, q[0]);
+        }
+        group_sum<kLong, 1>(q, lds, turn);
+        const float r = 1.0f / sqrtf(q[0] / static_cast<float>(cols) + a.eps);
+        for (int v = threadIdx.x; v < nv; v += kLong) {
+            Lane<T>::widen(load_vec<T>(x, v, cols), f);
+            load_f32<V>(a.w[k], v, cols, 1.0f, w);
+            load_f32<V>(a.b[k], v, cols, 0.0f, b);
+#pragma unroll
+            for (int e = 0; e < V; ++e) f[e] = fmaf((f[e] - mean) * r, w[e], b[e]);
+            store_vec<T>(y, v, cols, f);
+        }
+        if (threadIdx.x == 0) {
+            if (a.mean[k]) a.mean[k][row] = mean;
+            if (a.rstd[k]) a.rstd[k][row] = r;
+        }
+    }
+}
+
+// The column sums of long rows: a workgroup takes 256 columns of a run of
+// rows.  Launched before norm_grad_long_kernel, which may overwrite dy or x.
+template <typename T>
+__global__ void __launch_bounds__(256) norm_columns_kernel(const NormGradArgs a, int runs) {
+    const int k = blockIdx.z;
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c >= a.cols) return;
+    float dw = 0.0f, db = 0.0f;
+    for (int64_t row = blockIdx.y; row < a.rows[k]; row += runs) {
+        const float d = Lane<T>::get(reinterpret_cast<uintptr_t>(a.dy[k]) + row * a.dy_ld + static_cast<uintptr_t>(c) * sizeof(T));
+        const float x = Lane<T>::get(reinterpret_cast<uintptr_t>(a.x[k]) + row * a.x_ld + static_cast<uintptr_t>(c) * sizeof(T));
+        dw = fmaf(d, (x - a.mean[k][row]) * a.rstd[k][row], dw);
+        db += d;
+    }
+    float* part = a.part + (static_cast<int64_t>(k) * runs + blockIdx.y) * 2 * a.cols;
+    part[c] = dw;
+    part[a.cols + c] = db;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kLong) norm_grad_long_kernel(const NormGradArgs a) {
+    constexpr int V = Lane<T>::kVec;
+    __shared__ float lds[4 * (kLong / 64)];
+    const int k = worker_of(a, blockIdx.x);
+    const int cols = a.cols, nv = (cols + V - 1) / V;
+    const int64_t step = a.wg[k + 1] - a.wg[k];
+    const float inv = 1.0f / static_cast<float>(cols);
+    int turn = 0;
+    for (int64_t row = blockIdx.x - a.wg[k]; row < a.rows[k]; row += step) {
+        const uintptr_t x = reinterpret_cast<uintptr_t>(a.x[k]) + row * a.x_ld;
+        const uintptr_t dy = reinterpret_cast<uintptr_t>(a.dy[k]) + row * a.dy_ld;
+        const uintptr_t dx = reinterpret_cast<uintptr_t>(a.dx[k]) + row * a.dx_ld;
+        const float mean = a.mean[k][row], r = a.rstd[k][row];
+        float f[V], d[V], w[V], s[2] = {0.0f, 0.0f};
+        for (int v = threadIdx.x; v < nv; v += kLong) {
+            Lane<T>::widen(load_vec<T>(x, v, cols), f);
+            Lane<T>::widen(load_vec<T>(dy, v, cols), d);
+            load_f32<V>(a.w[k], v, cols, 1.0f, w);
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (v * V + e < cols) {
+                    s[0] = fmaf(d[e], w[e], s[0]);
+                    s[1] = fmaf(d[e] * w[e], (f[e] - mean) * r, s[1]);
+                }
+        }
+        group_sum<kLong, 2>(s, lds, turn);
+        const float c0 = s[0] * inv, c1 = s[1] * inv;
+        for (int v = threadIdx.x; v < nv; v += kLong) {
+            Lane<T>::widen(load_vec<T>(x, v, cols), f);
+            Lane<T>::widen(load_vec<T>(dy, v, cols), d);
+            load_f32<V>(a.w[k], v, cols, 1.0f, w);
+#pragma unroll
+            for (int e = 0; e < V; ++e) f[e] = r * (d[e] * w[e] - c0 - (f[e] - mean) * r * c1);
+            store_vec<T>(dx, v, cols, f);
+        }
+    }
+}
+
+// dw and db of every worker from its workgroups' column sums: 64 columns a
+// workgroup, whose 16 waves take the partial sums in turn.
+__global__ void __launch_bounds__(1024) norm_finish_kernel(const NormGradArgs a) {
+    __shared__ float lds[16][64];
+    const int k = blockIdx.z, which = blockIdx.y, cols = a.cols;
+    const int c = blockIdx.x * 64 + threadIdx.x % 64, wave = threadIdx.x / 64;
+    float s = 0.0f;
+    if (c < cols)
+        for (uint32_t b = a.wg[k] + wave; b < a.wg[k + 1]; b += 16) s += a.part[static_cast<int64_t>(b) * 2 * cols + which * cols + c];
+    lds[wave][threadIdx.x % 64] = s;
+    __syncthreads();
+    if (wave == 0 && c < cols) {
+#pragma unroll
+        for (int q = 1; q < 16; ++q) s += lds[q][threadIdx.x];
+        put_weight(which ? a.db[k] : a.dw[k], a.w_dtype, c, s);
+    }
+}
+
+// Lanes of a row and vectors of a lane.
+struct Shape {
+    int L, NV;  // L = 0: a long row
+};
+
+// The fewest lanes that hold a row in one vector each, up to a wave; then a
+// wave with up to 16 elements a lane, a workgroup of 256 with 8 or 16, and one
+// of 512 with 16 or 32 (more do not fit the registers of so many lanes next to
+// the scale and the column sums).
+Shape shape_of(int64_t cols, int es) {
+    const int v = 16 / es;
+    for (int l = 8; l <= 64; l *= 2)
+        if (cols <= l * v) return {l, 1};
+    const struct { int l, e; } more[] = {{64, 8}, {64, 16}, {256, 8}, {256, 16}, {512, 16}, {512, 32}};
+    for (auto m : more)
+        if (cols <= static_cast<int64_t>(m.l) * m.e) return {m.l, m.e / v};
+    return {0, 0};
+}
+
+// Rows that a workgroup takes at a time, and how many workgroups a launch has
+// at most.
+int rows_at_a_time(Shape s) { return s.L == 0 || s.L >= 256 ? 1 : 256 / s.L; }
+
+// Spreads `most` workgroups over the workers so that each takes about as many
+// batches of rows; fills wg[0..K].  Every worker with rows has at least one,
+// and with `always` every worker.
+void spread(int K, const int64_t* rows, int batch, int64_t most, int64_t least, bool always, uint32_t* wg) {
+    int64_t total = 0;
+    for (int k = 0; k < K; ++k) total += (rows[k] + batch - 1) / batch;
+    int64_t each = (total + most - 1) / most;
+    if (each < least) each = least;
+    wg[0] = 0;
+    for (int k = 0; k < K; ++k) {
+        const int64_t b = (rows[k] + batch - 1) / batch;
+        int64_t n = (b + each - 1) / each;
+        if (n < 1 && always) n = 1;
+        wg[k + 1] = wg[k] + static_cast<uint32_t>(n);
+    }
+}
+
+constexpr int64_t kMostForward = 2048, kMostForwardWide = 512;
+constexpr int64_t kMostBackward = 1024, kMostBackwardWide = 256;
+constexpr int64_t kLeastBackward = 4;  // batches of rows of a workgroup
+constexpr int kRuns = 64;              // of rows, for the column sums of long rows
+
+void spread_backward(int K, const int64_t* rows, Shape s, uint32_t* wg) {
+    spread(K, rows, rows_at_a_time(s), s.L == 0 || s.L == 512 ? kMostBackwardWide : kMostBackward, kLeastBackward, true, wg);
+}
+
+template <typename T, int L, int NV>
+void run_norm(const NormArgs& a, hipStream_t s) {
+    norm_kernel<T, L, NV><<<a.wg[a.K], L > 256 ? L : 256, 0, s>>>(a);
+}
+template <typename T, int L, int NV>
+void run_norm_grad(const NormGradArgs& a, hipStream_t s) {
+    norm_grad_kernel<T, L, NV><<<a.wg[a.K], L > 256 ? L : 256, 0, s>>>(a);
+}
+
+// CALL<T, L, NV> for the shape of the row.
+#define TC_NORM_SHAPES(CALL, T)                                               \
+    {                                                                         \
+        constexpr int V = Lane<T>::kVec;                                      \
+        switch (sh.L * 64 + sh.NV * V) {                                      \
+            case 8 * 64 + V: CALL<T, 8, 1>(a, s); break;                      \
+            case 16 * 64 + V: CALL<T, 16, 1>(a, s); break;                    \
+            case 32 * 64 + V: CALL<T, 32, 1>(a, s); break;                    \
+            case 64 * 64 + 4: CALL<T, 64, 4 / V + (V > 4)>(a, s); break;      \
+            case 64 * 64 + 8: CALL<T, 64, 8 / V>(a, s); break;                \
+            case 64 * 64 + 16: CALL<T, 64, 16 / V>(a, s); break;              \
+            case 256 * 64 + 8: CALL<T, 256, 8 / V>(a, s); break;              \
+            case 256 * 64 + 16: CALL<T, 256, 16 / V>(a, s); break;            \
+            case 512 * 64 + 16: CALL<T, 512, 16 / V>(a, s); break;            \
+            default: CALL<T, 512, 32 / V>(a, s); break;                       \
+        }                                                                     \
+    }
+
+}  // namespace
+
+hipError_t launch_layernorm(int K, const int64_t* rows, int64_t cols, const void* const* x, int64_t x_ld, int dtype,
+                            const float* const* w, const float* const* b, void* const* y, int64_t y_ld,
+                            float* const* mean, float* const* rstd, float eps, hipStream_t s) {
+    const int es = dtype == TC_BF16 ? 2 : 4;
+    const Shape sh = shape_of(cols, es);
+    for (int k0 = 0; k0 < K; k0 += kWorkers) {
+        NormArgs a{};
+        a.K = K - k0 < kWorkers ? K - k0 : kWorkers;
+        a.cols = static_cast<int32_t>(cols);
+        a.x_ld = x_ld * es;
+        a.y_ld = y_ld * es;
+        a.eps = eps;
+        for (int k = 0; k < a.K; ++k) {
+            a.x[k] = x[k0 + k];
+            a.w[k] = w ? w[k0 + k] : nullptr;
+            a.b[k] = b ? b[k0 + k] : nullptr;
+            a.y[k] = y[k0 + k];
+            a.mean[k] = mean ? mean[k0 + k] : nullptr;
+            a.rstd[k] = rstd ? rstd[k0 + k] : nullptr;
+            a.rows[k] = rows[k0 + k];
+        }
+        spread(a.K, a.rows, rows_at_a_time(sh), sh.L == 0 || sh.L == 512 ? kMostForwardWide : kMostForward, 1, false, a.wg);
+        if (a.wg[a.K] == 0) continue;
+        if (sh.L == 0) {
+            if (dtype == TC_BF16)
+                norm_long_kernel<__bf16><<<a.wg[a.K], kLong, 0, s>>>(a);
+            else
+                norm_long_kernel<float><<<a.wg[a.K], kLong, 0, s>>>(a);
+        } else if (dtype == TC_BF16) {
+            TC_NORM_SHAPES(run_norm, __bf16)
+        } else {
+            TC_NORM_SHAPES(run_norm, float)
+        }
+        if (hipError_t e = hipGetLastError()) return e;
+    }
+    return hipSuccess;
+}
+
+int64_t layernorm_workspace(int K, const int64_t* rows, int64_t cols) {
+    // of the type that takes more workgroups
+    int64_t most = 0;
+    for (int es : {2, 4}) {
+        const Shape sh = shape_of(cols, es);
+        for (int k0 = 0; k0 < K; k0 += kWorkers) {
+            uint32_t wg[kWorkers + 1];
+            const int n = K - k0 < kWorkers ? K - k0 : kWorkers;
+            spread_backward(n, rows + k0, sh, wg);
+            const int64_t parts = sh.L == 0 ? static_cast<int64_t>(n) * kRuns : wg[n];
+            most = most > parts ? most : parts;
+        }
+    }
+    return most * 2 * cols * 4;
+}
+
+hipError_t launch_layernorm_backward(int K, const int64_t* rows, int64_t cols, const void* const* dy, int64_t dy_ld,
+                                     const void* const* x, int64_t x_ld, int dtype, const float* const* w,
+                                     const float* const* mean, const float* const* rstd, void* const* dx, int64_t dx_ld,
+                                     void* const* dw, void* const* db, int w_dtype, void* workspace, hipStream_t s) {
+    const int es = dtype == TC_BF16 ? 2 : 4;
+    const Shape sh = shape_of(cols, es);
+    for (int k0 = 0; k0 < K; k0 += kWorkers) {
+        NormGradArgs a{};
+        a.K = K - k0 < kWorkers ? K - k0 : kWorkers;
+        a.cols = static_cast<int32_t>(cols);
+        a.dy_ld = dy_ld * es;
+        a.x_ld = x_ld * es;
+        a.dx_ld = dx_ld * es;
+        a.part = static_cast<float*>(workspace);
+        a.w_dtype = w_dtype;
+        for (int k = 0; k < a.K; ++k) {
+            a.dy[k] = dy[k0 + k];
+            a.x[k] = x[k0 + k];
+            a.w[k] = w ? w[k0 + k] : nullptr;
+            a.mean[k] = mean[k0 + k];
+            a.rstd[k] = rstd[k0 + k];
+            a.dx[k] = dx[k0 + k];
+            a.dw[k] = dw[k0 + k];
+            a.db[k] = db[k0 + k];
+            a.rows[k] = rows[k0 + k];
+        }
+        spread_backward(a.K, a.rows, sh, a.wg);
+        if (sh.L == 0) {
+            const dim3 grid(static_cast<uint32_t>((cols + 255) / 256), kRuns, a.K);
+            if (dtype == TC_BF16) {
+                norm_columns_kernel<__bf16><<<grid, 256, 0, s>>>(a, kRuns);
+                norm_grad_long_kernel<__bf16><<<a.wg[a.K], kLong, 0, s>>>(a);
+            } else {
+                norm_columns_kernel<float><<<grid, 256, 0, s>>>(a, kRuns);
+                norm_grad_long_kernel<float><<<a.wg[a.K], kLong, 0, s>>>(a);
+            }
+            for (int k = 0; k <= a.K; ++k) a.wg[k] = static_cast<uint32_t>(k) * kRuns;
+        } else {
+            a.direct = a.wg[a.K] == static_cast<uint32_t>(a.K);
+            if (dtype == TC_BF16) {
+                TC_NORM_SHAPES(run_norm_grad, __bf16)
+            } else {
+                TC_NORM_SHAPES(run_norm_grad, float)
+            }
+        }
+        if (hipError_t e = hipGetLastError()) return e;
+        if (!a.direct) norm_finish_kernel<<<dim3(static_cast<uint32_t>((cols + 63) / 64), 2, a.K), 1024, 0, s>>>(a);
+        if (hipError_t e = hipGetLastError()) return e;
+    }
+    return hipSuccess;
+}
+
+}  // namespace tc
