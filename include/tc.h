@@ -427,6 +427,52 @@ int32_t tc_layernorm_backward(int32_t K, const int64_t* rows, int64_t cols, cons
                               void* const* dweight, void* const* dbias, int32_t w_dtype, void* workspace,
                               int64_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------
+ * tc_orthogonalize: the momentum update of K copies of a group, with every
+ * matrix of the group orthogonalised by Newton-Schulz steps (what an
+ * optimizer for matrices makes of a gradient; the result takes the gradient's
+ * place in easgd_step, sgd_step or sync_sgd_step).  Per copy and element
+ *     m = mu * m + g;    u = nesterov ? g + mu * m : m     (no momentum: u = g)
+ * then for a tensor that is a matrix, with |u| its Frobenius norm,
+ *     X = u / (|u| + eps);   per step i, with (a, b, c) = coeff[3i .. 3i+2],
+ *     X = a X + b (X X^T) X + c (X X^T)^2 X;    out = scale * X
+ * and for every other tensor out = scale * u.
+ *
+ * tc_ortho_create: the plan for K copies of group g.  rows, cols: host arrays
+ * of n; tensor t is a row-major rows[t] x cols[t] matrix (rows[t] * cols[t] ==
+ * sizes[t]; the shorter side at most TC_MAX_ORTHO_SIDE), or no matrix (0, 0).
+ * scale: host array of n finite factors, or NULL for ones.  All are copied;
+ * the plan owns device tables only.  The group must outlive it.  NULL on
+ * error.
+ * ---------------------------------------------------------------------- */
+#define TC_MAX_ORTHO_SIDE (1 << 16)
+#define TC_MAX_ORTHO_STEPS 64
+
+typedef struct tc_ortho tc_ortho; /* opaque, library-owned */
+
+tc_ortho* tc_ortho_create(const tc_group* g, int32_t K, const int64_t* rows, const int64_t* cols, const float* scale);
+
+/* NULL-safe.  Must not be called while work that uses the plan is pending. */
+void tc_ortho_destroy(tc_ortho* o);
+
+/* Bytes of workspace that tc_orthogonalize needs; -1 if o is NULL. */
+int64_t tc_ortho_workspace(const tc_ortho* o);
+
+/* grad: host array of K device pointers to flat buffers of N elements of
+ * g_dtype.  momentum: K flat binary32 buffers, updated in place, or NULL.  out:
+ * K flat buffers of out_dtype (written); out[k] may be grad[k] itself where the
+ * types are the same, and apart from that all buffers are disjoint.  Products
+ * are accurate to binary32 (the sums are kept in it) and out is rounded once;
+ * an element of a matrix that is not finite makes that matrix's out NaN, and
+ * no other's.  coeff: host array of 3 * steps finite coefficients; refused
+ * (TC_EINVAL) if from singular values in [0, 1] they let one grow past about
+ * 4, or a step multiply one by more than about 16.  eps > 0.  workspace:
+ * tc_ortho_workspace bytes, 256-byte aligned, that nothing else uses until the
+ * call's work is done. */
+int32_t tc_orthogonalize(const tc_ortho* o, const void* const* grad, int32_t g_dtype, float* const* momentum,
+                         float mu, int32_t nesterov, void* const* out, int32_t out_dtype, int32_t steps,
+                         const float* coeff, float eps, void* workspace, int64_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -107,6 +107,10 @@ def lib(path: str = LIBRARY) -> ctypes.CDLL:
         "tc_layernorm_workspace": (i64, [i32, ctypes.POINTER(i64), i64]),
         "tc_layernorm_backward": (i32, [i32, ctypes.POINTER(i64), i64, _VPP, i64, _VPP, i64, i32, _VPP, _VPP, _VPP, _VPP,
                                         i64, _VPP, _VPP, i32, _VP, i64, _VP]),
+        "tc_ortho_create": (_VP, [_VP, i32, ctypes.POINTER(i64), ctypes.POINTER(i64), ctypes.POINTER(f32)]),
+        "tc_ortho_destroy": (None, [_VP]),
+        "tc_ortho_workspace": (i64, [_VP]),
+        "tc_orthogonalize": (i32, [_VP, _VPP, i32, _VPP, f32, i32, _VPP, i32, i32, ctypes.POINTER(f32), f32, _VP, i64, _VP]),
     }
     for name, (res, args) in sig.items():
         fn = getattr(L, name)
@@ -554,3 +558,65 @@ def layernorm_backward(dys: Sequence[torch.Tensor], xs: Sequence[torch.Tensor], 
         _row_vectors(means, rows, f32, "mean"), _row_vectors(rstds, rows, f32, "rstd"), dxp, dx_ld,
         _row_vectors(dweights, wide, (wdt,), "dweight"), _row_vectors(dbiases, wide, (wdt,), "dbias"), _DTYPES[wdt],
         ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream)))
+
+
+# ------------------------------------------------------- orthogonalised update
+
+class OrthoPlan:
+    """Which tensors of a group are matrices: shapes[t] is (rows, columns), or
+    None for a tensor whose update is taken as it is; scales[t] multiplies
+    tensor t's update (None: ones).  For K copies (tc_ortho_create)."""
+
+    def __init__(self, group: Group, K: int, shapes, scales: Optional[Sequence[float]] = None):
+        if len(shapes) != group.n:
+            raise ValueError(f"need {group.n} shapes, got {len(shapes)}")
+        if scales is not None and len(scales) != group.n:
+            raise ValueError(f"need {group.n} scales, got {len(scales)}")
+        sides = [(0, 0) if s is None else (int(s[0]), int(s[1])) for s in shapes]
+        rows, cols = [(ctypes.c_int64 * group.n)(*[s[i] for s in sides]) for i in range(2)]
+        factors = None if scales is None else (ctypes.c_float * group.n)(*[float(s) for s in scales])
+        h = lib().tc_ortho_create(group.handle, int(K), rows, cols, factors)
+        if not h:
+            raise TCError(TC_EINVAL, last_error())
+        self._h = h
+        self.group, self.K = group, int(K)
+        self.workspace = lib().tc_ortho_workspace(h)
+
+    @property
+    def handle(self):
+        return self._h
+
+    def __del__(self):
+        h, self._h = getattr(self, "_h", None), None
+        if h and _lib is not None:
+            _lib.tc_ortho_destroy(h)
+
+
+def ortho_workspace(plan: OrthoPlan) -> int:
+    """Bytes of workspace that orthogonalize needs (tc_ortho_workspace)."""
+    return plan.workspace
+
+
+def orthogonalize(plan: OrthoPlan, gs: Sequence[torch.Tensor], outs: Sequence[torch.Tensor],
+                  momenta: Optional[Sequence[torch.Tensor]] = None, mu: float = 0.95, nesterov: bool = True,
+                  steps: int = 5, coefficients=(3.4445, -4.7750, 2.0315), eps: float = 1e-7,
+                  workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """outs[k] = the momentum update of the flat gradient gs[k], its matrices
+    orthogonalised by Newton-Schulz steps; momenta (binary32) are updated in
+    place (None: the gradient itself is the update).  coefficients: (a, b, c)
+    for every step, or one triple a step (tc_orthogonalize)."""
+    n = plan.group.numel
+    if len(gs) != plan.K or len(outs) != plan.K or (momenta is not None and len(momenta) != plan.K):
+        raise ValueError(f"need {plan.K} gradients, updates and momenta")
+    triples = coefficients if hasattr(coefficients[0], "__len__") else [coefficients] * int(steps)
+    if len(triples) != int(steps) or any(len(t) != 3 for t in triples):
+        raise ValueError(f"need three coefficients, or three for each of the {steps} steps")
+    coeff = (ctypes.c_float * (3 * len(triples)))(*[float(v) for t in triples for v in t])
+    gdt, odt = _gdt(gs), _gdt(outs)
+    gp = _ptr_array([_dev_ptr(t, n, (gdt,), f"grad[{k}]") for k, t in enumerate(gs)])
+    op = _ptr_array([_dev_ptr(t, n, (odt,), f"out[{k}]") for k, t in enumerate(outs)])
+    mp = None if momenta is None else _ptr_array([_dev_ptr(t, n, (torch.float32,), f"momentum[{k}]") for k, t in enumerate(momenta)])
+    ws = _scratch(workspace, plan.workspace, gs[0].device, stream)
+    _check(lib().tc_orthogonalize(plan.handle, gp, _DTYPES[gdt], mp, float(mu), int(bool(nesterov)), op, _DTYPES[odt],
+                                  int(steps), coeff, float(eps), ws.data_ptr(), ws.numel() * ws.element_size(),
+                                  _stream(stream)))

@@ -4,6 +4,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
+#include <new>
 #include <string>
 
 #include "tc_internal.h"
@@ -811,5 +812,101 @@ TC_API int32_t tc_layernorm_backward(int32_t K, const int64_t* rows, int64_t col
     hipError_t e = launch_layernorm_backward(K, rows, cols, dy, dy_ld, x, x_ld, dtype, weight, mean, rstd, dx, dx_ld,
                                              dweight, dbias, w_dtype, workspace, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "tc_layernorm_backward launch");
+    return TC_OK;
+}
+
+// ------------------------------------------------------- orthogonalised update
+
+TC_API tc_ortho* tc_ortho_create(const tc_group* g, int32_t K, const int64_t* rows, const int64_t* cols,
+                                 const float* scale) {
+    clear_error();
+    if (!g || !rows || !cols) { set_error("tc_ortho_create: NULL argument"); return nullptr; }
+    if (K < 1 || K > TC_MAX_K) { set_error("K = %d outside [1, %d]", K, TC_MAX_K); return nullptr; }
+    if (check_device(g) != TC_OK) return nullptr;
+    for (int32_t t = 0; t < g->n; ++t) {
+        if (scale && !std::isfinite(scale[t])) { set_error("scale[%d] is not finite", t); return nullptr; }
+        if (rows[t] == 0 && cols[t] == 0) continue;  // no matrix
+        if (rows[t] < 0 || cols[t] < 0 || (rows[t] > 0 && cols[t] != g->sizes[t] / rows[t]) || rows[t] * cols[t] != g->sizes[t]) {
+            set_error("tensor %d has %lld elements and is no %lld x %lld matrix", t, (long long)g->sizes[t],
+                      (long long)rows[t], (long long)cols[t]);
+            return nullptr;
+        }
+        if (std::min(rows[t], cols[t]) > TC_MAX_ORTHO_SIDE || std::max(rows[t], cols[t]) > INT32_MAX / 2) {
+            set_error("tensor %d: a %lld x %lld matrix is too large", t, (long long)rows[t], (long long)cols[t]);
+            return nullptr;
+        }
+    }
+    hipError_t e = hipSuccess;
+    tc_ortho* o = nullptr;
+    try {
+        o = make_ortho(g, K, rows, cols, scale, &e);
+    } catch (const std::bad_alloc&) {
+        set_error("out of host memory");
+        return nullptr;
+    }
+    if (!o) hip_fail(e, "tc_ortho_create (device tables)");
+    return o;
+}
+
+TC_API void tc_ortho_destroy(tc_ortho* o) {
+    if (o) destroy_ortho(o);
+}
+
+TC_API int64_t tc_ortho_workspace(const tc_ortho* o) { return o ? ortho_workspace(o) : -1; }
+
+TC_API int32_t tc_orthogonalize(const tc_ortho* o, const void* const* grad, int32_t g_dtype, float* const* momentum,
+                                float mu, int32_t nesterov, void* const* out, int32_t out_dtype, int32_t steps,
+                                const float* coeff, float eps, void* workspace, int64_t workspace_bytes, void* stream) {
+    clear_error();
+    if (!o) return fail(TC_EINVAL, "the plan is NULL");
+    const tc_group* g = ortho_group(o);
+    const int32_t K = ortho_copies(o);
+    const int gs = elem_size(g_dtype), os = elem_size(out_dtype);
+    if (!gs || !os) { set_error("unknown dtype %d", gs ? out_dtype : g_dtype); return TC_EINVAL; }
+    if (steps < 1 || steps > TC_MAX_ORTHO_STEPS) { set_error("steps = %d outside [1, %d]", steps, TC_MAX_ORTHO_STEPS); return TC_EINVAL; }
+    if (!coeff) return fail(TC_EINVAL, "coeff is NULL");
+    for (int i = 0; i < 3 * steps; ++i)
+        if (!std::isfinite(coeff[i])) return fail(TC_EINVAL, "the coefficients must be finite");
+    if (!std::isfinite(mu) || !std::isfinite(eps) || eps <= 0.0f) return fail(TC_EINVAL, "mu must be finite, eps finite and positive");
+    if (!ortho_in_range(steps, coeff)) return fail(TC_EINVAL, "the coefficients let the iteration leave its range");
+    if (int32_t r = check_device(g)) return r;
+    if (g->N == 0) return TC_OK;
+    if (!grad || !out) return fail(TC_EINVAL, "NULL buffer");
+    const int64_t gb = g->N * gs, ob = g->N * os, mb = g->N * 4, need = ortho_workspace(o);
+    if (need > 0 && (!workspace || !aligned(workspace, 256))) return fail(TC_EINVAL, "workspace is NULL or not 256-byte aligned");
+    if (workspace_bytes < need) {
+        set_error("the workspace has %lld bytes, %lld are needed", (long long)workspace_bytes, (long long)need);
+        return TC_EINVAL;
+    }
+    for (int32_t k = 0; k < K; ++k) {
+        if (!grad[k] || !out[k] || (momentum && !momentum[k])) { set_error("a buffer of copy %d is NULL", k); return TC_EINVAL; }
+        if (!aligned(grad[k], gs) || !aligned(out[k], os) || (momentum && !aligned(momentum[k], 4))) {
+            set_error("a buffer of copy %d is not element-aligned", k);
+            return TC_EINVAL;
+        }
+        if (need > 0 && (overlap(grad[k], gb, workspace, need) || overlap(out[k], ob, workspace, need) ||
+                         (momentum && overlap(momentum[k], mb, workspace, need)))) {
+            set_error("a buffer of copy %d overlaps the workspace", k);
+            return TC_EINVAL;
+        }
+    }
+    for (int32_t k = 0; k < K; ++k)
+        for (int32_t q = 0; q < K; ++q) {
+            // a copy's update may take the place of its own gradient
+            if (overlap(out[k], ob, grad[q], gb) && !(k == q && out[k] == grad[q] && g_dtype == out_dtype)) {
+                set_error("out[%d] overlaps grad[%d]", k, q);
+                return TC_EINVAL;
+            }
+            if (q < k && overlap(out[k], ob, out[q], ob)) { set_error("out[%d] overlaps out[%d]", k, q); return TC_EINVAL; }
+            if (!momentum) continue;
+            if (overlap(momentum[k], mb, grad[q], gb) || overlap(momentum[k], mb, out[q], ob) ||
+                (q < k && overlap(momentum[k], mb, momentum[q], mb))) {
+                set_error("momentum[%d] overlaps a buffer of copy %d", k, q);
+                return TC_EINVAL;
+            }
+        }
+    hipError_t e = launch_ortho(o, grad, g_dtype, momentum, mu, nesterov != 0, out, out_dtype, steps, coeff, eps, workspace,
+                                static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "tc_orthogonalize launch");
     return TC_OK;
 }

@@ -172,6 +172,19 @@ hipError_t launch_layernorm_backward(int K, const int64_t* rows, int64_t cols, c
                                      const float* const* mean, const float* const* rstd, void* const* dx, int64_t dx_ld,
                                      void* const* dw, void* const* db, int w_dtype, void* workspace, hipStream_t stream);
 
+// The orthogonalised momentum update: the plan (null and an error on failure),
+// what it needs, whether the coefficients keep the values in range, the call.
+tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const int64_t* cols, const float* scale,
+                     hipError_t* e);
+void destroy_ortho(tc_ortho* o);
+const tc_group* ortho_group(const tc_ortho* o);
+int32_t ortho_copies(const tc_ortho* o);
+int64_t ortho_workspace(const tc_ortho* o);
+bool ortho_in_range(int steps, const float* coeff);
+hipError_t launch_ortho(const tc_ortho* o, const void* const* g, int g_dtype, float* const* m, float mu, int nesterov,
+                        void* const* out, int out_dtype, int steps, const float* coeff, float eps, void* workspace,
+                        hipStream_t stream);
+
 }  // namespace tc
 
 // One cut of the flat index space into chunks of `chunk` elements (the last
