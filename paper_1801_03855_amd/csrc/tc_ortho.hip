@@ -20,9 +20,15 @@
 // lo = the nearest to the rest): hi hi + hi lo + lo hi leaves out only lo lo,
 // 2^-22 of a term, which is binary32's accuracy at a third of binary16's rate
 // (binary32 matrix instructions run at a sixteenth).  Binary16's range is
-// enough because the iteration bounds its values: |X| and X X^T are held times
-// 2^12 (up to 16, smallest step 2^-36), P and products of P times 2^8 (up to
-// 255); coefficients that leave these ranges are refused on the host.
+// enough because the iteration bounds its values: X and X X^T are held times
+// 2^12 (up to 16, smallest step 2^-36), polynomials times 2^10 (up to 63);
+// coefficients that leave these ranges are refused on the host.  Two things
+// keep the products from losing what the operands hold.  P is held without its
+// a I, which is added in binary32 where P is used: along the large singular
+// values a I and the rest cancel, and a rounding of P's large diagonal would
+// stay.  And the matrix cores' sums of 128 terms are added up in registers of
+// their own: on 512 x 4,608, summed in the matrix cores alone, the result was
+// 1.7e-5 off, with both 3e-6 (a binary32 product's iteration: 4e-6).
 //
 // Layout.  A matrix in the workspace is rows of blocks of 32 elements, 64
 // bytes of hi followed by 64 bytes of lo, padded with zeros to multiples of a
@@ -47,6 +53,7 @@ struct OrthoMat {
     int32_t m, n;        // m <= n: X is rows x cols, or its transpose (flip)
     int32_t mp, np;      // padded
     int32_t flip;
+    int32_t pair;        // takes two steps to a Gram matrix
     float scale;
     int64_t x, xt[2];    // X [mp][np], its transpose [np][mp] (two, in turn)
     int64_t s[3];        // symmetric [mp][mp] matrices
@@ -56,6 +63,12 @@ struct OrthoMat {
 
 struct OrthoTile {
     int32_t mat, i, j;
+};
+
+// Tiles of the products of one launch.
+struct OrthoList {
+    const OrthoTile* d = nullptr;
+    int32_t n = 0;
 };
 
 }  // namespace tc
@@ -69,17 +82,16 @@ struct tc_ortho {
     int64_t norms = 0;       // and of the matrices' factors
     std::vector<tc::OrthoMat> mats;
     std::vector<int32_t> of;  // tensor of each matrix
-    // chunks of the flat buffer; 64 x 64 tiles of X; tiles on and below the
-    // diagonal, longest sums along n first, and along m first; tiles of P X
-    int32_t nchunks = 0, nsplit = 0, nsym = 0, napply = 0;
+    // chunks of the flat buffer; 64 x 64 tiles of X
+    int32_t nchunks = 0, nsplit = 0;
     void* d_blob = nullptr;
     const tc::OrthoMat* d_mats = nullptr;
     const int32_t* d_of = nullptr;
     const tc::OrthoTile* d_chunks = nullptr;  // mat, first element / kChunk, -
     const tc::OrthoTile* d_split = nullptr;
-    const tc::OrthoTile* d_gram = nullptr;
-    const tc::OrthoTile* d_sym = nullptr;
-    const tc::OrthoTile* d_apply = nullptr;
+    tc::OrthoList gram, sym, apply;  // all matrices
+    tc::OrthoList sym_pair;          // those that take two steps to a Gram matrix
+    tc::OrthoList gram_one, sym_one, apply_one;  // and one
 };
 
 namespace tc {
@@ -94,7 +106,8 @@ typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 constexpr int kChunk = 4096;  // elements of a workgroup of the first pass
 constexpr int kTile = 128;    // rows and columns of a product's tile
 constexpr int kBlock = 32;    // elements of a block of hi and lo
-constexpr float kScaleX = 4096.0f, kScaleP = 256.0f;
+constexpr float kScaleX = 4096.0f, kScaleP = 1024.0f;
+constexpr int kRun = 4;       // stages summed in the matrix cores at a time, where sums are kept apart
 constexpr int kCopies = TC_MAX_K;
 
 // ------------------------------------------------ momentum and the matrix norm
@@ -238,11 +251,20 @@ __global__ void __launch_bounds__(256) ortho_split_kernel(const UpdateArgs a, co
 // -------------------------------------------------------------------- products
 
 enum Kind {
-    kGram,   // A = X X^T
-    kPoly,   // P = a I + b A + c A A
-    kMul,    // symmetric product of two commuting matrices
-    kApply,  // X <- Q X, both ways
-    kFinal   // out = S Q X
+    kGram,   // X X^T
+    kSym,    // product of two symmetric matrices that commute, and multiples of up to two more
+    kApply,  // X <- a X + Q X, both ways
+    kFinal   // out = S (a X + Q X)
+};
+
+// What a product of one kind of matrix takes: left and right are indices of
+// symmetric matrices (right of kApply and kFinal: of a transpose of X), and so
+// is dst.
+struct Operation {
+    int32_t left, right, dst;
+    int32_t add[2];  // symmetric matrices added; -1: none
+    float factor;    // of the product, to the scale of the result
+    float f[2];      // of what is added
 };
 
 struct GemmArgs {
@@ -250,151 +272,246 @@ struct GemmArgs {
     const OrthoTile* tiles;
     char* ws;
     int64_t copy_bytes;
-    int32_t left, right, dst;  // which symmetric matrix, or which transpose of X
     int32_t out_dtype;
-    float a, b, c;             // kPoly
-    float factor;              // of the sum, to the scale of the result
+    Operation op[2];  // of matrices that take one step to a Gram matrix, and two
 };
 
 struct Outs {
     void* out[kCopies];
 };
 
-// Four values as two halves each, along a row of a matrix: element e and the
-// next three, e a multiple of 4.
-__device__ __forceinline__ void put4(char* row, int e, const float* v) {
-    f16x4 hi, lo;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const Split s = split(v[i]);
-        hi[i] = s.hi;
-        lo[i] = s.lo;
-    }
-    char* p = row + e / kBlock * 128 + e % kBlock * 2;
-    *reinterpret_cast<f16x4*>(p) = hi;
-    *reinterpret_cast<f16x4*>(p + 64) = lo;
+typedef __attribute__((address_space(3))) char lds_char;
+typedef __attribute__((address_space(1))) const char global_char;
+
+__device__ __forceinline__ uint32_t pack(float v) {
+    const Split s = split(v);
+    return __builtin_bit_cast(uint16_t, s.hi) | static_cast<uint32_t>(__builtin_bit_cast(uint16_t, s.lo)) << 16;
 }
 
-__device__ __forceinline__ void put1(char* row, int e, float v) {
-    const Split s = split(v);
+// Eight packed values to elements e .. e + 7 of a row, e a multiple of 8.
+__device__ __forceinline__ void put8(char* row, int e, const uint32_t* v) {
+    u32x4 hi, lo;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        hi[i] = (v[2 * i] & 0xffffu) | v[2 * i + 1] << 16;
+        lo[i] = v[2 * i] >> 16 | (v[2 * i + 1] & 0xffff0000u);
+    }
     char* p = row + e / kBlock * 128 + e % kBlock * 2;
-    *reinterpret_cast<_Float16*>(p) = s.hi;
-    *reinterpret_cast<_Float16*>(p + 64) = s.lo;
+    *reinterpret_cast<u32x4*>(p) = hi;
+    *reinterpret_cast<u32x4*>(p + 64) = lo;
+}
+
+// v += f times elements e .. e + 7 of a row.
+__device__ __forceinline__ void add8(const char* row, int e, float f, float* v) {
+    const char* p = row + e / kBlock * 128 + e % kBlock * 2;
+    const f16x8 hi = *reinterpret_cast<const f16x8*>(p), lo = *reinterpret_cast<const f16x8*>(p + 64);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = fmaf(f, static_cast<float>(hi[i]) + static_cast<float>(lo[i]), v[i]);
 }
 
 // One 128 x 128 tile of left right^T, both with rows along the summed axis:
-// four waves with 64 x 64 each, as 2 x 2 of 32 x 32 x 16 products.  32 elements
-// of the summed axis at a time, hi and lo, in two buffers of LDS: while one is
-// multiplied the next block's loads are under way in registers.  A row's 128
-// bytes are eight 16-byte pieces; piece p of row r lies at p ^ (r / 2 % 8), so
-// that 16 lanes reading one piece each of 16 rows touch all 64 banks once.
-template <int KIND>
+// four waves with 64 x 64 each, as 2 x 2 of 32 x 32 x 16 products.
+//
+// PRODUCTS: 3, hi hi + hi lo + lo hi; 2, without lo of left; 1, hi hi.  RUN:
+// blocks summed in the matrix cores at a time, 0 for all.
+//
+// A stage is 128 bytes of each of the 256 rows: a block of 32 elements, hi and
+// lo, or with one product the hi of two blocks.  Two buffers of LDS take
+// turns; the next stage is loaded straight into one while the other is
+// multiplied.  A row's 128 bytes are eight 16-byte pieces; piece p of row r
+// lies at p ^ (r / 2 % 8), so that 16 lanes reading one piece each of 16 rows
+// touch all 64 banks once.
+template <int KIND, int PRODUCTS, int RUN>
 __global__ void __launch_bounds__(256, 2) ortho_gemm_kernel(const GemmArgs a, const Outs outs) {
-    __shared__ __attribute__((aligned(16))) char lds[2][2][kTile * 128];
+    constexpr int kHalf = kTile * 128, kStage = 2 * kHalf;
+    constexpr int kSteps = PRODUCTS == 1 ? 4 : 2;  // products of 16 elements in a stage
+    constexpr bool kLong = KIND == kApply || KIND == kFinal;
+    __shared__ __attribute__((aligned(16))) char lds[2 * kStage];
     const OrthoTile tile = a.tiles[blockIdx.x];
     const OrthoMat& t = a.mats[tile.mat];
+    const Operation& op = a.op[t.pair];
     const int k = blockIdx.y;
     char* base = a.ws + k * a.copy_bytes;
     const int ti = tile.i * kTile, tj = tile.j * kTile;
     // rows of the tile come from left (index in m), columns from right
-    constexpr bool kLong = KIND == kApply || KIND == kFinal;
     const int len = KIND == kGram ? t.np : t.mp;  // of the summed axis
-    const int64_t ld = static_cast<int64_t>(len) * 4;
-    const char* left = base + (KIND == kGram ? t.x : t.s[a.left]) + ti * ld;
-    const char* right = base + (KIND == kGram ? t.x : kLong ? t.xt[a.right] : t.s[a.right]) + tj * ld;
-    const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+    const uint32_t ld = static_cast<uint32_t>(len) * 4;
+    const char* left = base + (KIND == kGram ? t.x : t.s[op.left]) + static_cast<int64_t>(ti) * ld;
+    const char* right = base + (KIND == kGram ? t.x : kLong ? t.xt[op.right] : t.s[op.right]) + static_cast<int64_t>(tj) * ld;
+    const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const int wr = wave / 2 * 64, wc = wave % 2 * 64;
-    const int row = tid / 8, piece = tid % 8;
-    const int64_t src = row * ld + piece * 16;
-    u32x4 ra[4], rb[4];
-    auto fetch = [&](int kb) {
+    // this wave's eight 1,024-byte pieces of a stage: eight rows each
+    uint32_t off[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            ra[q] = gld<u32x4>(reinterpret_cast<uintptr_t>(left + src + q * 32 * ld + static_cast<int64_t>(kb) * 128));
-            rb[q] = gld<u32x4>(reinterpret_cast<uintptr_t>(right + src + q * 32 * ld + static_cast<int64_t>(kb) * 128));
+    for (int q = 0; q < 4; ++q) {
+        const int r = (wave * 4 + q) * 8 + lane / 8, p = (lane % 8) ^ (r / 2 % 8);
+        off[q] = static_cast<uint32_t>(r) * ld + static_cast<uint32_t>(PRODUCTS == 1 ? p / 4 * 128 + p % 4 * 16 : p * 16);
+    }
+    auto fetch = [&](int stage, int buf) {
+        const int64_t at = static_cast<int64_t>(stage) * (PRODUCTS == 1 ? 256 : 128);
+        char* to = lds + buf * kStage + wave * 4096;
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            __builtin_amdgcn_global_load_lds((global_char*)(left + at + off[q]), (lds_char*)(to + q * 1024), 16, 0, 0);
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            __builtin_amdgcn_global_load_lds((global_char*)(right + at + off[q]), (lds_char*)(to + kHalf + q * 1024), 16, 0, 0);
+    };
+    f32x16 acc[2][2] = {}, sum[RUN ? 2 : 1][RUN ? 2 : 1] = {};
+    struct Operands {
+        f16x8 ah[2], al[2], bh[2], bl[2];
+    } now, next;
+    const int ra = (wr + lane % 32) * 128, rb = kHalf + (wc + lane % 32) * 128, turn = lane / 2 % 8;
+    auto read = [&](Operands& f, int buf, int step) {
+        const char* p = lds + buf * kStage;
+        const int hi = ((step * 2 + lane / 32) ^ turn) * 16, lo = ((step * 2 + lane / 32 + 4) ^ turn) * 16;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            f.ah[i] = *reinterpret_cast<const f16x8*>(p + ra + i * 4096 + hi);
+            f.bh[i] = *reinterpret_cast<const f16x8*>(p + rb + i * 4096 + hi);
+            if constexpr (PRODUCTS == 3) f.al[i] = *reinterpret_cast<const f16x8*>(p + ra + i * 4096 + lo);
+            if constexpr (PRODUCTS >= 2) f.bl[i] = *reinterpret_cast<const f16x8*>(p + rb + i * 4096 + lo);
         }
     };
-    auto stage = [&](int buf) {
+    auto multiply = [&](const Operands& f) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int r = row + q * 32, at = r * 128 + (piece ^ (r / 2 % 8)) * 16;
-            *reinterpret_cast<u32x4*>(lds[buf][0] + at) = ra[q];
-            *reinterpret_cast<u32x4*>(lds[buf][1] + at) = rb[q];
-        }
-    };
-    f32x16 acc[2][2] = {};
-    const int blocks = len / kBlock;
-    fetch(0);
-    stage(0);
-    __syncthreads();
-    for (int kb = 0; kb < blocks; ++kb) {
-        if (kb + 1 < blocks) fetch(kb + 1);
-        const char* la = lds[kb & 1][0];
-        const char* lb = lds[kb & 1][1];
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-            f16x8 ah[2], al[2], bh[2], bl[2];
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int r = wr + i * 32 + lane % 32, q = wc + i * 32 + lane % 32, p = s * 2 + lane / 32;
-                ah[i] = *reinterpret_cast<const f16x8*>(la + r * 128 + (p ^ (r / 2 % 8)) * 16);
-                al[i] = *reinterpret_cast<const f16x8*>(la + r * 128 + ((p + 4) ^ (r / 2 % 8)) * 16);
-                bh[i] = *reinterpret_cast<const f16x8*>(lb + q * 128 + (p ^ (q / 2 % 8)) * 16);
-                bl[i] = *reinterpret_cast<const f16x8*>(lb + q * 128 + ((p + 4) ^ (q / 2 % 8)) * 16);
-            }
+        for (int w = 3 - PRODUCTS; w < 3; ++w)  // lo hi, hi lo, hi hi
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah[i], bl[j], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(al[i], bh[j], acc[i][j], 0, 0, 0);
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(ah[i], bh[j], acc[i][j], 0, 0, 0);
-                }
+                for (int j = 0; j < 2; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(w == 0 ? f.al[i] : f.ah[i], w == 1 ? f.bl[j] : f.bh[j],
+                                                                       acc[i][j], 0, 0, 0);
+    };
+    // this wave's loads are done, then every wave's; and every wave has read
+    // its operands of the stage before
+    auto arrive = [&] {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+    const int stages = len / (kSteps * 16);
+    fetch(0, 0);
+    arrive();
+    read(now, 0, 0);
+    for (int st = 0; st < stages; ++st) {
+        // each step's products are issued while the next one's operands are on
+        // their way from LDS
+        const int buf = st & 1;
+        if (st + 1 < stages) fetch(st + 1, buf ^ 1);
+#pragma unroll
+        for (int step = 0; step < kSteps; step += 2) {
+            read(next, buf, step + 1);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(now);
+            __builtin_amdgcn_sched_barrier(0);
+            if (step + 2 < kSteps) {
+                read(now, buf, step + 2);
+            } else if (st + 1 < stages) {
+                arrive();
+                read(now, buf ^ 1, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(next);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        if (kb + 1 < blocks) stage((kb + 1) & 1);
-        __syncthreads();
+        if constexpr (RUN > 0) {
+            if (st % RUN == RUN - 1) {  // stages is a multiple of RUN
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        sum[i][j] += acc[i][j];
+                        acc[i][j] = f32x16{};
+                    }
+            }
+        }
     }
-    const int64_t ld_s = static_cast<int64_t>(t.mp) * 4;
-    // a lane has rows r .. r + 3 of one column in four consecutive registers
+    auto& total = [&]() -> auto& {
+        if constexpr (RUN > 0) return sum;
+        else return acc;
+    }();
+    // The tile through LDS, so that both orders leave in whole lines: column c
+    // holds its 128 rows as 32 pieces of four, piece p at p ^ (c % 32).
+    __syncthreads();
+    float* tiled = reinterpret_cast<float*>(lds);
+    auto piece = [&](int c, int p) { return c * kTile + (p ^ (c % 32)) * 4; };
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const int r = ti + wr + i * 32 + q * 8 + lane / 32 * 4, c = tj + wc + j * 32 + lane % 32;
-                float v[4];
+                // a lane has rows r .. r + 3 of one column in four consecutive registers
+                const int r = wr + i * 32 + q * 8 + lane / 32 * 4, c = wc + j * 32 + lane % 32;
+                f32x4 v;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = acc[i][j][q * 4 + e] * a.factor;
-                if constexpr (KIND == kFinal) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (r + e < t.m && c < t.n) {
-                            const int64_t at = t.flip ? static_cast<int64_t>(c) * t.cols + r + e : static_cast<int64_t>(r + e) * t.cols + c;
-                            store_any(reinterpret_cast<uintptr_t>(outs.out[k]), a.out_dtype, t.at + at, v[e] * t.scale);
-                        }
-                } else if constexpr (KIND == kApply) {
-                    put4(base + t.xt[a.dst] + static_cast<int64_t>(c) * t.mp * 4, r, v);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) put1(base + t.x + static_cast<int64_t>(r + e) * t.np * 4, c, v[e]);
-                } else {
-                    if constexpr (KIND == kPoly) {
-                        // b A + a I, at the scale of P; A is symmetric
-                        const char* p = base + t.s[a.left] + c * ld_s + r / kBlock * 128 + r % kBlock * 2;
-                        const f16x4 hi = *reinterpret_cast<const f16x4*>(p), lo = *reinterpret_cast<const f16x4*>(p + 64);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            v[e] = fmaf(a.b, static_cast<float>(hi[e]) + static_cast<float>(lo[e]), v[e]);
-                            if (r + e == c) v[e] += a.a;
-                        }
-                    }
-                    char* d = base + t.s[a.dst];
-                    put4(d + c * ld_s, r, v);
-                    if (tile.i != tile.j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) put1(d + (r + e) * ld_s, c, v[e]);
-                }
+                for (int e = 0; e < 4; ++e) v[e] = total[i][j][q * 4 + e] * op.factor;
+                *reinterpret_cast<f32x4*>(tiled + piece(c, r / 4)) = v;
             }
+    __syncthreads();
+    const int64_t ld_m = static_cast<int64_t>(t.mp) * 4, ld_n = static_cast<int64_t>(t.np) * 4;
+    const bool natural = kLong ? KIND == kApply || !t.flip : tile.i != tile.j;
+    // 16 lanes a column, eight rows each
+    for (int c = tid / 16; c < kTile; c += 16) {
+        const int r = tid % 16 * 8;
+        float v[8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const f32x4 x = *reinterpret_cast<const f32x4*>(tiled + piece(c, r / 4 + h));
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[4 * h + e] = x[e];
+        }
+        if constexpr (kLong) add8(base + t.xt[op.right] + (tj + c) * ld_m, ti + r, op.f[0], v);
+        if constexpr (KIND == kSym) {
+            // (a symmetric matrix: its row tj + c)
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+                if (op.add[q] >= 0) add8(base + t.s[op.add[q]] + (tj + c) * ld_m, ti + r, op.f[q], v);
+        }
+        if constexpr (KIND == kFinal) {
+            if (t.flip) {
+                if (tj + c < t.n)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (ti + r + e < t.m)
+                            store_any(reinterpret_cast<uintptr_t>(outs.out[k]), a.out_dtype,
+                                      t.at + static_cast<int64_t>(tj + c) * t.cols + ti + r + e, v[e] * t.scale);
+            } else {
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    *reinterpret_cast<f32x4*>(tiled + piece(c, r / 4 + h)) = f32x4{v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+            }
+        } else {
+            uint32_t u[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) u[e] = pack(v[e]);
+            put8(base + (KIND == kApply ? t.xt[op.dst] : t.s[op.dst]) + (tj + c) * ld_m, ti + r, u);
+            if (natural)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    *reinterpret_cast<u32x4*>(tiled + piece(c, r / 4 + h)) = u32x4{u[4 * h], u[4 * h + 1], u[4 * h + 2], u[4 * h + 3]};
+        }
+    }
+    if (!natural) return;
+    __syncthreads();
+    if constexpr (KIND == kFinal) {
+        for (int q = tid; q < kTile * kTile; q += 256) {
+            const int r = q / kTile, c = q % kTile;
+            if (ti + r < t.m && tj + c < t.n)
+                store_any(reinterpret_cast<uintptr_t>(outs.out[k]), a.out_dtype, t.at + static_cast<int64_t>(ti + r) * t.cols + tj + c,
+                          tiled[piece(c, r / 4) + r % 4] * t.scale);
+        }
+    } else {
+        // four lanes a row's block of 32 columns, eight each
+        for (int q = tid / 4; q < kTile * (kTile / kBlock); q += 64) {
+            const int r = q % kTile, c = q / kTile * kBlock + tid % 4 * 8;
+            uint32_t u[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) u[e] = reinterpret_cast<uint32_t*>(tiled)[piece(c + e, r / 4) + r % 4];
+            put8(base + (KIND == kApply ? t.x : t.s[op.dst]) + (ti + r) * (KIND == kApply ? ld_n : ld_m), tj + c, u);
+        }
+    }
 }
 
 // Appended to a list of tiles in the order they are launched.
@@ -404,6 +521,14 @@ void order_by(std::vector<OrthoTile>& v, const std::vector<OrthoMat>& mats, bool
         return (along_n ? a.np : a.mp) > (along_n ? b.np : b.mp);
     });
 }
+
+// Whether a matrix takes two steps to a Gram matrix.  Two steps take
+// 3 m^2 n + 5 m^3 operations instead of 6 m^2 n + 2 m^3, and two launches more
+// between products of the long side, which on less than twice the length do
+// not pay.  P1 P is also larger than P, and its roundings with it: on matrices
+// of one tile, where there is little to gain, one step at a time is three
+// times as accurate (128 x 1,152: 1.2e-6 against 3.9e-6).
+bool takes_pairs(int64_t m, int64_t n) { return m > kTile && n >= 2 * m; }
 
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
@@ -416,7 +541,7 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
     o->g = g;
     o->K = K;
     o->mats.resize(g->n);
-    std::vector<OrthoTile> chunks, split, gram, sym, apply;
+    std::vector<OrthoTile> chunks, split, gram[2], sym[2], apply[2];  // by OrthoMat::pair
     int64_t bytes = 0, sums = 0;
     auto take = [&](int64_t n) {
         const int64_t at = bytes;
@@ -442,6 +567,7 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
         q.n = std::max(q.rows, q.cols);
         q.mp = static_cast<int32_t>(round_up(q.m, kTile));
         q.np = static_cast<int32_t>(round_up(q.n, kTile));
+        q.pair = takes_pairs(q.m, q.n);
         q.index = o->matrices++;
         o->of.push_back(t);
         const int64_t x = static_cast<int64_t>(q.mp) * q.np * 4, s = static_cast<int64_t>(q.mp) * q.mp * 4;
@@ -452,27 +578,31 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
         for (int32_t i = 0; i < q.mp / 64; ++i)
             for (int32_t j = 0; j < q.np / 64; ++j) split.push_back({t, i, j});
         for (int32_t i = 0; i < q.mp / kTile; ++i)
-            for (int32_t j = 0; j <= i; ++j) sym.push_back({t, i, j});
+            for (int32_t j = 0; j <= i; ++j) sym[q.pair].push_back({t, i, j});
         for (int32_t j = 0; j < q.np / kTile; ++j)
-            for (int32_t i = 0; i < q.mp / kTile; ++i) apply.push_back({t, i, j});
+            for (int32_t i = 0; i < q.mp / kTile; ++i) apply[q.pair].push_back({t, i, j});
     }
     o->sums = take(sums * 8);
     o->norms = take(static_cast<int64_t>(o->matrices) * 8);
     o->copy_bytes = bytes;
-    gram = sym;
-    order_by(gram, o->mats, true);
-    order_by(sym, o->mats, false);
-    order_by(apply, o->mats, false);
-    o->nchunks = static_cast<int32_t>(chunks.size());
-    o->nsplit = static_cast<int32_t>(split.size());
-    o->nsym = static_cast<int32_t>(sym.size());
-    o->napply = static_cast<int32_t>(apply.size());
-    for (const auto* v : {&chunks, &split, &gram, &apply})
+    for (int i = 0; i < 2; ++i) gram[i] = sym[i];
+    std::vector<OrthoTile> all[3];
+    std::vector<OrthoTile>* kinds[3] = {gram, sym, apply};
+    for (int i = 0; i < 3; ++i) {
+        all[i] = kinds[i][0];
+        all[i].insert(all[i].end(), kinds[i][1].begin(), kinds[i][1].end());
+        // the longest sums first
+        order_by(all[i], o->mats, i == 0);
+        for (int q = 0; q < 2; ++q) order_by(kinds[i][q], o->mats, i == 0);
+    }
+    for (const auto* v : {&chunks, &split, &all[1], &all[2]})
         if (v->size() >= (size_t{1} << 32) / 256) {  // workgroups of 256 in one dimension of a grid
             delete o;
             *e = hipErrorInvalidValue;
             return nullptr;
         }
+    o->nchunks = static_cast<int32_t>(chunks.size());
+    o->nsplit = static_cast<int32_t>(split.size());
     // one block of device memory for all tables
     std::vector<char> host;
     auto put = [&](const void* p, size_t n) {
@@ -483,9 +613,10 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
     };
     const size_t at_mats = put(o->mats.data(), o->mats.size() * sizeof(OrthoMat));
     const size_t at_of = put(o->of.data(), o->of.size() * 4);
-    const std::vector<OrthoTile>* lists[] = {&chunks, &split, &gram, &sym, &apply};
-    size_t at[5];
-    for (int i = 0; i < 5; ++i) at[i] = put(lists[i]->data(), lists[i]->size() * sizeof(OrthoTile));
+    const std::vector<OrthoTile>* lists[] = {&chunks, &split, &all[0], &all[1], &all[2], &sym[1], &gram[0], &sym[0], &apply[0]};
+    constexpr int kLists = sizeof lists / sizeof *lists;
+    size_t at[kLists];
+    for (int i = 0; i < kLists; ++i) at[i] = put(lists[i]->data(), lists[i]->size() * sizeof(OrthoTile));
     if ((*e = hipMalloc(&o->d_blob, host.size())) != hipSuccess ||
         (*e = hipMemcpy(o->d_blob, host.data(), host.size(), hipMemcpyHostToDevice)) != hipSuccess) {
         destroy_ortho(o);
@@ -494,8 +625,10 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
     const char* d = static_cast<const char*>(o->d_blob);
     o->d_mats = reinterpret_cast<const OrthoMat*>(d + at_mats);
     o->d_of = reinterpret_cast<const int32_t*>(d + at_of);
-    const OrthoTile** to[] = {&o->d_chunks, &o->d_split, &o->d_gram, &o->d_sym, &o->d_apply};
-    for (int i = 0; i < 5; ++i) *to[i] = reinterpret_cast<const OrthoTile*>(d + at[i]);
+    o->d_chunks = reinterpret_cast<const OrthoTile*>(d + at[0]);
+    o->d_split = reinterpret_cast<const OrthoTile*>(d + at[1]);
+    OrthoList* to[] = {&o->gram, &o->sym, &o->apply, &o->sym_pair, &o->gram_one, &o->sym_one, &o->apply_one};
+    for (int i = 2; i < kLists; ++i) *to[i - 2] = {reinterpret_cast<const OrthoTile*>(d + at[i]), static_cast<int32_t>(lists[i]->size())};
     return o;
 }
 
@@ -513,7 +646,7 @@ int64_t ortho_workspace(const tc_ortho* o) { return o->copy_bytes * o->K; }
 // them s |q(x)|, q = a + b x + c x^2; both extremes lie at the ends or where a
 // derivative is 0.
 bool ortho_in_range(int steps, const float* coeff) {
-    double s = 1.0, q_before = 1.0;
+    double s = 1.0, q_before = 1.0, a_before = 1.0;
     for (int i = 0; i < steps; ++i) {
         const double a = coeff[3 * i], b = coeff[3 * i + 1], c = coeff[3 * i + 2], x = s * s;
         auto q = [&](double v) { return std::fabs(a + v * (b + c * v)); };
@@ -535,11 +668,13 @@ bool ortho_in_range(int steps, const float* coeff) {
         } else if (b != 0) {
             at(-a / (3 * b));
         }
-        // what is stored: X X^T (x), P A (s p), P A P (p^2), P (q), P P (q q), X (p); 1/64 for rounding
+        // what is stored: X X^T (x), P A (s p), P A P (p^2), P - a I, P1 P - a1 a I, X (p); 1/64 for rounding
         const double lim_x = 65504.0 / kScaleX * (63.0 / 64.0), lim_p = 65504.0 / kScaleP * (63.0 / 64.0);
         const bool second = i % 2 == 1;
-        if (!(x <= lim_x && s * ps <= lim_x && ps * ps <= lim_x && qs <= lim_p && (!second || qs * q_before <= lim_p))) return false;
+        const double pair = qs * q_before + std::fabs(a * a_before);
+        if (!(x <= lim_x && s * ps <= lim_x && ps * ps <= lim_x && qs + std::fabs(a) <= lim_p && (!second || pair <= lim_p))) return false;
         q_before = qs;
+        a_before = a;
         s = ps;
     }
     return true;
@@ -575,54 +710,78 @@ hipError_t launch_ortho(const tc_ortho* o, const void* const* g, int g_dtype, fl
     a.ws = u.ws;
     a.copy_bytes = o->copy_bytes;
     a.out_dtype = out_dtype;
-    // symmetric matrices: [0] A, then P A P, then P1 P; [1] P; [2] P A, then P1
-    auto gram = [&] {
-        a.tiles = o->d_gram;
-        a.dst = 0;
-        a.factor = 1.0f / kScaleX;
-        ortho_gemm_kernel<kGram><<<dim3(o->nsym, K), 256, 0, s>>>(a, outs);
+    // A result in bfloat16 needs less: X X^T from hi alone, and a I + P
+    // without P's lo where a step's rounding is not multiplied by many after
+    // it.
+    const bool brief = out_dtype == TC_BF16;
+    auto launch = [&](auto kernel, const OrthoList& list) {
+        if (list.n == 0) return;
+        a.tiles = list.d;
+        kernel<<<dim3(list.n, K), 256, 0, s>>>(a, outs);
     };
-    auto poly = [&](const float* c, int dst) {
-        a.tiles = o->d_sym;
-        a.left = a.right = 0;
-        a.dst = dst;
-        a.a = c[0] * kScaleP;
-        a.b = c[1] * (kScaleP / kScaleX);
-        a.factor = c[2] * (kScaleP / kScaleX / kScaleX);
-        ortho_gemm_kernel<kPoly><<<dim3(o->nsym, K), 256, 0, s>>>(a, outs);
+    auto gram = [&](const OrthoList& list) {
+        a.op[0] = a.op[1] = {0, 0, 0, {-1, -1}, 1.0f / kScaleX, {0.0f, 0.0f}};
+        if (brief)
+            launch(ortho_gemm_kernel<kGram, 1, 0>, list);
+        else if (o->sym_pair.n)
+            launch(ortho_gemm_kernel<kGram, 3, kRun>, list);
+        else
+            launch(ortho_gemm_kernel<kGram, 3, 0>, list);
     };
-    auto mul = [&](int left, int right, int dst) {  // left is a P
-        a.tiles = o->d_sym;
-        a.left = left;
-        a.right = right;
-        a.dst = dst;
-        a.factor = 1.0f / kScaleP;
-        ortho_gemm_kernel<kMul><<<dim3(o->nsym, K), 256, 0, s>>>(a, outs);
+    auto sym = [&](const OrthoList& list, Operation p) {
+        a.op[0] = a.op[1] = p;
+        if (brief || o->sym_pair.n == 0)
+            launch(ortho_gemm_kernel<kSym, 3, 0>, list);
+        else
+            launch(ortho_gemm_kernel<kSym, 3, kRun>, list);
     };
-    int from = 0;
+    // R = P - a I of the Gram matrix in [0]
+    constexpr float kXtoP = kScaleP / kScaleX;
+    auto rest = [&](const OrthoList& list, const float* c, int dst) {
+        sym(list, {0, 0, dst, {0, -1}, c[2] * (kXtoP / kScaleX), {c[1] * kXtoP, 0.0f}});
+    };
+    int from[2] = {0, 0};  // which transpose of X is the current one
+    // X <- (f I + [left]) X: of matrices of one step to a Gram matrix, of two
+    struct Factor {
+        int32_t left;
+        float f;
+    };
+    auto apply = [&](const OrthoList& list, Factor one, Factor pair, bool last, bool full) {
+        for (int q = 0; q < 2; ++q) {
+            const Factor& p = q ? pair : one;
+            const float scale = last ? 1.0f / kScaleX : 1.0f;
+            a.op[q] = {p.left, from[q], 1 - from[q], {-1, -1}, scale / kScaleP, {p.f * scale, 0.0f}};
+        }
+        if (last && full)
+            launch(ortho_gemm_kernel<kFinal, 3, 0>, list);
+        else if (last)
+            launch(ortho_gemm_kernel<kFinal, 2, 0>, list);
+        else if (full)
+            launch(ortho_gemm_kernel<kApply, 3, 0>, list);
+        else
+            launch(ortho_gemm_kernel<kApply, 2, 0>, list);
+    };
+    // The symmetric matrices, with R = P - a I: [0] A, then P A P, then
+    // S = P1 P - a1 a I; [1] R (P1's where one step is taken at a time);
+    // [2] P A, then R1.
     for (int i = 0; i < steps; i += 2) {
-        const bool pair = i + 1 < steps, last = i + 2 >= steps;
-        gram();
-        poly(coeff + 3 * i, 1);
-        int q = 1;
-        if (pair) {
-            mul(1, 0, 2);
-            mul(1, 2, 0);
-            poly(coeff + 3 * i + 3, 2);
-            mul(2, 1, 0);
-            q = 0;
+        const bool two = i + 1 < steps, last = i + 2 >= steps;
+        const float *c0 = coeff + 3 * i, *c1 = c0 + 3;
+        gram(o->gram);
+        rest(o->sym, c0, 1);
+        if (two) {
+            sym(o->sym_pair, {1, 0, 2, {0, -1}, 1.0f / kScaleP, {c0[0], 0.0f}});   // P A = R A + a A
+            sym(o->sym_pair, {1, 2, 0, {2, -1}, 1.0f / kScaleP, {c0[0], 0.0f}});   // P A P = R (P A) + a (P A)
+            rest(o->sym_pair, c1, 2);                                              // R1
+            sym(o->sym_pair, {2, 1, 0, {1, 2}, 1.0f / kScaleP, {c1[0], c0[0]}});   // S = R1 R + a1 R + a R1
+            apply(o->apply_one, {1, c0[0]}, {}, false, !brief);
+            from[0] = 1 - from[0];
+            gram(o->gram_one);
+            rest(o->sym_one, c1, 1);
         }
-        a.tiles = o->d_apply;
-        a.left = q;
-        a.right = from;
-        a.dst = from = 1 - from;
-        a.factor = 1.0f / kScaleP;
-        if (last) {
-            a.factor /= kScaleX;
-            ortho_gemm_kernel<kFinal><<<dim3(o->napply, K), 256, 0, s>>>(a, outs);
-        } else {
-            ortho_gemm_kernel<kApply><<<dim3(o->napply, K), 256, 0, s>>>(a, outs);
-        }
+        const Factor one = {1, two ? c1[0] : c0[0]}, pair = two ? Factor{0, c0[0] * c1[0]} : one;
+        apply(o->apply, one, pair, last, !brief || (i > 0 && !last && o->sym_pair.n));
+        for (int& f : from) f = 1 - f;
         if (hipError_t e = hipGetLastError()) return e;
     }
     return hipSuccess;
