@@ -135,6 +135,41 @@ __device__ __forceinline__ void store_any(uintptr_t p, int dtype, int64_t i, flo
         gst<float>(p + i * 4, v);
 }
 
+typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+
+// Elements i .. i + n - 1 of a flat buffer, n <= 4, at any alignment.
+__device__ __forceinline__ f32x4 load_four(uintptr_t p, int dtype, int64_t i, int n) {
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (n < 4) {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (e < n) v[e] = load_any(p, dtype, i + e);
+    } else if (dtype == TC_BF16) {
+        const u16x4 h = gld_u<u16x4>(p + i * 2);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(static_cast<uint32_t>(h[e]) << 16);
+    } else {
+        v = gld_u<f32x4>(p + i * 4);
+    }
+    return v;
+}
+
+__device__ __forceinline__ void store_four(uintptr_t p, int dtype, int64_t i, int n, f32x4 v) {
+    if (n < 4) {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (e < n) store_any(p, dtype, i + e, v[e]);
+    } else if (dtype == TC_BF16) {
+        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+        bf16x4 h;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) h[e] = static_cast<__bf16>(v[e]);
+        gst_u<u16x4>(p + i * 2, __builtin_bit_cast(u16x4, h));
+    } else {
+        gst_u<f32x4>(p + i * 4, v);
+    }
+}
+
 // The update from a gradient and a momentum that has it in already.
 __device__ __forceinline__ float update_of(float g, float m, float mu, int nesterov) { return nesterov ? fmaf(mu, m, g) : m; }
 
@@ -146,20 +181,39 @@ __global__ void __launch_bounds__(256) ortho_update_kernel(const UpdateArgs a) {
     const OrthoMat& t = a.mats[c.mat];
     const int k = blockIdx.y;
     const int64_t first = t.at + static_cast<int64_t>(c.i) * kChunk;
-    const int64_t end = min(first + kChunk, t.at + t.size);
+    const int left = static_cast<int>(min(static_cast<int64_t>(kChunk), t.at + t.size - first));
     const uintptr_t g = reinterpret_cast<uintptr_t>(a.g[k]), m = reinterpret_cast<uintptr_t>(a.m[k]);
+    constexpr int N = kChunk / 1024;  // vectors of four elements a lane
+    f32x4 u[N], v[N];
+    int n[N];
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+        const int e = (q * 256 + threadIdx.x) * 4;
+        n[q] = min(4, left - e);
+        if (n[q] <= 0) continue;
+        u[q] = load_four(g, a.g_dtype, first + e, n[q]);
+        if (a.momentum) v[q] = load_four(m, TC_F32, first + e, n[q]);
+    }
     double sum = 0.0;
-    for (int64_t e = first + threadIdx.x; e < end; e += 256) {
-        float u = load_any(g, a.g_dtype, e);
+#pragma unroll
+    for (int q = 0; q < N; ++q) {
+        if (n[q] <= 0) continue;
+        const int64_t e = first + (q * 256 + threadIdx.x) * 4;
         if (a.momentum) {
-            const float v = fmaf(a.mu, gld<float>(m + e * 4), u);
-            gst<float>(m + e * 4, v);
-            u = update_of(u, v, a.mu, a.nesterov);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[q][i] = fmaf(a.mu, v[q][i], u[q][i]);
+                u[q][i] = update_of(u[q][i], v[q][i], a.mu, a.nesterov);
+            }
+            store_four(m, TC_F32, e, n[q], v[q]);
         }
-        if (t.m == 0)
-            store_any(reinterpret_cast<uintptr_t>(a.out[k]), a.out_dtype, e, t.scale * u);
-        else
-            sum = fma(static_cast<double>(u), static_cast<double>(u), sum);
+        if (t.m == 0) {
+            store_four(reinterpret_cast<uintptr_t>(a.out[k]), a.out_dtype, e, n[q], u[q] * t.scale);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)  // (zeros past the end)
+                sum = fma(static_cast<double>(u[q][i]), static_cast<double>(u[q][i]), sum);
+        }
     }
     if (t.m == 0) return;
 #pragma unroll
@@ -199,8 +253,42 @@ __device__ __forceinline__ Split split(float v) {
     return {hi, static_cast<_Float16>(v - static_cast<float>(hi))};
 }
 
+__device__ __forceinline__ uint32_t pack(float v) {
+    const Split s = split(v);
+    return __builtin_bit_cast(uint16_t, s.hi) | static_cast<uint32_t>(__builtin_bit_cast(uint16_t, s.lo)) << 16;
+}
+
+// Eight packed values to elements e .. e + 7 of a row, e a multiple of 8.
+__device__ __forceinline__ void put8(char* row, int e, const uint32_t* v) {
+    u32x4 hi, lo;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        hi[i] = (v[2 * i] & 0xffffu) | v[2 * i + 1] << 16;
+        lo[i] = v[2 * i] >> 16 | (v[2 * i + 1] & 0xffff0000u);
+    }
+    char* p = row + e / kBlock * 128 + e % kBlock * 2;
+    *reinterpret_cast<u32x4*>(p) = hi;
+    *reinterpret_cast<u32x4*>(p + 64) = lo;
+}
+
+// Their hi alone, in a row that has nothing else.
+__device__ __forceinline__ void put8_hi(char* row, int e, const uint32_t* v) {
+    u32x4 hi;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) hi[i] = (v[2 * i] & 0xffffu) | v[2 * i + 1] << 16;
+    *reinterpret_cast<u32x4*>(row + static_cast<int64_t>(e) * 2) = hi;
+}
+
+// v += f times elements e .. e + 7 of a row.
+__device__ __forceinline__ void add8(const char* row, int e, float f, float* v) {
+    const char* p = row + e / kBlock * 128 + e % kBlock * 2;
+    const f16x8 hi = *reinterpret_cast<const f16x8*>(p), lo = *reinterpret_cast<const f16x8*>(p + 64);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = fmaf(f, static_cast<float>(hi[i]) + static_cast<float>(lo[i]), v[i]);
+}
+
 // X and its transpose from u: 64 x 64 tiles through LDS.
-__global__ void __launch_bounds__(256) ortho_split_kernel(const UpdateArgs a, const OrthoTile* tiles, int64_t norms) {
+__global__ void __launch_bounds__(256) ortho_split_kernel(const UpdateArgs a, const OrthoTile* tiles, int64_t norms, bool brief) {
     __shared__ uint32_t lds[64][65];
     const OrthoTile c = tiles[blockIdx.x];
     const OrthoMat& t = a.mats[c.mat];
@@ -210,40 +298,42 @@ __global__ void __launch_bounds__(256) ortho_split_kernel(const UpdateArgs a, co
     const uintptr_t g = reinterpret_cast<uintptr_t>(a.g[k]), m = reinterpret_cast<uintptr_t>(a.m[k]);
     // the tile in the order of the source: its rows are X's, or X^T's
     const int r0 = (t.flip ? c.j : c.i) * 64, c0 = (t.flip ? c.i : c.j) * 64;
-    for (int q = threadIdx.x; q < 64 * 64; q += 256) {
-        const int r = q / 64, e = q % 64;
-        float v = 0.0f;
-        if (r0 + r < t.rows && c0 + e < t.cols) {
-            const int64_t i = t.at + static_cast<int64_t>(r0 + r) * t.cols + c0 + e;
-            float u = load_any(g, a.g_dtype, i);
-            if (a.momentum) u = update_of(u, gld<float>(m + i * 4), a.mu, a.nesterov);
-            v = static_cast<float>(static_cast<double>(u) * inv);
-        }
-        const Split s = split(v);
-        lds[r][e] = __builtin_bit_cast(uint16_t, s.hi) | static_cast<uint32_t>(__builtin_bit_cast(uint16_t, s.lo)) << 16;
+    f32x4 u[4], v[4];
+    int n[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        const int r = q * 16 + threadIdx.x / 16, e = threadIdx.x % 16 * 4;
+        n[q] = r0 + r < t.rows ? max(0, min(4, t.cols - c0 - e)) : 0;
+        u[q] = v[q] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (n[q] == 0) continue;
+        const int64_t i = t.at + static_cast<int64_t>(r0 + r) * t.cols + c0 + e;
+        u[q] = load_four(g, a.g_dtype, i, n[q]);
+        if (a.momentum) v[q] = load_four(m, TC_F32, i, n[q]);
     }
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float w = a.momentum ? update_of(u[q][i], v[q][i], a.mu, a.nesterov) : u[q][i];
+            lds[q * 16 + threadIdx.x / 16][threadIdx.x % 16 * 4 + i] = n[q] ? pack(static_cast<float>(static_cast<double>(w) * inv)) : 0;
+        }
     __syncthreads();
-    // 16 elements a lane, in both orders
-    const int r = threadIdx.x / 4, e0 = threadIdx.x % 4 * 16;
+    // eight elements a lane, in both orders
 #pragma unroll
     for (int turned = 0; turned < 2; ++turned) {
-        uint32_t hi[8], lo[8];
-#pragma unroll
-        for (int q = 0; q < 8; ++q) {
-            const uint32_t v0 = turned ? lds[e0 + 2 * q][r] : lds[r][e0 + 2 * q];
-            const uint32_t v1 = turned ? lds[e0 + 2 * q + 1][r] : lds[r][e0 + 2 * q + 1];
-            hi[q] = (v0 & 0xffffu) | v1 << 16;
-            lo[q] = v0 >> 16 | (v1 & 0xffff0000u);
-        }
         // rows of the source are rows of X unless flipped
         const bool to_x = (turned != 0) == (t.flip != 0);
-        const int row = (to_x ? c.i : c.j) * 64 + r, col = (to_x ? c.j : c.i) * 64 + e0;
         const int64_t ld = static_cast<int64_t>(to_x ? t.np : t.mp) * 4;
-        char* p = base + (to_x ? t.x : t.xt[0]) + row * ld + col / kBlock * 128 + col % kBlock * 2;
+        for (int q = threadIdx.x; q < 64 * 8; q += 256) {
+            const int r = q / 8, e0 = q % 8 * 8;
+            uint32_t w[8];
 #pragma unroll
-        for (int q = 0; q < 2; ++q) {
-            *reinterpret_cast<u32x4*>(p + q * 16) = u32x4{hi[4 * q], hi[4 * q + 1], hi[4 * q + 2], hi[4 * q + 3]};
-            *reinterpret_cast<u32x4*>(p + 64 + q * 16) = u32x4{lo[4 * q], lo[4 * q + 1], lo[4 * q + 2], lo[4 * q + 3]};
+            for (int i = 0; i < 8; ++i) w[i] = turned ? lds[e0 + i][r] : lds[r][e0 + i];
+            const int row = (to_x ? c.i : c.j) * 64 + r, col = (to_x ? c.j : c.i) * 64 + e0;
+            if (to_x && brief)
+                put8_hi(base + t.x + row * (ld / 2), col, w);
+            else
+                put8(base + (to_x ? t.x : t.xt[0]) + row * ld, col, w);
         }
     }
 }
@@ -283,32 +373,6 @@ struct Outs {
 typedef __attribute__((address_space(3))) char lds_char;
 typedef __attribute__((address_space(1))) const char global_char;
 
-__device__ __forceinline__ uint32_t pack(float v) {
-    const Split s = split(v);
-    return __builtin_bit_cast(uint16_t, s.hi) | static_cast<uint32_t>(__builtin_bit_cast(uint16_t, s.lo)) << 16;
-}
-
-// Eight packed values to elements e .. e + 7 of a row, e a multiple of 8.
-__device__ __forceinline__ void put8(char* row, int e, const uint32_t* v) {
-    u32x4 hi, lo;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        hi[i] = (v[2 * i] & 0xffffu) | v[2 * i + 1] << 16;
-        lo[i] = v[2 * i] >> 16 | (v[2 * i + 1] & 0xffff0000u);
-    }
-    char* p = row + e / kBlock * 128 + e % kBlock * 2;
-    *reinterpret_cast<u32x4*>(p) = hi;
-    *reinterpret_cast<u32x4*>(p + 64) = lo;
-}
-
-// v += f times elements e .. e + 7 of a row.
-__device__ __forceinline__ void add8(const char* row, int e, float f, float* v) {
-    const char* p = row + e / kBlock * 128 + e % kBlock * 2;
-    const f16x8 hi = *reinterpret_cast<const f16x8*>(p), lo = *reinterpret_cast<const f16x8*>(p + 64);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = fmaf(f, static_cast<float>(hi[i]) + static_cast<float>(lo[i]), v[i]);
-}
-
 // One 128 x 128 tile of left right^T, both with rows along the summed axis:
 // four waves with 64 x 64 each, as 2 x 2 of 32 x 32 x 16 products.
 //
@@ -316,12 +380,13 @@ __device__ __forceinline__ void add8(const char* row, int e, float f, float* v) 
 // blocks summed in the matrix cores at a time, 0 for all.
 //
 // A stage is 128 bytes of each of the 256 rows: a block of 32 elements, hi and
-// lo, or with one product the hi of two blocks.  Two buffers of LDS take
+// lo, or with one product 64 elements' hi, which is all that X [m][n] then has
+// (kApply: BRIEF).  Two buffers of LDS take
 // turns; the next stage is loaded straight into one while the other is
 // multiplied.  A row's 128 bytes are eight 16-byte pieces; piece p of row r
 // lies at p ^ (r / 2 % 8), so that 16 lanes reading one piece each of 16 rows
 // touch all 64 banks once.
-template <int KIND, int PRODUCTS, int RUN>
+template <int KIND, int PRODUCTS, int RUN, bool BRIEF = false>
 __global__ void __launch_bounds__(256, 2) ortho_gemm_kernel(const GemmArgs a, const Outs outs) {
     constexpr int kHalf = kTile * 128, kStage = 2 * kHalf;
     constexpr int kSteps = PRODUCTS == 1 ? 4 : 2;  // products of 16 elements in a stage
@@ -335,7 +400,7 @@ __global__ void __launch_bounds__(256, 2) ortho_gemm_kernel(const GemmArgs a, co
     const int ti = tile.i * kTile, tj = tile.j * kTile;
     // rows of the tile come from left (index in m), columns from right
     const int len = KIND == kGram ? t.np : t.mp;  // of the summed axis
-    const uint32_t ld = static_cast<uint32_t>(len) * 4;
+    const uint32_t ld = static_cast<uint32_t>(len) * (PRODUCTS == 1 ? 2 : 4);
     const char* left = base + (KIND == kGram ? t.x : t.s[op.left]) + static_cast<int64_t>(ti) * ld;
     const char* right = base + (KIND == kGram ? t.x : kLong ? t.xt[op.right] : t.s[op.right]) + static_cast<int64_t>(tj) * ld;
     const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
@@ -345,10 +410,10 @@ __global__ void __launch_bounds__(256, 2) ortho_gemm_kernel(const GemmArgs a, co
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         const int r = (wave * 4 + q) * 8 + lane / 8, p = (lane % 8) ^ (r / 2 % 8);
-        off[q] = static_cast<uint32_t>(r) * ld + static_cast<uint32_t>(PRODUCTS == 1 ? p / 4 * 128 + p % 4 * 16 : p * 16);
+        off[q] = static_cast<uint32_t>(r) * ld + static_cast<uint32_t>(p) * 16;
     }
     auto fetch = [&](int stage, int buf) {
-        const int64_t at = static_cast<int64_t>(stage) * (PRODUCTS == 1 ? 256 : 128);
+        const int64_t at = static_cast<int64_t>(stage) * 128;
         char* to = lds + buf * kStage + wave * 4096;
 #pragma unroll
         for (int q = 0; q < 4; ++q)
@@ -473,10 +538,15 @@ __global__ void __launch_bounds__(256, 2) ortho_gemm_kernel(const GemmArgs a, co
             if (t.flip) {
                 if (tj + c < t.n)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (ti + r + e < t.m)
-                            store_any(reinterpret_cast<uintptr_t>(outs.out[k]), a.out_dtype,
-                                      t.at + static_cast<int64_t>(tj + c) * t.cols + ti + r + e, v[e] * t.scale);
+                    for (int h = 0; h < 2; ++h) {
+                        const int n = min(4, t.m - (ti + r + 4 * h));
+                        if (n <= 0) continue;
+                        f32x4 w;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) w[e] = v[4 * h + e] * t.scale;
+                        store_four(reinterpret_cast<uintptr_t>(outs.out[k]), a.out_dtype,
+                                   t.at + static_cast<int64_t>(tj + c) * t.cols + ti + r + 4 * h, n, w);
+                    }
             } else {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
@@ -495,20 +565,27 @@ __global__ void __launch_bounds__(256, 2) ortho_gemm_kernel(const GemmArgs a, co
     }
     if (!natural) return;
     __syncthreads();
-    if constexpr (KIND == kFinal) {
-        for (int q = tid; q < kTile * kTile; q += 256) {
-            const int r = q / kTile, c = q % kTile;
-            if (ti + r < t.m && tj + c < t.n)
-                store_any(reinterpret_cast<uintptr_t>(outs.out[k]), a.out_dtype, t.at + static_cast<int64_t>(ti + r) * t.cols + tj + c,
-                          tiled[piece(c, r / 4) + r % 4] * t.scale);
-        }
-    } else {
-        // four lanes a row's block of 32 columns, eight each
-        for (int q = tid / 4; q < kTile * (kTile / kBlock); q += 64) {
-            const int r = q % kTile, c = q / kTile * kBlock + tid % 4 * 8;
-            uint32_t u[8];
+    // four lanes a row's block of 32 columns, eight each
+    for (int q = tid / 4; q < kTile * (kTile / kBlock); q += 64) {
+        const int r = q % kTile, c = q / kTile * kBlock + tid % 4 * 8;
+        uint32_t u[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) u[e] = reinterpret_cast<uint32_t*>(tiled)[piece(c + e, r / 4) + r % 4];
+        for (int e = 0; e < 8; ++e) u[e] = reinterpret_cast<uint32_t*>(tiled)[piece(c + e, r / 4) + r % 4];
+        if constexpr (KIND == kFinal) {
+            if (ti + r < t.m)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int n = min(4, t.n - (tj + c + 4 * h));
+                    if (n <= 0) continue;
+                    f32x4 v;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(u[4 * h + e]) * t.scale;
+                    store_four(reinterpret_cast<uintptr_t>(outs.out[k]), a.out_dtype,
+                               t.at + static_cast<int64_t>(ti + r) * t.cols + tj + c + 4 * h, n, v);
+                }
+        } else if constexpr (BRIEF) {
+            put8_hi(base + t.x + (ti + r) * (ld_n / 2), tj + c, u);
+        } else {
             put8(base + (KIND == kApply ? t.x : t.s[op.dst]) + (ti + r) * (KIND == kApply ? ld_n : ld_m), tj + c, u);
         }
     }
@@ -701,19 +778,19 @@ hipError_t launch_ortho(const tc_ortho* o, const void* const* g, int g_dtype, fl
     u.out_dtype = out_dtype;
     u.momentum = m != nullptr;
     const uint32_t K = o->K;
+    // A result in bfloat16 needs less: X X^T from hi alone, and a I + P
+    // without P's lo where a step's rounding is not multiplied by many after
+    // it.
+    const bool brief = out_dtype == TC_BF16;
     ortho_update_kernel<<<dim3(o->nchunks, K), 256, 0, s>>>(u);
     if (o->matrices == 0) return hipGetLastError();
     ortho_norm_kernel<<<dim3(o->matrices, K), 256, 0, s>>>(o->d_mats, o->d_of, u.ws, o->copy_bytes, o->sums, o->norms, eps);
-    ortho_split_kernel<<<dim3(o->nsplit, K), 256, 0, s>>>(u, o->d_split, o->norms);
+    ortho_split_kernel<<<dim3(o->nsplit, K), 256, 0, s>>>(u, o->d_split, o->norms, brief);
     GemmArgs a{};
     a.mats = o->d_mats;
     a.ws = u.ws;
     a.copy_bytes = o->copy_bytes;
     a.out_dtype = out_dtype;
-    // A result in bfloat16 needs less: X X^T from hi alone, and a I + P
-    // without P's lo where a step's rounding is not multiplied by many after
-    // it.
-    const bool brief = out_dtype == TC_BF16;
     auto launch = [&](auto kernel, const OrthoList& list) {
         if (list.n == 0) return;
         a.tiles = list.d;
@@ -756,10 +833,12 @@ hipError_t launch_ortho(const tc_ortho* o, const void* const* g, int g_dtype, fl
             launch(ortho_gemm_kernel<kFinal, 3, 0>, list);
         else if (last)
             launch(ortho_gemm_kernel<kFinal, 2, 0>, list);
-        else if (full)
+        else if (!brief)
             launch(ortho_gemm_kernel<kApply, 3, 0>, list);
+        else if (full)
+            launch(ortho_gemm_kernel<kApply, 3, 0, true>, list);
         else
-            launch(ortho_gemm_kernel<kApply, 2, 0>, list);
+            launch(ortho_gemm_kernel<kApply, 2, 0, true>, list);
     };
     // The symmetric matrices, with R = P - a I: [0] A, then P A P, then
     // S = P1 P - a1 a I; [1] R (P1's where one step is taken at a time);
