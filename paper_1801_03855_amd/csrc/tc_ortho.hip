@@ -50,7 +50,7 @@ struct OrthoMat {
     int64_t at;          // first element in a flat buffer
     int64_t size;        // elements
     int32_t rows, cols;  // as stored
-    int32_t m, n;        // m <= n: X is rows x cols, or its transpose (flip)
+    int32_t m, n;        // m <= n: X is rows x cols, or its transpose (flip); 0: no matrix
     int32_t mp, np;      // padded
     int32_t flip;
     int32_t pair;        // takes two steps to a Gram matrix
@@ -82,6 +82,9 @@ struct tc_ortho {
     int64_t norms = 0;       // and of the matrices' factors
     std::vector<tc::OrthoMat> mats;
     std::vector<int32_t> of;  // tensor of each matrix
+    // small matrices, taken whole by a workgroup, in two sizes of LDS
+    const int32_t* d_small[2] = {nullptr, nullptr};
+    int32_t nsmall[2] = {0, 0};
     // chunks of the flat buffer; 64 x 64 tiles of X
     int32_t nchunks = 0, nsplit = 0;
     void* d_blob = nullptr;
@@ -591,6 +594,148 @@ __global__ void __launch_bounds__(256, 2) ortho_gemm_kernel(const GemmArgs a, co
     }
 }
 
+// ------------------------------------------------------------ small matrices
+
+constexpr int kSmallSide = 64;
+constexpr int kSmallThreads = 512;
+constexpr int kSmallLds = 48 * 1024, kMostLds = 160 * 1024;
+
+// LDS of a small matrix: X, X X^T and R, rows of a multiple of 16 elements and
+// four more (an odd multiple of four: 16 rows' pieces of 16 bytes touch every
+// bank once).
+__host__ __device__ inline int64_t small_row(int64_t v) { return (v + 15) / 16 * 16 + 4; }
+int64_t small_lds(int64_t m, int64_t n) {
+    const int64_t mp = (m + 15) / 16 * 16;
+    return (mp * small_row(n) + 2 * mp * small_row(m)) * 4 + 256;
+}
+
+struct SmallArgs {
+    UpdateArgs u;
+    const int32_t* which;  // tensors
+    int32_t steps;
+    float eps;
+    float coeff[3 * TC_MAX_ORTHO_STEPS];
+};
+
+// All steps of a matrix of at most 64 rows (or columns) that fits LDS, in one
+// workgroup: a group of such matrices is bound by the time of launches and of
+// dependent steps, and pays neither memory traffic nor more than one launch
+// here.  The products are binary32 ones, 16 x 16 x 4.  In each, a lane holds
+// for its row (of the left) and column (of the right) elements 4 q .. 4 q + 3
+// of 16 of the summed axis, q = lane / 16, and the four products take one each.
+template <int LDS>
+__global__ void __launch_bounds__(kSmallThreads) ortho_small_kernel(const SmallArgs a) {
+    __shared__ __attribute__((aligned(16))) char lds[LDS];
+    const OrthoMat& t = a.u.mats[a.which[blockIdx.x]];
+    const int k = blockIdx.y, tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+    constexpr int kWaves = kSmallThreads / 64;
+    const int mt = (t.m + 15) / 16, nt = (t.n + 15) / 16;  // tiles
+    const int lx = nt * 16 + 4, la = mt * 16 + 4;
+    double* part = reinterpret_cast<double*>(lds);
+    float* x = reinterpret_cast<float*>(lds + 256);
+    float* ga = x + mt * 16 * lx;
+    float* gr = ga + mt * 16 * la;
+    const uintptr_t g = reinterpret_cast<uintptr_t>(a.u.g[k]), m = reinterpret_cast<uintptr_t>(a.u.m[k]);
+    const uint32_t cols = t.cols, size = static_cast<uint32_t>(t.size);
+    for (int e = tid; e < mt * 16 * lx; e += kSmallThreads) x[e] = 0.0f;
+    __syncthreads();
+    double sum = 0.0;
+    for (uint32_t e = tid; e < size; e += kSmallThreads) {
+        float u = load_any(g, a.u.g_dtype, t.at + e);
+        if (a.u.momentum) {
+            const float v = fmaf(a.u.mu, gld<float>(m + (t.at + e) * 4), u);
+            gst<float>(m + (t.at + e) * 4, v);
+            u = update_of(u, v, a.u.mu, a.u.nesterov);
+        }
+        const uint32_t r = e / cols, c = e - r * cols;
+        x[t.flip ? c * lx + r : r * lx + c] = u;
+        sum = fma(static_cast<double>(u), static_cast<double>(u), sum);
+    }
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) sum += __shfl_xor(sum, s, 64);
+    if (lane == 0) part[wave] = sum;
+    __syncthreads();
+    sum = part[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) sum += part[w];
+    const double inv = 1.0 / (sqrt(sum) + static_cast<double>(a.eps));
+    for (int e = tid; e < mt * 16 * lx; e += kSmallThreads) x[e] = static_cast<float>(static_cast<double>(x[e]) * inv);
+    __syncthreads();
+    const int row = lane % 16, q = lane / 16;
+    // tile (i, j) of left right^T over `len` (a multiple of 16), rows of lu and lv elements
+    auto product = [&](const float* u, int lu, const float* v, int lv, int len) {
+        f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+        const float *pu = u + row * lu + q * 4, *pv = v + row * lv + q * 4;
+        for (int e = 0; e < len; e += 16) {
+            const f32x4 l = *reinterpret_cast<const f32x4*>(pu + e), r = *reinterpret_cast<const f32x4*>(pv + e);
+#pragma unroll
+            for (int s = 0; s < 4; ++s) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(l[s], r[s], acc, 0, 0, 0);
+        }
+        return acc;
+    };
+    for (int step = 0; step < a.steps; ++step) {
+        const float ca = a.coeff[3 * step], cb = a.coeff[3 * step + 1], cc = a.coeff[3 * step + 2];
+        // a lane's results: rows 4 q .. 4 q + 3 of column `row`
+        for (int w = wave; w < mt * (mt + 1) / 2; w += kWaves) {
+            int i = 0;
+            while ((i + 1) * (i + 2) / 2 <= w) ++i;
+            const int j = w - i * (i + 1) / 2;
+            const f32x4 acc = product(x + i * 16 * lx, lx, x + j * 16 * lx, lx, nt * 16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                ga[(i * 16 + q * 4 + e) * la + j * 16 + row] = acc[e];
+                ga[(j * 16 + row) * la + i * 16 + q * 4 + e] = acc[e];
+            }
+        }
+        __syncthreads();
+        for (int w = wave; w < mt * mt; w += kWaves) {
+            const int i = w / mt, j = w % mt;
+            const f32x4 acc = product(ga + i * 16 * la, la, ga + j * 16 * la, la, mt * 16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int at = (i * 16 + q * 4 + e) * la + j * 16 + row;
+                gr[at] = fmaf(cc, acc[e], cb * ga[at]);
+            }
+        }
+        __syncthreads();
+        // X <- a X + R X: a wave has 16 columns to itself
+        for (int j = wave; j < nt; j += kWaves) {
+            float b[kSmallSide / 16][4];
+#pragma unroll
+            for (int h = 0; h < kSmallSide / 16; ++h)
+                if (h < mt)
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) b[h][s] = x[(h * 16 + q * 4 + s) * lx + j * 16 + row];
+            f32x4 out[kSmallSide / 16];
+#pragma unroll
+            for (int i = 0; i < kSmallSide / 16; ++i)
+                if (i < mt) {
+                    f32x4 acc = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                    for (int h = 0; h < kSmallSide / 16; ++h)
+                        if (h < mt) {
+                            const f32x4 l = *reinterpret_cast<const f32x4*>(gr + (i * 16 + row) * la + h * 16 + q * 4);
+#pragma unroll
+                            for (int s = 0; s < 4; ++s) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(l[s], b[h][s], acc, 0, 0, 0);
+                        }
+                    // (b[i] has X at just these places)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) out[i][e] = fmaf(ca, b[i][e], acc[e]);
+                }
+#pragma unroll
+            for (int i = 0; i < kSmallSide / 16; ++i)
+                if (i < mt)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[(i * 16 + q * 4 + e) * lx + j * 16 + row] = out[i][e];
+        }
+        __syncthreads();
+    }
+    for (uint32_t e = tid; e < size; e += kSmallThreads) {
+        const uint32_t r = e / cols, c = e - r * cols;
+        store_any(reinterpret_cast<uintptr_t>(a.u.out[k]), a.u.out_dtype, t.at + e, x[t.flip ? c * lx + r : r * lx + c] * t.scale);
+    }
+}
+
 // Appended to a list of tiles in the order they are launched.
 void order_by(std::vector<OrthoTile>& v, const std::vector<OrthoMat>& mats, bool along_n) {
     std::stable_sort(v.begin(), v.end(), [&](const OrthoTile& x, const OrthoTile& y) {
@@ -619,6 +764,7 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
     o->K = K;
     o->mats.resize(g->n);
     std::vector<OrthoTile> chunks, split, gram[2], sym[2], apply[2];  // by OrthoMat::pair
+    std::vector<int32_t> small[2];
     int64_t bytes = 0, sums = 0;
     auto take = [&](int64_t n) {
         const int64_t at = bytes;
@@ -634,14 +780,21 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
         const int64_t nc = (q.size + kChunk - 1) / kChunk;
         q.chunk0 = static_cast<int32_t>(sums);
         q.chunks = static_cast<int32_t>(nc);
-        for (int64_t i = 0; i < nc; ++i) chunks.push_back({t, static_cast<int32_t>(i), 0});
-        if (q.size == 0 || rows[t] == 0) continue;
-        sums += nc;
+        const bool matrix = q.size > 0 && rows[t] > 0;
+        const int64_t lds = matrix && std::min(rows[t], cols[t]) <= kSmallSide ? small_lds(std::min(rows[t], cols[t]), std::max(rows[t], cols[t])) : INT64_MAX;
+        if (lds > kMostLds)
+            for (int64_t i = 0; i < nc; ++i) chunks.push_back({t, static_cast<int32_t>(i), 0});
+        if (!matrix) continue;
         q.rows = static_cast<int32_t>(rows[t]);
         q.cols = static_cast<int32_t>(cols[t]);
         q.flip = q.rows > q.cols;
         q.m = std::min(q.rows, q.cols);
         q.n = std::max(q.rows, q.cols);
+        if (lds <= kMostLds) {
+            small[lds > kSmallLds].push_back(t);
+            continue;
+        }
+        sums += nc;
         q.mp = static_cast<int32_t>(round_up(q.m, kTile));
         q.np = static_cast<int32_t>(round_up(q.n, kTile));
         q.pair = takes_pairs(q.m, q.n);
@@ -660,7 +813,7 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
             for (int32_t i = 0; i < q.mp / kTile; ++i) apply[q.pair].push_back({t, i, j});
     }
     o->sums = take(sums * 8);
-    o->norms = take(static_cast<int64_t>(o->matrices) * 8);
+    o->norms = take(static_cast<int64_t>(o->matrices) * 8);  // (nothing if there is no large matrix)
     o->copy_bytes = bytes;
     for (int i = 0; i < 2; ++i) gram[i] = sym[i];
     std::vector<OrthoTile> all[3];
@@ -690,6 +843,8 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
     };
     const size_t at_mats = put(o->mats.data(), o->mats.size() * sizeof(OrthoMat));
     const size_t at_of = put(o->of.data(), o->of.size() * 4);
+    size_t at_small[2];
+    for (int i = 0; i < 2; ++i) at_small[i] = put(small[i].data(), small[i].size() * 4);
     const std::vector<OrthoTile>* lists[] = {&chunks, &split, &all[0], &all[1], &all[2], &sym[1], &gram[0], &sym[0], &apply[0]};
     constexpr int kLists = sizeof lists / sizeof *lists;
     size_t at[kLists];
@@ -702,6 +857,10 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
     const char* d = static_cast<const char*>(o->d_blob);
     o->d_mats = reinterpret_cast<const OrthoMat*>(d + at_mats);
     o->d_of = reinterpret_cast<const int32_t*>(d + at_of);
+    for (int i = 0; i < 2; ++i) {
+        o->d_small[i] = reinterpret_cast<const int32_t*>(d + at_small[i]);
+        o->nsmall[i] = static_cast<int32_t>(small[i].size());
+    }
     o->d_chunks = reinterpret_cast<const OrthoTile*>(d + at[0]);
     o->d_split = reinterpret_cast<const OrthoTile*>(d + at[1]);
     OrthoList* to[] = {&o->gram, &o->sym, &o->apply, &o->sym_pair, &o->gram_one, &o->sym_one, &o->apply_one};
@@ -782,7 +941,18 @@ hipError_t launch_ortho(const tc_ortho* o, const void* const* g, int g_dtype, fl
     // without P's lo where a step's rounding is not multiplied by many after
     // it.
     const bool brief = out_dtype == TC_BF16;
-    ortho_update_kernel<<<dim3(o->nchunks, K), 256, 0, s>>>(u);
+    if (o->nsmall[0] + o->nsmall[1] > 0) {
+        SmallArgs sm{};
+        sm.u = u;
+        sm.steps = steps;
+        sm.eps = eps;
+        std::copy(coeff, coeff + 3 * steps, sm.coeff);
+        sm.which = o->d_small[1];
+        if (o->nsmall[1]) ortho_small_kernel<kMostLds><<<dim3(o->nsmall[1], K), kSmallThreads, 0, s>>>(sm);
+        sm.which = o->d_small[0];
+        if (o->nsmall[0]) ortho_small_kernel<kSmallLds><<<dim3(o->nsmall[0], K), kSmallThreads, 0, s>>>(sm);
+    }
+    if (o->nchunks) ortho_update_kernel<<<dim3(o->nchunks, K), 256, 0, s>>>(u);
     if (o->matrices == 0) return hipGetLastError();
     ortho_norm_kernel<<<dim3(o->matrices, K), 256, 0, s>>>(o->d_mats, o->d_of, u.ws, o->copy_bytes, o->sums, o->norms, eps);
     ortho_split_kernel<<<dim3(o->nsplit, K), 256, 0, s>>>(u, o->d_split, o->norms, brief);

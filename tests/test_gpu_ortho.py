@@ -353,14 +353,20 @@ def test_refusals(tc):
     refused(tc.TCError, call, plan, gs, [outs[0], outs[0]])
     refused(tc.TCError, call, plan, gs, [gs[1], outs[1]])
     refused(tc.TCError, call, plan, gs, outs, [ms[0], gs[0]])
-    refused(tc.TCError, call, plan, gs, outs, workspace=torch.zeros(256, dtype=torch.uint8, device=DEV))
-    big = torch.zeros(tc.ortho_workspace(plan) + 512, dtype=torch.uint8, device=DEV)
-    refused(tc.TCError, call, plan, gs, outs, workspace=big[8:])
-    refused(tc.TCError, call, plan, gs, [big[:104].view(torch.float32), outs[1]], workspace=big)
-    refused(ValueError, call, plan, gs, outs, workspace=big.cpu())
+    # a matrix of 100 rows needs a workspace (those of the first plan fit a workgroup's own memory)
+    assert tc.ortho_workspace(plan) == 0
+    large = tc.OrthoPlan(tc.Group([100 * 120]), 1, [(100, 120)])
+    g1, o1 = torch.ones(12000, device=DEV), torch.zeros(12000, device=DEV)
+    refused(tc.TCError, call, large, [g1], [o1], workspace=torch.zeros(256, dtype=torch.uint8, device=DEV))
+    big = torch.zeros(tc.ortho_workspace(large) + 512, dtype=torch.uint8, device=DEV)
+    refused(tc.TCError, call, large, [g1], [o1], workspace=big[8:])
+    refused(tc.TCError, call, large, [g1], [big[:48000].view(torch.float32)], workspace=big)
+    refused(ValueError, call, large, [g1], [o1], workspace=big.cpu())
+    assert float(o1.abs().max()) == 0.0
     assert all(float(o.abs().max()) == 0.0 for o in outs)
     assert tc.lib().tc_orthogonalize(None, None, 0, None, 0.9, 0, None, 0, 1, None, 1e-7, None, 0, None) == tc.TC_EINVAL
     assert not tc.lib().tc_ortho_create(None, 1, None, None, None)
     assert tc.lib().tc_ortho_workspace(None) == -1
     tc.lib().tc_ortho_destroy(None)
-    call(plan, gs, outs, ms, workspace=big)
+    call(plan, gs, outs, ms)
+    call(large, [g1], [o1], workspace=big)
