@@ -384,17 +384,16 @@ typedef __attribute__((address_space(1))) const char global_char;
 //
 // A stage is 128 bytes of each of the 256 rows: a block of 32 elements, hi and
 // lo, or with one product 64 elements' hi, which is all that X [m][n] then has
-// (kApply: BRIEF).  Two buffers of LDS take
-// turns; the next stage is loaded straight into one while the other is
-// multiplied.  A row's 128 bytes are eight 16-byte pieces; piece p of row r
+// (kApply: BRIEF).  STAGES buffers of LDS take turns, each loaded straight
+// from memory while others are multiplied.  A row's 128 bytes are eight 16-byte pieces; piece p of row r
 // lies at p ^ (r / 2 % 8), so that 16 lanes reading one piece each of 16 rows
 // touch all 64 banks once.
-template <int KIND, int PRODUCTS, int RUN, bool BRIEF = false>
-__global__ void __launch_bounds__(256, 2) ortho_gemm_kernel(const GemmArgs a, const Outs outs) {
+template <int KIND, int PRODUCTS, int RUN, int STAGES, bool BRIEF = false>
+__global__ void __launch_bounds__(256, STAGES == 2 ? 2 : 1) ortho_gemm_kernel(const GemmArgs a, const Outs outs) {
     constexpr int kHalf = kTile * 128, kStage = 2 * kHalf;
     constexpr int kSteps = PRODUCTS == 1 ? 4 : 2;  // products of 16 elements in a stage
     constexpr bool kLong = KIND == kApply || KIND == kFinal;
-    __shared__ __attribute__((aligned(16))) char lds[2 * kStage];
+    __shared__ __attribute__((aligned(16))) char lds[STAGES * kStage];
     const OrthoTile tile = a.tiles[blockIdx.x];
     const OrthoMat& t = a.mats[tile.mat];
     const Operation& op = a.op[t.pair];
@@ -451,22 +450,26 @@ __global__ void __launch_bounds__(256, 2) ortho_gemm_kernel(const GemmArgs a, co
                     acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(w == 0 ? f.al[i] : f.ah[i], w == 1 ? f.bl[j] : f.bh[j],
                                                                        acc[i][j], 0, 0, 0);
     };
-    // this wave's loads are done, then every wave's; and every wave has read
-    // its operands of the stage before
+    // the loads of the oldest stage under way are done, in every wave; and
+    // every wave has read its operands of the stage before
     auto arrive = [&] {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 2) * 8) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
     const int stages = len / (kSteps * 16);
-    fetch(0, 0);
+#pragma unroll
+    for (int st = 0; st < STAGES - 1; ++st) fetch(min(st, stages - 1), st);
     arrive();
     read(now, 0, 0);
+    int buf = 0;
     for (int st = 0; st < stages; ++st) {
-        // each step's products are issued while the next one's operands are on
-        // their way from LDS
-        const int buf = st & 1;
-        if (st + 1 < stages) fetch(st + 1, buf ^ 1);
+        // Each step's products are issued while the next one's operands are on
+        // their way from LDS.  The buffer that the stage before this one left
+        // is loaded with the stage STAGES - 1 ahead (past the end the last one
+        // again, so that the count of loads under way stays the same).
+        if (STAGES > 2 || st + 1 < stages) fetch(min(st + STAGES - 1, stages - 1), buf == 0 ? STAGES - 1 : buf - 1);
+        const int then = buf + 1 == STAGES ? 0 : buf + 1;
 #pragma unroll
         for (int step = 0; step < kSteps; step += 2) {
             read(next, buf, step + 1);
@@ -477,12 +480,13 @@ __global__ void __launch_bounds__(256, 2) ortho_gemm_kernel(const GemmArgs a, co
                 read(now, buf, step + 2);
             } else if (st + 1 < stages) {
                 arrive();
-                read(now, buf ^ 1, 0);
+                read(now, then, 0);
             }
             __builtin_amdgcn_sched_barrier(0);
             multiply(next);
             __builtin_amdgcn_sched_barrier(0);
         }
+        buf = then;
         if constexpr (RUN > 0) {
             if (st % RUN == RUN - 1) {  // stages is a multiple of RUN
 #pragma unroll
@@ -640,16 +644,30 @@ __global__ void __launch_bounds__(kSmallThreads) ortho_small_kernel(const SmallA
     for (int e = tid; e < mt * 16 * lx; e += kSmallThreads) x[e] = 0.0f;
     __syncthreads();
     double sum = 0.0;
-    for (uint32_t e = tid; e < size; e += kSmallThreads) {
-        float u = load_any(g, a.u.g_dtype, t.at + e);
-        if (a.u.momentum) {
-            const float v = fmaf(a.u.mu, gld<float>(m + (t.at + e) * 4), u);
-            gst<float>(m + (t.at + e) * 4, v);
-            u = update_of(u, v, a.u.mu, a.u.nesterov);
+    constexpr int N = 8;  // elements of a lane whose loads are under way together
+    for (uint32_t e0 = tid; e0 < size; e0 += N * kSmallThreads) {
+        float u[N], v[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint32_t e = e0 + i * kSmallThreads;
+            u[i] = v[i] = 0.0f;
+            if (e >= size) continue;
+            u[i] = load_any(g, a.u.g_dtype, t.at + e);
+            if (a.u.momentum) v[i] = gld<float>(m + (t.at + e) * 4);
         }
-        const uint32_t r = e / cols, c = e - r * cols;
-        x[t.flip ? c * lx + r : r * lx + c] = u;
-        sum = fma(static_cast<double>(u), static_cast<double>(u), sum);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const uint32_t e = e0 + i * kSmallThreads;
+            if (e >= size) continue;
+            if (a.u.momentum) {
+                const float w = fmaf(a.u.mu, v[i], u[i]);
+                gst<float>(m + (t.at + e) * 4, w);
+                u[i] = update_of(u[i], w, a.u.mu, a.u.nesterov);
+            }
+            const uint32_t r = e / cols, c = e - r * cols;
+            x[t.flip ? c * lx + r : r * lx + c] = u[i];
+            sum = fma(static_cast<double>(u[i]), static_cast<double>(u[i]), sum);
+        }
     }
 #pragma unroll
     for (int s = 32; s > 0; s >>= 1) sum += __shfl_xor(sum, s, 64);
@@ -771,6 +789,17 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
         bytes += round_up(n, 256);
         return at;
     };
+    // what the matrix takes of a workgroup's LDS if it is taken whole
+    auto lds_of = [&](int32_t t) {
+        const int64_t m = std::min(rows[t], cols[t]), n = std::max(rows[t], cols[t]);
+        return m == 0 ? 0 : m <= kSmallSide ? small_lds(m, n) : INT64_MAX;
+    };
+    // Next to larger matrices only the smallest are: the others' tiles cost
+    // the larger ones' launches nothing, and a workgroup of their own up to
+    // 70 us.
+    int64_t most = kMostLds;
+    for (int32_t t = 0; t < g->n; ++t)
+        if (lds_of(t) > kMostLds) most = kSmallLds;
     for (int32_t t = 0; t < g->n; ++t) {
         OrthoMat& q = o->mats[t];
         q = OrthoMat{};
@@ -781,8 +810,8 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
         q.chunk0 = static_cast<int32_t>(sums);
         q.chunks = static_cast<int32_t>(nc);
         const bool matrix = q.size > 0 && rows[t] > 0;
-        const int64_t lds = matrix && std::min(rows[t], cols[t]) <= kSmallSide ? small_lds(std::min(rows[t], cols[t]), std::max(rows[t], cols[t])) : INT64_MAX;
-        if (lds > kMostLds)
+        const bool whole = matrix && lds_of(t) <= most;
+        if (!whole)
             for (int64_t i = 0; i < nc; ++i) chunks.push_back({t, static_cast<int32_t>(i), 0});
         if (!matrix) continue;
         q.rows = static_cast<int32_t>(rows[t]);
@@ -790,8 +819,8 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
         q.flip = q.rows > q.cols;
         q.m = std::min(q.rows, q.cols);
         q.n = std::max(q.rows, q.cols);
-        if (lds <= kMostLds) {
-            small[lds > kSmallLds].push_back(t);
+        if (whole) {
+            small[lds_of(t) > kSmallLds].push_back(t);
             continue;
         }
         sums += nc;
@@ -916,6 +945,24 @@ bool ortho_in_range(int steps, const float* coeff) {
     return true;
 }
 
+namespace {
+
+// Up to as many tiles as the chip has CUs, a tile's time is that of its own
+// loads: four stages, three of them under way, instead of two.
+constexpr int64_t kFewTiles = 256;
+
+template <int KIND, int PRODUCTS, int RUN, bool BRIEF = false>
+void launch_product(GemmArgs& a, const Outs& outs, const OrthoList& list, uint32_t K, hipStream_t s) {
+    if (list.n == 0) return;
+    a.tiles = list.d;
+    if (static_cast<int64_t>(list.n) * K <= kFewTiles)
+        ortho_gemm_kernel<KIND, PRODUCTS, RUN, 4, BRIEF><<<dim3(list.n, K), 256, 0, s>>>(a, outs);
+    else
+        ortho_gemm_kernel<KIND, PRODUCTS, RUN, 2, BRIEF><<<dim3(list.n, K), 256, 0, s>>>(a, outs);
+}
+
+}  // namespace
+
 hipError_t launch_ortho(const tc_ortho* o, const void* const* g, int g_dtype, float* const* m, float mu, int nesterov,
                         void* const* out, int out_dtype, int steps, const float* coeff, float eps, void* workspace,
                         hipStream_t s) {
@@ -961,26 +1008,21 @@ hipError_t launch_ortho(const tc_ortho* o, const void* const* g, int g_dtype, fl
     a.ws = u.ws;
     a.copy_bytes = o->copy_bytes;
     a.out_dtype = out_dtype;
-    auto launch = [&](auto kernel, const OrthoList& list) {
-        if (list.n == 0) return;
-        a.tiles = list.d;
-        kernel<<<dim3(list.n, K), 256, 0, s>>>(a, outs);
-    };
     auto gram = [&](const OrthoList& list) {
         a.op[0] = a.op[1] = {0, 0, 0, {-1, -1}, 1.0f / kScaleX, {0.0f, 0.0f}};
         if (brief)
-            launch(ortho_gemm_kernel<kGram, 1, 0>, list);
+            launch_product<kGram, 1, 0>(a, outs, list, K, s);
         else if (o->sym_pair.n)
-            launch(ortho_gemm_kernel<kGram, 3, kRun>, list);
+            launch_product<kGram, 3, kRun>(a, outs, list, K, s);
         else
-            launch(ortho_gemm_kernel<kGram, 3, 0>, list);
+            launch_product<kGram, 3, 0>(a, outs, list, K, s);
     };
     auto sym = [&](const OrthoList& list, Operation p) {
         a.op[0] = a.op[1] = p;
         if (brief || o->sym_pair.n == 0)
-            launch(ortho_gemm_kernel<kSym, 3, 0>, list);
+            launch_product<kSym, 3, 0>(a, outs, list, K, s);
         else
-            launch(ortho_gemm_kernel<kSym, 3, kRun>, list);
+            launch_product<kSym, 3, kRun>(a, outs, list, K, s);
     };
     // R = P - a I of the Gram matrix in [0]
     constexpr float kXtoP = kScaleP / kScaleX;
@@ -1000,15 +1042,15 @@ hipError_t launch_ortho(const tc_ortho* o, const void* const* g, int g_dtype, fl
             a.op[q] = {p.left, from[q], 1 - from[q], {-1, -1}, scale / kScaleP, {p.f * scale, 0.0f}};
         }
         if (last && full)
-            launch(ortho_gemm_kernel<kFinal, 3, 0>, list);
+            launch_product<kFinal, 3, 0>(a, outs, list, K, s);
         else if (last)
-            launch(ortho_gemm_kernel<kFinal, 2, 0>, list);
+            launch_product<kFinal, 2, 0>(a, outs, list, K, s);
         else if (!brief)
-            launch(ortho_gemm_kernel<kApply, 3, 0>, list);
+            launch_product<kApply, 3, 0>(a, outs, list, K, s);
         else if (full)
-            launch(ortho_gemm_kernel<kApply, 3, 0, true>, list);
+            launch_product<kApply, 3, 0, true>(a, outs, list, K, s);
         else
-            launch(ortho_gemm_kernel<kApply, 2, 0, true>, list);
+            launch_product<kApply, 2, 0, true>(a, outs, list, K, s);
     };
     // The symmetric matrices, with R = P - a I: [0] A, then P A P, then
     // S = P1 P - a1 a I; [1] R (P1's where one step is taken at a time);
