@@ -63,6 +63,7 @@ struct OrthoMat {
 
 struct OrthoTile {
     int32_t mat, i, j;
+    int32_t copy;  // of a product's tile
 };
 
 // Tiles of the products of one launch.
@@ -397,7 +398,7 @@ __global__ void __launch_bounds__(256, STAGES == 2 ? 2 : 1) ortho_gemm_kernel(co
     const OrthoTile tile = a.tiles[blockIdx.x];
     const OrthoMat& t = a.mats[tile.mat];
     const Operation& op = a.op[t.pair];
-    const int k = blockIdx.y;
+    const int k = tile.copy;
     char* base = a.ws + k * a.copy_bytes;
     const int ti = tile.i * kTile, tj = tile.j * kTile;
     // rows of the tile come from left (index in m), columns from right
@@ -440,16 +441,15 @@ __global__ void __launch_bounds__(256, STAGES == 2 ? 2 : 1) ortho_gemm_kernel(co
             if constexpr (PRODUCTS >= 2) f.bl[i] = *reinterpret_cast<const f16x8*>(p + rb + i * 4096 + lo);
         }
     };
-    auto multiply = [&](const Operands& f) {
+    // products `from` to `to` of a step: lo hi, hi lo, hi hi, four each
+    auto multiply = [&](const Operands& f, int from, int to) {
 #pragma unroll
-        for (int w = 3 - PRODUCTS; w < 3; ++w)  // lo hi, hi lo, hi hi
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(w == 0 ? f.al[i] : f.ah[i], w == 1 ? f.bl[j] : f.bh[j],
-                                                                       acc[i][j], 0, 0, 0);
+        for (int n = from; n < to; ++n) {
+            const int w = 3 - PRODUCTS + n / 4, i = n / 2 % 2, j = n % 2;
+            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(w == 0 ? f.al[i] : f.ah[i], w == 1 ? f.bl[j] : f.bh[j], acc[i][j], 0, 0, 0);
+        }
     };
+    constexpr int kAll = 4 * PRODUCTS, kFirst = PRODUCTS == 1 ? 2 : 4;
     // the loads of the oldest stage under way are done, in every wave; and
     // every wave has read its operands of the stage before
     auto arrive = [&] {
@@ -464,17 +464,22 @@ __global__ void __launch_bounds__(256, STAGES == 2 ? 2 : 1) ortho_gemm_kernel(co
     read(now, 0, 0);
     int buf = 0;
     for (int st = 0; st < stages; ++st) {
-        // Each step's products are issued while the next one's operands are on
-        // their way from LDS.  The buffer that the stage before this one left
+        // The next step's operands are read after the first products of a
+        // step, and arrive under the others (asked for before them, the wait
+        // for the step's own operands would be for these too).  The buffer that the stage before this one left
         // is loaded with the stage STAGES - 1 ahead (past the end the last one
         // again, so that the count of loads under way stays the same).
         if (STAGES > 2 || st + 1 < stages) fetch(min(st + STAGES - 1, stages - 1), buf == 0 ? STAGES - 1 : buf - 1);
         const int then = buf + 1 == STAGES ? 0 : buf + 1;
 #pragma unroll
         for (int step = 0; step < kSteps; step += 2) {
+            multiply(now, 0, kFirst);
+            __builtin_amdgcn_sched_barrier(0);
             read(next, buf, step + 1);
             __builtin_amdgcn_sched_barrier(0);
-            multiply(now);
+            multiply(now, kFirst, kAll);
+            __builtin_amdgcn_sched_barrier(0);
+            multiply(next, 0, kFirst);
             __builtin_amdgcn_sched_barrier(0);
             if (step + 2 < kSteps) {
                 read(now, buf, step + 2);
@@ -483,7 +488,7 @@ __global__ void __launch_bounds__(256, STAGES == 2 ? 2 : 1) ortho_gemm_kernel(co
                 read(now, then, 0);
             }
             __builtin_amdgcn_sched_barrier(0);
-            multiply(next);
+            multiply(next, kFirst, kAll);
             __builtin_amdgcn_sched_barrier(0);
         }
         buf = then;
@@ -754,12 +759,62 @@ __global__ void __launch_bounds__(kSmallThreads) ortho_small_kernel(const SmallA
     }
 }
 
-// Appended to a list of tiles in the order they are launched.
-void order_by(std::vector<OrthoTile>& v, const std::vector<OrthoMat>& mats, bool along_n) {
-    std::stable_sort(v.begin(), v.end(), [&](const OrthoTile& x, const OrthoTile& y) {
-        const OrthoMat &a = mats[x.mat], &b = mats[y.mat];
-        return (along_n ? a.np : a.mp) > (along_n ? b.np : b.mp);
+// The tiles of one product of the given matrices, all copies, in the order they
+// are launched.  Workgroup w of a launch runs on XCD w % 8, each with an L2 of
+// its own, so tiles that share rows belong on one: squares of up to 8 x 8
+// tiles (16 panels of rows for 64 tiles) go to the XCD with the least to do so
+// far, those with the longest sums first.  A square is cut where it is more
+// than an eighth of an XCD's share.
+enum Which { kAlongN, kAlongM, kAcross };  // X X^T, products of symmetric matrices, P X
+std::vector<OrthoTile> tiles_of(const std::vector<OrthoMat>& mats, const std::vector<int32_t>& of, int K, Which which) {
+    struct Chunk {
+        int64_t cost;
+        int32_t len;
+        std::vector<OrthoTile> tiles;
+    };
+    auto length = [&](const OrthoMat& t) { return which == kAlongN ? t.np : t.mp; };
+    int64_t total = 0, count = 0;
+    for (int32_t t : of) {
+        const int64_t mi = mats[t].mp / kTile, ni = mats[t].np / kTile;
+        const int64_t n = which == kAcross ? mi * ni : mi * (mi + 1) / 2;
+        count += n * K;
+        total += n * K * length(mats[t]);
+    }
+    std::vector<Chunk> chunks;
+    for (int32_t t : of) {
+        const int32_t mi = mats[t].mp / kTile, nj = which == kAcross ? mats[t].np / kTile : mi, len = length(mats[t]);
+        for (int32_t k = 0; k < K; ++k)
+            for (int32_t j0 = 0; j0 < nj; j0 += 8)
+                for (int32_t i0 = 0; i0 < mi; i0 += 8) {
+                    chunks.push_back({0, len, {}});
+                    for (int32_t j = j0; j < std::min(j0 + 8, nj); ++j)
+                        for (int32_t i = i0; i < std::min(i0 + 8, mi); ++i) {
+                            if (which != kAcross && j > i) continue;
+                            if (chunks.back().cost + len > total / 64 && chunks.back().cost > 0) chunks.push_back({0, len, {}});
+                            chunks.back().tiles.push_back({t, i, j, k});
+                            chunks.back().cost += len;
+                        }
+                }
+    }
+    std::stable_sort(chunks.begin(), chunks.end(), [](const Chunk& x, const Chunk& y) {
+        return x.len != y.len ? x.len > y.len : x.cost > y.cost;
     });
+    std::vector<OrthoTile> queue[8], out;
+    int64_t load[8] = {};
+    for (Chunk& c : chunks) {
+        const int x = static_cast<int>(std::min_element(load, load + 8) - load);
+        load[x] += c.cost;
+        queue[x].insert(queue[x].end(), c.tiles.begin(), c.tiles.end());
+    }
+    size_t at[8] = {};
+    for (int64_t w = 0; w < count; ++w) {
+        size_t x = w % 8;
+        if (at[x] == queue[x].size())  // the others' are left: from the longest
+            for (size_t y = x = 0; y < 8; ++y)
+                if (queue[y].size() - at[y] > queue[x].size() - at[x]) x = y;
+        out.push_back(queue[x][at[x]++]);
+    }
+    return out;
 }
 
 // Whether a matrix takes two steps to a Gram matrix.  Two steps take
@@ -781,7 +836,8 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
     o->g = g;
     o->K = K;
     o->mats.resize(g->n);
-    std::vector<OrthoTile> chunks, split, gram[2], sym[2], apply[2];  // by OrthoMat::pair
+    std::vector<OrthoTile> chunks, split;
+    std::vector<int32_t> large[2];  // by OrthoMat::pair
     std::vector<int32_t> small[2];
     int64_t bytes = 0, sums = 0;
     auto take = [&](int64_t n) {
@@ -812,7 +868,7 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
         const bool matrix = q.size > 0 && rows[t] > 0;
         const bool whole = matrix && lds_of(t) <= most;
         if (!whole)
-            for (int64_t i = 0; i < nc; ++i) chunks.push_back({t, static_cast<int32_t>(i), 0});
+            for (int64_t i = 0; i < nc; ++i) chunks.push_back({t, static_cast<int32_t>(i), 0, 0});
         if (!matrix) continue;
         q.rows = static_cast<int32_t>(rows[t]);
         q.cols = static_cast<int32_t>(cols[t]);
@@ -835,27 +891,21 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
         q.xt[1] = take(x);
         for (auto& v : q.s) v = take(s);
         for (int32_t i = 0; i < q.mp / 64; ++i)
-            for (int32_t j = 0; j < q.np / 64; ++j) split.push_back({t, i, j});
-        for (int32_t i = 0; i < q.mp / kTile; ++i)
-            for (int32_t j = 0; j <= i; ++j) sym[q.pair].push_back({t, i, j});
-        for (int32_t j = 0; j < q.np / kTile; ++j)
-            for (int32_t i = 0; i < q.mp / kTile; ++i) apply[q.pair].push_back({t, i, j});
+            for (int32_t j = 0; j < q.np / 64; ++j) split.push_back({t, i, j, 0});
+        large[q.pair].push_back(t);
     }
     o->sums = take(sums * 8);
     o->norms = take(static_cast<int64_t>(o->matrices) * 8);  // (nothing if there is no large matrix)
     o->copy_bytes = bytes;
-    for (int i = 0; i < 2; ++i) gram[i] = sym[i];
-    std::vector<OrthoTile> all[3];
-    std::vector<OrthoTile>* kinds[3] = {gram, sym, apply};
-    for (int i = 0; i < 3; ++i) {
-        all[i] = kinds[i][0];
-        all[i].insert(all[i].end(), kinds[i][1].begin(), kinds[i][1].end());
-        // the longest sums first
-        order_by(all[i], o->mats, i == 0);
-        for (int q = 0; q < 2; ++q) order_by(kinds[i][q], o->mats, i == 0);
-    }
-    for (const auto* v : {&chunks, &split, &all[1], &all[2]})
-        if (v->size() >= (size_t{1} << 32) / 256) {  // workgroups of 256 in one dimension of a grid
+    std::vector<int32_t> all = large[0];
+    all.insert(all.end(), large[1].begin(), large[1].end());
+    const std::vector<OrthoTile> lists[] = {
+        chunks, split,
+        tiles_of(o->mats, all, K, kAlongN), tiles_of(o->mats, all, K, kAlongM), tiles_of(o->mats, all, K, kAcross),
+        tiles_of(o->mats, large[1], K, kAlongM),
+        tiles_of(o->mats, large[0], K, kAlongN), tiles_of(o->mats, large[0], K, kAlongM), tiles_of(o->mats, large[0], K, kAcross)};
+    for (const auto& v : lists)
+        if (v.size() >= (size_t{1} << 32) / 256) {  // workgroups of 256 in one dimension of a grid
             delete o;
             *e = hipErrorInvalidValue;
             return nullptr;
@@ -874,10 +924,9 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
     const size_t at_of = put(o->of.data(), o->of.size() * 4);
     size_t at_small[2];
     for (int i = 0; i < 2; ++i) at_small[i] = put(small[i].data(), small[i].size() * 4);
-    const std::vector<OrthoTile>* lists[] = {&chunks, &split, &all[0], &all[1], &all[2], &sym[1], &gram[0], &sym[0], &apply[0]};
     constexpr int kLists = sizeof lists / sizeof *lists;
     size_t at[kLists];
-    for (int i = 0; i < kLists; ++i) at[i] = put(lists[i]->data(), lists[i]->size() * sizeof(OrthoTile));
+    for (int i = 0; i < kLists; ++i) at[i] = put(lists[i].data(), lists[i].size() * sizeof(OrthoTile));
     if ((*e = hipMalloc(&o->d_blob, host.size())) != hipSuccess ||
         (*e = hipMemcpy(o->d_blob, host.data(), host.size(), hipMemcpyHostToDevice)) != hipSuccess) {
         destroy_ortho(o);
@@ -893,7 +942,7 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
     o->d_chunks = reinterpret_cast<const OrthoTile*>(d + at[0]);
     o->d_split = reinterpret_cast<const OrthoTile*>(d + at[1]);
     OrthoList* to[] = {&o->gram, &o->sym, &o->apply, &o->sym_pair, &o->gram_one, &o->sym_one, &o->apply_one};
-    for (int i = 2; i < kLists; ++i) *to[i - 2] = {reinterpret_cast<const OrthoTile*>(d + at[i]), static_cast<int32_t>(lists[i]->size())};
+    for (int i = 2; i < kLists; ++i) *to[i - 2] = {reinterpret_cast<const OrthoTile*>(d + at[i]), static_cast<int32_t>(lists[i].size())};
     return o;
 }
 
@@ -949,16 +998,16 @@ namespace {
 
 // Up to as many tiles as the chip has CUs, a tile's time is that of its own
 // loads: four stages, three of them under way, instead of two.
-constexpr int64_t kFewTiles = 256;
+constexpr int32_t kFewTiles = 256;
 
 template <int KIND, int PRODUCTS, int RUN, bool BRIEF = false>
-void launch_product(GemmArgs& a, const Outs& outs, const OrthoList& list, uint32_t K, hipStream_t s) {
+void launch_product(GemmArgs& a, const Outs& outs, const OrthoList& list, hipStream_t s) {
     if (list.n == 0) return;
     a.tiles = list.d;
-    if (static_cast<int64_t>(list.n) * K <= kFewTiles)
-        ortho_gemm_kernel<KIND, PRODUCTS, RUN, 4, BRIEF><<<dim3(list.n, K), 256, 0, s>>>(a, outs);
+    if (list.n <= kFewTiles)
+        ortho_gemm_kernel<KIND, PRODUCTS, RUN, 4, BRIEF><<<list.n, 256, 0, s>>>(a, outs);
     else
-        ortho_gemm_kernel<KIND, PRODUCTS, RUN, 2, BRIEF><<<dim3(list.n, K), 256, 0, s>>>(a, outs);
+        ortho_gemm_kernel<KIND, PRODUCTS, RUN, 2, BRIEF><<<list.n, 256, 0, s>>>(a, outs);
 }
 
 }  // namespace
@@ -1011,18 +1060,18 @@ hipError_t launch_ortho(const tc_ortho* o, const void* const* g, int g_dtype, fl
     auto gram = [&](const OrthoList& list) {
         a.op[0] = a.op[1] = {0, 0, 0, {-1, -1}, 1.0f / kScaleX, {0.0f, 0.0f}};
         if (brief)
-            launch_product<kGram, 1, 0>(a, outs, list, K, s);
+            launch_product<kGram, 1, 0>(a, outs, list, s);
         else if (o->sym_pair.n)
-            launch_product<kGram, 3, kRun>(a, outs, list, K, s);
+            launch_product<kGram, 3, kRun>(a, outs, list, s);
         else
-            launch_product<kGram, 3, 0>(a, outs, list, K, s);
+            launch_product<kGram, 3, 0>(a, outs, list, s);
     };
     auto sym = [&](const OrthoList& list, Operation p) {
         a.op[0] = a.op[1] = p;
         if (brief || o->sym_pair.n == 0)
-            launch_product<kSym, 3, 0>(a, outs, list, K, s);
+            launch_product<kSym, 3, 0>(a, outs, list, s);
         else
-            launch_product<kSym, 3, kRun>(a, outs, list, K, s);
+            launch_product<kSym, 3, kRun>(a, outs, list, s);
     };
     // R = P - a I of the Gram matrix in [0]
     constexpr float kXtoP = kScaleP / kScaleX;
@@ -1042,15 +1091,15 @@ hipError_t launch_ortho(const tc_ortho* o, const void* const* g, int g_dtype, fl
             a.op[q] = {p.left, from[q], 1 - from[q], {-1, -1}, scale / kScaleP, {p.f * scale, 0.0f}};
         }
         if (last && full)
-            launch_product<kFinal, 3, 0>(a, outs, list, K, s);
+            launch_product<kFinal, 3, 0>(a, outs, list, s);
         else if (last)
-            launch_product<kFinal, 2, 0>(a, outs, list, K, s);
+            launch_product<kFinal, 2, 0>(a, outs, list, s);
         else if (!brief)
-            launch_product<kApply, 3, 0>(a, outs, list, K, s);
+            launch_product<kApply, 3, 0>(a, outs, list, s);
         else if (full)
-            launch_product<kApply, 3, 0, true>(a, outs, list, K, s);
+            launch_product<kApply, 3, 0, true>(a, outs, list, s);
         else
-            launch_product<kApply, 2, 0, true>(a, outs, list, K, s);
+            launch_product<kApply, 2, 0, true>(a, outs, list, s);
     };
     // The symmetric matrices, with R = P - a I: [0] A, then P A P, then
     // S = P1 P - a1 a I; [1] R (P1's where one step is taken at a time);
