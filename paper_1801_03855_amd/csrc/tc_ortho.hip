@@ -66,10 +66,11 @@ struct OrthoTile {
     int32_t copy;  // of a product's tile
 };
 
-// Tiles of the products of one launch.
+// Tiles of the products of one launch, and their side.
 struct OrthoList {
     const OrthoTile* d = nullptr;
     int32_t n = 0;
+    int32_t side = 0;
 };
 
 }  // namespace tc
@@ -108,7 +109,7 @@ typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kChunk = 4096;  // elements of a workgroup of the first pass
-constexpr int kTile = 128;    // rows and columns of a product's tile
+constexpr int kTile = 128;    // rows and columns of a product's larger tile
 constexpr int kBlock = 32;    // elements of a block of hi and lo
 constexpr float kScaleX = 4096.0f, kScaleP = 1024.0f;
 constexpr int kRun = 4;       // stages summed in the matrix cores at a time, where sums are kept apart
@@ -377,21 +378,24 @@ struct Outs {
 typedef __attribute__((address_space(3))) char lds_char;
 typedef __attribute__((address_space(1))) const char global_char;
 
-// One 128 x 128 tile of left right^T, both with rows along the summed axis:
-// four waves with 64 x 64 each, as 2 x 2 of 32 x 32 x 16 products.
+// One tile of left right^T, both with rows along the summed axis, of four waves
+// with a quarter each, as 32 x 32 x 16 products: 128 x 128, or 64 x 64 where
+// the larger tiles would be fewer than the CUs.
 //
 // PRODUCTS: 3, hi hi + hi lo + lo hi; 2, without lo of left; 1, hi hi.  RUN:
 // blocks summed in the matrix cores at a time, 0 for all.
 //
-// A stage is 128 bytes of each of the 256 rows: a block of 32 elements, hi and
-// lo, or with one product 64 elements' hi, which is all that X [m][n] then has
-// (kApply: BRIEF).  STAGES buffers of LDS take turns, each loaded straight
-// from memory while others are multiplied.  A row's 128 bytes are eight 16-byte pieces; piece p of row r
+// A stage is 128 bytes of each of the 2 TILE rows: a block of 32 elements, hi
+// and lo, or with one product 64 elements' hi, which is all that X [m][n] then
+// has (kApply: BRIEF).  64 KB of LDS hold two or four stages, which are loaded
+// straight from memory while others are multiplied, so that a CU takes two
+// workgroups.  A row's 128 bytes are eight 16-byte pieces; piece p of row r
 // lies at p ^ (r / 2 % 8), so that 16 lanes reading one piece each of 16 rows
 // touch all 64 banks once.
-template <int KIND, int PRODUCTS, int RUN, int STAGES, bool BRIEF = false>
-__global__ void __launch_bounds__(256, STAGES == 2 ? 2 : 1) ortho_gemm_kernel(const GemmArgs a, const Outs outs) {
-    constexpr int kHalf = kTile * 128, kStage = 2 * kHalf;
+template <int KIND, int PRODUCTS, int RUN, int TILE, bool BRIEF = false>
+__global__ void __launch_bounds__(256, 2) ortho_gemm_kernel(const GemmArgs a, const Outs outs) {
+    constexpr int kHalf = TILE * 128, kStage = 2 * kHalf, STAGES = 65536 / kStage;
+    constexpr int kSide = TILE / 64, kLoads = TILE / 32;  // 32 x 32 products of a wave each way; loads of each operand
     constexpr int kSteps = PRODUCTS == 1 ? 4 : 2;  // products of 16 elements in a stage
     constexpr bool kLong = KIND == kApply || KIND == kFinal;
     __shared__ __attribute__((aligned(16))) char lds[STAGES * kStage];
@@ -400,60 +404,61 @@ __global__ void __launch_bounds__(256, STAGES == 2 ? 2 : 1) ortho_gemm_kernel(co
     const Operation& op = a.op[t.pair];
     const int k = tile.copy;
     char* base = a.ws + k * a.copy_bytes;
-    const int ti = tile.i * kTile, tj = tile.j * kTile;
+    const int ti = tile.i * TILE, tj = tile.j * TILE;
     // rows of the tile come from left (index in m), columns from right
     const int len = KIND == kGram ? t.np : t.mp;  // of the summed axis
     const uint32_t ld = static_cast<uint32_t>(len) * (PRODUCTS == 1 ? 2 : 4);
     const char* left = base + (KIND == kGram ? t.x : t.s[op.left]) + static_cast<int64_t>(ti) * ld;
     const char* right = base + (KIND == kGram ? t.x : kLong ? t.xt[op.right] : t.s[op.right]) + static_cast<int64_t>(tj) * ld;
     const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
-    const int wr = wave / 2 * 64, wc = wave % 2 * 64;
-    // this wave's eight 1,024-byte pieces of a stage: eight rows each
-    uint32_t off[4];
+    const int wr = wave / 2 * (TILE / 2), wc = wave % 2 * (TILE / 2);
+    // this wave's 1,024-byte pieces of a stage: eight rows each
+    uint32_t off[kLoads];
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        const int r = (wave * 4 + q) * 8 + lane / 8, p = (lane % 8) ^ (r / 2 % 8);
+    for (int q = 0; q < kLoads; ++q) {
+        const int r = (wave * kLoads + q) * 8 + lane / 8, p = (lane % 8) ^ (r / 2 % 8);
         off[q] = static_cast<uint32_t>(r) * ld + static_cast<uint32_t>(p) * 16;
     }
     auto fetch = [&](int stage, int buf) {
         const int64_t at = static_cast<int64_t>(stage) * 128;
-        char* to = lds + buf * kStage + wave * 4096;
+        char* to = lds + buf * kStage + wave * kLoads * 1024;
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
+        for (int q = 0; q < kLoads; ++q)
             __builtin_amdgcn_global_load_lds((global_char*)(left + at + off[q]), (lds_char*)(to + q * 1024), 16, 0, 0);
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
+        for (int q = 0; q < kLoads; ++q)
             __builtin_amdgcn_global_load_lds((global_char*)(right + at + off[q]), (lds_char*)(to + kHalf + q * 1024), 16, 0, 0);
     };
-    f32x16 acc[2][2] = {}, sum[RUN ? 2 : 1][RUN ? 2 : 1] = {};
+    f32x16 acc[kSide][kSide] = {}, sum[RUN ? kSide : 1][RUN ? kSide : 1] = {};
     struct Operands {
-        f16x8 ah[2], al[2], bh[2], bl[2];
+        f16x8 ah[kSide], al[kSide], bh[kSide], bl[kSide];
     } now, next;
     const int ra = (wr + lane % 32) * 128, rb = kHalf + (wc + lane % 32) * 128, turn = lane / 2 % 8;
     auto read = [&](Operands& f, int buf, int step) {
         const char* p = lds + buf * kStage;
         const int hi = ((step * 2 + lane / 32) ^ turn) * 16, lo = ((step * 2 + lane / 32 + 4) ^ turn) * 16;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kSide; ++i) {
             f.ah[i] = *reinterpret_cast<const f16x8*>(p + ra + i * 4096 + hi);
             f.bh[i] = *reinterpret_cast<const f16x8*>(p + rb + i * 4096 + hi);
             if constexpr (PRODUCTS == 3) f.al[i] = *reinterpret_cast<const f16x8*>(p + ra + i * 4096 + lo);
             if constexpr (PRODUCTS >= 2) f.bl[i] = *reinterpret_cast<const f16x8*>(p + rb + i * 4096 + lo);
         }
     };
-    // products `from` to `to` of a step: lo hi, hi lo, hi hi, four each
+    // products `from` to `to` of a step: lo hi, hi lo, hi hi of every place
     auto multiply = [&](const Operands& f, int from, int to) {
 #pragma unroll
         for (int n = from; n < to; ++n) {
-            const int w = 3 - PRODUCTS + n / 4, i = n / 2 % 2, j = n % 2;
+            constexpr int kOne = kSide * kSide;
+            const int w = 3 - PRODUCTS + n / kOne, i = n / kSide % kSide, j = n % kSide;
             acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(w == 0 ? f.al[i] : f.ah[i], w == 1 ? f.bl[j] : f.bh[j], acc[i][j], 0, 0, 0);
         }
     };
-    constexpr int kAll = 4 * PRODUCTS, kFirst = PRODUCTS == 1 ? 2 : 4;
+    constexpr int kAll = kSide * kSide * PRODUCTS, kFirst = (kAll + 2) / 3;
     // the loads of the oldest stage under way are done, in every wave; and
     // every wave has read its operands of the stage before
     auto arrive = [&] {
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 2) * 8) : "memory");
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES - 2) * 2 * kLoads) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
@@ -495,9 +500,9 @@ __global__ void __launch_bounds__(256, STAGES == 2 ? 2 : 1) ortho_gemm_kernel(co
         if constexpr (RUN > 0) {
             if (st % RUN == RUN - 1) {  // stages is a multiple of RUN
 #pragma unroll
-                for (int i = 0; i < 2; ++i)
+                for (int i = 0; i < kSide; ++i)
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) {
+                    for (int j = 0; j < kSide; ++j) {
                         sum[i][j] += acc[i][j];
                         acc[i][j] = f32x16{};
                     }
@@ -509,14 +514,14 @@ __global__ void __launch_bounds__(256, STAGES == 2 ? 2 : 1) ortho_gemm_kernel(co
         else return acc;
     }();
     // The tile through LDS, so that both orders leave in whole lines: column c
-    // holds its 128 rows as 32 pieces of four, piece p at p ^ (c % 32).
+    // holds its rows as TILE / 4 pieces of four, piece p at p ^ (c % (TILE / 4)).
     __syncthreads();
     float* tiled = reinterpret_cast<float*>(lds);
-    auto piece = [&](int c, int p) { return c * kTile + (p ^ (c % 32)) * 4; };
+    auto piece = [&](int c, int p) { return c * TILE + (p ^ (c % (TILE / 4))) * 4; };
 #pragma unroll
-    for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < kSide; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < kSide; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 // a lane has rows r .. r + 3 of one column in four consecutive registers
@@ -529,9 +534,10 @@ __global__ void __launch_bounds__(256, STAGES == 2 ? 2 : 1) ortho_gemm_kernel(co
     __syncthreads();
     const int64_t ld_m = static_cast<int64_t>(t.mp) * 4, ld_n = static_cast<int64_t>(t.np) * 4;
     const bool natural = kLong ? KIND == kApply || !t.flip : tile.i != tile.j;
-    // 16 lanes a column, eight rows each
-    for (int c = tid / 16; c < kTile; c += 16) {
-        const int r = tid % 16 * 8;
+    // eight rows of a column a lane
+    constexpr int kEights = TILE / 8;
+    for (int c = tid / kEights; c < TILE; c += 256 / kEights) {
+        const int r = tid % kEights * 8;
         float v[8];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -578,8 +584,8 @@ __global__ void __launch_bounds__(256, STAGES == 2 ? 2 : 1) ortho_gemm_kernel(co
     if (!natural) return;
     __syncthreads();
     // four lanes a row's block of 32 columns, eight each
-    for (int q = tid / 4; q < kTile * (kTile / kBlock); q += 64) {
-        const int r = q % kTile, c = q / kTile * kBlock + tid % 4 * 8;
+    for (int q = tid / 4; q < TILE * (TILE / kBlock); q += 64) {
+        const int r = q % TILE, c = q / TILE * kBlock + tid % 4 * 8;
         uint32_t u[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) u[e] = reinterpret_cast<uint32_t*>(tiled)[piece(c + e, r / 4) + r % 4];
@@ -765,30 +771,43 @@ __global__ void __launch_bounds__(kSmallThreads) ortho_small_kernel(const SmallA
 // tiles (16 panels of rows for 64 tiles) go to the XCD with the least to do so
 // far, those with the longest sums first.  A square is cut where it is more
 // than an eighth of an XCD's share.
+//
+// The tiles are 64 x 64 where 128 x 128 ones would leave the chip waiting for
+// the longest: where all tiles' sums, shared by the 256 CUs, are less than 7/8
+// of the longest sum.  (A block of 32 elements takes a CU about 0.7 us in a
+// large tile that it has to itself, 0.8 us in four small ones.  1,024 x 1,024,
+// one copy, 36 tiles a launch: 436 us with large tiles, 207 with small ones.
+// 2,048 x 2,048: 136 tiles of symmetric products, small; 256 of P X, large.)
 enum Which { kAlongN, kAlongM, kAcross };  // X X^T, products of symmetric matrices, P X
-std::vector<OrthoTile> tiles_of(const std::vector<OrthoMat>& mats, const std::vector<int32_t>& of, int K, Which which) {
+std::vector<OrthoTile> tiles_of(const std::vector<OrthoMat>& mats, const std::vector<int32_t>& of, int K, Which which, int* side) {
     struct Chunk {
         int64_t cost;
         int32_t len;
         std::vector<OrthoTile> tiles;
     };
     auto length = [&](const OrthoMat& t) { return which == kAlongN ? t.np : t.mp; };
-    int64_t total = 0, count = 0;
-    for (int32_t t : of) {
-        const int64_t mi = mats[t].mp / kTile, ni = mats[t].np / kTile;
-        const int64_t n = which == kAcross ? mi * ni : mi * (mi + 1) / 2;
-        count += n * K;
-        total += n * K * length(mats[t]);
+    int64_t total, count, longest = 0;
+    for (*side = kTile;; *side = kTile / 2) {
+        total = count = 0;
+        for (int32_t t : of) {
+            const int64_t mi = mats[t].mp / *side, ni = mats[t].np / *side;
+            const int64_t n = which == kAcross ? mi * ni : mi * (mi + 1) / 2;
+            count += n * K;
+            total += n * K * length(mats[t]);
+            longest = std::max<int64_t>(longest, length(mats[t]));
+        }
+        if (*side < kTile || total * 8 > longest * 256 * 7) break;
     }
+    const int32_t across = 8 * kTile / *side;  // tiles of a square
     std::vector<Chunk> chunks;
     for (int32_t t : of) {
-        const int32_t mi = mats[t].mp / kTile, nj = which == kAcross ? mats[t].np / kTile : mi, len = length(mats[t]);
+        const int32_t mi = mats[t].mp / *side, nj = which == kAcross ? mats[t].np / *side : mi, len = length(mats[t]);
         for (int32_t k = 0; k < K; ++k)
-            for (int32_t j0 = 0; j0 < nj; j0 += 8)
-                for (int32_t i0 = 0; i0 < mi; i0 += 8) {
+            for (int32_t j0 = 0; j0 < nj; j0 += across)
+                for (int32_t i0 = 0; i0 < mi; i0 += across) {
                     chunks.push_back({0, len, {}});
-                    for (int32_t j = j0; j < std::min(j0 + 8, nj); ++j)
-                        for (int32_t i = i0; i < std::min(i0 + 8, mi); ++i) {
+                    for (int32_t j = j0; j < std::min(j0 + across, nj); ++j)
+                        for (int32_t i = i0; i < std::min(i0 + across, mi); ++i) {
                             if (which != kAcross && j > i) continue;
                             if (chunks.back().cost + len > total / 64 && chunks.back().cost > 0) chunks.push_back({0, len, {}});
                             chunks.back().tiles.push_back({t, i, j, k});
@@ -899,11 +918,13 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
     o->copy_bytes = bytes;
     std::vector<int32_t> all = large[0];
     all.insert(all.end(), large[1].begin(), large[1].end());
+    int side[9] = {};
     const std::vector<OrthoTile> lists[] = {
         chunks, split,
-        tiles_of(o->mats, all, K, kAlongN), tiles_of(o->mats, all, K, kAlongM), tiles_of(o->mats, all, K, kAcross),
-        tiles_of(o->mats, large[1], K, kAlongM),
-        tiles_of(o->mats, large[0], K, kAlongN), tiles_of(o->mats, large[0], K, kAlongM), tiles_of(o->mats, large[0], K, kAcross)};
+        tiles_of(o->mats, all, K, kAlongN, &side[2]), tiles_of(o->mats, all, K, kAlongM, &side[3]),
+        tiles_of(o->mats, all, K, kAcross, &side[4]), tiles_of(o->mats, large[1], K, kAlongM, &side[5]),
+        tiles_of(o->mats, large[0], K, kAlongN, &side[6]), tiles_of(o->mats, large[0], K, kAlongM, &side[7]),
+        tiles_of(o->mats, large[0], K, kAcross, &side[8])};
     for (const auto& v : lists)
         if (v.size() >= (size_t{1} << 32) / 256) {  // workgroups of 256 in one dimension of a grid
             delete o;
@@ -942,7 +963,7 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
     o->d_chunks = reinterpret_cast<const OrthoTile*>(d + at[0]);
     o->d_split = reinterpret_cast<const OrthoTile*>(d + at[1]);
     OrthoList* to[] = {&o->gram, &o->sym, &o->apply, &o->sym_pair, &o->gram_one, &o->sym_one, &o->apply_one};
-    for (int i = 2; i < kLists; ++i) *to[i - 2] = {reinterpret_cast<const OrthoTile*>(d + at[i]), static_cast<int32_t>(lists[i].size())};
+    for (int i = 2; i < kLists; ++i) *to[i - 2] = {reinterpret_cast<const OrthoTile*>(d + at[i]), static_cast<int32_t>(lists[i].size()), side[i]};
     return o;
 }
 
@@ -996,18 +1017,14 @@ bool ortho_in_range(int steps, const float* coeff) {
 
 namespace {
 
-// Up to as many tiles as the chip has CUs, a tile's time is that of its own
-// loads: four stages, three of them under way, instead of two.
-constexpr int32_t kFewTiles = 256;
-
 template <int KIND, int PRODUCTS, int RUN, bool BRIEF = false>
 void launch_product(GemmArgs& a, const Outs& outs, const OrthoList& list, hipStream_t s) {
     if (list.n == 0) return;
     a.tiles = list.d;
-    if (list.n <= kFewTiles)
-        ortho_gemm_kernel<KIND, PRODUCTS, RUN, 4, BRIEF><<<list.n, 256, 0, s>>>(a, outs);
+    if (list.side == kTile)
+        ortho_gemm_kernel<KIND, PRODUCTS, RUN, kTile, BRIEF><<<list.n, 256, 0, s>>>(a, outs);
     else
-        ortho_gemm_kernel<KIND, PRODUCTS, RUN, 2, BRIEF><<<list.n, 256, 0, s>>>(a, outs);
+        ortho_gemm_kernel<KIND, PRODUCTS, RUN, kTile / 2, BRIEF><<<list.n, 256, 0, s>>>(a, outs);
 }
 
 }  // namespace
