@@ -284,12 +284,19 @@ __device__ __forceinline__ void put8_hi(char* row, int e, const uint32_t* v) {
     *reinterpret_cast<u32x4*>(row + static_cast<int64_t>(e) * 2) = hi;
 }
 
-// v += f times elements e .. e + 7 of a row.
-__device__ __forceinline__ void add8(const char* row, int e, float f, float* v) {
+// Elements e .. e + 7 of a row, and v += f times them.
+struct Eight {
+    f16x8 hi, lo;
+};
+
+__device__ __forceinline__ Eight get8(const char* row, int e) {
     const char* p = row + e / kBlock * 128 + e % kBlock * 2;
-    const f16x8 hi = *reinterpret_cast<const f16x8*>(p), lo = *reinterpret_cast<const f16x8*>(p + 64);
+    return {*reinterpret_cast<const f16x8*>(p), *reinterpret_cast<const f16x8*>(p + 64)};
+}
+
+__device__ __forceinline__ void add8(const Eight& x, float f, float* v) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = fmaf(f, static_cast<float>(hi[i]) + static_cast<float>(lo[i]), v[i]);
+    for (int i = 0; i < 8; ++i) v[i] = fmaf(f, static_cast<float>(x.hi[i]) + static_cast<float>(x.lo[i]), v[i]);
 }
 
 // X and its transpose from u: 64 x 64 tiles through LDS.
@@ -357,7 +364,7 @@ enum Kind {
 // is dst.
 struct Operation {
     int32_t left, right, dst;
-    int32_t add[2];  // symmetric matrices added; -1: none
+    int32_t add[2];  // symmetric matrices added to a symmetric product; second -1: none
     float factor;    // of the product, to the scale of the result
     float f[2];      // of what is added
 };
@@ -513,6 +520,22 @@ __global__ void __launch_bounds__(256, 2) ortho_gemm_kernel(const GemmArgs a, co
         if constexpr (RUN > 0) return sum;
         else return acc;
     }();
+    // eight rows of a column a lane, `kTurns` times: what is added to them is
+    // loaded while the tile goes through LDS
+    constexpr int kEights = TILE / 8, kTurns = TILE * kEights / 256;
+    const int64_t ld_m = static_cast<int64_t>(t.mp) * 4, ld_n = static_cast<int64_t>(t.np) * 4;
+    const int col0 = tid / kEights, r8 = tid % kEights * 8;
+    Eight extra[KIND == kSym ? 2 : 1][kTurns];
+#pragma unroll
+    for (int n = 0; n < kTurns; ++n) {
+        const int64_t at = (tj + col0 + n * (256 / kEights)) * ld_m;
+        if constexpr (kLong) extra[0][n] = get8(base + t.xt[op.right] + at, ti + r8);
+        if constexpr (KIND == kSym) {
+            // (a symmetric matrix: its row tj + c)
+            extra[0][n] = get8(base + t.s[op.add[0]] + at, ti + r8);
+            if (op.add[1] >= 0) extra[KIND == kSym][n] = get8(base + t.s[op.add[1]] + at, ti + r8);
+        }
+    }
     // The tile through LDS, so that both orders leave in whole lines: column c
     // holds its rows as TILE / 4 pieces of four, piece p at p ^ (c % (TILE / 4)).
     __syncthreads();
@@ -532,12 +555,10 @@ __global__ void __launch_bounds__(256, 2) ortho_gemm_kernel(const GemmArgs a, co
                 *reinterpret_cast<f32x4*>(tiled + piece(c, r / 4)) = v;
             }
     __syncthreads();
-    const int64_t ld_m = static_cast<int64_t>(t.mp) * 4, ld_n = static_cast<int64_t>(t.np) * 4;
     const bool natural = kLong ? KIND == kApply || !t.flip : tile.i != tile.j;
-    // eight rows of a column a lane
-    constexpr int kEights = TILE / 8;
-    for (int c = tid / kEights; c < TILE; c += 256 / kEights) {
-        const int r = tid % kEights * 8;
+#pragma unroll
+    for (int n = 0; n < kTurns; ++n) {
+        const int c = col0 + n * (256 / kEights), r = r8;
         float v[8];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -545,13 +566,9 @@ __global__ void __launch_bounds__(256, 2) ortho_gemm_kernel(const GemmArgs a, co
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[4 * h + e] = x[e];
         }
-        if constexpr (kLong) add8(base + t.xt[op.right] + (tj + c) * ld_m, ti + r, op.f[0], v);
-        if constexpr (KIND == kSym) {
-            // (a symmetric matrix: its row tj + c)
-#pragma unroll
-            for (int q = 0; q < 2; ++q)
-                if (op.add[q] >= 0) add8(base + t.s[op.add[q]] + (tj + c) * ld_m, ti + r, op.f[q], v);
-        }
+        if constexpr (KIND != kGram) add8(extra[0][n], op.f[0], v);
+        if constexpr (KIND == kSym)
+            if (op.add[1] >= 0) add8(extra[1][n], op.f[1], v);
         if constexpr (KIND == kFinal) {
             if (t.flip) {
                 if (tj + c < t.n)
@@ -773,11 +790,10 @@ __global__ void __launch_bounds__(kSmallThreads) ortho_small_kernel(const SmallA
 // than an eighth of an XCD's share.
 //
 // The tiles are 64 x 64 where 128 x 128 ones would leave the chip waiting for
-// the longest: where all tiles' sums, shared by the 256 CUs, are less than 7/8
-// of the longest sum.  (A block of 32 elements takes a CU about 0.7 us in a
-// large tile that it has to itself, 0.8 us in four small ones.  1,024 x 1,024,
-// one copy, 36 tiles a launch: 436 us with large tiles, 207 with small ones.
-// 2,048 x 2,048: 136 tiles of symmetric products, small; 256 of P X, large.)
+// the longest: where all tiles' sums, shared by the 256 CUs, are no more than
+// the longest sum.  (One copy in binary32, large tiles against small ones:
+// 1,024 x 1,024, 36 tiles of symmetric products and 64 of P X, 514 us against
+// 211; 2,048 x 2,048, 136 and 256, 920 against 831.)
 enum Which { kAlongN, kAlongM, kAcross };  // X X^T, products of symmetric matrices, P X
 std::vector<OrthoTile> tiles_of(const std::vector<OrthoMat>& mats, const std::vector<int32_t>& of, int K, Which which, int* side) {
     struct Chunk {
@@ -796,7 +812,7 @@ std::vector<OrthoTile> tiles_of(const std::vector<OrthoMat>& mats, const std::ve
             total += n * K * length(mats[t]);
             longest = std::max<int64_t>(longest, length(mats[t]));
         }
-        if (*side < kTile || total * 8 > longest * 256 * 7) break;
+        if (*side < kTile || total > longest * 256) break;
     }
     const int32_t across = 8 * kTile / *side;  // tiles of a square
     std::vector<Chunk> chunks;
