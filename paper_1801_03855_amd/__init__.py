@@ -130,10 +130,7 @@ def _check(status: int) -> None:
 
 
 def _ptr_array(ptrs: Sequence[Optional[int]]):
-    arr = (ctypes.c_void_p * max(1, len(ptrs)))()
-    for i, p in enumerate(ptrs):
-        arr[i] = p if p else None
-    return arr
+    return (ctypes.c_void_p * max(1, len(ptrs)))(*ptrs)
 
 
 def _stream(stream) -> Optional[int]:

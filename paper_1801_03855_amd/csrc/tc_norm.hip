@@ -11,7 +11,7 @@
 // a wave, or a whole workgroup of 256 or 512) that takes NV vectors of 16
 // bytes a lane; the variance is summed from the differences to the mean, so it
 // loses nothing where the mean is large.  Workgroups stay on one worker and
-// take its rows in turn, the next row's loads under way while one is reduced:
+// take its rows in turn, the next rows' loads under way while one is reduced:
 // the scale and shift stay in registers, and in the backward pass so do the
 // column sums of dw and db, in binary32, which are written once per workgroup
 // and added up by a second kernel in a fixed order (no atomics: the same
@@ -75,14 +75,14 @@ struct Lane<__bf16> {
 };
 
 // Vector v of a row at address a: whole, or what the row has of it with zeros
-// after the row's end.
-template <typename T>
+// after the row's end.  EDGE: the row may end inside a vector.
+template <typename T, bool EDGE>
 __device__ __forceinline__ u32x4 load_vec(uintptr_t a, int v, int cols) {
     constexpr int V = Lane<T>::kVec;
     const int left = cols - v * V;
     if (left >= V) return gld_u<u32x4>(a + static_cast<uintptr_t>(v) * 16);
     u32x4 r = {0, 0, 0, 0};
-    if (left > 0) {
+    if (EDGE && left > 0) {
         float f[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) f[i] = i < left ? Lane<T>::get(a + static_cast<uintptr_t>(v) * 16 + i * sizeof(T)) : 0.0f;
@@ -91,13 +91,13 @@ __device__ __forceinline__ u32x4 load_vec(uintptr_t a, int v, int cols) {
     return r;
 }
 
-template <typename T>
+template <typename T, bool EDGE>
 __device__ __forceinline__ void store_vec(uintptr_t a, int v, int cols, const float* f) {
     constexpr int V = Lane<T>::kVec;
     const int left = cols - v * V;
     if (left >= V) {
         gst_u<u32x4>(a + static_cast<uintptr_t>(v) * 16, Lane<T>::narrow(f));
-    } else {
+    } else if (EDGE) {
 #pragma unroll
         for (int i = 0; i < V; ++i)
             if (i < left) Lane<T>::put(a + static_cast<uintptr_t>(v) * 16 + i * sizeof(T), f[i]);
@@ -106,7 +106,7 @@ __device__ __forceinline__ void store_vec(uintptr_t a, int v, int cols, const fl
 
 // V binary32 values (a scale, a shift) for the columns of vector v; `fill`
 // past the row's end and where there is no such buffer.
-template <int V>
+template <int V, bool EDGE>
 __device__ __forceinline__ void load_f32(const float* p, int v, int cols, float fill, float* f) {
     const int left = cols - v * V;
     const uintptr_t a = reinterpret_cast<uintptr_t>(p) + static_cast<uintptr_t>(v) * V * 4;
@@ -119,7 +119,7 @@ __device__ __forceinline__ void load_f32(const float* p, int v, int cols, float 
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < V; ++i) f[i] = p && i < left ? gld<float>(a + i * 4) : fill;
+        for (int i = 0; i < V; ++i) f[i] = EDGE && p && i < left ? gld<float>(a + i * 4) : fill;
     }
 }
 
@@ -194,7 +194,13 @@ __device__ __forceinline__ int worker_of(const A& a, uint32_t b) {
     return k;
 }
 
-template <typename T, int L, int NV>
+// Whether element e of vector v is in the row.
+template <bool EDGE, int V>
+__device__ __forceinline__ bool in_row(int v, int e, int cols) {
+    return EDGE ? v * V + e < cols : v * V < cols;
+}
+
+template <typename T, int L, int NV, bool EDGE>
 __global__ void __launch_bounds__(L > 256 ? L : 256) norm_kernel(const NormArgs a) {
     constexpr int V = Lane<T>::kVec;
     constexpr int kThreads = L > 256 ? L : 256;
@@ -207,25 +213,25 @@ __global__ void __launch_bounds__(L > 256 ? L : 256) norm_kernel(const NormArgs 
     const int64_t rows = a.rows[k];
     const uintptr_t x0 = reinterpret_cast<uintptr_t>(a.x[k]), y0 = reinterpret_cast<uintptr_t>(a.y[k]);
     int turn = 0;
-    u32x4 next[NV];
+    u32x4 ahead[2][NV];  // the next two rows
+    auto fetch = [&](u32x4 (&to)[NV], int64_t at) {
+        if (at < rows)
 #pragma unroll
-    for (int i = 0; i < NV; ++i) next[i] = row < rows ? load_vec<T>(x0 + row * a.x_ld, lane + i * L, cols) : u32x4{0, 0, 0, 0};
+            for (int i = 0; i < NV; ++i) to[i] = load_vec<T, EDGE>(x0 + at * a.x_ld, lane + i * L, cols);
+    };
+    fetch(ahead[0], row);
+    fetch(ahead[1], row + step);
     float w[NV][V], b[NV][V];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        load_f32<V>(a.w[k], lane + i * L, cols, 1.0f, w[i]);
-        load_f32<V>(a.b[k], lane + i * L, cols, 0.0f, b[i]);
+        load_f32<V, EDGE>(a.w[k], lane + i * L, cols, 1.0f, w[i]);
+        load_f32<V, EDGE>(a.b[k], lane + i * L, cols, 0.0f, b[i]);
     }
-    // rows - (a row of the first group) is the same for all groups' loop ends
-    // when L > 64, where the barriers are; below that there are none
-    for (; row < rows; row += step) {
+    auto one = [&](u32x4 (&from)[NV]) {
         float x[NV][V];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) Lane<T>::widen(next[i], x[i]);
-        const int64_t then = row + step;
-        if (then < rows)
-#pragma unroll
-            for (int i = 0; i < NV; ++i) next[i] = load_vec<T>(x0 + then * a.x_ld, lane + i * L, cols);
+        for (int i = 0; i < NV; ++i) Lane<T>::widen(from[i], x[i]);
+        fetch(from, row + 2 * step);
         float s[1] = {0.0f};
 #pragma unroll
         for (int i = 0; i < NV; ++i)
@@ -235,26 +241,30 @@ __global__ void __launch_bounds__(L > 256 ? L : 256) norm_kernel(const NormArgs 
         const float mean = s[0] / static_cast<float>(cols);
         float q[1] = {0.0f};
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int left = cols - (lane + i * L) * V;
+        for (int i = 0; i < NV; ++i)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 x[i][e] -= mean;
-                q[0] = e < left ? fmaf(x[i][e], x[i][e], q[0]) : q[0];
+                q[0] = in_row<EDGE, V>(lane + i * L, e, cols) ? fmaf(x[i][e], x[i][e], q[0]) : q[0];
             }
-        }
         group_sum<L, 1>(q, lds, turn);
         const float r = 1.0f / sqrtf(q[0] / static_cast<float>(cols) + a.eps);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
 #pragma unroll
             for (int e = 0; e < V; ++e) x[i][e] = fmaf(x[i][e] * r, w[i][e], b[i][e]);
-            store_vec<T>(y0 + row * a.y_ld, lane + i * L, cols, x[i]);
+            store_vec<T, EDGE>(y0 + row * a.y_ld, lane + i * L, cols, x[i]);
         }
         if (lane == 0) {
             if (a.mean[k]) a.mean[k][row] = mean;
             if (a.rstd[k]) a.rstd[k][row] = r;
         }
+        row += step;
+    };
+    // (where L > 64 and there are barriers, all of a workgroup have one row)
+    while (row < rows) {
+        one(ahead[0]);
+        if (row < rows) one(ahead[1]);
     }
 }
 
@@ -266,11 +276,15 @@ __device__ __forceinline__ void put_weight(void* p, int dtype, int64_t c, float 
         Lane<float>::put(a + c * 4, v);
 }
 
-template <typename T, int L, int NV>
+template <typename T, int L, int NV, bool EDGE>
 __global__ void __launch_bounds__(L > 256 ? L : 256) norm_grad_kernel(const NormGradArgs a) {
     constexpr int V = Lane<T>::kVec;
     constexpr int kThreads = L > 256 ? L : 256;
     constexpr int G = kThreads / L;
+    // rows ahead: two, or one where two do not fit the registers
+    constexpr int kAhead = NV * V > 16 ? 1 : 2;
+    // and there the scale is read anew for every row, from the L2
+    constexpr int kHeld = NV * V > 16 ? 1 : NV;
     // the sums of a row's waves, and at the end the column sums of the groups
     constexpr int kCols = L * NV * V;
     __shared__ float lds[G > 1 ? G * kCols : 4 * (L / 64)];
@@ -285,58 +299,69 @@ __global__ void __launch_bounds__(L > 256 ? L : 256) norm_grad_kernel(const Norm
     const float* rstds = a.rstd[k];
     const float inv = 1.0f / static_cast<float>(cols);
     int turn = 0;
-    u32x4 nx[NV], nd[NV];
-    float nm = 0.0f, nr = 0.0f;
-    auto fetch = [&](int64_t at) {
+    struct Row {
+        u32x4 x[NV], d[NV];
+        float mean, r;
+    } ahead[kAhead];
+    auto fetch = [&](Row& to, int64_t at) {
+        if (at >= rows) return;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            nx[i] = load_vec<T>(x0 + at * a.x_ld, lane + i * L, cols);
-            nd[i] = load_vec<T>(d0 + at * a.dy_ld, lane + i * L, cols);
+            to.x[i] = load_vec<T, EDGE>(x0 + at * a.x_ld, lane + i * L, cols);
+            to.d[i] = load_vec<T, EDGE>(d0 + at * a.dy_ld, lane + i * L, cols);
         }
-        nm = means[at];
-        nr = rstds[at];
+        to.mean = means[at];
+        to.r = rstds[at];
     };
-    if (row < rows) fetch(row);
-    float w[NV][V], dw[NV][V], db[NV][V];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) fetch(ahead[i], row + i * step);
+    float w[kHeld][V], dw[NV][V], db[NV][V];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        load_f32<V>(a.w[k], lane + i * L, cols, 1.0f, w[i]);
+        if (kHeld == NV) load_f32<V, EDGE>(a.w[k], lane + i * L, cols, 1.0f, w[i % kHeld]);
 #pragma unroll
         for (int e = 0; e < V; ++e) dw[i][e] = db[i][e] = 0.0f;
     }
-    for (; row < rows; row += step) {
+    auto one = [&](Row& from) {
         float x[NV][V], d[NV][V];
-        const float mean = nm, r = nr;
+        const float mean = from.mean, r = from.r;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            Lane<T>::widen(nx[i], x[i]);
-            Lane<T>::widen(nd[i], d[i]);
+            Lane<T>::widen(from.x[i], x[i]);
+            Lane<T>::widen(from.d[i], d[i]);
         }
-        if (row + step < rows) fetch(row + step);
+        fetch(from, row + kAhead * step);
         float s[2] = {0.0f, 0.0f};
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
+        for (int i = 0; i < NV; ++i) {
+            if (kHeld < NV) load_f32<V, EDGE>(a.w[k], lane + i * L, cols, 1.0f, w[0]);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 // past the row's end dy is 0 and adds nothing, unless the mean
                 // or r is infinite: those columns are never stored, but they
                 // would put a NaN into the row's sums
-                const bool in = cols - (lane + i * L) * V > e;
-                x[i][e] = in ? (x[i][e] - mean) * r : 0.0f;
+                x[i][e] = in_row<EDGE, V>(lane + i * L, e, cols) ? (x[i][e] - mean) * r : 0.0f;
                 dw[i][e] = fmaf(d[i][e], x[i][e], dw[i][e]);
                 db[i][e] += d[i][e];
-                d[i][e] *= w[i][e];
+                d[i][e] *= w[i % kHeld][e];
                 s[0] += d[i][e];
                 s[1] = fmaf(d[i][e], x[i][e], s[1]);
             }
+        }
         group_sum<L, 2>(s, lds, turn);
         const float c0 = s[0] * inv, c1 = s[1] * inv;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
 #pragma unroll
             for (int e = 0; e < V; ++e) x[i][e] = r * (d[i][e] - c0 - x[i][e] * c1);
-            store_vec<T>(o0 + row * a.dx_ld, lane + i * L, cols, x[i]);
+            store_vec<T, EDGE>(o0 + row * a.dx_ld, lane + i * L, cols, x[i]);
         }
+        row += step;
+    };
+    while (row < rows) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (row < rows) one(ahead[i]);
     }
     // the workgroup's column sums
     float* part = a.part + static_cast<int64_t>(blockIdx.x) * 2 * cols;
@@ -396,14 +421,14 @@ __global__ void __launch_bounds__(kLong) norm_long_kernel(const NormArgs a) {
         const uintptr_t y = reinterpret_cast<uintptr_t>(a.y[k]) + row * a.y_ld;
         float f[V], w[V], b[V], s[1] = {0.0f}, q[1] = {0.0f};
         for (int v = threadIdx.x; v < nv; v += kLong) {
-            Lane<T>::widen(load_vec<T>(x, v, cols), f);
+            Lane<T>::widen(load_vec<T, true>(x, v, cols), f);
 #pragma unroll
             for (int e = 0; e < V; ++e) s[0] += f[e];
         }
         group_sum<kLong, 1>(s, lds, turn);
         const float mean = s[0] / static_cast<float>(cols);
         for (int v = threadIdx.x; v < nv; v += kLong) {
-            Lane<T>::widen(load_vec<T>(x, v, cols), f);
+            Lane<T>::widen(load_vec<T, true>(x, v, cols), f);
 #pragma unroll
             for (int e = 0; e < V; ++e)
                 if (v * V + e < cols) q[0] = fmaf(f[e] - mean, f[e] - mean, q[0]);
@@ -411,12 +436,12 @@ __global__ void __launch_bounds__(kLong) norm_long_kernel(const NormArgs a) {
         group_sum<kLong, 1>(q, lds, turn);
         const float r = 1.0f / sqrtf(q[0] / static_cast<float>(cols) + a.eps);
         for (int v = threadIdx.x; v < nv; v += kLong) {
-            Lane<T>::widen(load_vec<T>(x, v, cols), f);
-            load_f32<V>(a.w[k], v, cols, 1.0f, w);
-            load_f32<V>(a.b[k], v, cols, 0.0f, b);
+            Lane<T>::widen(load_vec<T, true>(x, v, cols), f);
+            load_f32<V, true>(a.w[k], v, cols, 1.0f, w);
+            load_f32<V, true>(a.b[k], v, cols, 0.0f, b);
 #pragma unroll
             for (int e = 0; e < V; ++e) f[e] = fmaf((f[e] - mean) * r, w[e], b[e]);
-            store_vec<T>(y, v, cols, f);
+            store_vec<T, true>(y, v, cols, f);
         }
         if (threadIdx.x == 0) {
             if (a.mean[k]) a.mean[k][row] = mean;
@@ -460,9 +485,9 @@ __global__ void __launch_bounds__(kLong) norm_grad_long_kernel(const NormGradArg
         const float mean = a.mean[k][row], r = a.rstd[k][row];
         float f[V], d[V], w[V], s[2] = {0.0f, 0.0f};
         for (int v = threadIdx.x; v < nv; v += kLong) {
-            Lane<T>::widen(load_vec<T>(x, v, cols), f);
-            Lane<T>::widen(load_vec<T>(dy, v, cols), d);
-            load_f32<V>(a.w[k], v, cols, 1.0f, w);
+            Lane<T>::widen(load_vec<T, true>(x, v, cols), f);
+            Lane<T>::widen(load_vec<T, true>(dy, v, cols), d);
+            load_f32<V, true>(a.w[k], v, cols, 1.0f, w);
 #pragma unroll
             for (int e = 0; e < V; ++e)
                 if (v * V + e < cols) {
@@ -473,12 +498,12 @@ __global__ void __launch_bounds__(kLong) norm_grad_long_kernel(const NormGradArg
         group_sum<kLong, 2>(s, lds, turn);
         const float c0 = s[0] * inv, c1 = s[1] * inv;
         for (int v = threadIdx.x; v < nv; v += kLong) {
-            Lane<T>::widen(load_vec<T>(x, v, cols), f);
-            Lane<T>::widen(load_vec<T>(dy, v, cols), d);
-            load_f32<V>(a.w[k], v, cols, 1.0f, w);
+            Lane<T>::widen(load_vec<T, true>(x, v, cols), f);
+            Lane<T>::widen(load_vec<T, true>(dy, v, cols), d);
+            load_f32<V, true>(a.w[k], v, cols, 1.0f, w);
 #pragma unroll
             for (int e = 0; e < V; ++e) f[e] = r * (d[e] * w[e] - c0 - (f[e] - mean) * r * c1);
-            store_vec<T>(dx, v, cols, f);
+            store_vec<T, true>(dx, v, cols, f);
         }
     }
 }
@@ -552,11 +577,17 @@ void spread_backward(int K, const int64_t* rows, Shape s, uint32_t* wg) {
 
 template <typename T, int L, int NV>
 void run_norm(const NormArgs& a, hipStream_t s) {
-    norm_kernel<T, L, NV><<<a.wg[a.K], L > 256 ? L : 256, 0, s>>>(a);
+    if (a.cols % Lane<T>::kVec)
+        norm_kernel<T, L, NV, true><<<a.wg[a.K], L > 256 ? L : 256, 0, s>>>(a);
+    else
+        norm_kernel<T, L, NV, false><<<a.wg[a.K], L > 256 ? L : 256, 0, s>>>(a);
 }
 template <typename T, int L, int NV>
 void run_norm_grad(const NormGradArgs& a, hipStream_t s) {
-    norm_grad_kernel<T, L, NV><<<a.wg[a.K], L > 256 ? L : 256, 0, s>>>(a);
+    if (a.cols % Lane<T>::kVec)
+        norm_grad_kernel<T, L, NV, true><<<a.wg[a.K], L > 256 ? L : 256, 0, s>>>(a);
+    else
+        norm_grad_kernel<T, L, NV, false><<<a.wg[a.K], L > 256 ? L : 256, 0, s>>>(a);
 }
 
 // CALL<T, L, NV> for the shape of the row.
