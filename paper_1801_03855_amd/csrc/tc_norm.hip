@@ -566,13 +566,27 @@ void spread(int K, const int64_t* rows, int batch, int64_t most, int64_t least, 
     }
 }
 
-constexpr int64_t kMostForward = 2048, kMostForwardWide = 512;
-constexpr int64_t kMostBackward = 1024, kMostBackwardWide = 256;
+// Workgroups of a launch at most.  Backward: those that the chip holds at once,
+// by the registers that the elements of a lane take (32,768 rows of 4,096
+// bfloat16: 768 workgroups 175 us, 1,024, of which the last 256 ran alone,
+// 185).  Forward more, of which the next ones start as others end (2,048
+// workgroups 107 us, 1,024 112), but of a whole row to 512 lanes no more than
+// fit.
+int64_t most_forward(Shape s, int es) {
+    const int e = s.NV * 16 / es;
+    if (s.L == 0) return 512;
+    if (s.L == 512) return e > 16 ? 256 : 512;
+    return 2048;
+}
+int64_t most_backward(Shape s, int es) {
+    if (s.L == 0 || s.L == 512) return 256;
+    return s.NV * 16 / es > 8 ? (es == 2 ? 768 : 512) : 1024;
+}
 constexpr int64_t kLeastBackward = 4;  // batches of rows of a workgroup
 constexpr int kRuns = 64;              // of rows, for the column sums of long rows
 
-void spread_backward(int K, const int64_t* rows, Shape s, uint32_t* wg) {
-    spread(K, rows, rows_at_a_time(s), s.L == 0 || s.L == 512 ? kMostBackwardWide : kMostBackward, kLeastBackward, true, wg);
+void spread_backward(int K, const int64_t* rows, Shape s, int es, uint32_t* wg) {
+    spread(K, rows, rows_at_a_time(s), most_backward(s, es), kLeastBackward, true, wg);
 }
 
 template <typename T, int L, int NV>
@@ -631,7 +645,7 @@ hipError_t launch_layernorm(int K, const int64_t* rows, int64_t cols, const void
             a.rstd[k] = rstd ? rstd[k0 + k] : nullptr;
             a.rows[k] = rows[k0 + k];
         }
-        spread(a.K, a.rows, rows_at_a_time(sh), sh.L == 0 || sh.L == 512 ? kMostForwardWide : kMostForward, 1, false, a.wg);
+        spread(a.K, a.rows, rows_at_a_time(sh), most_forward(sh, es), 1, false, a.wg);
         if (a.wg[a.K] == 0) continue;
         if (sh.L == 0) {
             if (dtype == TC_BF16)
@@ -656,7 +670,7 @@ int64_t layernorm_workspace(int K, const int64_t* rows, int64_t cols) {
         for (int k0 = 0; k0 < K; k0 += kWorkers) {
             uint32_t wg[kWorkers + 1];
             const int n = K - k0 < kWorkers ? K - k0 : kWorkers;
-            spread_backward(n, rows + k0, sh, wg);
+            spread_backward(n, rows + k0, sh, es, wg);
             const int64_t parts = sh.L == 0 ? static_cast<int64_t>(n) * kRuns : wg[n];
             most = most > parts ? most : parts;
         }
@@ -690,7 +704,7 @@ hipError_t launch_layernorm_backward(int K, const int64_t* rows, int64_t cols, c
             a.db[k] = db[k0 + k];
             a.rows[k] = rows[k0 + k];
         }
-        spread_backward(a.K, a.rows, sh, a.wg);
+        spread_backward(a.K, a.rows, sh, es, a.wg);
         if (sh.L == 0) {
             const dim3 grid(static_cast<uint32_t>((cols + 255) / 256), kRuns, a.K);
             if (dtype == TC_BF16) {

@@ -327,6 +327,7 @@ def test_refusals(tc):
     refused(TypeError, tc.layernorm, [x], [w.bfloat16()], None, [y])
     refused(ValueError, tc.layernorm, [x], [w, w], None, [y])
     refused(ValueError, tc.layernorm, [x, torch.zeros(4, 64, device=DEV)[:, :32]], None, None, [y, y.clone()])
+    refused(tc.TCError, tc.layernorm, [x[:1].expand(4, 32)], None, None, [y])
     refused(tc.TCError, tc.layernorm, [x], None, None, [y], eps=-1.0)
     refused(tc.TCError, tc.layernorm, [x], None, None, [y], eps=float("nan"))
     refused(tc.TCError, tc.layernorm, [x[:3]], None, None, [x[1:]])
