@@ -440,12 +440,14 @@ int32_t tc_layernorm_backward(int32_t K, const int64_t* rows, int64_t cols, cons
  *
  * tc_ortho_create: the plan for K copies of group g.  rows, cols: host arrays
  * of n; tensor t is a row-major rows[t] x cols[t] matrix (rows[t] * cols[t] ==
- * sizes[t]; the shorter side at most TC_MAX_ORTHO_SIDE), or no matrix (0, 0).
+ * sizes[t]; the shorter side at most TC_MAX_ORTHO_SIDE, the longer at most
+ * TC_MAX_ORTHO_LONG), or no matrix (0, 0).
  * scale: host array of n finite factors, or NULL for ones.  All are copied;
  * the plan owns device tables only.  The group must outlive it.  NULL on
  * error.
  * ---------------------------------------------------------------------- */
 #define TC_MAX_ORTHO_SIDE (1 << 16)
+#define TC_MAX_ORTHO_LONG (1 << 22)
 #define TC_MAX_ORTHO_STEPS 64
 
 typedef struct tc_ortho tc_ortho; /* opaque, library-owned */
@@ -461,9 +463,12 @@ int64_t tc_ortho_workspace(const tc_ortho* o);
 /* grad: host array of K device pointers to flat buffers of N elements of
  * g_dtype.  momentum: K flat binary32 buffers, updated in place, or NULL.  out:
  * K flat buffers of out_dtype (written); out[k] may be grad[k] itself where the
- * types are the same, and apart from that all buffers are disjoint.  Products
- * are accurate to binary32 (the sums are kept in it) and out is rounded once;
- * an element of a matrix that is not finite makes that matrix's out NaN, and
+ * types are the same, and apart from that all buffers are disjoint.  With a
+ * binary32 out the products are accurate to binary32; with a bfloat16 out some
+ * leave out parts below 2^-11 of their terms, which moves the result by less
+ * than its rounding does.  Sums are kept in binary32, the norm in binary64, and
+ * out is rounded once.  (X is held in steps of 2^-36: of a matrix whose norm is
+ * not much above 2^-36 of eps, nothing is left.)  An element of a matrix that is not finite makes that matrix's out NaN, and
  * no other's.  coeff: host array of 3 * steps finite coefficients; refused
  * (TC_EINVAL) if from singular values in [0, 1] they let one grow past about
  * 4, or a step multiply one by more than about 16.  eps > 0.  workspace:

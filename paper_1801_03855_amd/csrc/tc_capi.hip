@@ -831,7 +831,7 @@ TC_API tc_ortho* tc_ortho_create(const tc_group* g, int32_t K, const int64_t* ro
                       (long long)rows[t], (long long)cols[t]);
             return nullptr;
         }
-        if (std::min(rows[t], cols[t]) > TC_MAX_ORTHO_SIDE || std::max(rows[t], cols[t]) > INT32_MAX / 2) {
+        if (std::min(rows[t], cols[t]) > TC_MAX_ORTHO_SIDE || std::max(rows[t], cols[t]) > TC_MAX_ORTHO_LONG) {
             set_error("tensor %d: a %lld x %lld matrix is too large", t, (long long)rows[t], (long long)cols[t]);
             return nullptr;
         }

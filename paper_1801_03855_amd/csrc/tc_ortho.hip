@@ -799,7 +799,7 @@ std::vector<OrthoTile> tiles_of(const std::vector<OrthoMat>& mats, const std::ve
     struct Chunk {
         int64_t cost;
         int32_t len;
-        std::vector<OrthoTile> tiles;
+        size_t first, count;  // of the tiles
     };
     auto length = [&](const OrthoMat& t) { return which == kAlongN ? t.np : t.mp; };
     int64_t total, count, longest = 0;
@@ -816,17 +816,20 @@ std::vector<OrthoTile> tiles_of(const std::vector<OrthoMat>& mats, const std::ve
     }
     const int32_t across = 8 * kTile / *side;  // tiles of a square
     std::vector<Chunk> chunks;
+    std::vector<OrthoTile> tiles;
+    tiles.reserve(count);
     for (int32_t t : of) {
         const int32_t mi = mats[t].mp / *side, nj = which == kAcross ? mats[t].np / *side : mi, len = length(mats[t]);
         for (int32_t k = 0; k < K; ++k)
             for (int32_t j0 = 0; j0 < nj; j0 += across)
                 for (int32_t i0 = 0; i0 < mi; i0 += across) {
-                    chunks.push_back({0, len, {}});
+                    chunks.push_back({0, len, tiles.size(), 0});
                     for (int32_t j = j0; j < std::min(j0 + across, nj); ++j)
                         for (int32_t i = i0; i < std::min(i0 + across, mi); ++i) {
                             if (which != kAcross && j > i) continue;
-                            if (chunks.back().cost + len > total / 64 && chunks.back().cost > 0) chunks.push_back({0, len, {}});
-                            chunks.back().tiles.push_back({t, i, j, k});
+                            if (chunks.back().cost + len > total / 64 && chunks.back().cost > 0) chunks.push_back({0, len, tiles.size(), 0});
+                            tiles.push_back({t, i, j, k});
+                            ++chunks.back().count;
                             chunks.back().cost += len;
                         }
                 }
@@ -836,11 +839,12 @@ std::vector<OrthoTile> tiles_of(const std::vector<OrthoMat>& mats, const std::ve
     });
     std::vector<OrthoTile> queue[8], out;
     int64_t load[8] = {};
-    for (Chunk& c : chunks) {
+    for (const Chunk& c : chunks) {
         const int x = static_cast<int>(std::min_element(load, load + 8) - load);
         load[x] += c.cost;
-        queue[x].insert(queue[x].end(), c.tiles.begin(), c.tiles.end());
+        queue[x].insert(queue[x].end(), tiles.begin() + c.first, tiles.begin() + c.first + c.count);
     }
+    out.reserve(count);
     size_t at[8] = {};
     for (int64_t w = 0; w < count; ++w) {
         size_t x = w % 8;
@@ -934,13 +938,15 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
     o->copy_bytes = bytes;
     std::vector<int32_t> all = large[0];
     all.insert(all.end(), large[1].begin(), large[1].end());
+    // (without pairs the last lists are the first ones again)
+    const std::vector<int32_t> none, &one = large[1].empty() ? none : large[0];
     int side[9] = {};
     const std::vector<OrthoTile> lists[] = {
         chunks, split,
         tiles_of(o->mats, all, K, kAlongN, &side[2]), tiles_of(o->mats, all, K, kAlongM, &side[3]),
         tiles_of(o->mats, all, K, kAcross, &side[4]), tiles_of(o->mats, large[1], K, kAlongM, &side[5]),
-        tiles_of(o->mats, large[0], K, kAlongN, &side[6]), tiles_of(o->mats, large[0], K, kAlongM, &side[7]),
-        tiles_of(o->mats, large[0], K, kAcross, &side[8])};
+        tiles_of(o->mats, one, K, kAlongN, &side[6]), tiles_of(o->mats, one, K, kAlongM, &side[7]),
+        tiles_of(o->mats, one, K, kAcross, &side[8])};
     for (const auto& v : lists)
         if (v.size() >= (size_t{1} << 32) / 256) {  // workgroups of 256 in one dimension of a grid
             delete o;
@@ -980,6 +986,11 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
     o->d_split = reinterpret_cast<const OrthoTile*>(d + at[1]);
     OrthoList* to[] = {&o->gram, &o->sym, &o->apply, &o->sym_pair, &o->gram_one, &o->sym_one, &o->apply_one};
     for (int i = 2; i < kLists; ++i) *to[i - 2] = {reinterpret_cast<const OrthoTile*>(d + at[i]), static_cast<int32_t>(lists[i].size()), side[i]};
+    if (large[1].empty()) {
+        o->gram_one = o->gram;
+        o->sym_one = o->sym;
+        o->apply_one = o->apply;
+    }
     return o;
 }
 

@@ -160,6 +160,52 @@ def test_every_number_of_steps(tc, steps, triple):
     check(out, g, shapes, [triple] * steps)
 
 
+@pytest.mark.parametrize("steps", [1, 2, 3, 4, 5, 6])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_long_and_square_matrices_together(tc, steps, dtype):
+    """Matrices more than twice as long as wide take two steps to a product of
+    the long side, square ones and narrow ones one: side by side, in both
+    orientations and several copies, after every number of steps."""
+    gen = torch.Generator().manual_seed(50 + steps)
+    shapes = [(150, 310), 3, (145, 150), (420, 131), (40, 50), (100, 700), (257, 514)]
+    gs = [flat(gen, shapes, kind, dtype) for kind in ("directions", "gauss", "decay")]
+    outs = [torch.full_like(g, 7.0) for g in gs]
+    tc.orthogonalize(plan_for(tc, 3, shapes), gs, outs, steps=steps)
+    for g, o in zip(gs, outs):
+        check(o, g, shapes, [QUINTIC] * steps)
+
+
+@pytest.mark.parametrize("triples", [[(0.0, 1.0, 0.0)], [(0.0, 1.5, -0.5), CUBIC], [(2.0, 0.0, -1.0), (0.0, 0.0, 1.0), QUINTIC],
+                                     [CUBIC, (0.0, 1.0, 0.0), (0.0, 1.0, 0.0)]])
+def test_coefficients_that_are_zero(tc, triples):
+    gen = torch.Generator().manual_seed(60)
+    shapes = [(140, 300), (30, 60), (150, 160)]
+    g = flat(gen, shapes, "one", torch.float32)
+    out = torch.empty_like(g)
+    if triples[0] == (2.0, 0.0, -1.0):
+        # 2 x - x^5 reaches 1.27 on [0, 1], whose fifth power is 3.3, which the
+        # quintic would make over 200
+        with pytest.raises(tc.TCError):
+            tc.orthogonalize(plan_for(tc, 1, shapes), [g], [out], steps=len(triples), coefficients=triples)
+        triples = triples[:2]
+    tc.orthogonalize(plan_for(tc, 1, shapes), [g], [out], steps=len(triples), coefficients=triples)
+    check(out, g, shapes, triples)
+
+
+@pytest.mark.parametrize("shape", [(64, 64), (64, 65), (63, 483), (64, 484), (64, 485), (64, 500), (65, 66), (1, 2500), (1, 2600),
+                                   (16, 700), (17, 700), (2000, 16), (48, 180), (128, 128), (128, 129), (129, 258), (129, 257)])
+def test_where_the_paths_meet(tc, shape):
+    """Sizes around the limits of what a workgroup takes whole and of the tiles."""
+    gen = torch.Generator().manual_seed(70)
+    g = flat(gen, [2, shape, 1], "directions", torch.float32)
+    for others in ([], [(200, 200)]):  # small matrices take another path next to large ones
+        shapes = [2, shape, 1] + others
+        u = torch.cat([g, flat(gen, others, "gauss", torch.float32)]) if others else g
+        out = torch.empty_like(u)
+        tc.orthogonalize(plan_for(tc, 1, shapes), [u], [out])
+        check(out, u, shapes, [QUINTIC] * 5)
+
+
 def test_coefficients_of_each_step(tc):
     gen = torch.Generator().manual_seed(77)
     shapes = [(150, 170), (40, 40)]
@@ -330,6 +376,7 @@ def test_refusals(tc):
     refused(tc.TCError, tc.OrthoPlan, group, 0, [None, None])
     refused(tc.TCError, tc.OrthoPlan, group, 65, [None, None])
     refused(tc.TCError, tc.OrthoPlan, group, 1, [None, None], [1.0, float("inf")])
+    refused(tc.TCError, tc.OrthoPlan, tc.Group([(1 << 22) + 1]), 1, [(1, (1 << 22) + 1)])
     refused(ValueError, tc.OrthoPlan, group, 1, [None])
     refused(ValueError, tc.OrthoPlan, group, 1, [None, None], [1.0])
     plan = tc.OrthoPlan(group, 2, [(2, 3), (4, 5)])
