@@ -474,10 +474,12 @@ __global__ void __launch_bounds__(256, kOneStage ? 4 : 2) ortho_gemm_kernel(cons
         }
     };
     constexpr int kAll = kSide * kSide * PRODUCTS, kFirst = (kAll + 2) / 3;
-    // the loads of the oldest stage under way are done, in every wave; and
-    // every wave has read its operands of the stage before
+    // The loads of the oldest stage under way are done, in every wave; and
+    // every wave has its operands of the stage before: without the wait for
+    // them here, products and their wait could be moved past the barrier, and
+    // the next loads into the buffer would run against the reads.
     auto arrive = [&] {
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((STAGES > 2 ? STAGES - 2 : 0) * 2 * kLoads) : "memory");
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((STAGES > 2 ? STAGES - 2 : 0) * 2 * kLoads) : "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
@@ -500,9 +502,10 @@ __global__ void __launch_bounds__(256, kOneStage ? 4 : 2) ortho_gemm_kernel(cons
                 read(now, 0, step);
                 multiply(now, 0, kAll);
             }
-            // (each wave has its operands: its products have been issued)
-            asm volatile("" ::: "memory");
+            // every wave has its operands before the buffer is loaded again
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
             continue;
         }
         // The next step's operands are read after the first products of a

@@ -344,6 +344,27 @@ def test_same_bits_again_on_another_stream_and_from_a_graph(tc):
         assert all(torch.equal(a, b) for a, b in zip(out3 + m3, want + want_m)), turn
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("shapes,K", [([(512, 1152), (256, 2304), (512, 2048), (130, 512)] * 3, 8), ([(1030, 1500), (700, 2900)], 6),
+                                      ([(2000, 2100)], 2), ([(300, 310)], 1)])
+def test_same_bits_with_every_cu_at_work(tc, shapes, K, dtype):
+    """Many tiles at once, again and again: a load into a buffer that another
+    wave still reads would show as other bits now and then."""
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(90)
+    n = sum(size_of(s) for s in shapes)
+    gs = [torch.randn(n, generator=gen, device=DEV).to(dtype) for _ in range(K)]
+    plan = plan_for(tc, K, shapes)
+    first, again = [[torch.empty_like(g) for g in gs] for _ in range(2)]
+    tc.orthogonalize(plan, gs, first)
+    for _ in range(12):
+        tc.orthogonalize(plan, gs, again)
+        assert all(torch.equal(a, b) for a, b in zip(again, first))
+    for s, got, u in ((s, a, b) for (s, a), (_, b) in zip(pieces(first[-1], shapes), pieces(gs[-1], shapes))):
+        check_matrix(got.cpu(), u.cpu(), [QUINTIC] * 5)
+        break
+
+
 def test_flat_buffers_at_any_alignment(tc):
     gen = torch.Generator().manual_seed(19)
     shapes = [(64, 100), 3, (200, 141)]
