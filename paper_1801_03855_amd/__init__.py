@@ -25,6 +25,12 @@ Tensor layout (the K copies interleaved in one buffer):
     pack_tensor(tl, T); unpack_tensor(tl, T)            # tc_pack_tensor / tc_unpack_tensor
     reduce_tensor(g, K, T, out, "avg")      # tc_reduce_tensor
     easgd_step_tensor(g, K, X, G, xc, eta, rho)         # easgd_step_tensor
+
+What makes the gradients and the updates:
+    layernorm(xs, ws, bs, ys, means, rstds)             # tc_layernorm
+    layernorm_backward(dys, xs, ws, means, rstds, dxs, dws, dbs)   # tc_layernorm_backward
+    plan = OrthoPlan(g, K, shapes)                      # tc_ortho_create
+    orthogonalize(plan, gs, outs, momenta)              # tc_orthogonalize
 """
 
 from __future__ import annotations
