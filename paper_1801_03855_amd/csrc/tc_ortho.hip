@@ -416,8 +416,8 @@ __device__ __forceinline__ void put_out(void* out, int dtype, int64_t at, int le
 // their operands run at 1,280 to 1,400, with the clock at 1.3 GHz.
 //
 // A stage is 128 bytes of each of the 2 TILE rows: a block of 32 elements, hi
-// and lo, or with one product 64 elements' hi, which is all that X [m][n] then
-// has (kApply: BRIEF).  64 KB of LDS hold two or four stages, which are loaded
+// and lo, or with one product 64 elements' hi (which is all that X [m][n] has
+// where its products take no more; kApply: BRIEF).  64 KB of LDS hold two or four stages, which are loaded
 // straight from memory while others are multiplied, so that a CU takes two
 // workgroups; or (kOneStage) 32 KB one, nothing is loaded ahead, and four
 // workgroups cover for each other.  That pays where sums are short, and
@@ -439,7 +439,8 @@ __global__ void __launch_bounds__(256, kOneStage ? 4 : 2) ortho_gemm_kernel(cons
     const int ti = tile.i * TILE, tj = tile.j * TILE;
     // rows of the tile come from left (index in m), columns from right
     const int len = KIND == kGram ? t.np : t.mp;  // of the summed axis
-    const uint32_t ld = static_cast<uint32_t>(len) * (PRODUCTS == 1 ? 2 : 4);
+    constexpr bool kHiOnly = KIND == kGram && PRODUCTS == 1;  // (rows that have no lo)
+    const uint32_t ld = static_cast<uint32_t>(len) * (kHiOnly ? 2 : 4);
     const char* left = base + (KIND == kGram ? t.x : t.s[op.left]) + static_cast<int64_t>(ti) * ld;
     const char* right = base + (KIND == kGram ? t.x : kLong ? t.xt[op.right] : t.s[op.right]) + static_cast<int64_t>(tj) * ld;
     const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
@@ -449,10 +450,10 @@ __global__ void __launch_bounds__(256, kOneStage ? 4 : 2) ortho_gemm_kernel(cons
 #pragma unroll
     for (int q = 0; q < kLoads; ++q) {
         const int r = (wave * kLoads + q) * 8 + lane / 8, p = (lane % 8) ^ (r / 2 % 8);
-        off[q] = static_cast<uint32_t>(r) * ld + static_cast<uint32_t>(p) * 16;
+        off[q] = static_cast<uint32_t>(r) * ld + static_cast<uint32_t>(PRODUCTS == 1 && !kHiOnly ? p / 4 * 128 + p % 4 * 16 : p * 16);
     }
     auto fetch = [&](int stage, int buf) {
-        const int64_t at = static_cast<int64_t>(stage) * 128;
+        const int64_t at = static_cast<int64_t>(stage) * (PRODUCTS == 1 && !kHiOnly ? 256 : 128);
         char* to = lds + buf * kStage + wave * kLoads * 1024;
 #pragma unroll
         for (int q = 0; q < kLoads; ++q)
@@ -1127,9 +1128,10 @@ hipError_t launch_ortho(const tc_ortho* o, const void* const* g, int g_dtype, fl
     u.out_dtype = out_dtype;
     u.momentum = m != nullptr;
     const uint32_t K = o->K;
-    // A result in bfloat16 needs less: X X^T from hi alone, and a I + P
-    // without P's lo where a step's rounding is not multiplied by many after
-    // it.
+    // A result in bfloat16 needs less: X X^T from hi alone, P X without P's lo,
+    // and in the last step without X's either (a X is added whole), except
+    // where it would show.  Off by 1.7e-3 to 2.1e-3 of the result's norm, of
+    // which 1.65e-3 are its rounding.
     const bool brief = out_dtype == TC_BF16;
     if (o->nsmall[0] + o->nsmall[1] > 0) {
         SmallArgs sm{};
@@ -1184,10 +1186,12 @@ hipError_t launch_ortho(const tc_ortho* o, const void* const* g, int g_dtype, fl
             const float scale = last ? 1.0f / kScaleX : 1.0f;
             a.op[q] = {p.left, from[q], 1 - from[q], {-1, -1}, scale / kScaleP, {p.f * scale, 0.0f}};
         }
-        if (last && full)
+        if (last && !brief)
             launch_product<kFinal, 3, 0>(a, outs, list, s);
-        else if (last)
+        else if (last && full)
             launch_product<kFinal, 2, 0>(a, outs, list, s);
+        else if (last)
+            launch_product<kFinal, 1, 0>(a, outs, list, s);
         else if (!brief)
             launch_product<kApply, 3, 0>(a, outs, list, s);
         else if (full)
@@ -1208,13 +1212,15 @@ hipError_t launch_ortho(const tc_ortho* o, const void* const* g, int g_dtype, fl
             sym(o->sym_pair, {1, 2, 0, {2, -1}, 1.0f / kScaleP, {c0[0], 0.0f}});   // P A P = R (P A) + a (P A)
             rest(o->sym_pair, c1, 2);                                              // R1
             sym(o->sym_pair, {2, 1, 0, {1, 2}, 1.0f / kScaleP, {c1[0], c0[0]}});   // S = R1 R + a1 R + a R1
-            apply(o->apply_one, {1, c0[0]}, {}, false, !brief);
+            apply(o->apply_one, {1, c0[0]}, {}, false, false);
             from[0] = 1 - from[0];
             gram(o->gram_one);
             rest(o->sym_one, c1, 1);
         }
         const Factor one = {1, two ? c1[0] : c0[0]}, pair = two ? Factor{0, c0[0] * c1[0]} : one;
-        apply(o->apply, one, pair, last, !brief || (i > 0 && !last && o->sym_pair.n));
+        // in full: where the next steps multiply what is left out, or the last
+        // ones are two at once, whose S is large
+        apply(o->apply, one, pair, last, o->sym_pair.n && (last ? two : i > 0));
         for (int& f : from) f = 1 - f;
         if (hipError_t e = hipGetLastError()) return e;
     }
