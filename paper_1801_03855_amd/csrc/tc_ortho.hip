@@ -55,15 +55,19 @@ struct OrthoMat {
     int32_t flip;
     int32_t pair;        // takes two steps to a Gram matrix
     float scale;
-    int64_t x, xt[2];    // X [mp][np], its transpose [np][mp] (two, in turn)
-    int64_t s[3];        // symmetric [mp][mp] matrices
+    int64_t x, xt;       // X [mp][np]; then its transpose [np][mp] (two, in
+                         // turn), then three symmetric [mp][mp] matrices
     int32_t chunk0, chunks;  // partial sums of |u|^2
     int32_t index;           // of the matrix among the matrices
 };
 
 struct OrthoTile {
     int32_t mat, i, j;
-    int32_t copy;  // of a product's tile
+    // of a product's tile: the copy, and what the product needs of the matrix
+    // (a load of its own, after the tile's, would be waited for)
+    int16_t copy, pair;
+    int32_t mp, np;
+    int64_t x;
 };
 
 // Tiles of the products of one launch, and their side.
@@ -352,7 +356,7 @@ __global__ void __launch_bounds__(256) ortho_split_kernel(const UpdateArgs a, co
             if (to_x && brief)
                 put8_hi(base + t.x + row * (ld / 2), col, w);
             else
-                put8(base + (to_x ? t.x : t.xt[0]) + row * ld, col, w);
+                put8(base + (to_x ? t.x : t.xt) + row * ld, col, w);
         }
     }
 }
@@ -432,17 +436,21 @@ __global__ void __launch_bounds__(256, kOneStage ? 4 : 2) ortho_gemm_kernel(cons
     constexpr bool kLong = KIND == kApply || KIND == kFinal;
     __shared__ __attribute__((aligned(16))) char lds[STAGES * kStage];
     const OrthoTile tile = a.tiles[blockIdx.x];
-    const OrthoMat& t = a.mats[tile.mat];
-    const Operation& op = a.op[t.pair];
+    const OrthoMat& t = a.mats[tile.mat];  // (read at the end, for the result)
+    const Operation& op = a.op[tile.pair];
     const int k = tile.copy;
-    char* base = a.ws + k * a.copy_bytes;
+    const int64_t ld_m = static_cast<int64_t>(tile.mp) * 4, ld_n = static_cast<int64_t>(tile.np) * 4;
+    char* const x = a.ws + k * a.copy_bytes + tile.x;
+    const int64_t x_bytes = ld_n * tile.mp, s_bytes = ld_m * tile.mp;
+    auto xt = [&](int i) { return x + (1 + i) * x_bytes; };
+    auto sym = [&](int i) { return x + 3 * x_bytes + i * s_bytes; };
     const int ti = tile.i * TILE, tj = tile.j * TILE;
     // rows of the tile come from left (index in m), columns from right
-    const int len = KIND == kGram ? t.np : t.mp;  // of the summed axis
+    const int len = KIND == kGram ? tile.np : tile.mp;  // of the summed axis
     constexpr bool kHiOnly = KIND == kGram && PRODUCTS == 1;  // (rows that have no lo)
     const uint32_t ld = static_cast<uint32_t>(len) * (kHiOnly ? 2 : 4);
-    const char* left = base + (KIND == kGram ? t.x : t.s[op.left]) + static_cast<int64_t>(ti) * ld;
-    const char* right = base + (KIND == kGram ? t.x : kLong ? t.xt[op.right] : t.s[op.right]) + static_cast<int64_t>(tj) * ld;
+    const char* left = (KIND == kGram ? x : sym(op.left)) + static_cast<int64_t>(ti) * ld;
+    const char* right = (KIND == kGram ? x : kLong ? xt(op.right) : sym(op.right)) + static_cast<int64_t>(tj) * ld;
     const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const int wr = wave / 2 * (TILE / 2), wc = wave % 2 * (TILE / 2);
     // this wave's 1,024-byte pieces of a stage: eight rows each
@@ -574,7 +582,6 @@ __global__ void __launch_bounds__(256, kOneStage ? 4 : 2) ortho_gemm_kernel(cons
     // the tile goes through LDS.
     constexpr int kParts = kOneStage ? 2 : 1, kPart = TILE / kParts;
     constexpr int kEights = TILE / 8, kTurns = kPart * kEights / 256;
-    const int64_t ld_m = static_cast<int64_t>(t.mp) * 4, ld_n = static_cast<int64_t>(t.np) * 4;
     const int col0 = tid / kEights, r = tid % kEights * 8;
     const bool natural = kLong ? KIND == kApply || !t.flip : tile.i != tile.j;
     float* tiled = reinterpret_cast<float*>(lds);
@@ -585,11 +592,11 @@ __global__ void __launch_bounds__(256, kOneStage ? 4 : 2) ortho_gemm_kernel(cons
         Eight extra[KIND == kSym ? 2 : 1][kOneStage ? 1 : kTurns];
         auto more = [&](int n, int to) {
             const int64_t at = (tc + col0 + n * (256 / kEights)) * ld_m;
-            if constexpr (kLong) extra[0][to] = get8(base + t.xt[op.right] + at, ti + r);
+            if constexpr (kLong) extra[0][to] = get8(xt(op.right) + at, ti + r);
             if constexpr (KIND == kSym) {
                 // (a symmetric matrix: its row tc + c)
-                extra[0][to] = get8(base + t.s[op.add[0]] + at, ti + r);
-                if (op.add[1] >= 0) extra[KIND == kSym][to] = get8(base + t.s[op.add[1]] + at, ti + r);
+                extra[0][to] = get8(sym(op.add[0]) + at, ti + r);
+                if (op.add[1] >= 0) extra[KIND == kSym][to] = get8(sym(op.add[1]) + at, ti + r);
             }
         };
         if constexpr (!kOneStage)
@@ -619,9 +626,9 @@ __global__ void __launch_bounds__(256, kOneStage ? 4 : 2) ortho_gemm_kernel(cons
             float v[8];
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const f32x4 x = *reinterpret_cast<const f32x4*>(tiled + piece(c, r / 4 + h));
+                const f32x4 w = *reinterpret_cast<const f32x4*>(tiled + piece(c, r / 4 + h));
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[4 * h + e] = x[e];
+                for (int e = 0; e < 4; ++e) v[4 * h + e] = w[e];
             }
             if constexpr (KIND != kGram) add8(extra[0][own], op.f[0], v);
             if constexpr (KIND == kSym)
@@ -638,7 +645,7 @@ __global__ void __launch_bounds__(256, kOneStage ? 4 : 2) ortho_gemm_kernel(cons
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) u[e] = pack(v[e]);
-                put8(base + (KIND == kApply ? t.xt[op.dst] : t.s[op.dst]) + (tc + c) * ld_m, ti + r, u);
+                put8((KIND == kApply ? xt(op.dst) : sym(op.dst)) + (tc + c) * ld_m, ti + r, u);
             }
             if (natural)
 #pragma unroll
@@ -659,9 +666,9 @@ __global__ void __launch_bounds__(256, kOneStage ? 4 : 2) ortho_gemm_kernel(cons
                 for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(u[e]);
                 if (ti + row < t.m) put_out(outs.out[k], a.out_dtype, t.at + static_cast<int64_t>(ti + row) * t.cols + tc + c, t.n - (tc + c), v);
             } else if constexpr (BRIEF) {
-                put8_hi(base + t.x + (ti + row) * (ld_n / 2), tc + c, u);
+                put8_hi(x + (ti + row) * (ld_n / 2), tc + c, u);
             } else {
-                put8(base + (KIND == kApply ? t.x : t.s[op.dst]) + (ti + row) * (KIND == kApply ? ld_n : ld_m), tc + c, u);
+                put8((KIND == kApply ? x : sym(op.dst)) + (ti + row) * (KIND == kApply ? ld_n : ld_m), tc + c, u);
             }
         }
     }
@@ -871,7 +878,7 @@ std::vector<OrthoTile> tiles_of(const std::vector<OrthoMat>& mats, const std::ve
                         for (int32_t i = i0; i < std::min(i0 + across, mi); ++i) {
                             if (which != kAcross && j > i) continue;
                             if (chunks.back().cost + len > total / 64 && chunks.back().cost > 0) chunks.push_back({0, len, tiles.size(), 0});
-                            tiles.push_back({t, i, j, k});
+                            tiles.push_back({t, i, j, static_cast<int16_t>(k), static_cast<int16_t>(mats[t].pair), mats[t].mp, mats[t].np, mats[t].x});
                             ++chunks.back().count;
                             chunks.back().cost += len;
                         }
@@ -950,7 +957,7 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
         const bool matrix = q.size > 0 && rows[t] > 0;
         const bool whole = matrix && lds_of(t) <= most;
         if (!whole)
-            for (int64_t i = 0; i < nc; ++i) chunks.push_back({t, static_cast<int32_t>(i), 0, 0});
+            for (int64_t i = 0; i < nc; ++i) chunks.push_back({t, static_cast<int32_t>(i), 0, 0, 0, 0, 0, 0});
         if (!matrix) continue;
         q.rows = static_cast<int32_t>(rows[t]);
         q.cols = static_cast<int32_t>(cols[t]);
@@ -968,12 +975,10 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
         q.index = o->matrices++;
         o->of.push_back(t);
         const int64_t x = static_cast<int64_t>(q.mp) * q.np * 4, s = static_cast<int64_t>(q.mp) * q.mp * 4;
-        q.x = take(x);
-        q.xt[0] = take(x);
-        q.xt[1] = take(x);
-        for (auto& v : q.s) v = take(s);
+        q.x = take(3 * x + 3 * s);
+        q.xt = q.x + x;
         for (int32_t i = 0; i < q.mp / 64; ++i)
-            for (int32_t j = 0; j < q.np / 64; ++j) split.push_back({t, i, j, 0});
+            for (int32_t j = 0; j < q.np / 64; ++j) split.push_back({t, i, j, 0, 0, 0, 0, 0});
         large[q.pair].push_back(t);
     }
     o->sums = take(sums * 8);
