@@ -96,6 +96,34 @@ __device__ __forceinline__ u32x4 load_vec(uintptr_t a, int v, int cols) {
     return r;
 }
 
+// The same where it is needed only later.  A load of single elements would be
+// waited for at once, with all loads before it; so of the vector that the row
+// ends inside, the row's last 16 bytes are loaded, which are in the row where
+// it has that many, and `settle` moves their elements down to their places
+// (12,764 rows of 8,513 bfloat16, forward: 188 us by elements, 109 so; two
+// workers' 22,424 rows of 722, backward: 59 and 50).  Not for the long rows'
+// kernels, whose lanes may have stored over the elements before by then.
+template <typename T, bool EDGE>
+__device__ __forceinline__ u32x4 load_ahead(uintptr_t a, int v, int cols) {
+    constexpr int V = Lane<T>::kVec;
+    if (!EDGE || cols < V) return load_vec<T, EDGE>(a, v, cols);
+    const int c = v * V;
+    u32x4 r = {0, 0, 0, 0};
+    if (c < cols) r = gld_u<u32x4>(a + static_cast<uintptr_t>(c + V <= cols ? c : cols - V) * sizeof(T));
+    return r;
+}
+template <typename T, bool EDGE>
+__device__ __forceinline__ void settle(float* f, int v, int cols) {
+    constexpr int V = Lane<T>::kVec;
+    if (!EDGE || cols < V || v != cols / V) return;
+    const int by = V - cols % V;
+#pragma unroll
+    for (int m = V / 2; m > 0; m >>= 1)
+        if (by & m)
+#pragma unroll
+            for (int e = 0; e < V; ++e) f[e] = e + m < V ? f[e + m] : 0.0f;
+}
+
 template <typename T, bool EDGE>
 __device__ __forceinline__ void store_vec(uintptr_t a, int v, int cols, const float* f) {
     constexpr int V = Lane<T>::kVec;
@@ -222,7 +250,7 @@ __global__ void __launch_bounds__(L > 256 ? L : 256) norm_kernel(const NormArgs 
     auto fetch = [&](u32x4 (&to)[NV], int64_t at) {
         if (at < rows)
 #pragma unroll
-            for (int i = 0; i < NV; ++i) to[i] = load_vec<T, EDGE>(x0 + at * a.x_ld, lane + i * L, cols);
+            for (int i = 0; i < NV; ++i) to[i] = load_ahead<T, EDGE>(x0 + at * a.x_ld, lane + i * L, cols);
     };
     fetch(ahead[0], row);
     fetch(ahead[1], row + step);
@@ -235,7 +263,10 @@ __global__ void __launch_bounds__(L > 256 ? L : 256) norm_kernel(const NormArgs 
     auto one = [&](u32x4 (&from)[NV]) {
         float x[NV][V];
 #pragma unroll
-        for (int i = 0; i < NV; ++i) Lane<T>::widen(from[i], x[i]);
+        for (int i = 0; i < NV; ++i) {
+            Lane<T>::widen(from[i], x[i]);
+            settle<T, EDGE>(x[i], lane + i * L, cols);
+        }
         fetch(from, row + 2 * step);
         float s[1] = {0.0f};
 #pragma unroll
@@ -286,7 +317,8 @@ __global__ void __launch_bounds__(L > 256 ? L : 256) norm_grad_kernel(const Norm
     constexpr int V = Lane<T>::kVec;
     constexpr int kThreads = L > 256 ? L : 256;
     constexpr int G = kThreads / L;
-    // rows ahead: two, or one where two do not fit the registers
+    // rows ahead: two, or one where two do not fit the registers (with 24
+    // elements of bfloat16 they do: 12,764 rows of 8,513 183 us, with one 184)
     constexpr int kAhead = NV * V > 16 ? 1 : 2;
     // and there the scale is held in LDS, each lane's own part, which needs no
     // barrier (read from the L2 for every row instead: 2,048 rows of 16,384 in
@@ -315,8 +347,8 @@ __global__ void __launch_bounds__(L > 256 ? L : 256) norm_grad_kernel(const Norm
         if (at >= rows) return;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            to.x[i] = load_vec<T, EDGE>(x0 + at * a.x_ld, lane + i * L, cols);
-            to.d[i] = load_vec<T, EDGE>(d0 + at * a.dy_ld, lane + i * L, cols);
+            to.x[i] = load_ahead<T, EDGE>(x0 + at * a.x_ld, lane + i * L, cols);
+            to.d[i] = load_ahead<T, EDGE>(d0 + at * a.dy_ld, lane + i * L, cols);
         }
         to.mean = means[at];
         to.r = rstds[at];
@@ -342,6 +374,8 @@ __global__ void __launch_bounds__(L > 256 ? L : 256) norm_grad_kernel(const Norm
         for (int i = 0; i < NV; ++i) {
             Lane<T>::widen(from.x[i], x[i]);
             Lane<T>::widen(from.d[i], d[i]);
+            settle<T, EDGE>(x[i], lane + i * L, cols);
+            settle<T, EDGE>(d[i], lane + i * L, cols);
         }
         fetch(from, row + kAhead * step);
         float s[2] = {0.0f, 0.0f};
@@ -553,13 +587,14 @@ struct Shape {
 
 // The fewest lanes that hold a row in one vector each, up to a wave; then a
 // wave with up to 16 elements a lane, a workgroup of 256 with 8 or 16, and one
-// of 512 with 16 or 32 (more do not fit the registers of so many lanes next to
-// the scale and the column sums).
+// of 512 with 16, 24 or 32 (more do not fit the registers of so many lanes next
+// to the scale and the column sums; two workers' 4,000 rows of 9,000 in float,
+// backward: 342 us with 32, which spill, 178 with 24).
 Shape shape_of(int64_t cols, int es) {
     const int v = 16 / es;
     for (int l = 8; l <= 64; l *= 2)
         if (cols <= l * v) return {l, 1};
-    const struct { int l, e; } more[] = {{64, 8}, {64, 16}, {256, 8}, {256, 16}, {512, 16}, {512, 32}};
+    const struct { int l, e; } more[] = {{64, 8}, {64, 16}, {256, 8}, {256, 16}, {512, 16}, {512, 24}, {512, 32}};
     for (auto m : more)
         if (cols <= static_cast<int64_t>(m.l) * m.e) return {m.l, m.e / v};
     return {0, 0};
@@ -638,6 +673,7 @@ void run_norm_grad(const NormGradArgs& a, hipStream_t s) {
             case 256 * 64 + 8: CALL<T, 256, 8 / V>(a, s); break;              \
             case 256 * 64 + 16: CALL<T, 256, 16 / V>(a, s); break;            \
             case 512 * 64 + 16: CALL<T, 512, 16 / V>(a, s); break;            \
+            case 512 * 64 + 24: CALL<T, 512, 24 / V>(a, s); break;            \
             default: CALL<T, 512, 32 / V>(a, s); break;                       \
         }                                                                     \
     }

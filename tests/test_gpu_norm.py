@@ -370,3 +370,31 @@ def test_abi_refuses_null_arrays(tc):
     assert L.tc_layernorm(1, rows, 8, p, 8, 3, None, None, p, 8, None, None, 1e-5, None) == tc.TC_EINVAL
     assert L.tc_layernorm_workspace(1, None, 8) == -1
     assert L.tc_layernorm_backward(1, rows, 8, p, 8, p, 8, 0, None, None, None, p, 8, None, None, 0, None, 0, None) == tc.TC_EINVAL
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("base", [8, 24, 64, 1016, 1024, 4096, 8192, 12280, 12288])
+def test_every_remainder_of_a_vector(tc, base, dtype):
+    """Rows that end 0 to 7 elements into a 16-byte vector, in place, in views
+    whose columns past the row's end are NaN and stay as they are."""
+    gen = torch.Generator().manual_seed(base)
+    for cols in range(base, base + 8):
+        rows = [5, 0, 9]
+        wide = [[torch.full((r, cols + 9), float("nan"), dtype=dtype, device=DEV) for r in rows] for _ in range(2)]
+        xs, dys, ws, bs = make(gen, rows, cols, dtype, 0, offset=cols % 3)
+        vx, vd = [[t[:, 1:cols + 1] for t in ts] for ts in wide]
+        for v, t in zip(vx + vd, xs + dys):
+            v.copy_(t)
+        means = [torch.empty(r, device=DEV) for r in rows]
+        rstds = [torch.empty(r, device=DEV) for r in rows]
+        tc.layernorm(vx, ws, bs, vx, means, rstds)
+        for k, x in enumerate(xs):
+            check_forward(x, ws[k], bs[k], vx[k], means[k], rstds[k], 1e-5)
+            vx[k].copy_(x)
+        dws, dbs = [[torch.empty(cols, device=DEV) for _ in rows] for _ in range(2)]
+        tc.layernorm_backward(vd, vx, ws, means, rstds, vd, dws, dbs)
+        for k, x in enumerate(xs):
+            check_backward(dys[k], x, ws[k], means[k], rstds[k], vd[k], dws[k], dbs[k])
+        for ts in wide:
+            for t in ts:
+                assert bool(torch.isnan(t[:, 0]).all()) and bool(torch.isnan(t[:, cols + 1:]).all())
