@@ -909,10 +909,14 @@ std::vector<OrthoTile> tiles_of(const std::vector<OrthoMat>& mats, const std::ve
 // Whether a matrix takes two steps to a Gram matrix.  Two steps take
 // 3 m^2 n + 5 m^3 operations instead of 6 m^2 n + 2 m^3, and two launches more
 // between products of the long side, which on less than twice the length do
-// not pay.  P1 P is also larger than P, and its roundings with it: on matrices
-// of one tile, where there is little to gain, one step at a time is three
-// times as accurate (128 x 1,152: 1.2e-6 against 3.9e-6).
-bool takes_pairs(int64_t m, int64_t n) { return m > kTile && n >= 2 * m; }
+// not pay.  P1 P is also larger than P, and its roundings with it, while those
+// of a binary32 iteration shrink with m: below two whole tiles one step at a
+// time is twice as accurate (160 x 640: 1.05e-6 against 2.4e-6, a binary32
+// iteration 1.45e-6; 256 x 1,024: 1.35e-6 against 2.3e-6, and 1.5e-6) and no
+// slower (four layers of 160 and 640, 2 copies: 247 us against 290).  From
+// there two steps save more than they cost (ResNet-50 group, 8 copies: 6.9 ms
+// with its matrices of 256 rows in pairs, 7.3 without).
+bool takes_pairs(int64_t m, int64_t n) { return m >= 2 * kTile && n >= 2 * m; }
 
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 

@@ -384,6 +384,52 @@ def test_flat_buffers_at_any_alignment(tc):
             assert float(t[:shift].float().min()) == 7.0 and float(t[shift + n:].float().min()) == 7.0
 
 
+@pytest.mark.parametrize("steps", [2, 4, 5])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_around_the_sizes_that_take_two_steps_at_once(tc, steps, dtype):
+    gen = torch.Generator().manual_seed(19)
+    shapes = [(255, 600), (256, 512), (511, 256), (257, 514), (600, 257), (300, 599), (1300, 300)]
+    triples = [QUINTIC] * steps
+    us = [flat(gen, shapes, "directions", torch.float32)]
+    outs = [torch.full((us[0].numel(),), 7.0, dtype=dtype, device=DEV)]
+    tc.orthogonalize(plan_for(tc, 1, shapes), us, outs, steps=steps, coefficients=triples)
+    check(outs[0], us[0], shapes, triples)
+
+
+@pytest.mark.parametrize("triples", [[(0.0, 1.0, 0.0)], [(0.0, 1.5, -0.5), CUBIC], [(2.0, 0.0, -1.0), (0.0, 0.0, 1.0)],
+                                     [CUBIC, (0.0, 1.0, 0.0), (0.0, 1.0, 0.0)]])
+def test_zero_coefficients_of_two_steps_at_once(tc, triples):
+    gen = torch.Generator().manual_seed(61)
+    shapes = [(260, 600), (30, 60), (520, 256)]
+    g = flat(gen, shapes, "one", torch.float32)
+    out = torch.empty_like(g)
+    tc.orthogonalize(plan_for(tc, 1, shapes), [g], [out], steps=len(triples), coefficients=triples)
+    check(out, g, shapes, triples)
+
+
+@pytest.mark.parametrize("shape", [(64, 200), (128, 512), (129, 258), (516, 129), (160, 640), (200, 1000), (255, 600), (300, 400)])
+def test_as_accurate_as_a_binary32_iteration(tc, shape):
+    """No further from 64 bits than the same steps in binary32, and a fifth of
+    that for what is chance (the errors of two roundings of one thing, each an
+    average over all elements)."""
+    gen = torch.Generator().manual_seed(sum(shape))
+    errs = [0.0, 0.0]
+    for _ in range(3):
+        u = matrix(gen, shape, "directions").to(torch.float32)
+        want, norms = formula(u, [QUINTIC] * 5)
+        x = u / (u.norm() + EPS)
+        x = x.t().contiguous() if shape[0] > shape[1] else x
+        for a, b, c in [QUINTIC] * 5:
+            g = x @ x.t().contiguous()
+            x = a * x + (b * g + c * (g @ g)) @ x
+        x = x.t() if shape[0] > shape[1] else x
+        out = torch.empty(u.numel(), device=DEV)
+        tc.orthogonalize(plan_for(tc, 1, [shape]), [u.reshape(-1).to(DEV)], [out])
+        for i, got in enumerate((x, out.view(shape).cpu())):
+            errs[i] += float((got.double() - want).norm()) / norms[-1]
+    assert errs[1] <= 1.2 * errs[0], f"{errs[1] / 3:.2e} against {errs[0] / 3:.2e}"
+
+
 def test_refusals(tc):
     group = tc.Group([6, 20])
 
