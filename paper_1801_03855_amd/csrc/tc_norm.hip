@@ -19,7 +19,7 @@
 //
 // Eight workers' 4,096 rows of 4,096 bfloat16: forward 0.10 ms, 5.2 TB/s (a
 // plain copy on the same machine: 5.3); backward 0.16 to 0.17 ms, 4.7 to 5.0.
-// 2,048 rows of 16,384: backward 58 us, 4.0 TB/s with the partial column sums,
+// 2,048 rows of 16,384: backward 53 us, 4.4 TB/s with the partial column sums,
 // one workgroup of 512 lanes a CU being all that the registers hold.
 //
 // Rows are at any alignment of their element: on gfx950 a 16-byte access at
