@@ -571,6 +571,10 @@ __global__ void __launch_bounds__(256, kOneStage ? 4 : 2) ortho_gemm_kernel(cons
             }
         }
     }
+    // The loads past the end are still under way, and the tile is written over
+    // their buffers: each wave waits for its own, and all meet at the barrier
+    // before the first of those writes.
+    if constexpr (STAGES > 2) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     auto& total = [&]() -> auto& {
         if constexpr (RUN > 0) return sum;
         else return acc;
