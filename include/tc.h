@@ -463,17 +463,16 @@ int64_t tc_ortho_workspace(const tc_ortho* o);
 /* grad: host array of K device pointers to flat buffers of N elements of
  * g_dtype.  momentum: K flat binary32 buffers, updated in place, or NULL.  out:
  * K flat buffers of out_dtype (written); out[k] may be grad[k] itself where the
- * types are the same, and apart from that all buffers are disjoint.  With a
- * binary32 out the products are accurate to binary32; with a bfloat16 out some
- * leave out parts below 2^-11 of their terms, which moves the result by less
- * than its rounding does.  Sums are kept in binary32, the norm in binary64, and
- * out is rounded once.  (X is held in steps of 2^-36: of a matrix whose norm is
- * not much above 2^-36 of eps, nothing is left.)  An element of a matrix that is not finite makes that matrix's out NaN, and
- * no other's.  coeff: host array of 3 * steps finite coefficients; refused
- * (TC_EINVAL) if from singular values in [0, 1] they let one grow past about
- * 4, or a step multiply one by more than about 16.  eps > 0.  workspace:
- * tc_ortho_workspace bytes, 256-byte aligned, that nothing else uses until the
- * call's work is done. */
+ * types are the same, and apart from that all buffers are disjoint.  The
+ * products take 22 bits of their operands or more, sums are kept in binary32,
+ * the norm in binary64, and out is rounded once, whatever its type.  (X is held
+ * in steps of 2^-36: of a matrix whose norm is not much above 2^-36 of eps,
+ * nothing is left.)  An element of a matrix that is not finite makes that
+ * matrix's out NaN, and no other's.  coeff: host array of 3 * steps finite
+ * coefficients; refused (TC_EINVAL) if from singular values in [0, 1] they let
+ * one grow past about 4, or a step multiply one by more than about 16.  eps >
+ * 0.  workspace: tc_ortho_workspace bytes, 256-byte aligned, that nothing else
+ * uses until the call's work is done. */
 int32_t tc_orthogonalize(const tc_ortho* o, const void* const* grad, int32_t g_dtype, float* const* momentum,
                          float mu, int32_t nesterov, void* const* out, int32_t out_dtype, int32_t steps,
                          const float* coeff, float eps, void* workspace, int64_t workspace_bytes, void* stream);

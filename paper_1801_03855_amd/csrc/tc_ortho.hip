@@ -283,14 +283,6 @@ __device__ __forceinline__ void put8(char* row, int e, const uint32_t* v) {
     *reinterpret_cast<u32x4*>(p + 64) = lo;
 }
 
-// Their hi alone, in a row that has nothing else.
-__device__ __forceinline__ void put8_hi(char* row, int e, const uint32_t* v) {
-    u32x4 hi;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) hi[i] = (v[2 * i] & 0xffffu) | v[2 * i + 1] << 16;
-    *reinterpret_cast<u32x4*>(row + static_cast<int64_t>(e) * 2) = hi;
-}
-
 // Elements e .. e + 7 of a row, and v += f times them.
 struct Eight {
     f16x8 hi, lo;
@@ -311,7 +303,7 @@ __device__ __forceinline__ void add8(const Eight& x, float f, float* v) {
 // an element) rather than written by the first pass and read here (as many).
 // Bound by memory: 16 bytes an element, 5.1 TB/s on the ResNet-50 group, 8
 // copies (0.64 ms).
-__global__ void __launch_bounds__(256) ortho_split_kernel(const UpdateArgs a, const OrthoTile* tiles, int64_t norms, bool brief) {
+__global__ void __launch_bounds__(256) ortho_split_kernel(const UpdateArgs a, const OrthoTile* tiles, int64_t norms) {
     __shared__ uint32_t lds[64][65];
     const OrthoTile c = tiles[blockIdx.x];
     const OrthoMat& t = a.mats[c.mat];
@@ -353,10 +345,7 @@ __global__ void __launch_bounds__(256) ortho_split_kernel(const UpdateArgs a, co
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = turned ? lds[e0 + i][r] : lds[r][e0 + i];
             const int row = (to_x ? c.i : c.j) * 64 + r, col = (to_x ? c.j : c.i) * 64 + e0;
-            if (to_x && brief)
-                put8_hi(base + t.x + row * (ld / 2), col, w);
-            else
-                put8(base + (to_x ? t.x : t.xt) + row * ld, col, w);
+            put8(base + (to_x ? t.x : t.xt) + row * ld, col, w);
         }
     }
 }
@@ -409,30 +398,28 @@ __device__ __forceinline__ void put_out(void* out, int dtype, int64_t at, int le
 // with a quarter each, as 32 x 32 x 16 products: 128 x 128, or 64 x 64 where
 // the larger tiles would be fewer than the CUs.
 //
-// PRODUCTS: 3, hi hi + hi lo + lo hi; 2, without lo of left; 1, hi hi.  RUN:
-// blocks summed in the matrix cores at a time, 0 for all.
+// RUN: blocks summed in the matrix cores at a time, 0 for all.
 //
-// Measured, in binary16 products: 1,190 TFLOP/s on X X^T of the VGG-16 group
-// with one, 1,400 on its symmetric products and 1,100 on its P X with three;
-// 830, 560 and 700 on the ResNet-50 group, 8 copies, whose sums are a tenth as
-// long and whose tiles are read and written at 2.5 TB/s meanwhile.  On long
-// sums the card's power bounds it: the same products without the loads of
-// their operands run at 1,280 to 1,400, with the clock at 1.3 GHz.
+// Measured, in binary16 products: 1,400 TFLOP/s on the symmetric products of
+// the VGG-16 group and 1,100 on its P X; 830 on X X^T of the ResNet-50 group,
+// 8 copies, 560 and 700 on the other two, whose sums are a tenth as long and
+// whose tiles are read and written at 2.5 TB/s meanwhile.  On long sums the
+// card's power bounds it: the same products without the loads of their
+// operands run at 1,280 to 1,400, with the clock at 1.3 GHz.
 //
 // A stage is 128 bytes of each of the 2 TILE rows: a block of 32 elements, hi
-// and lo, or with one product 64 elements' hi (which is all that X [m][n] has
-// where its products take no more; kApply: BRIEF).  64 KB of LDS hold two or four stages, which are loaded
-// straight from memory while others are multiplied, so that a CU takes two
-// workgroups; or (kOneStage) 32 KB one, nothing is loaded ahead, and four
-// workgroups cover for each other.  That pays where sums are short, and
-// beginnings and ends of tiles much of the time.  A row's 128 bytes are eight
-// 16-byte pieces; piece p of row r lies at p ^ (r / 2 % 8), so that 16 lanes
-// reading one piece each of 16 rows touch all 64 banks once.
-template <int KIND, int PRODUCTS, int RUN, int TILE, bool BRIEF, bool kOneStage>
+// and lo.  64 KB of LDS hold two or four stages, which are loaded straight from
+// memory while others are multiplied, so that a CU takes two workgroups; or
+// (kOneStage) 32 KB one, nothing is loaded ahead, and four workgroups cover
+// for each other.  That pays where sums are short, and beginnings and ends of
+// tiles much of the time.  A row's 128 bytes are eight 16-byte pieces; piece p
+// of row r lies at p ^ (r / 2 % 8), so that 16 lanes reading one piece each of
+// 16 rows touch all 64 banks once.
+template <int KIND, int RUN, int TILE, bool kOneStage>
 __global__ void __launch_bounds__(256, kOneStage ? 4 : 2) ortho_gemm_kernel(const GemmArgs a, const Outs outs) {
     constexpr int kHalf = TILE * 128, kStage = 2 * kHalf, STAGES = kOneStage ? 1 : 65536 / kStage;
     constexpr int kSide = TILE / 64, kLoads = TILE / 32;  // 32 x 32 products of a wave each way; loads of each operand
-    constexpr int kSteps = PRODUCTS == 1 ? 4 : 2;  // products of 16 elements in a stage
+    constexpr int kSteps = kBlock / 16;  // products of 16 elements in a stage
     constexpr bool kLong = KIND == kApply || KIND == kFinal;
     __shared__ __attribute__((aligned(16))) char lds[STAGES * kStage];
     const OrthoTile tile = a.tiles[blockIdx.x];
@@ -447,8 +434,7 @@ __global__ void __launch_bounds__(256, kOneStage ? 4 : 2) ortho_gemm_kernel(cons
     const int ti = tile.i * TILE, tj = tile.j * TILE;
     // rows of the tile come from left (index in m), columns from right
     const int len = KIND == kGram ? tile.np : tile.mp;  // of the summed axis
-    constexpr bool kHiOnly = KIND == kGram && PRODUCTS == 1;  // (rows that have no lo)
-    const uint32_t ld = static_cast<uint32_t>(len) * (kHiOnly ? 2 : 4);
+    const uint32_t ld = static_cast<uint32_t>(len) * 4;
     const char* left = (KIND == kGram ? x : sym(op.left)) + static_cast<int64_t>(ti) * ld;
     const char* right = (KIND == kGram ? x : kLong ? xt(op.right) : sym(op.right)) + static_cast<int64_t>(tj) * ld;
     const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
@@ -458,10 +444,10 @@ __global__ void __launch_bounds__(256, kOneStage ? 4 : 2) ortho_gemm_kernel(cons
 #pragma unroll
     for (int q = 0; q < kLoads; ++q) {
         const int r = (wave * kLoads + q) * 8 + lane / 8, p = (lane % 8) ^ (r / 2 % 8);
-        off[q] = static_cast<uint32_t>(r) * ld + static_cast<uint32_t>(PRODUCTS == 1 && !kHiOnly ? p / 4 * 128 + p % 4 * 16 : p * 16);
+        off[q] = static_cast<uint32_t>(r) * ld + static_cast<uint32_t>(p * 16);
     }
     auto fetch = [&](int stage, int buf) {
-        const int64_t at = static_cast<int64_t>(stage) * (PRODUCTS == 1 && !kHiOnly ? 256 : 128);
+        const int64_t at = static_cast<int64_t>(stage) * 128;
         char* to = lds + buf * kStage + wave * kLoads * 1024;
 #pragma unroll
         for (int q = 0; q < kLoads; ++q)
@@ -482,8 +468,8 @@ __global__ void __launch_bounds__(256, kOneStage ? 4 : 2) ortho_gemm_kernel(cons
         for (int i = 0; i < kSide; ++i) {
             f.ah[i] = *reinterpret_cast<const f16x8*>(p + ra + i * 4096 + hi);
             f.bh[i] = *reinterpret_cast<const f16x8*>(p + rb + i * 4096 + hi);
-            if constexpr (PRODUCTS == 3) f.al[i] = *reinterpret_cast<const f16x8*>(p + ra + i * 4096 + lo);
-            if constexpr (PRODUCTS >= 2) f.bl[i] = *reinterpret_cast<const f16x8*>(p + rb + i * 4096 + lo);
+            f.al[i] = *reinterpret_cast<const f16x8*>(p + ra + i * 4096 + lo);
+            f.bl[i] = *reinterpret_cast<const f16x8*>(p + rb + i * 4096 + lo);
         }
     };
     // products `from` to `to` of a step: lo hi, hi lo, hi hi of every place
@@ -491,11 +477,11 @@ __global__ void __launch_bounds__(256, kOneStage ? 4 : 2) ortho_gemm_kernel(cons
 #pragma unroll
         for (int n = from; n < to; ++n) {
             constexpr int kOne = kSide * kSide;
-            const int w = 3 - PRODUCTS + n / kOne, i = n / kSide % kSide, j = n % kSide;
+            const int w = n / kOne, i = n / kSide % kSide, j = n % kSide;
             acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(w == 0 ? f.al[i] : f.ah[i], w == 1 ? f.bl[j] : f.bh[j], acc[i][j], 0, 0, 0);
         }
     };
-    constexpr int kAll = kSide * kSide * PRODUCTS, kFirst = (kAll + 2) / 3;
+    constexpr int kAll = kSide * kSide * 3, kFirst = (kAll + 2) / 3;
     // The loads of the oldest stage under way are done, in every wave; and
     // every wave has its operands of the stage before: without the wait for
     // them here, products and their wait could be moved past the barrier, and
@@ -505,7 +491,7 @@ __global__ void __launch_bounds__(256, kOneStage ? 4 : 2) ortho_gemm_kernel(cons
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    const int stages = len / (kSteps * 16);
+    const int stages = len / kBlock;
     if constexpr (!kOneStage) {
 #pragma unroll
         for (int st = 0; st < STAGES - 1; ++st) fetch(min(st, stages - 1), st);
@@ -538,26 +524,21 @@ __global__ void __launch_bounds__(256, kOneStage ? 4 : 2) ortho_gemm_kernel(cons
         // of loads under way stays the same).
         if (STAGES > 2 || st + 1 < stages) fetch(min(st + STAGES - 1, stages - 1), buf == 0 ? STAGES - 1 : buf - 1);
         const int then = buf + 1 == STAGES ? 0 : buf + 1;
-#pragma unroll
-        for (int step = 0; step < kSteps; step += 2) {
-            multiply(now, 0, kFirst);
-            __builtin_amdgcn_sched_barrier(0);
-            read(next, buf, step + 1);
-            __builtin_amdgcn_sched_barrier(0);
-            multiply(now, kFirst, kAll);
-            __builtin_amdgcn_sched_barrier(0);
-            multiply(next, 0, kFirst);
-            __builtin_amdgcn_sched_barrier(0);
-            if (step + 2 < kSteps) {
-                read(now, buf, step + 2);
-            } else if (st + 1 < stages) {
-                arrive();
-                read(now, then, 0);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-            multiply(next, kFirst, kAll);
-            __builtin_amdgcn_sched_barrier(0);
+        multiply(now, 0, kFirst);
+        __builtin_amdgcn_sched_barrier(0);
+        read(next, buf, 1);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(now, kFirst, kAll);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(next, 0, kFirst);
+        __builtin_amdgcn_sched_barrier(0);
+        if (st + 1 < stages) {
+            arrive();
+            read(now, then, 0);
         }
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(next, kFirst, kAll);
+        __builtin_amdgcn_sched_barrier(0);
         buf = then;
         if constexpr (RUN > 0) {
             if (st % RUN == RUN - 1) {  // stages is a multiple of RUN
@@ -669,8 +650,6 @@ __global__ void __launch_bounds__(256, kOneStage ? 4 : 2) ortho_gemm_kernel(cons
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(u[e]);
                 if (ti + row < t.m) put_out(outs.out[k], a.out_dtype, t.at + static_cast<int64_t>(ti + row) * t.cols + tc + c, t.n - (tc + c), v);
-            } else if constexpr (BRIEF) {
-                put8_hi(x + (ti + row) * (ld_n / 2), tc + c, u);
             } else {
                 put8((KIND == kApply ? x : sym(op.dst)) + (ti + row) * (KIND == kApply ? ld_n : ld_m), tc + c, u);
             }
@@ -1105,17 +1084,17 @@ namespace {
 // short (P X of the ResNet-50 group, 8 copies, mostly 256 and 512 terms: 1,145
 // us with two stages, 900 with one, the last one with the result; of the
 // VGG-16 group, 4,096 terms: 5.5 ms with two, 5.9 with one).
-template <int KIND, int PRODUCTS, int RUN, bool BRIEF = false>
+template <int KIND, int RUN>
 void launch_product(GemmArgs& a, const Outs& outs, const OrthoList& list, hipStream_t s) {
     if (list.n == 0) return;
     a.tiles = list.d;
     constexpr bool kLong = KIND == kApply || KIND == kFinal;
     if (list.side != kTile)
-        ortho_gemm_kernel<KIND, PRODUCTS, RUN, kTile / 2, BRIEF, false><<<list.n, 256, 0, s>>>(a, outs);
+        ortho_gemm_kernel<KIND, RUN, kTile / 2, false><<<list.n, 256, 0, s>>>(a, outs);
     else if (kLong && list.short_sums)
-        ortho_gemm_kernel<KIND, PRODUCTS, RUN, kTile, BRIEF, kLong><<<list.n, 256, 0, s>>>(a, outs);
+        ortho_gemm_kernel<KIND, RUN, kTile, kLong><<<list.n, 256, 0, s>>>(a, outs);
     else
-        ortho_gemm_kernel<KIND, PRODUCTS, RUN, kTile, BRIEF, false><<<list.n, 256, 0, s>>>(a, outs);
+        ortho_gemm_kernel<KIND, RUN, kTile, false><<<list.n, 256, 0, s>>>(a, outs);
 }
 
 }  // namespace
@@ -1141,11 +1120,6 @@ hipError_t launch_ortho(const tc_ortho* o, const void* const* g, int g_dtype, fl
     u.out_dtype = out_dtype;
     u.momentum = m != nullptr;
     const uint32_t K = o->K;
-    // A result in bfloat16 needs less: X X^T from hi alone, P X without P's lo,
-    // and in the last step without X's either (a X is added whole), except
-    // where it would show.  Off by 1.7e-3 to 2.1e-3 of the result's norm, of
-    // which 1.65e-3 are its rounding.
-    const bool brief = out_dtype == TC_BF16;
     if (o->nsmall[0] + o->nsmall[1] > 0) {
         SmallArgs sm{};
         sm.u = u;
@@ -1160,7 +1134,7 @@ hipError_t launch_ortho(const tc_ortho* o, const void* const* g, int g_dtype, fl
     if (o->nchunks) ortho_update_kernel<<<dim3(o->nchunks, K), 256, 0, s>>>(u);
     if (o->matrices == 0) return hipGetLastError();
     ortho_norm_kernel<<<dim3(o->matrices, K), 256, 0, s>>>(o->d_mats, o->d_of, u.ws, o->copy_bytes, o->sums, o->norms, eps);
-    ortho_split_kernel<<<dim3(o->nsplit, K), 256, 0, s>>>(u, o->d_split, o->norms, brief);
+    ortho_split_kernel<<<dim3(o->nsplit, K), 256, 0, s>>>(u, o->d_split, o->norms);
     GemmArgs a{};
     a.mats = o->d_mats;
     a.ws = u.ws;
@@ -1168,19 +1142,17 @@ hipError_t launch_ortho(const tc_ortho* o, const void* const* g, int g_dtype, fl
     a.out_dtype = out_dtype;
     auto gram = [&](const OrthoList& list) {
         a.op[0] = a.op[1] = {0, 0, 0, {-1, -1}, 1.0f / kScaleX, {0.0f, 0.0f}};
-        if (brief)
-            launch_product<kGram, 1, 0>(a, outs, list, s);
-        else if (o->sym_pair.n)
-            launch_product<kGram, 3, kRun>(a, outs, list, s);
+        if (o->sym_pair.n)
+            launch_product<kGram, kRun>(a, outs, list, s);
         else
-            launch_product<kGram, 3, 0>(a, outs, list, s);
+            launch_product<kGram, 0>(a, outs, list, s);
     };
     auto sym = [&](const OrthoList& list, Operation p) {
         a.op[0] = a.op[1] = p;
-        if (brief || o->sym_pair.n == 0)
-            launch_product<kSym, 3, 0>(a, outs, list, s);
+        if (o->sym_pair.n)
+            launch_product<kSym, kRun>(a, outs, list, s);
         else
-            launch_product<kSym, 3, kRun>(a, outs, list, s);
+            launch_product<kSym, 0>(a, outs, list, s);
     };
     // R = P - a I of the Gram matrix in [0]
     constexpr float kXtoP = kScaleP / kScaleX;
@@ -1193,24 +1165,16 @@ hipError_t launch_ortho(const tc_ortho* o, const void* const* g, int g_dtype, fl
         int32_t left;
         float f;
     };
-    auto apply = [&](const OrthoList& list, Factor one, Factor pair, bool last, bool full) {
+    auto apply = [&](const OrthoList& list, Factor one, Factor pair, bool last) {
         for (int q = 0; q < 2; ++q) {
             const Factor& p = q ? pair : one;
             const float scale = last ? 1.0f / kScaleX : 1.0f;
             a.op[q] = {p.left, from[q], 1 - from[q], {-1, -1}, scale / kScaleP, {p.f * scale, 0.0f}};
         }
-        if (last && !brief)
-            launch_product<kFinal, 3, 0>(a, outs, list, s);
-        else if (last && full)
-            launch_product<kFinal, 2, 0>(a, outs, list, s);
-        else if (last)
-            launch_product<kFinal, 1, 0>(a, outs, list, s);
-        else if (!brief)
-            launch_product<kApply, 3, 0>(a, outs, list, s);
-        else if (full)
-            launch_product<kApply, 3, 0, true>(a, outs, list, s);
+        if (last)
+            launch_product<kFinal, 0>(a, outs, list, s);
         else
-            launch_product<kApply, 2, 0, true>(a, outs, list, s);
+            launch_product<kApply, 0>(a, outs, list, s);
     };
     // The symmetric matrices, with R = P - a I: [0] A, then P A P, then
     // S = P1 P - a1 a I; [1] R (P1's where one step is taken at a time);
@@ -1225,15 +1189,13 @@ hipError_t launch_ortho(const tc_ortho* o, const void* const* g, int g_dtype, fl
             sym(o->sym_pair, {1, 2, 0, {2, -1}, 1.0f / kScaleP, {c0[0], 0.0f}});   // P A P = R (P A) + a (P A)
             rest(o->sym_pair, c1, 2);                                              // R1
             sym(o->sym_pair, {2, 1, 0, {1, 2}, 1.0f / kScaleP, {c1[0], c0[0]}});   // S = R1 R + a1 R + a R1
-            apply(o->apply_one, {1, c0[0]}, {}, false, false);
+            apply(o->apply_one, {1, c0[0]}, {}, false);
             from[0] = 1 - from[0];
             gram(o->gram_one);
             rest(o->sym_one, c1, 1);
         }
         const Factor one = {1, two ? c1[0] : c0[0]}, pair = two ? Factor{0, c0[0] * c1[0]} : one;
-        // in full: where the next steps multiply what is left out, or the last
-        // ones are two at once, whose S is large
-        apply(o->apply, one, pair, last, o->sym_pair.n && (last ? two : i > 0));
+        apply(o->apply, one, pair, last);
         for (int& f : from) f = 1 - f;
         if (hipError_t e = hipGetLastError()) return e;
     }

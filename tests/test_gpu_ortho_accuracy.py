@@ -1,0 +1,92 @@
+"""How far the orthogonalised update is from 64 bits, next to the same iteration
+in binary32.
+
+A binary32 iteration's error is what its products' sums and roundings leave,
+carried through the steps that follow.  The kernels' products keep 22 bits of
+their operands and sum in binary32, so their error is of the same kind: two
+roundings of one thing, each an average over all elements and over three
+matrices, which chance moves by less than a fifth.  A product that lost the
+second half of an operand would be off by hundreds of times as much.
+"""
+
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+QUINTIC = tuple(float(np.float32(v)) for v in (3.4445, -4.7750, 2.0315))
+EPS = float(np.float32(1e-7))
+
+
+@pytest.fixture(scope="module")
+def tc():
+    import paper_1801_03855_amd as tc
+    tc.lib()
+    return tc
+
+
+def matrix(gen, shape, kind):
+    """Few directions and noise, as a batch leaves a gradient, or noise alone."""
+    r, c = shape
+    g = torch.randn(r, c, generator=gen, device=DEV).mul_(0.004)
+    if kind == "directions":
+        k = 1 + min(r, c) // 8
+        g.addmm_(torch.randn(r, k, generator=gen, device=DEV), torch.randn(k, c, generator=gen, device=DEV), alpha=0.01 / k ** 0.5)
+    return g
+
+
+def iterate(u, steps, dtype):
+    """The formula in `dtype`, products by products of two matrices."""
+    x = u.to(dtype)
+    x = x / (x.norm() + EPS)
+    flip = x.shape[0] > x.shape[1]
+    x = x.t().contiguous() if flip else x
+    a, b, c = QUINTIC
+    for _ in range(steps):
+        g = x @ x.t().contiguous()
+        x = a * x + (b * g + c * (g @ g)) @ x
+    return x.t() if flip else x
+
+
+def update(tc, us, dtype=torch.float32, steps=5):
+    """One copy of a group of the matrices us."""
+    plan = tc.OrthoPlan(tc.Group([u.numel() for u in us]), 1, [tuple(u.shape) for u in us])
+    out = torch.empty(sum(u.numel() for u in us), dtype=dtype, device=DEV)
+    tc.orthogonalize(plan, [torch.cat([u.reshape(-1) for u in us])], [out], steps=steps)
+    return [p.view(u.shape) for p, u in zip(out.split([u.numel() for u in us]), us)]
+
+
+def generator(seed):
+    gen = torch.Generator(device=DEV)
+    gen.manual_seed(seed)
+    return gen
+
+
+def off(got, want):
+    return float((got.double() - want).norm() / want.norm())
+
+
+@pytest.mark.parametrize("steps", [1, 2, 5, 8])
+@pytest.mark.parametrize("shapes", [[(65, 65)], [(100, 1000)], [(512, 512)], [(700, 1500), (130, 200), (40, 50)], [(256, 2304), (1000, 300)]])
+def test_a_bfloat16_result_is_the_binary32_one_rounded(tc, shapes, steps):
+    gen = generator(sum(map(sum, shapes)) + steps)
+    for kind in ("directions", "gauss"):
+        us = [matrix(gen, s, kind) for s in shapes]
+        for wide, brief in zip(update(tc, us, steps=steps), update(tc, us, torch.bfloat16, steps)):
+            assert torch.equal(wide.to(torch.bfloat16), brief)
+
+
+@pytest.mark.parametrize("steps", [5, 8, 12, 24])
+@pytest.mark.parametrize("shape", [(128, 512), (250, 400), (512, 512), (600, 1300)])
+def test_a_bfloat16_result_after_many_steps(tc, shape, steps):
+    """The rounding of the exact result, and twice a binary32 iteration's error
+    (the steps do not contract: from 12 on the errors of both have grown a
+    hundredfold, and chance with them)."""
+    gen = generator(steps)
+    for kind in ("directions", "gauss"):
+        u = matrix(gen, shape, kind)
+        want = iterate(u, steps, torch.float64)
+        got = off(update(tc, [u], torch.bfloat16, steps)[0], want)
+        assert got <= off(want.to(torch.bfloat16), want) + 2 * off(iterate(u, steps, torch.float32), want)
