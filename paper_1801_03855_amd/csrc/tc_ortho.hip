@@ -26,9 +26,16 @@
 // keep the products from losing what the operands hold.  P is held without its
 // a I, which is added in binary32 where P is used: along the large singular
 // values a I and the rest cancel, and a rounding of P's large diagonal would
-// stay.  And the matrix cores' sums of 128 terms are added up in registers of
-// their own: on 512 x 4,608, summed in the matrix cores alone, the result was
-// 1.7e-5 off, with both 3e-6 (a binary32 product's iteration: 4e-6).
+// stay.  And X X^T and the symmetric products are summed in the matrix cores
+// 128 terms at a time, which are added up in registers of their own: small
+// terms are cut off against a large sum there.  Without that the result of
+// 512 x 4,608 was 1.7e-5 off, with it 3.5e-6 (a binary32 product's iteration:
+// 3.8e-6), of 200 x 20,000, one step at a time, 3.9e-6 and 0.9e-6 (2.8e-6).
+// P X, whose sums are the shorter side and which is added to a X, is summed
+// whole: 4,096 x 4,096 and 4,096 x 8,192 are 1.8e-6 and 2.0e-6 off so (3.3e-6
+// both).  None of this goes by the other matrices of the group, nor
+// does the order of a sum, so a matrix over the size that one workgroup takes
+// has the same bits whatever its neighbours.
 //
 // Layout.  A matrix in the workspace is rows of blocks of 32 elements, 64
 // bytes of hi followed by 64 bytes of lo, padded with zeros to multiples of a
@@ -117,7 +124,7 @@ constexpr int kChunk = 4096;  // elements of a workgroup of the first pass
 constexpr int kTile = 128;    // rows and columns of a product's larger tile
 constexpr int kBlock = 32;    // elements of a block of hi and lo
 constexpr float kScaleX = 4096.0f, kScaleP = 1024.0f;
-constexpr int kRun = 4;       // stages summed in the matrix cores at a time, where sums are kept apart
+constexpr int kRun = 4;       // stages summed in the matrix cores at a time in X X^T and symmetric products
 constexpr int kCopies = TC_MAX_K;
 
 // ------------------------------------------------ momentum and the matrix norm
@@ -398,8 +405,6 @@ __device__ __forceinline__ void put_out(void* out, int dtype, int64_t at, int le
 // with a quarter each, as 32 x 32 x 16 products: 128 x 128, or 64 x 64 where
 // the larger tiles would be fewer than the CUs.
 //
-// RUN: blocks summed in the matrix cores at a time, 0 for all.
-//
 // Measured, in binary16 products: 1,400 TFLOP/s on the symmetric products of
 // the VGG-16 group and 1,100 on its P X; 830 on X X^T of the ResNet-50 group,
 // 8 copies, 560 and 700 on the other two, whose sums are a tenth as long and
@@ -415,12 +420,12 @@ __device__ __forceinline__ void put_out(void* out, int dtype, int64_t at, int le
 // tiles much of the time.  A row's 128 bytes are eight 16-byte pieces; piece p
 // of row r lies at p ^ (r / 2 % 8), so that 16 lanes reading one piece each of
 // 16 rows touch all 64 banks once.
-template <int KIND, int RUN, int TILE, bool kOneStage>
+template <int KIND, int TILE, bool kOneStage>
 __global__ void __launch_bounds__(256, kOneStage ? 4 : 2) ortho_gemm_kernel(const GemmArgs a, const Outs outs) {
     constexpr int kHalf = TILE * 128, kStage = 2 * kHalf, STAGES = kOneStage ? 1 : 65536 / kStage;
     constexpr int kSide = TILE / 64, kLoads = TILE / 32;  // 32 x 32 products of a wave each way; loads of each operand
     constexpr int kSteps = kBlock / 16;  // products of 16 elements in a stage
-    constexpr bool kLong = KIND == kApply || KIND == kFinal;
+    constexpr bool kLong = KIND == kApply || KIND == kFinal, kApart = !kLong;  // (sums of kRun stages)
     __shared__ __attribute__((aligned(16))) char lds[STAGES * kStage];
     const OrthoTile tile = a.tiles[blockIdx.x];
     const OrthoMat& t = a.mats[tile.mat];  // (read at the end, for the result)
@@ -456,7 +461,7 @@ __global__ void __launch_bounds__(256, kOneStage ? 4 : 2) ortho_gemm_kernel(cons
         for (int q = 0; q < kLoads; ++q)
             __builtin_amdgcn_global_load_lds((global_char*)(right + at + off[q]), (lds_char*)(to + kHalf + q * 1024), 16, 0, 0);
     };
-    f32x16 acc[kSide][kSide] = {}, sum[RUN ? kSide : 1][RUN ? kSide : 1] = {};
+    f32x16 acc[kSide][kSide] = {}, sum[kApart ? kSide : 1][kApart ? kSide : 1] = {};
     struct Operands {
         f16x8 ah[kSide], al[kSide], bh[kSide], bl[kSide];
     } now, next;
@@ -540,8 +545,8 @@ __global__ void __launch_bounds__(256, kOneStage ? 4 : 2) ortho_gemm_kernel(cons
         multiply(next, kFirst, kAll);
         __builtin_amdgcn_sched_barrier(0);
         buf = then;
-        if constexpr (RUN > 0) {
-            if (st % RUN == RUN - 1) {  // stages is a multiple of RUN
+        if constexpr (kApart) {
+            if (st % kRun == kRun - 1) {  // stages is a multiple of kRun
 #pragma unroll
                 for (int i = 0; i < kSide; ++i)
 #pragma unroll
@@ -557,7 +562,7 @@ __global__ void __launch_bounds__(256, kOneStage ? 4 : 2) ortho_gemm_kernel(cons
     // before the first of those writes.
     if constexpr (STAGES > 2) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     auto& total = [&]() -> auto& {
-        if constexpr (RUN > 0) return sum;
+        if constexpr (kApart) return sum;
         else return acc;
     }();
     // The tile leaves through LDS, in one part or two of its columns, so that
@@ -1084,17 +1089,17 @@ namespace {
 // short (P X of the ResNet-50 group, 8 copies, mostly 256 and 512 terms: 1,145
 // us with two stages, 900 with one, the last one with the result; of the
 // VGG-16 group, 4,096 terms: 5.5 ms with two, 5.9 with one).
-template <int KIND, int RUN>
+template <int KIND>
 void launch_product(GemmArgs& a, const Outs& outs, const OrthoList& list, hipStream_t s) {
     if (list.n == 0) return;
     a.tiles = list.d;
     constexpr bool kLong = KIND == kApply || KIND == kFinal;
     if (list.side != kTile)
-        ortho_gemm_kernel<KIND, RUN, kTile / 2, false><<<list.n, 256, 0, s>>>(a, outs);
+        ortho_gemm_kernel<KIND, kTile / 2, false><<<list.n, 256, 0, s>>>(a, outs);
     else if (kLong && list.short_sums)
-        ortho_gemm_kernel<KIND, RUN, kTile, kLong><<<list.n, 256, 0, s>>>(a, outs);
+        ortho_gemm_kernel<KIND, kTile, kLong><<<list.n, 256, 0, s>>>(a, outs);
     else
-        ortho_gemm_kernel<KIND, RUN, kTile, false><<<list.n, 256, 0, s>>>(a, outs);
+        ortho_gemm_kernel<KIND, kTile, false><<<list.n, 256, 0, s>>>(a, outs);
 }
 
 }  // namespace
@@ -1142,17 +1147,11 @@ hipError_t launch_ortho(const tc_ortho* o, const void* const* g, int g_dtype, fl
     a.out_dtype = out_dtype;
     auto gram = [&](const OrthoList& list) {
         a.op[0] = a.op[1] = {0, 0, 0, {-1, -1}, 1.0f / kScaleX, {0.0f, 0.0f}};
-        if (o->sym_pair.n)
-            launch_product<kGram, kRun>(a, outs, list, s);
-        else
-            launch_product<kGram, 0>(a, outs, list, s);
+        launch_product<kGram>(a, outs, list, s);
     };
     auto sym = [&](const OrthoList& list, Operation p) {
         a.op[0] = a.op[1] = p;
-        if (o->sym_pair.n)
-            launch_product<kSym, kRun>(a, outs, list, s);
-        else
-            launch_product<kSym, 0>(a, outs, list, s);
+        launch_product<kSym>(a, outs, list, s);
     };
     // R = P - a I of the Gram matrix in [0]
     constexpr float kXtoP = kScaleP / kScaleX;
@@ -1172,9 +1171,9 @@ hipError_t launch_ortho(const tc_ortho* o, const void* const* g, int g_dtype, fl
             a.op[q] = {p.left, from[q], 1 - from[q], {-1, -1}, scale / kScaleP, {p.f * scale, 0.0f}};
         }
         if (last)
-            launch_product<kFinal, 0>(a, outs, list, s);
+            launch_product<kFinal>(a, outs, list, s);
         else
-            launch_product<kApply, 0>(a, outs, list, s);
+            launch_product<kApply>(a, outs, list, s);
     };
     // The symmetric matrices, with R = P - a I: [0] A, then P A P, then
     // S = P1 P - a1 a I; [1] R (P1's where one step is taken at a time);

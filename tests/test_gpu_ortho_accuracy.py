@@ -90,3 +90,37 @@ def test_a_bfloat16_result_after_many_steps(tc, shape, steps):
         want = iterate(u, steps, torch.float64)
         got = off(update(tc, [u], torch.bfloat16, steps)[0], want)
         assert got <= off(want.to(torch.bfloat16), want) + 2 * off(iterate(u, steps, torch.float32), want)
+
+
+def no_further_than_binary32(tc, groups, seed, steps=5):
+    """`groups` of matrices' shapes, whose update's error added up over three
+    draws of each is at most a binary32 iteration's and a fifth, matrix by matrix."""
+    gen = generator(seed)
+    errs = [[0.0, 0.0] for _ in groups]
+    for _ in range(3):
+        us = [matrix(gen, s, "directions") for s in groups]
+        for e, u, got in zip(errs, us, update(tc, us, steps=steps)):
+            want = iterate(u, steps, torch.float64)
+            e[0] += off(iterate(u, steps, torch.float32), want)
+            e[1] += off(got, want)
+    for s, (plain, ours) in zip(groups, errs):
+        assert ours <= 1.2 * plain, f"{s}: {ours / 3:.2e} against {plain / 3:.2e}"
+
+
+@pytest.mark.parametrize("shape", [(200, 20000), (128, 50000), (20000, 200), (255, 9000), (2000, 2100)])
+def test_long_sums_of_one_step_at_a_time(tc, shape):
+    no_further_than_binary32(tc, [shape], sum(shape))
+
+
+@pytest.mark.parametrize("shape", [(200, 390), (255, 3000), (513, 600), (600, 1300), (1500, 700)])
+def test_a_matrix_has_the_same_bits_whatever_its_neighbours(tc, shape):
+    """Alone, next to matrices of another number of steps to a Gram matrix, and
+    next to enough that tiles are larger and stages fewer."""
+    gen = generator(sum(shape))
+    u = matrix(gen, shape, "directions")
+    alone, = update(tc, [u])
+    for others in ([(600, 1300)], [(300, 310)], [(700, 1500), (1030, 1500)], [(512, 1152), (300, 300), (256, 2304)] * 12):
+        for at in (0, len(others)):
+            us = [matrix(gen, s, "gauss") for s in others]
+            us.insert(at, u)
+            assert torch.equal(update(tc, us)[at], alone), (others[:3], at)
