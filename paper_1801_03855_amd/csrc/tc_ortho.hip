@@ -897,14 +897,18 @@ std::vector<OrthoTile> tiles_of(const std::vector<OrthoMat>& mats, const std::ve
 // Whether a matrix takes two steps to a Gram matrix.  Two steps take
 // 3 m^2 n + 5 m^3 operations instead of 6 m^2 n + 2 m^3, and two launches more
 // between products of the long side, which on less than twice the length do
-// not pay.  P1 P is also larger than P, and its roundings with it, while those
-// of a binary32 iteration shrink with m: below two whole tiles one step at a
-// time is twice as accurate (160 x 640: 1.05e-6 against 2.4e-6, a binary32
-// iteration 1.45e-6; 256 x 1,024: 1.35e-6 against 2.3e-6, and 1.5e-6) and no
-// slower (four layers of 160 and 640, 2 copies: 247 us against 290).  From
-// there two steps save more than they cost (ResNet-50 group, 8 copies: 6.9 ms
-// with its matrices of 256 rows in pairs, 7.3 without).
-bool takes_pairs(int64_t m, int64_t n) { return m >= 2 * kTile && n >= 2 * m; }
+// not pay.  P1 P is also larger than P, and the roundings of it and of the one
+// X X^T with it: against a binary32 iteration, whose roundings grow with m, it
+// is further off below about 450 rows, and below about 1,000 on sums past
+// 10,000 terms.  Errors (1e-6) of one step at a time, of two, and in binary32,
+// five steps from 1/8 as many directions as rows and noise:
+//   256 x 1,024   0.95  2.3  1.5      512 x 16,384    1.7  5.2  6.5
+//   300 x 600     1.1   2.4  1.7      512 x 24,576    1.7  6.0  4.4
+//   384 x 768     1.4   2.5  2.2      768 x 9,216     1.8  3.8  5.0
+//   512 x 1,024   1.5   2.5  2.6      768 x 18,432    1.8  5.0  3.6
+//   512 x 8,192   1.6   4.1  4.9      1,024 x 49,152  2.0  4.9  9.6
+// (ResNet-50 group, 8 copies: 7.2 ms, with pairs from 256 rows 6.9.)
+bool takes_pairs(int64_t m, int64_t n) { return n >= 2 * m && (m >= 8 * kTile || (m >= 4 * kTile && n <= 8192)); }
 
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 

@@ -13,6 +13,8 @@ import numpy as np
 import pytest
 import torch
 
+from tests.test_gpu_ortho import CUBIC, check, flat, plan_for
+
 pytestmark = pytest.mark.gpu
 
 DEV = "cuda:0"
@@ -38,7 +40,7 @@ def matrix(gen, shape, kind):
 
 
 def iterate(u, steps, dtype):
-    """The formula in `dtype`, products by products of two matrices."""
+    """The formula in `dtype`, product by product."""
     x = u.to(dtype)
     x = x / (x.norm() + EPS)
     flip = x.shape[0] > x.shape[1]
@@ -124,3 +126,31 @@ def test_a_matrix_has_the_same_bits_whatever_its_neighbours(tc, shape):
             us = [matrix(gen, s, "gauss") for s in others]
             us.insert(at, u)
             assert torch.equal(update(tc, us)[at], alone), (others[:3], at)
+
+
+@pytest.mark.parametrize("steps", [2, 5])
+@pytest.mark.parametrize("shape", [(256, 512), (256, 2304), (600, 257), (300, 600), (300, 2000), (384, 768), (900, 448), (511, 1100),
+                                   (512, 20000), (640, 30720), (768, 18432)])
+def test_where_one_step_at_a_time_is_more_accurate(tc, shape, steps):
+    no_further_than_binary32(tc, [shape], sum(shape) + steps, steps)
+
+
+@pytest.mark.parametrize("steps", [2, 3, 5])
+@pytest.mark.parametrize("shape", [(512, 1024), (512, 4608), (1030, 515), (768, 2304), (1024, 4096), (512, 8192),
+                                   (1000, 8192), (1024, 65536), (1536, 20000)])
+def test_matrices_that_take_two_steps_at_once(tc, shape, steps):
+    no_further_than_binary32(tc, [shape], sum(shape) + steps, steps)
+
+
+@pytest.mark.parametrize("triples", [[(0.0, 1.0, 0.0)], [(0.0, 1.5, -0.5), CUBIC], [(2.0, 0.0, -1.0), (0.0, 0.0, 1.0)],
+                                     [CUBIC, (0.0, 1.0, 0.0), (0.0, 1.0, 0.0)], [QUINTIC] * 2, [QUINTIC] * 4])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_any_coefficients_of_two_steps_at_once(tc, triples, dtype):
+    """Matrices of one and of two steps to a Gram matrix side by side, against
+    the formula."""
+    gen = torch.Generator().manual_seed(62)
+    shapes = [(520, 1100), (511, 1023), 7, (30, 60), (1030, 513), (300, 200)]
+    g = flat(gen, shapes, "one" if triples[0][0] != QUINTIC[0] else "directions", torch.float32)
+    out = torch.empty_like(g, dtype=dtype)
+    tc.orthogonalize(plan_for(tc, 1, shapes), [g], [out], steps=len(triples), coefficients=triples)
+    check(out, g, shapes, triples)
