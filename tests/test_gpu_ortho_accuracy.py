@@ -154,3 +154,14 @@ def test_any_coefficients_of_two_steps_at_once(tc, triples, dtype):
     out = torch.empty_like(g, dtype=dtype)
     tc.orthogonalize(plan_for(tc, 1, shapes), [g], [out], steps=len(triples), coefficients=triples)
     check(out, g, shapes, triples)
+
+
+@pytest.mark.parametrize("groups", [
+    [(512, 1152), (300, 300), (256, 2304), (600, 1300)] * 12,   # 128 x 128 tiles, short sums: P X with one stage
+    [(2000, 2100), (1500, 3100)],                                # 128 x 128 tiles, long sums: P X with two
+    [(4096, 2000)], [(700, 5000), (1100, 600), (1001, 1003)], [(130, 512), (40, 50), (1024, 1024)],
+])
+def test_groups_that_take_every_kind_of_tile(tc, groups):
+    """The formula's tests allow hundreds of roundings; these would show one
+    operand without its second half."""
+    no_further_than_binary32(tc, groups, 5 * len(groups))
