@@ -469,10 +469,14 @@ int64_t tc_ortho_workspace(const tc_ortho* o);
  * in steps of 2^-36: of a matrix whose norm is not much above 2^-36 of eps,
  * nothing is left.)  An element of a matrix that is not finite makes that
  * matrix's out NaN, and no other's.  coeff: host array of 3 * steps finite
- * coefficients; refused (TC_EINVAL) if from singular values in [0, 1] they let
- * one grow past about 4, or a step multiply one by more than about 16.  eps >
- * 0.  workspace: tc_ortho_workspace bytes, 256-byte aligned, that nothing else
- * uses until the call's work is done. */
+ * coefficients; refused (TC_EINVAL) if from singular values in [0, 1], whose
+ * squares are x, they let one grow past 3.98, or |b x + c x^2| of a step past
+ * 62.9.  Matrices whose shorter side is 512 or more and half the longer one or
+ * less may take two steps at once: with one in the group, the factor by which
+ * two steps of a pair (the first and second, third and fourth, ...) multiply a
+ * singular value has to be within 62.9 of a1 a2.  eps > 0.  workspace:
+ * tc_ortho_workspace bytes, 256-byte aligned, that nothing else uses until the
+ * call's work is done. */
 int32_t tc_orthogonalize(const tc_ortho* o, const void* const* grad, int32_t g_dtype, float* const* momentum,
                          float mu, int32_t nesterov, void* const* out, int32_t out_dtype, int32_t steps,
                          const float* coeff, float eps, void* workspace, int64_t workspace_bytes, void* stream);

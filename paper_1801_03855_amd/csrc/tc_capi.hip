@@ -868,7 +868,7 @@ TC_API int32_t tc_orthogonalize(const tc_ortho* o, const void* const* grad, int3
     for (int i = 0; i < 3 * steps; ++i)
         if (!std::isfinite(coeff[i])) return fail(TC_EINVAL, "the coefficients must be finite");
     if (!std::isfinite(mu) || !std::isfinite(eps) || eps <= 0.0f) return fail(TC_EINVAL, "mu must be finite, eps finite and positive");
-    if (!ortho_in_range(steps, coeff)) return fail(TC_EINVAL, "the coefficients let the iteration leave its range");
+    if (!ortho_in_range(o, steps, coeff)) return fail(TC_EINVAL, "the coefficients let the iteration leave its range");
     if (int32_t r = check_device(g)) return r;
     if (g->N == 0) return TC_OK;
     if (!grad || !out) return fail(TC_EINVAL, "NULL buffer");

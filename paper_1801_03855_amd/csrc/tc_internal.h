@@ -180,7 +180,7 @@ void destroy_ortho(tc_ortho* o);
 const tc_group* ortho_group(const tc_ortho* o);
 int32_t ortho_copies(const tc_ortho* o);
 int64_t ortho_workspace(const tc_ortho* o);
-bool ortho_in_range(int steps, const float* coeff);
+bool ortho_in_range(const tc_ortho* o, int steps, const float* coeff);
 hipError_t launch_ortho(const tc_ortho* o, const void* const* g, int g_dtype, float* const* m, float mu, int nesterov,
                         void* const* out, int out_dtype, int steps, const float* coeff, float eps, void* workspace,
                         hipStream_t stream);

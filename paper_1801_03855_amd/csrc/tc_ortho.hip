@@ -43,6 +43,7 @@
 // and [n][m] for P X: in both products the operands' rows then run along the
 // summed axis.
 #include <algorithm>
+#include <array>
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -1048,25 +1049,46 @@ const tc_group* ortho_group(const tc_ortho* o) { return o->g; }
 int32_t ortho_copies(const tc_ortho* o) { return o->K; }
 int64_t ortho_workspace(const tc_ortho* o) { return o->copy_bytes * o->K; }
 
+// The largest |f| over [0, top] of a polynomial of degree 12 at most, and up to
+// 0.3% more: |f| is nowhere larger than the largest of its values at N
+// Chebyshev points over cos(12 pi / (2 N)) (Ehlich and Zeller 1964).
+template <typename F>
+double largest(double top, F f) {
+    constexpr int kPoints = 256;
+    static const std::array<double, kPoints> points = [] {
+        std::array<double, kPoints> p;
+        for (int i = 0; i < kPoints; ++i) p[i] = 0.5 + 0.5 * std::cos((i + 0.5) * std::acos(-1.0) / kPoints);
+        return p;
+    }();
+    static const double room = std::cos(12 * std::acos(-1.0) / (2 * kPoints));
+    double most = 0.0;
+    for (double p : points) {
+        const double v = std::fabs(f(top * p));
+        if (!(v <= most)) most = v;  // (also where it is no number)
+    }
+    return most / room;
+}
+
 // Whether values stay in the ranges the formats hold.  s bounds the singular
 // values before a step (1 at first: |X| <= 1), and with x = s^2 the step makes
-// them s |q(x)|, q = a + b x + c x^2; both extremes lie at the ends or where a
-// derivative is 0.
-bool ortho_in_range(int steps, const float* coeff) {
-    double s = 1.0, q_before = 1.0, a_before = 1.0;
+// them s |q(x)|, q = a + b x + c x^2.  What is stored, by its largest
+// eigenvalue or singular value, with 1/64 of the range for rounding: A = X X^T
+// (x), P - a I (q - a), X (s q), and of matrices that take two steps to a Gram
+// matrix P A (x q), P A P (x q^2), both no more than the bounds of X allow, and
+// S = P1 P - a1 a I (q1(x q^2) q - a1 a).
+bool ortho_in_range(const tc_ortho* o, int steps, const float* coeff) {
+    const double lim_x = 65504.0 / kScaleX * (63.0 / 64.0), lim_p = 65504.0 / kScaleP * (63.0 / 64.0);
+    double x = 1.0, before = 1.0;  // largest x of this step and the one before
     for (int i = 0; i < steps; ++i) {
-        const double a = coeff[3 * i], b = coeff[3 * i + 1], c = coeff[3 * i + 2], x = s * s;
-        auto q = [&](double v) { return std::fabs(a + v * (b + c * v)); };
-        auto p = [&](double v) { return std::sqrt(v) * q(v); };
-        double qs = std::max(q(0), q(x)), ps = p(x);
+        const double a = coeff[3 * i], b = coeff[3 * i + 1], c = coeff[3 * i + 2];
+        // where s q(s^2) has a derivative of 0, as a value of s^2
+        double after = x * std::pow(a + x * (b + c * x), 2);
         auto at = [&](double v) {
-            if (v > 0 && v < x) {
-                qs = std::max(qs, q(v));
-                ps = std::max(ps, p(v));
-            }
+            if (v > 0 && v < x) after = std::max(after, v * std::pow(a + v * (b + c * v), 2));
         };
+        double rest = std::fabs(x * (b + c * x));
         if (c != 0) {
-            at(-b / (2 * c));
+            if (const double v = -b / (2 * c); v > 0 && v < x) rest = std::max(rest, std::fabs(v * (b + c * v)));
             const double disc = 9 * b * b - 20 * a * c;
             if (disc >= 0) {
                 at((-3 * b + std::sqrt(disc)) / (10 * c));
@@ -1075,14 +1097,17 @@ bool ortho_in_range(int steps, const float* coeff) {
         } else if (b != 0) {
             at(-a / (3 * b));
         }
-        // what is stored: X X^T (x), P A (s p), P A P (p^2), P - a I, P1 P - a1 a I, X (p); 1/64 for rounding
-        const double lim_x = 65504.0 / kScaleX * (63.0 / 64.0), lim_p = 65504.0 / kScaleP * (63.0 / 64.0);
-        const bool second = i % 2 == 1;
-        const double pair = qs * q_before + std::fabs(a * a_before);
-        if (!(x <= lim_x && s * ps <= lim_x && ps * ps <= lim_x && qs + std::fabs(a) <= lim_p && (!second || pair <= lim_p))) return false;
-        q_before = qs;
-        a_before = a;
-        s = ps;
+        if (!(after <= lim_x && rest <= lim_p)) return false;
+        if (i % 2 == 1 && o->sym_pair.n) {
+            const double a0 = coeff[3 * i - 3], b0 = coeff[3 * i - 2], c0 = coeff[3 * i - 1];
+            const double both = largest(before, [&](double v) {
+                const double q = a0 + v * (b0 + c0 * v), w = v * q * q;
+                return (a + w * (b + c * w)) * q - a * a0;
+            });
+            if (!(both <= lim_p)) return false;
+        }
+        before = x;
+        x = after;
     }
     return true;
 }
