@@ -46,6 +46,7 @@
 #include <array>
 #include <cmath>
 #include <cstring>
+#include <memory>
 #include <new>
 
 #include "tc_internal.h"
@@ -833,32 +834,46 @@ __global__ void __launch_bounds__(kSmallThreads) ortho_small_kernel(const SmallA
 // 1,024 x 1,024, 36 tiles of symmetric products and 64 of P X, 514 us against
 // 211; 2,048 x 2,048, 136 and 256, 920 against 831.)
 enum Which { kAlongN, kAlongM, kAcross };  // X X^T, products of symmetric matrices, P X
-std::vector<OrthoTile> tiles_of(const std::vector<OrthoMat>& mats, const std::vector<int32_t>& of, int K, Which which, int* side, bool* short_sums) {
+struct Tiling {
+    int side;
+    int64_t count, total;  // of the tiles, and of the terms of their sums
+    bool short_sums;
+};
+
+int32_t length(const OrthoMat& t, Which which) { return which == kAlongN ? t.np : t.mp; }
+
+Tiling tiling_of(const std::vector<OrthoMat>& mats, const std::vector<int32_t>& of, int K, Which which) {
+    Tiling r{};
+    for (r.side = kTile;; r.side = kTile / 2) {
+        int64_t longest = 0;
+        r.total = r.count = 0;
+        for (int32_t t : of) {
+            const int64_t mi = mats[t].mp / r.side, ni = mats[t].np / r.side;
+            const int64_t n = which == kAcross ? mi * ni : mi * (mi + 1) / 2;
+            r.count += n * K;
+            r.total += n * K * length(mats[t], which);
+            longest = std::max<int64_t>(longest, length(mats[t], which));
+        }
+        if (r.side < kTile || r.total > longest * 256) break;
+    }
+    r.short_sums = r.total <= r.count * 1024;
+    return r;
+}
+
+std::vector<OrthoTile> tiles_of(const std::vector<OrthoMat>& mats, const std::vector<int32_t>& of, int K, Which which, const Tiling& tiling) {
     struct Chunk {
         int64_t cost;
         int32_t len;
         size_t first, count;  // of the tiles
     };
-    auto length = [&](const OrthoMat& t) { return which == kAlongN ? t.np : t.mp; };
-    int64_t total, count, longest = 0;
-    for (*side = kTile;; *side = kTile / 2) {
-        total = count = 0;
-        for (int32_t t : of) {
-            const int64_t mi = mats[t].mp / *side, ni = mats[t].np / *side;
-            const int64_t n = which == kAcross ? mi * ni : mi * (mi + 1) / 2;
-            count += n * K;
-            total += n * K * length(mats[t]);
-            longest = std::max<int64_t>(longest, length(mats[t]));
-        }
-        if (*side < kTile || total > longest * 256) break;
-    }
-    *short_sums = total <= count * 1024;
-    const int32_t across = 8 * kTile / *side;  // tiles of a square
+    const int side = tiling.side;
+    const int64_t total = tiling.total, count = tiling.count;
+    const int32_t across = 8 * kTile / side;  // tiles of a square
     std::vector<Chunk> chunks;
     std::vector<OrthoTile> tiles;
     tiles.reserve(count);
     for (int32_t t : of) {
-        const int32_t mi = mats[t].mp / *side, nj = which == kAcross ? mats[t].np / *side : mi, len = length(mats[t]);
+        const int32_t mi = mats[t].mp / side, nj = which == kAcross ? mats[t].np / side : mi, len = length(mats[t], which);
         for (int32_t k = 0; k < K; ++k)
             for (int32_t j0 = 0; j0 < nj; j0 += across)
                 for (int32_t i0 = 0; i0 < mi; i0 += across) {
@@ -917,11 +932,20 @@ int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 
 tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const int64_t* cols, const float* scale, hipError_t* e) {
     *e = hipErrorOutOfMemory;
-    auto* o = new (std::nothrow) tc_ortho();
+    // (released where the host's memory runs out below, too)
+    std::unique_ptr<tc_ortho, void (*)(tc_ortho*)> o(new (std::nothrow) tc_ortho(), destroy_ortho);
     if (!o) return nullptr;
     o->g = g;
     o->K = K;
     o->mats.resize(g->n);
+    // Workgroups of 256 in one dimension of a grid are fewer than 2^24: lists
+    // that are longer are refused before they are built.
+    constexpr int64_t kMostTiles = (int64_t{1} << 32) / 256 - 1;
+    auto refuse = [&] {
+        *e = hipErrorInvalidValue;
+        return nullptr;
+    };
+    int64_t nchunks = 0, nsplit = 0;
     std::vector<OrthoTile> chunks, split;
     std::vector<int32_t> large[2];  // by OrthoMat::pair
     std::vector<int32_t> small[2];
@@ -953,8 +977,10 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
         q.chunks = static_cast<int32_t>(nc);
         const bool matrix = q.size > 0 && rows[t] > 0;
         const bool whole = matrix && lds_of(t) <= most;
-        if (!whole)
+        if (!whole) {
+            if ((nchunks += nc) > kMostTiles) return refuse();
             for (int64_t i = 0; i < nc; ++i) chunks.push_back({t, static_cast<int32_t>(i), 0, 0, 0, 0, 0, 0});
+        }
         if (!matrix) continue;
         q.rows = static_cast<int32_t>(rows[t]);
         q.cols = static_cast<int32_t>(cols[t]);
@@ -974,6 +1000,7 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
         const int64_t x = static_cast<int64_t>(q.mp) * q.np * 4, s = static_cast<int64_t>(q.mp) * q.mp * 4;
         q.x = take(3 * x + 3 * s);
         q.xt = q.x + x;
+        if ((nsplit += static_cast<int64_t>(q.mp / 64) * (q.np / 64)) > kMostTiles) return refuse();
         for (int32_t i = 0; i < q.mp / 64; ++i)
             for (int32_t j = 0; j < q.np / 64; ++j) split.push_back({t, i, j, 0, 0, 0, 0, 0});
         large[q.pair].push_back(t);
@@ -985,22 +1012,18 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
     all.insert(all.end(), large[1].begin(), large[1].end());
     // (without pairs the last lists are the first ones again)
     const std::vector<int32_t> none, &one = large[1].empty() ? none : large[0];
-    int side[9] = {};
-    bool short_sums[9] = {};
-    const std::vector<OrthoTile> lists[] = {
-        chunks, split,
-        tiles_of(o->mats, all, K, kAlongN, &side[2], &short_sums[2]), tiles_of(o->mats, all, K, kAlongM, &side[3], &short_sums[3]),
-        tiles_of(o->mats, all, K, kAcross, &side[4], &short_sums[4]), tiles_of(o->mats, large[1], K, kAlongM, &side[5], &short_sums[5]),
-        tiles_of(o->mats, one, K, kAlongN, &side[6], &short_sums[6]), tiles_of(o->mats, one, K, kAlongM, &side[7], &short_sums[7]),
-        tiles_of(o->mats, one, K, kAcross, &side[8], &short_sums[8])};
-    for (const auto& v : lists)
-        if (v.size() >= (size_t{1} << 32) / 256) {  // workgroups of 256 in one dimension of a grid
-            delete o;
-            *e = hipErrorInvalidValue;
-            return nullptr;
-        }
-    o->nchunks = static_cast<int32_t>(chunks.size());
-    o->nsplit = static_cast<int32_t>(split.size());
+    const struct {
+        const std::vector<int32_t>& of;
+        Which which;
+    } products[] = {{all, kAlongN}, {all, kAlongM}, {all, kAcross}, {large[1], kAlongM}, {one, kAlongN}, {one, kAlongM}, {one, kAcross}};
+    constexpr int kProducts = sizeof products / sizeof *products, kLists = 2 + kProducts;
+    Tiling tilings[kProducts];
+    for (int i = 0; i < kProducts; ++i)
+        if ((tilings[i] = tiling_of(o->mats, products[i].of, K, products[i].which)).count > kMostTiles) return refuse();
+    std::vector<OrthoTile> lists[kLists] = {std::move(chunks), std::move(split)};
+    for (int i = 0; i < kProducts; ++i) lists[2 + i] = tiles_of(o->mats, products[i].of, K, products[i].which, tilings[i]);
+    o->nchunks = static_cast<int32_t>(nchunks);
+    o->nsplit = static_cast<int32_t>(nsplit);
     // one block of device memory for all tables
     std::vector<char> host;
     auto put = [&](const void* p, size_t n) {
@@ -1013,14 +1036,11 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
     const size_t at_of = put(o->of.data(), o->of.size() * 4);
     size_t at_small[2];
     for (int i = 0; i < 2; ++i) at_small[i] = put(small[i].data(), small[i].size() * 4);
-    constexpr int kLists = sizeof lists / sizeof *lists;
     size_t at[kLists];
     for (int i = 0; i < kLists; ++i) at[i] = put(lists[i].data(), lists[i].size() * sizeof(OrthoTile));
     if ((*e = hipMalloc(&o->d_blob, host.size())) != hipSuccess ||
-        (*e = hipMemcpy(o->d_blob, host.data(), host.size(), hipMemcpyHostToDevice)) != hipSuccess) {
-        destroy_ortho(o);
+        (*e = hipMemcpy(o->d_blob, host.data(), host.size(), hipMemcpyHostToDevice)) != hipSuccess)
         return nullptr;
-    }
     const char* d = static_cast<const char*>(o->d_blob);
     o->d_mats = reinterpret_cast<const OrthoMat*>(d + at_mats);
     o->d_of = reinterpret_cast<const int32_t*>(d + at_of);
@@ -1031,13 +1051,14 @@ tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const in
     o->d_chunks = reinterpret_cast<const OrthoTile*>(d + at[0]);
     o->d_split = reinterpret_cast<const OrthoTile*>(d + at[1]);
     OrthoList* to[] = {&o->gram, &o->sym, &o->apply, &o->sym_pair, &o->gram_one, &o->sym_one, &o->apply_one};
-    for (int i = 2; i < kLists; ++i) *to[i - 2] = {reinterpret_cast<const OrthoTile*>(d + at[i]), static_cast<int32_t>(lists[i].size()), side[i], short_sums[i]};
+    for (int i = 0; i < kProducts; ++i)
+        *to[i] = {reinterpret_cast<const OrthoTile*>(d + at[2 + i]), static_cast<int32_t>(tilings[i].count), tilings[i].side, tilings[i].short_sums};
     if (large[1].empty()) {
         o->gram_one = o->gram;
         o->sym_one = o->sym;
         o->apply_one = o->apply;
     }
-    return o;
+    return o.release();
 }
 
 void destroy_ortho(tc_ortho* o) {
@@ -1062,10 +1083,7 @@ double largest(double top, F f) {
     }();
     static const double room = std::cos(12 * std::acos(-1.0) / (2 * kPoints));
     double most = 0.0;
-    for (double p : points) {
-        const double v = std::fabs(f(top * p));
-        if (!(v <= most)) most = v;  // (also where it is no number)
-    }
+    for (double p : points) most = std::max(most, std::fabs(f(top * p)));
     return most / room;
 }
 
