@@ -395,9 +395,9 @@ int32_t easgd_pipeline_tensor(const tc_tensorlist* grads, const tc_tensorlist* p
  * ones, zeros.  mean, rstd: K device pointers to rows[k] binary32 values that
  * receive mu and rstd for the backward pass; NULL: not written.  Statistics
  * are summed in binary32, from the differences to mu; y is rounded once.  y[k]
- * may be x[k] itself (with the same stride), and shares nothing else with any
- * x or y; views of one wider buffer may interleave.  A worker without rows
- * needs no pointers.  cols in [1, TC_MAX_NORM_COLS], eps >= 0.
+ * may be x[k] itself (with the same stride); apart from that y, mean and rstd
+ * share no byte with each other or with what is read.  Views of one wider
+ * buffer may interleave.  A worker without rows needs no pointers.  cols in [1, TC_MAX_NORM_COLS], eps >= 0.
  * ---------------------------------------------------------------------- */
 #define TC_MAX_NORM_COLS (1 << 24)
 
@@ -415,12 +415,12 @@ int64_t tc_layernorm_workspace(int32_t K, const int64_t* rows, int64_t cols);
  * (zeros for a worker without rows).  dy, x, dx: rows of dtype, as above; dx[k]
  * may be dy[k] or x[k] itself.  mean, rstd: as tc_layernorm wrote them.
  * weight: NULL for ones.  dweight, dbias: K device pointers to cols values of
- * w_dtype (pieces of a flat gradient buffer, at any alignment of the type),
- * all disjoint from each other and from the other buffers.  Sums are kept in
- * binary32 and added in an order that only the shapes decide: the same inputs
- * give the same bits.  workspace: at least tc_layernorm_workspace bytes of
- * device memory, 16-byte aligned, that nothing else uses until the call's work
- * is done. */
+ * w_dtype (pieces of a flat gradient buffer, at any alignment of the type).
+ * Sums are kept in binary32 and added in an order that only the shapes decide:
+ * the same inputs give the same bits.  workspace: at least
+ * tc_layernorm_workspace bytes of device memory, 16-byte aligned, that nothing
+ * else uses until the call's work is done.  dx apart from the above, dweight,
+ * dbias and the workspace share no byte with each other or with what is read. */
 int32_t tc_layernorm_backward(int32_t K, const int64_t* rows, int64_t cols, const void* const* dy, int64_t dy_ld,
                               const void* const* x, int64_t x_ld, int32_t dtype, const float* const* weight,
                               const float* const* mean, const float* const* rstd, void* const* dx, int64_t dx_ld,

@@ -657,18 +657,69 @@ struct Rows {
     const char* name;
 };
 
-int64_t extent(const Rows& r, int64_t rows, int64_t cols) { return ((rows - 1) * r.ld + cols) * r.es; }
+// Memory that a call reads or writes: one block, or `width` bytes every `line`
+// (line > 0).
+struct Span {
+    uintptr_t lo, hi;
+    int64_t line, width;
+    const char* name;
+    int32_t k;
+    bool rows, written;
+};
 
-// Rows of the two buffers share a byte.  Views of one wider buffer (equal
-// strides) may interleave without sharing any.
-bool rows_overlap(const Rows& a, const void* p, int64_t ra, const Rows& b, const void* q, int64_t rb, int64_t cols) {
-    if (ra == 0 || rb == 0 || !overlap(p, extent(a, ra, cols), q, extent(b, rb, cols))) return false;
-    const int64_t line = a.ld * a.es;
-    if (line != b.ld * b.es) return true;
-    int64_t at = static_cast<int64_t>(reinterpret_cast<uintptr_t>(q) - reinterpret_cast<uintptr_t>(p)) % line;
-    if (at < 0) at += line;
-    return at < cols * a.es || at + cols * b.es > line;
+// A block shares a byte with rows.
+bool block_in_rows(const Span& block, const Span& rows) {
+    if (block.lo < rows.lo) return block.hi > rows.lo;
+    const int64_t at = static_cast<int64_t>(block.lo - rows.lo) % rows.line;
+    // the row it starts in or behind; the next one, if there is one
+    return at < rows.width || static_cast<uintptr_t>(rows.line - at) < std::min(block.hi, rows.hi) - block.lo;
 }
+
+// Two spans share a byte.  Views of one wider buffer (equal strides) may
+// interleave without sharing any.
+bool share(const Span& a, const Span& b) {
+    if (a.lo >= b.hi || b.lo >= a.hi) return false;
+    if (!a.line) return !b.line || block_in_rows(a, b);
+    if (!b.line) return block_in_rows(b, a);
+    if (a.line != b.line) return true;
+    int64_t at = static_cast<int64_t>(b.lo - a.lo) % a.line;
+    if (at < 0) at += a.line;
+    return at < a.width || at + b.width > a.line;
+}
+
+// What one call reads and writes, every worker's.
+struct Spans {
+    Span s[8 * TC_MAX_K + 1];
+    int n = 0;
+
+    void add(const void* p, int64_t bytes, const char* name, int32_t k, bool written) {
+        const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+        if (p && bytes > 0) s[n++] = {at, at + bytes, 0, 0, name, k, false, written};
+    }
+    void add(const Rows& r, int32_t k, int64_t rows, int64_t cols, bool written) {
+        if (rows == 0) return;
+        add(r.p[k], ((rows - 1) * r.ld + cols) * r.es, r.name, k, written);
+        s[n - 1].rows = true;
+        if (rows > 1) {
+            s[n - 1].line = r.ld * r.es;
+            s[n - 1].width = cols * r.es;
+        }
+    }
+    // What is written shares nothing with what else is written or read, except
+    // that a worker's rows may take the place of its own, element for element.
+    int32_t check() {
+        std::sort(s, s + n, [](const Span& a, const Span& b) { return a.lo < b.lo; });
+        for (int i = 0; i < n; ++i)
+            for (int j = i + 1; j < n && s[j].lo < s[i].hi; ++j) {
+                const Span &a = s[i], &b = s[j];
+                if ((!a.written && !b.written) || !share(a, b)) continue;
+                if (a.rows && b.rows && a.written != b.written && a.k == b.k && a.lo == b.lo && a.line == b.line) continue;
+                set_error("%s[%d] overlaps %s[%d]", a.name, a.k, b.name, b.k);
+                return TC_EINVAL;
+            }
+        return TC_OK;
+    }
+};
 
 int32_t check_rows(int32_t K, const int64_t* rows, int64_t cols, const Rows& r) {
     if (!r.p) { set_error("%s is NULL", r.name); return TC_EINVAL; }
@@ -684,25 +735,6 @@ int32_t check_rows(int32_t K, const int64_t* rows, int64_t cols, const Rows& r) 
         return TC_EINVAL;
     }
     if (most > 0 && r.ld > INT64_MAX / 8 / most) { set_error("%s is too large", r.name); return TC_EINVAL; }
-    return TC_OK;
-}
-
-// The rows written (out) share nothing with each other or with the rows read
-// (in), except that a worker's out may be its own in, element for element.
-int32_t check_written(int32_t K, const int64_t* rows, int64_t cols, const Rows& out, const Rows* in, int n) {
-    for (int32_t k = 0; k < K; ++k)
-        for (int32_t q = 0; q < K; ++q) {
-            if (q < k && rows_overlap(out, out.p[k], rows[k], out, out.p[q], rows[q], cols)) {
-                set_error("%s[%d] overlaps %s[%d]", out.name, k, out.name, q);
-                return TC_EINVAL;
-            }
-            for (int i = 0; i < n; ++i) {
-                if (!rows_overlap(out, out.p[k], rows[k], in[i], in[i].p[q], rows[q], cols)) continue;
-                if (q == k && out.p[k] == in[i].p[k] && (out.ld == in[i].ld || rows[k] == 1)) continue;
-                set_error("%s[%d] overlaps %s[%d]", out.name, k, in[i].name, q);
-                return TC_EINVAL;
-            }
-        }
     return TC_OK;
 }
 
@@ -742,13 +774,23 @@ TC_API int32_t tc_layernorm(int32_t K, const int64_t* rows, int64_t cols, const 
     const Rows in{x, x_ld, es, "x"}, out{y, y_ld, es, "y"};
     if (int32_t r = check_rows(K, rows, cols, in)) return r;
     if (int32_t r = check_rows(K, rows, cols, out)) return r;
-    if (int32_t r = check_written(K, rows, cols, out, &in, 1)) return r;
     const struct { const void* const* p; const char* name; } vectors[] = {
         {reinterpret_cast<const void* const*>(weight), "weight"}, {reinterpret_cast<const void* const*>(bias), "bias"},
         {reinterpret_cast<const void* const*>(mean), "mean"}, {reinterpret_cast<const void* const*>(rstd), "rstd"}};
     for (auto& v : vectors)
         if (v.p)
             if (int32_t r = check_vectors(K, rows, v.p, 4, v.name)) return r;
+    Spans spans;
+    for (int32_t k = 0; k < K; ++k) {
+        if (rows[k] == 0) continue;
+        spans.add(in, k, rows[k], cols, false);
+        spans.add(out, k, rows[k], cols, true);
+        if (weight) spans.add(weight[k], cols * 4, "weight", k, false);
+        if (bias) spans.add(bias[k], cols * 4, "bias", k, false);
+        if (mean) spans.add(mean[k], rows[k] * 4, "mean", k, true);
+        if (rstd) spans.add(rstd[k], rows[k] * 4, "rstd", k, true);
+    }
+    if (int32_t r = spans.check()) return r;
     hipError_t e = launch_layernorm(K, rows, cols, x, x_ld, dtype, weight, bias, y, y_ld, mean, rstd, eps,
                                     static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "tc_layernorm launch");
@@ -774,7 +816,6 @@ TC_API int32_t tc_layernorm_backward(int32_t K, const int64_t* rows, int64_t col
     if (int32_t r = check_rows(K, rows, cols, in[0])) return r;
     if (int32_t r = check_rows(K, rows, cols, in[1])) return r;
     if (int32_t r = check_rows(K, rows, cols, out)) return r;
-    if (int32_t r = check_written(K, rows, cols, out, in, 2)) return r;
     if (!mean || !rstd || !dweight || !dbias) return fail(TC_EINVAL, "mean, rstd, dweight or dbias is NULL");
     if (weight)
         if (int32_t r = check_vectors(K, rows, reinterpret_cast<const void* const*>(weight), 4, "weight")) return r;
@@ -782,33 +823,24 @@ TC_API int32_t tc_layernorm_backward(int32_t K, const int64_t* rows, int64_t col
     if (int32_t r = check_vectors(K, rows, reinterpret_cast<const void* const*>(rstd), 4, "rstd")) return r;
     if (int32_t r = check_vectors(K, nullptr, const_cast<const void* const*>(dweight), ws, "dweight")) return r;
     if (int32_t r = check_vectors(K, nullptr, const_cast<const void* const*>(dbias), ws, "dbias")) return r;
-    // what is written as sums over rows shares nothing with what else is
-    // written, nor with what the rows' kernels read
-    const int64_t wb = cols * ws;
-    for (int32_t k = 0; k < K; ++k) {
-        for (int32_t q = 0; q < K; ++q) {
-            if ((q < k && (overlap(dweight[k], wb, dweight[q], wb) || overlap(dbias[k], wb, dbias[q], wb))) ||
-                overlap(dweight[k], wb, dbias[q], wb)) {
-                set_error("dweight or dbias of workers %d and %d overlap", k, q);
-                return TC_EINVAL;
-            }
-            for (const void* p : {const_cast<const void*>(dweight[k]), const_cast<const void*>(dbias[k])}) {
-                bool bad = weight && rows[q] > 0 && overlap(p, wb, weight[q], cols * 4);
-                for (const Rows* r : {&in[0], &in[1], &out})
-                    bad = bad || (rows[q] > 0 && overlap(p, wb, r->p[q], extent(*r, rows[q], cols)));
-                if (bad) {
-                    set_error("dweight[%d] or dbias[%d] overlaps a buffer of worker %d", k, k, q);
-                    return TC_EINVAL;
-                }
-            }
-        }
-    }
     const int64_t need = layernorm_workspace(K, rows, cols);
     if (!workspace || !aligned(workspace, 16)) return fail(TC_EINVAL, "workspace is NULL or not 16-byte aligned");
     if (workspace_bytes < need) {
         set_error("the workspace has %lld bytes, %lld are needed", (long long)workspace_bytes, (long long)need);
         return TC_EINVAL;
     }
+    Spans spans;
+    for (int32_t k = 0; k < K; ++k) {
+        spans.add(dweight[k], cols * ws, "dweight", k, true);
+        spans.add(dbias[k], cols * ws, "dbias", k, true);
+        if (rows[k] == 0) continue;
+        for (const Rows* r : {&in[0], &in[1], &out}) spans.add(*r, k, rows[k], cols, r == &out);
+        if (weight) spans.add(weight[k], cols * 4, "weight", k, false);
+        spans.add(mean[k], rows[k] * 4, "mean", k, false);
+        spans.add(rstd[k], rows[k] * 4, "rstd", k, false);
+    }
+    spans.add(workspace, need, "workspace", 0, true);
+    if (int32_t r = spans.check()) return r;
     hipError_t e = launch_layernorm_backward(K, rows, cols, dy, dy_ld, x, x_ld, dtype, weight, mean, rstd, dx, dx_ld,
                                              dweight, dbias, w_dtype, workspace, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "tc_layernorm_backward launch");
