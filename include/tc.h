@@ -397,7 +397,9 @@ int32_t easgd_pipeline_tensor(const tc_tensorlist* grads, const tc_tensorlist* p
  * are summed in binary32, from the differences to mu; y is rounded once.  y[k]
  * may be x[k] itself (with the same stride); apart from that y, mean and rstd
  * share no byte with each other or with what is read.  Views of one wider
- * buffer may interleave.  A worker without rows needs no pointers.  cols in [1, TC_MAX_NORM_COLS], eps >= 0.
+ * buffer may interleave.  A worker without rows needs no pointers.  The rows
+ * are on the current device (TC_EINVAL if x is device memory of another).
+ * cols in [1, TC_MAX_NORM_COLS], eps >= 0.
  * ---------------------------------------------------------------------- */
 #define TC_MAX_NORM_COLS (1 << 24)
 

@@ -152,9 +152,15 @@ def _stream(stream) -> Optional[int]:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
-def _dev_ptr(t: torch.Tensor, n: int, dtypes=(torch.float32,), what: str = "tensor") -> int:
+def _elsewhere(t: torch.Tensor, device: Optional[int], what: str) -> ValueError:
     if not t.is_cuda:
-        raise ValueError(f"{what} must be a GPU tensor")
+        return ValueError(f"{what} must be a GPU tensor")
+    return ValueError(f"{what} is on {t.device}, the first worker's rows are on device {device}")
+
+
+def _dev_ptr(t: torch.Tensor, n: int, dtypes=(torch.float32,), what: str = "tensor", device: Optional[int] = None) -> int:
+    if not t.is_cuda if device is None else t.get_device() != device:
+        raise _elsewhere(t, device, what)
     if t.dtype not in dtypes:
         raise TypeError(f"{what} has dtype {t.dtype}, expected one of {dtypes}")
     if not t.is_contiguous() or t.numel() < n:
@@ -474,14 +480,14 @@ def easgd_pipeline_tensor(grads: TensorList, params: TensorList, g_tensor: Optio
 
 # --------------------------------------------------------------- layer norm
 
-def _row_ptrs(ts, rows, cols: int, dtype: torch.dtype, what: str):
+def _row_ptrs(ts, rows, cols: int, dtype: torch.dtype, device: int, what: str):
     """(device pointers, row stride in elements) of the K workers' rows."""
     if len(ts) != len(rows):
         raise ValueError(f"need {len(rows)} tensors as {what}, got {len(ts)}")
     ptrs, ld = [], None
     for k, (t, r) in enumerate(zip(ts, rows)):
-        if not t.is_cuda:
-            raise ValueError(f"{what}[{k}] must be a GPU tensor")
+        if t.get_device() != device or device < 0:
+            raise _elsewhere(t, device, f"{what}[{k}]")
         if t.dtype is not dtype:
             raise TypeError(f"{what}[{k}] has dtype {t.dtype}, expected {dtype}")
         if t.shape != (r, cols):
@@ -498,12 +504,12 @@ def _row_ptrs(ts, rows, cols: int, dtype: torch.dtype, what: str):
     return _ptr_array(ptrs), cols if ld is None else ld
 
 
-def _row_vectors(ts, sizes, dtypes, what: str):
+def _row_vectors(ts, sizes, dtypes, device: int, what: str):
     if ts is None:
         return None
     if len(ts) != len(sizes):
         raise ValueError(f"need {len(sizes)} tensors as {what}, got {len(ts)}")
-    return _ptr_array([_dev_ptr(t, n, dtypes, what) if n else None for t, n in zip(ts, sizes)])
+    return _ptr_array([_dev_ptr(t, n, dtypes, what, device) if n else None for t, n in zip(ts, sizes)])
 
 
 def _norm_rows(xs):
@@ -521,12 +527,13 @@ def layernorm(xs: Sequence[torch.Tensor], weights, biases, ys: Sequence[torch.Te
     stride free) with its own scale and shift (None: ones, zeros); means and
     rstds receive each row's statistics for the backward pass (tc_layernorm)."""
     arr, rows, cols, dt = _norm_rows(xs)
-    xp, x_ld = _row_ptrs(xs, rows, cols, dt, "x")
-    yp, y_ld = _row_ptrs(ys, rows, cols, dt, "y")
+    dev = xs[0].get_device()
+    xp, x_ld = _row_ptrs(xs, rows, cols, dt, dev, "x")
+    yp, y_ld = _row_ptrs(ys, rows, cols, dt, dev, "y")
     wide, f32 = [cols] * len(rows), (torch.float32,)
-    _check(lib().tc_layernorm(len(rows), arr, cols, xp, x_ld, _DTYPES[dt], _row_vectors(weights, wide, f32, "weight"),
-                              _row_vectors(biases, wide, f32, "bias"), yp, y_ld, _row_vectors(means, rows, f32, "mean"),
-                              _row_vectors(rstds, rows, f32, "rstd"), float(eps), _stream(stream)))
+    _check(lib().tc_layernorm(len(rows), arr, cols, xp, x_ld, _DTYPES[dt], _row_vectors(weights, wide, f32, dev, "weight"),
+                              _row_vectors(biases, wide, f32, dev, "bias"), yp, y_ld, _row_vectors(means, rows, f32, dev, "mean"),
+                              _row_vectors(rstds, rows, f32, dev, "rstd"), float(eps), _stream(stream)))
 
 
 def layernorm_workspace(rows: Sequence[int], cols: int) -> int:
@@ -556,17 +563,20 @@ def layernorm_backward(dys: Sequence[torch.Tensor], xs: Sequence[torch.Tensor], 
     """The gradients of layernorm: dxs[k] of worker k's rows, and dweights[k],
     dbiases[k] (binary32 or bfloat16) summed over them (tc_layernorm_backward)."""
     arr, rows, cols, dt = _norm_rows(xs)
-    dyp, dy_ld = _row_ptrs(dys, rows, cols, dt, "dy")
-    xp, x_ld = _row_ptrs(xs, rows, cols, dt, "x")
-    dxp, dx_ld = _row_ptrs(dxs, rows, cols, dt, "dx")
+    dev = xs[0].get_device()
+    dyp, dy_ld = _row_ptrs(dys, rows, cols, dt, dev, "dy")
+    xp, x_ld = _row_ptrs(xs, rows, cols, dt, dev, "x")
+    dxp, dx_ld = _row_ptrs(dxs, rows, cols, dt, dev, "dx")
     wide, f32 = [cols] * len(rows), (torch.float32,)
     wdt = _gdt(dweights)
     need = lib().tc_layernorm_workspace(len(rows), arr, cols)
     ws = _scratch(workspace, need, xs[0].device, stream)
+    if ws.get_device() != dev:
+        raise _elsewhere(ws, dev, "the workspace")
     _check(lib().tc_layernorm_backward(
-        len(rows), arr, cols, dyp, dy_ld, xp, x_ld, _DTYPES[dt], _row_vectors(weights, wide, f32, "weight"),
-        _row_vectors(means, rows, f32, "mean"), _row_vectors(rstds, rows, f32, "rstd"), dxp, dx_ld,
-        _row_vectors(dweights, wide, (wdt,), "dweight"), _row_vectors(dbiases, wide, (wdt,), "dbias"), _DTYPES[wdt],
+        len(rows), arr, cols, dyp, dy_ld, xp, x_ld, _DTYPES[dt], _row_vectors(weights, wide, f32, dev, "weight"),
+        _row_vectors(means, rows, f32, dev, "mean"), _row_vectors(rstds, rows, f32, dev, "rstd"), dxp, dx_ld,
+        _row_vectors(dweights, wide, (wdt,), dev, "dweight"), _row_vectors(dbiases, wide, (wdt,), dev, "dbias"), _DTYPES[wdt],
         ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream)))
 
 

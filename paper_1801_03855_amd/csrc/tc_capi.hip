@@ -749,6 +749,24 @@ int32_t check_vectors(int32_t K, const int64_t* rows, const void* const* p, int 
     return TC_OK;
 }
 
+// The rows' memory belongs to the current device, whose stream the call's work
+// goes to (calls without a group have no device of their own to compare).
+int32_t check_row_device(int32_t K, const int64_t* rows, const void* const* p, const char* name) {
+    int dev = -1;
+    if (hipError_t e = hipGetDevice(&dev)) return hip_fail(e, "hipGetDevice");
+    for (int32_t k = 0; k < K; ++k) {
+        if (rows[k] == 0) continue;
+        hipPointerAttribute_t at{};
+        if (hipPointerGetAttributes(&at, p[k]) != hipSuccess) {
+            (void)hipGetLastError();  // not the runtime's memory: nothing is known of it
+        } else if (at.type == hipMemoryTypeDevice && at.device != dev) {
+            set_error("%s[%d] is on device %d but device %d is current", name, k, at.device, dev);
+            return TC_EINVAL;
+        }
+    }
+    return TC_OK;
+}
+
 int32_t check_norm(int32_t K, const int64_t* rows, int64_t cols, int32_t dtype) {
     if (K < 1 || K > TC_MAX_K) { set_error("K = %d outside [1, %d]", K, TC_MAX_K); return TC_EINVAL; }
     if (!rows) return fail(TC_EINVAL, "rows is NULL");
@@ -791,6 +809,7 @@ TC_API int32_t tc_layernorm(int32_t K, const int64_t* rows, int64_t cols, const 
         if (rstd) spans.add(rstd[k], rows[k] * 4, "rstd", k, true);
     }
     if (int32_t r = spans.check()) return r;
+    if (int32_t r = check_row_device(K, rows, x, "x")) return r;
     hipError_t e = launch_layernorm(K, rows, cols, x, x_ld, dtype, weight, bias, y, y_ld, mean, rstd, eps,
                                     static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "tc_layernorm launch");
@@ -841,6 +860,7 @@ TC_API int32_t tc_layernorm_backward(int32_t K, const int64_t* rows, int64_t col
     }
     spans.add(workspace, need, "workspace", 0, true);
     if (int32_t r = spans.check()) return r;
+    if (int32_t r = check_row_device(K, rows, x, "x")) return r;
     hipError_t e = launch_layernorm_backward(K, rows, cols, dy, dy_ld, x, x_ld, dtype, weight, mean, rstd, dx, dx_ld,
                                              dweight, dbias, w_dtype, workspace, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "tc_layernorm_backward launch");
