@@ -637,7 +637,14 @@ int64_t most_backward(Shape s, int es) {
     if (s.L == 0 || s.L == 512) return 256;
     return s.NV * 16 / es > 8 ? (es == 2 ? 768 : 512) : 1024;
 }
-constexpr int64_t kLeastBackward = 4;  // batches of rows of a workgroup
+// Batches of rows of a workgroup, backward, at least: fewer workgroups leave
+// fewer column sums to add up, more of them more of the chip at work.  With 1,
+// 2, 4 and 8, in us: 512 x 4,096 bfloat16 32.4, 20.7, 17.3, 19.7; 1,024 x 1,024
+// float 14.2, 12.2, 12.4, 15.7; 4,096 x 256 float 29.0, 18.7, 14.0, 13.7; 512 x
+// 8,192 float 25.8, 25.5, 24.1, 28.9.  Few rows lose by it: 64 x 1,024 float
+// 6.5, 7.4, 9.4, 13.4; 256 x 16,384 float 44.7, 48.6, 65.3, 105 (bfloat16 38.3,
+// 31.4, 33.5, 39.7).
+constexpr int64_t kLeastBackward = 4;
 constexpr int kRuns = 64;              // of rows, for the column sums of long rows
 
 void spread_backward(int K, const int64_t* rows, Shape s, int es, uint32_t* wg) {
