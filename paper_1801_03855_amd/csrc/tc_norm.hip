@@ -17,10 +17,13 @@
 // and added up by a second kernel in a fixed order (no atomics: the same
 // inputs give the same bits).
 //
-// Eight workers' 4,096 rows of 4,096 bfloat16: forward 0.10 ms, 5.2 TB/s (a
-// plain copy on the same machine: 5.3); backward 0.16 to 0.17 ms, 4.7 to 5.0.
-// 2,048 rows of 16,384: backward 53 us, 4.4 TB/s with the partial column sums,
-// one workgroup of 512 lanes a CU being all that the registers hold.
+// Eight workers' 4,096 rows of 4,096 bfloat16: forward 0.103 ms, 5.2 TB/s;
+// backward 0.173 ms, 4.65 TB/s (the rows' kernel 0.16 to 0.17).  On the same
+// machine a copy by ordinary accesses reaches 5.0 to 5.3 TB/s, the library's
+// own, whose loads and stores pass the caches by, 6.5.  2,048 rows of 16,384:
+// backward 67 us, the rows' kernel 53, 4.4 TB/s with the partial column sums,
+// one workgroup of 512 lanes a CU being all that the registers hold (in float,
+// past 12,288 columns, not quite: 152 to 208 bytes a lane spill).
 //
 // Rows are at any alignment of their element: on gfx950 a 16-byte access at
 // any address is one instruction.

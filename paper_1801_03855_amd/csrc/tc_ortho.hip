@@ -407,12 +407,12 @@ __device__ __forceinline__ void put_out(void* out, int dtype, int64_t at, int le
 // with a quarter each, as 32 x 32 x 16 products: 128 x 128, or 64 x 64 where
 // the larger tiles would be fewer than the CUs.
 //
-// Measured, in binary16 products: 1,400 TFLOP/s on the symmetric products of
-// the VGG-16 group and 1,100 on its P X; 830 on X X^T of the ResNet-50 group,
-// 8 copies, 560 and 700 on the other two, whose sums are a tenth as long and
-// whose tiles are read and written at 2.5 TB/s meanwhile.  On long sums the
-// card's power bounds it: the same products without the loads of their
-// operands run at 1,280 to 1,400, with the clock at 1.3 GHz.
+// Measured, in TFLOP/s of binary16 products: X X^T of the VGG-16 group, 2
+// copies, 790, its symmetric products 770 to 920, P X 1,000 to 1,110; of the
+// ResNet-50 group, 8 copies, whose sums are a tenth as long and whose tiles are
+// read and written at 2.5 TB/s meanwhile, 880, 680 and 660 to 720.  On long
+// sums the card's power is a part of what bounds it: the same products without
+// the loads of their operands run at 1,280 to 1,400, with the clock at 1.3 GHz.
 //
 // A stage is 128 bytes of each of the 2 TILE rows: a block of 32 elements, hi
 // and lo.  64 KB of LDS hold two or four stages, which are loaded straight from
