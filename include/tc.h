@@ -430,6 +430,112 @@ int32_t tc_layernorm_backward(int32_t K, const int64_t* rows, int64_t cols, cons
                               int64_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------------
+ * tc_dropout: dropout of K workers' rows from a counter-based generator, with
+ * an optional residual added in the same pass (what stands between the layers
+ * whose gradients fill a group).  Worker k has rows[k] >= 0 rows of cols
+ * elements of dtype; with T = p * 2^16 rounded to the nearest integer,
+ *     keep = u >= T;   y = (keep ? x * 2^16 / (2^16 - T) : 0) + residual
+ * in binary32, rounded once; an element that is dropped may hold anything.
+ *
+ * u is 16 bits of Philox 4x32 with 10 rounds, key (low, high half of the seed).
+ * Columns 8j .. 8j+7 of row i share one counter: with q = i * ceil(cols / 8) +
+ * j, its words are q's low half; q's high half + (k << 16); the step's low 32
+ * bits; (the step's bits 32 to 47) << 16 | site.  Column 8j + e has the low
+ * (e even) or high (e odd) half of word e / 2 of the result.  The mask depends
+ * on nothing else: not on strides, types or addresses.
+ *
+ * random: device pointer to two 64-bit integers, the seed and the step, read
+ * when the kernel runs: a captured call that is replayed after the program has
+ * changed the step has another mask.  site in [0, 65536) tells the calls of one
+ * step apart.  p in [0, 1]; with T = 2^16 nothing is kept.  x, residual (NULL:
+ * none), y: host arrays of K device pointers; a row starts every x_ld (r_ld,
+ * y_ld) elements, at least cols, at any alignment of dtype.  y[k] may be x[k]
+ * or residual[k] itself (with the same stride); apart from that y shares no
+ * byte with anything that is read or written.  A worker without rows needs no
+ * pointers.  The rows are on the current device.  cols in [1,
+ * TC_MAX_NORM_COLS], rows[k] * cols at most 2^48.
+ * ---------------------------------------------------------------------- */
+int32_t tc_dropout(int32_t K, const int64_t* rows, int64_t cols, const void* const* x, int64_t x_ld, int32_t dtype,
+                   const void* const* residual, int64_t r_ld, void* const* y, int64_t y_ld, float p,
+                   const int64_t* random, int64_t site, void* stream);
+
+/* The gradient of tc_dropout: dx = keep ? dy * 2^16 / (2^16 - T) : 0 with the
+ * mask of the call that had the same seed, step, site, p, rows and cols (the
+ * residual's gradient is dy itself).  dx[k] may be dy[k] itself.  Other
+ * arguments as above. */
+int32_t tc_dropout_backward(int32_t K, const int64_t* rows, int64_t cols, const void* const* dy, int64_t dy_ld,
+                            int32_t dtype, void* const* dx, int64_t dx_ld, float p, const int64_t* random,
+                            int64_t site, void* stream);
+
+/* ------------------------------------------------------------------------
+ * tc_cross_entropy: softmax cross entropy of K workers' rows over the classes
+ * of each worker's own weight, without keeping the logits (the loss whose
+ * gradients fill a group).  Worker k has rows[k] >= 0 rows x of cols elements
+ * of dtype, a row-major classes x cols weight of w_dtype and classes biases of
+ * w_dtype; per row
+ *     z = x weight^T + bias;   lse = log(sum exp z);   loss = lse - z[label].
+ * A row whose label is outside [0, classes) is left out: its loss is 0, and
+ * whatever it holds reaches nothing but its own lse.
+ *
+ * rows: host array of K counts.  x: host array of K device pointers; a row
+ * starts every x_ld elements, at least cols, at any alignment of dtype.  weight,
+ * bias: K device pointers at any alignment of w_dtype (pieces of a flat
+ * parameter buffer), which workers may share; bias NULL: none; a bias of
+ * -infinity takes its class out.  label: K device pointers to rows[k] 64-bit
+ * integers.  loss, lse: K device pointers to rows[k] binary32 values that
+ * receive the rows' losses and logs of sums (the backward pass needs them).
+ * Binary32 operands are taken with 22 bits or more next to the operand's
+ * largest value, products are summed and exponentials taken in binary32.  The
+ * same inputs give the same bits.  loss, lse and the workspace share no byte
+ * with each other or with what is read.  A worker without rows needs no
+ * pointers.  The rows are on the current device.  cols in [1, TC_MAX_CE_COLS],
+ * classes in [1, TC_MAX_CLASSES], rows[k] at most TC_MAX_CE_ROWS.  workspace: at
+ * least tc_cross_entropy_workspace bytes of device memory, 256-byte aligned,
+ * that nothing else uses until the call's work is done.
+ * ---------------------------------------------------------------------- */
+#define TC_MAX_CE_COLS (1 << 18)
+#define TC_MAX_CE_ROWS (1 << 24)
+#define TC_MAX_CLASSES (1 << 24)
+
+/* Bytes of workspace for these sizes and types; -1 on bad arguments. */
+int64_t tc_cross_entropy_workspace(int32_t K, const int64_t* rows, int64_t cols, int64_t classes, int32_t dtype,
+                                   int32_t w_dtype);
+
+int32_t tc_cross_entropy(int32_t K, const int64_t* rows, int64_t cols, int64_t classes, const void* const* x,
+                         int64_t x_ld, int32_t dtype, const void* const* weight, const void* const* bias,
+                         int32_t w_dtype, const int64_t* const* label, float* const* loss, float* const* lse,
+                         void* workspace, int64_t workspace_bytes, void* stream);
+
+/* Bytes of workspace of tc_cross_entropy_backward; -1 on bad arguments. */
+int64_t tc_cross_entropy_backward_workspace(int32_t K, const int64_t* rows, int64_t cols, int64_t classes,
+                                            int32_t dtype, int32_t w_dtype, int32_t dw_dtype);
+
+/* Gradients of tc_cross_entropy.  With f the factor of a row, scale * dloss (0
+ * for a row that is left out), and p = exp(z - lse),
+ *     g = p - [class == label]
+ *     dx      = f * sum over the classes of g * weight
+ *     dweight = sum over the rows of f * g * x,   dbias = sum over the rows of f * g
+ * (zeros for a worker without rows; dx of a row that is left out is 0, whatever
+ * it holds).  x, weight, bias, label as above; lse: as tc_cross_entropy wrote
+ * it.  dloss: K device pointers to rows[k] binary32 values, or NULL for ones.
+ * dx: rows of dtype every dx_ld elements; dx[k] may be x[k] itself (with the
+ * same stride).  dweight (classes x cols), dbias: K device pointers to values
+ * of dw_dtype, at any alignment of the type (pieces of a flat gradient buffer);
+ * dbias NULL: not wanted.  Sums are kept in binary32, g is held with 11 bits
+ * next to 1 (22 where the result it goes to is binary32) or more, and results
+ * are rounded once.  The same inputs give the same bits.  workspace: at least
+ * tc_cross_entropy_backward_workspace bytes, 256-byte aligned, that nothing
+ * else uses until the call's work is done.  dx apart from the above, dweight,
+ * dbias and the workspace share no byte with each other or with what is
+ * read. */
+int32_t tc_cross_entropy_backward(int32_t K, const int64_t* rows, int64_t cols, int64_t classes, const void* const* x,
+                                  int64_t x_ld, int32_t dtype, const void* const* weight, const void* const* bias,
+                                  int32_t w_dtype, const int64_t* const* label, const float* const* lse,
+                                  const float* const* dloss, float scale, void* const* dx, int64_t dx_ld,
+                                  void* const* dweight, void* const* dbias, int32_t dw_dtype, void* workspace,
+                                  int64_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * tc_orthogonalize: the momentum update of K copies of a group, with every
  * matrix of the group orthogonalised by Newton-Schulz steps (what an
  * optimizer for matrices makes of a gradient; the result takes the gradient's

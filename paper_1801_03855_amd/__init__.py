@@ -29,6 +29,10 @@ Tensor layout (the K copies interleaved in one buffer):
 What makes the gradients and the updates:
     layernorm(xs, ws, bs, ys, means, rstds)             # tc_layernorm
     layernorm_backward(dys, xs, ws, means, rstds, dxs, dws, dbs)   # tc_layernorm_backward
+    dropout(xs, residuals, ys, random, site, p)         # tc_dropout
+    dropout_backward(dys, dxs, random, site, p)         # tc_dropout_backward
+    cross_entropy(xs, ws, bs, labels, losses, lses)     # tc_cross_entropy
+    cross_entropy_backward(xs, ws, bs, labels, lses, dlosses, dxs, dws, dbs, scale)   # tc_cross_entropy_backward
     plan = OrthoPlan(g, K, shapes)                      # tc_ortho_create
     orthogonalize(plan, gs, outs, momenta)              # tc_orthogonalize
 """
@@ -113,6 +117,14 @@ def lib(path: str = LIBRARY) -> ctypes.CDLL:
         "tc_layernorm_workspace": (i64, [i32, ctypes.POINTER(i64), i64]),
         "tc_layernorm_backward": (i32, [i32, ctypes.POINTER(i64), i64, _VPP, i64, _VPP, i64, i32, _VPP, _VPP, _VPP, _VPP,
                                         i64, _VPP, _VPP, i32, _VP, i64, _VP]),
+        "tc_dropout": (i32, [i32, ctypes.POINTER(i64), i64, _VPP, i64, i32, _VPP, i64, _VPP, i64, f32, _VP, i64, _VP]),
+        "tc_dropout_backward": (i32, [i32, ctypes.POINTER(i64), i64, _VPP, i64, i32, _VPP, i64, f32, _VP, i64, _VP]),
+        "tc_cross_entropy_workspace": (i64, [i32, ctypes.POINTER(i64), i64, i64, i32, i32]),
+        "tc_cross_entropy": (i32, [i32, ctypes.POINTER(i64), i64, i64, _VPP, i64, i32, _VPP, _VPP, i32, _VPP, _VPP, _VPP, _VP,
+                                   i64, _VP]),
+        "tc_cross_entropy_backward_workspace": (i64, [i32, ctypes.POINTER(i64), i64, i64, i32, i32, i32]),
+        "tc_cross_entropy_backward": (i32, [i32, ctypes.POINTER(i64), i64, i64, _VPP, i64, i32, _VPP, _VPP, i32, _VPP, _VPP,
+                                            _VPP, f32, _VPP, i64, _VPP, _VPP, i32, _VP, i64, _VP]),
         "tc_ortho_create": (_VP, [_VP, i32, ctypes.POINTER(i64), ctypes.POINTER(i64), ctypes.POINTER(f32)]),
         "tc_ortho_destroy": (None, [_VP]),
         "tc_ortho_workspace": (i64, [_VP]),
@@ -578,6 +590,144 @@ def layernorm_backward(dys: Sequence[torch.Tensor], xs: Sequence[torch.Tensor], 
         _row_vectors(means, rows, f32, dev, "mean"), _row_vectors(rstds, rows, f32, dev, "rstd"), dxp, dx_ld,
         _row_vectors(dweights, wide, (wdt,), dev, "dweight"), _row_vectors(dbiases, wide, (wdt,), dev, "dbias"), _DTYPES[wdt],
         ws.data_ptr(), ws.numel() * ws.element_size(), _stream(stream)))
+
+
+# --------------------------------------------------------------------- dropout
+
+def _random_ptr(t: torch.Tensor, device: int) -> int:
+    if t.get_device() != device:
+        raise _elsewhere(t, device, "random")
+    if t.dtype is not torch.int64 or t.shape != (2,) or not t.is_contiguous():
+        raise ValueError("random must be two 64-bit integers, the seed and the step")
+    return t.data_ptr()
+
+
+def dropout(xs: Sequence[torch.Tensor], residuals, ys: Sequence[torch.Tensor], random: torch.Tensor, site: int = 0,
+            p: float = 0.1, stream=None) -> None:
+    """ys[k] = dropout of worker k's rows xs[k] ([rows_k, columns], row stride
+    free), plus residuals[k] (None: nothing is added).  random: a GPU tensor of
+    two int64, the seed and the step, read when the kernel runs; site tells the
+    calls of one step apart.  The mask is a function of these, the worker and an
+    element's place, and dropout_backward makes it again (tc_dropout)."""
+    arr, rows, cols, dt = _norm_rows(xs)
+    dev = xs[0].get_device()
+    xp, x_ld = _row_ptrs(xs, rows, cols, dt, dev, "x")
+    rp, r_ld = (None, cols) if residuals is None else _row_ptrs(residuals, rows, cols, dt, dev, "residual")
+    yp, y_ld = _row_ptrs(ys, rows, cols, dt, dev, "y")
+    _check(lib().tc_dropout(len(rows), arr, cols, xp, x_ld, _DTYPES[dt], rp, r_ld, yp, y_ld, float(p),
+                            _random_ptr(random, dev), int(site), _stream(stream)))
+
+
+def dropout_backward(dys: Sequence[torch.Tensor], dxs: Sequence[torch.Tensor], random: torch.Tensor, site: int = 0,
+                     p: float = 0.1, stream=None) -> None:
+    """The gradient of dropout: dxs[k] from dys[k], with the mask of the call
+    that had the same random, site, p and shapes (tc_dropout_backward)."""
+    arr, rows, cols, dt = _norm_rows(dys)
+    dev = dys[0].get_device()
+    dyp, dy_ld = _row_ptrs(dys, rows, cols, dt, dev, "dy")
+    dxp, dx_ld = _row_ptrs(dxs, rows, cols, dt, dev, "dx")
+    _check(lib().tc_dropout_backward(len(rows), arr, cols, dyp, dy_ld, _DTYPES[dt], dxp, dx_ld, float(p),
+                                     _random_ptr(random, dev), int(site), _stream(stream)))
+
+
+# --------------------------------------------------------------- cross entropy
+
+def _row_array(rows: Sequence[int]):
+    return (ctypes.c_int64 * max(1, len(rows)))(*[int(r) for r in rows])
+
+
+def _needed(n: int) -> int:
+    if n < 0:
+        raise TCError(TC_EINVAL, last_error())
+    return n
+
+
+def cross_entropy_workspace(rows: Sequence[int], cols: int, classes: int, dtype: torch.dtype = torch.float32,
+                            w_dtype: torch.dtype = torch.float32) -> int:
+    """Bytes of workspace that cross_entropy needs (tc_cross_entropy_workspace)."""
+    return _needed(lib().tc_cross_entropy_workspace(len(rows), _row_array(rows), int(cols), int(classes), _DTYPES[dtype],
+                                                    _DTYPES[w_dtype]))
+
+
+def cross_entropy_backward_workspace(rows: Sequence[int], cols: int, classes: int, dtype: torch.dtype = torch.float32,
+                                     w_dtype: torch.dtype = torch.float32, dw_dtype: torch.dtype = torch.float32) -> int:
+    """Bytes of workspace that cross_entropy_backward needs (tc_cross_entropy_backward_workspace)."""
+    return _needed(lib().tc_cross_entropy_backward_workspace(len(rows), _row_array(rows), int(cols), int(classes),
+                                                             _DTYPES[dtype], _DTYPES[w_dtype], _DTYPES[dw_dtype]))
+
+
+def _matrices(ts, K: int, shape, dtypes, device: int, what: str):
+    """Device pointers of the K workers' contiguous tensors of one shape, or None."""
+    if ts is None:
+        return None
+    if len(ts) != K:
+        raise ValueError(f"need {K} tensors as {what}, got {len(ts)}")
+    for k, t in enumerate(ts):
+        if tuple(t.shape) != shape:
+            raise ValueError(f"{what}[{k}] has shape {tuple(t.shape)}, expected {shape}")
+    n = 1
+    for s in shape:
+        n *= s
+    return _ptr_array([_dev_ptr(t, n, dtypes, f"{what}[{k}]", device) for k, t in enumerate(ts)])
+
+
+def _loss_args(xs, weights, biases, labels):
+    """(workers, row counts, columns, classes, types, device, the shared arguments' pointers)."""
+    arr, rows, cols, dt = _norm_rows(xs)
+    dev = xs[0].get_device()
+    if len(weights) != len(rows) or weights[0].dim() != 2:
+        raise ValueError("need one [classes, columns] weight per worker")
+    classes, wdt = weights[0].shape[0], _gdt(weights)
+    xp, x_ld = _row_ptrs(xs, rows, cols, dt, dev, "x")
+    wp = _matrices(weights, len(rows), (classes, cols), (wdt,), dev, "weight")
+    bp = _matrices(biases, len(rows), (classes,), (wdt,), dev, "bias")
+    return arr, rows, cols, classes, dt, wdt, dev, (xp, x_ld, _DTYPES[dt], wp, bp, _DTYPES[wdt],
+                                                    _row_vectors(labels, rows, (torch.int64,), dev, "label"))
+
+
+def _loss_scratch(workspace, need: int, dev: int, device, stream) -> torch.Tensor:
+    ws = _scratch(workspace, _needed(need), device, stream)
+    if ws.get_device() != dev:
+        raise _elsewhere(ws, dev, "the workspace")
+    return ws
+
+
+def cross_entropy(xs: Sequence[torch.Tensor], weights: Sequence[torch.Tensor], biases, labels: Sequence[torch.Tensor],
+                  losses: Sequence[torch.Tensor], lses: Sequence[torch.Tensor], workspace: Optional[torch.Tensor] = None,
+                  stream=None) -> None:
+    """losses[k] = softmax cross entropy of worker k's rows xs[k] ([rows_k,
+    columns], row stride free) over the classes of its own weight ([classes,
+    columns]) and bias (None: none), one value a row; lses receive the logs of
+    the sums for the backward pass.  labels: int64; a row whose label is outside
+    [0, classes) is left out, with a loss of 0.  The logits are never kept
+    (tc_cross_entropy)."""
+    arr, rows, cols, classes, dt, wdt, dev, shared = _loss_args(xs, weights, biases, labels)
+    f32 = (torch.float32,)
+    need = lib().tc_cross_entropy_workspace(len(rows), arr, cols, classes, _DTYPES[dt], _DTYPES[wdt])
+    ws = _loss_scratch(workspace, need, dev, xs[0].device, stream)
+    _check(lib().tc_cross_entropy(len(rows), arr, cols, classes, *shared, _row_vectors(losses, rows, f32, dev, "loss"),
+                                  _row_vectors(lses, rows, f32, dev, "lse"), ws.data_ptr(), ws.numel() * ws.element_size(),
+                                  _stream(stream)))
+
+
+def cross_entropy_backward(xs: Sequence[torch.Tensor], weights: Sequence[torch.Tensor], biases, labels, lses, dlosses,
+                           dxs: Sequence[torch.Tensor], dweights: Sequence[torch.Tensor], dbiases, scale: float = 1.0,
+                           workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """The gradients of cross_entropy, of scale * the sum of dlosses[k] * losses[k]
+    (None: ones): dxs[k] of worker k's rows, dweights[k] and dbiases[k] (None: not
+    wanted; binary32 or bfloat16) of its weight and bias.  lses: as cross_entropy
+    wrote them (tc_cross_entropy_backward)."""
+    arr, rows, cols, classes, dt, wdt, dev, shared = _loss_args(xs, weights, biases, labels)
+    f32, gdt = (torch.float32,), _gdt(dweights)
+    dxp, dx_ld = _row_ptrs(dxs, rows, cols, dt, dev, "dx")
+    need = lib().tc_cross_entropy_backward_workspace(len(rows), arr, cols, classes, _DTYPES[dt], _DTYPES[wdt], _DTYPES[gdt])
+    ws = _loss_scratch(workspace, need, dev, xs[0].device, stream)
+    _check(lib().tc_cross_entropy_backward(
+        len(rows), arr, cols, classes, *shared, _row_vectors(lses, rows, f32, dev, "lse"),
+        _row_vectors(dlosses, rows, f32, dev, "dloss"), float(scale), dxp, dx_ld,
+        _matrices(dweights, len(rows), (classes, cols), (gdt,), dev, "dweight"),
+        _matrices(dbiases, len(rows), (classes,), (gdt,), dev, "dbias"), _DTYPES[gdt], ws.data_ptr(),
+        ws.numel() * ws.element_size(), _stream(stream)))
 
 
 # ------------------------------------------------------- orthogonalised update

@@ -689,7 +689,7 @@ bool share(const Span& a, const Span& b) {
 
 // What one call reads and writes, every worker's.
 struct Spans {
-    Span s[8 * TC_MAX_K + 1];
+    Span s[10 * TC_MAX_K + 1];
     int n = 0;
 
     void add(const void* p, int64_t bytes, const char* name, int32_t k, bool written) {
@@ -865,6 +865,206 @@ TC_API int32_t tc_layernorm_backward(int32_t K, const int64_t* rows, int64_t col
                                              dweight, dbias, w_dtype, workspace, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "tc_layernorm_backward launch");
     return TC_OK;
+}
+
+// ---------------------------------------------------------------------- dropout
+
+namespace {
+
+// Both directions: residual only forward, `in` and `out` the names of the rows.
+int32_t run_dropout(int32_t K, const int64_t* rows, int64_t cols, const Rows& in, int32_t dtype, const Rows* residual,
+                    const Rows& out, float p, const int64_t* random, int64_t site, void* stream) {
+    if (!(p >= 0.0f && p <= 1.0f)) return fail(TC_EINVAL, "p must be in [0, 1]");
+    if (site < 0 || site > 65535) { set_error("site = %lld outside [0, 65535]", (long long)site); return TC_EINVAL; }
+    if (!random || !aligned(random, 8)) return fail(TC_EINVAL, "random is NULL or not 8-byte aligned");
+    for (int32_t k = 0; k < K; ++k)
+        if (rows[k] > (int64_t{1} << 48) / cols) { set_error("rows[%d] * cols is more than 2^48", k); return TC_EINVAL; }
+    if (int32_t r = check_rows(K, rows, cols, in)) return r;
+    if (residual)
+        if (int32_t r = check_rows(K, rows, cols, *residual)) return r;
+    if (int32_t r = check_rows(K, rows, cols, out)) return r;
+    Spans spans;
+    for (int32_t k = 0; k < K; ++k) {
+        spans.add(in, k, rows[k], cols, false);
+        if (residual) spans.add(*residual, k, rows[k], cols, false);
+        spans.add(out, k, rows[k], cols, true);
+    }
+    spans.add(random, 16, "random", 0, false);
+    if (int32_t r = spans.check()) return r;
+    if (int32_t r = check_row_device(K, rows, in.p, in.name)) return r;
+    const uint32_t threshold = static_cast<uint32_t>(std::floor(static_cast<double>(p) * 65536.0 + 0.5));
+    hipError_t e = launch_dropout(K, rows, cols, in.p, in.ld, dtype, residual ? residual->p : nullptr,
+                                  residual ? residual->ld : 0, const_cast<void* const*>(out.p), out.ld, threshold, random,
+                                  static_cast<uint32_t>(site), static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, "dropout launch");
+    return TC_OK;
+}
+
+}  // namespace
+
+TC_API int32_t tc_dropout(int32_t K, const int64_t* rows, int64_t cols, const void* const* x, int64_t x_ld, int32_t dtype,
+                          const void* const* residual, int64_t r_ld, void* const* y, int64_t y_ld, float p,
+                          const int64_t* random, int64_t site, void* stream) {
+    clear_error();
+    if (int32_t r = check_norm(K, rows, cols, dtype)) return r;
+    const int es = elem_size(dtype);
+    const Rows add{residual, r_ld, es, "residual"};
+    return run_dropout(K, rows, cols, {x, x_ld, es, "x"}, dtype, residual ? &add : nullptr, {y, y_ld, es, "y"}, p, random,
+                       site, stream);
+}
+
+TC_API int32_t tc_dropout_backward(int32_t K, const int64_t* rows, int64_t cols, const void* const* dy, int64_t dy_ld,
+                                   int32_t dtype, void* const* dx, int64_t dx_ld, float p, const int64_t* random,
+                                   int64_t site, void* stream) {
+    clear_error();
+    if (int32_t r = check_norm(K, rows, cols, dtype)) return r;
+    const int es = elem_size(dtype);
+    return run_dropout(K, rows, cols, {dy, dy_ld, es, "dy"}, dtype, nullptr, {dx, dx_ld, es, "dx"}, p, random, site, stream);
+}
+
+// ---------------------------------------------------------------- cross entropy
+
+namespace {
+
+int32_t check_loss(int32_t K, const int64_t* rows, int64_t cols, int64_t classes, int32_t dtype, int32_t w_dtype) {
+    if (int32_t r = check_norm(K, rows, cols, dtype)) return r;
+    if (cols > TC_MAX_CE_COLS) { set_error("cols = %lld is more than %d", (long long)cols, TC_MAX_CE_COLS); return TC_EINVAL; }
+    if (classes < 1 || classes > TC_MAX_CLASSES) {
+        set_error("classes = %lld outside [1, %d]", (long long)classes, TC_MAX_CLASSES);
+        return TC_EINVAL;
+    }
+    for (int32_t k = 0; k < K; ++k)
+        if (rows[k] > TC_MAX_CE_ROWS) { set_error("rows[%d] = %lld is more than %d", k, (long long)rows[k], TC_MAX_CE_ROWS); return TC_EINVAL; }
+    if (!elem_size(w_dtype)) { set_error("unknown dtype %d of weight and bias", w_dtype); return TC_EINVAL; }
+    return TC_OK;
+}
+
+int32_t run_loss(LossCall& c, int64_t workspace_bytes, void* stream, const char* name) {
+    const int32_t K = c.K;
+    const int64_t *rows = c.rows, cols = c.cols, classes = c.classes;
+    const int es = elem_size(c.dtype), ws = elem_size(c.w_dtype), dws = elem_size(c.dw_dtype);
+    const Rows in{c.x, c.x_ld, es, "x"}, out{c.dx, c.dx_ld, es, "dx"};
+    if (int32_t r = check_rows(K, rows, cols, in)) return r;
+    if (c.backward)
+        if (int32_t r = check_rows(K, rows, cols, out)) return r;
+    // one vector (or matrix) a worker
+    const struct Vector {
+        const void* const* p;
+        int64_t each;  // elements; 0: one a row
+        int es;
+        const char* name;
+        bool wanted, written, always;
+    } vectors[] = {
+        {c.weight, classes * cols, ws, "weight", true, false, false},
+        {c.bias, classes, ws, "bias", c.bias != nullptr, false, false},
+        {reinterpret_cast<const void* const*>(c.label), 0, 8, "label", true, false, false},
+        {reinterpret_cast<const void* const*>(c.loss), 0, 4, "loss", !c.backward, true, false},
+        {c.backward ? reinterpret_cast<const void* const*>(c.lse_in) : reinterpret_cast<const void* const*>(c.lse), 0, 4,
+         "lse", true, !c.backward, false},
+        {reinterpret_cast<const void* const*>(c.dloss), 0, 4, "dloss", c.dloss != nullptr, false, false},
+        {const_cast<const void* const*>(c.dweight), classes * cols, dws, "dweight", c.backward, true, true},
+        {const_cast<const void* const*>(c.dbias), classes, dws, "dbias", c.dbias != nullptr, true, true},
+    };
+    for (const Vector& v : vectors) {
+        if (!v.wanted) continue;
+        if (!v.p) { set_error("%s is NULL", v.name); return TC_EINVAL; }
+        if (int32_t r = check_vectors(K, v.always ? nullptr : rows, v.p, v.es, v.name)) return r;
+    }
+    const int64_t need = cross_entropy_workspace(K, rows, cols, classes, c.dtype, c.w_dtype, c.backward, c.dw_dtype);
+    if (!c.workspace || !aligned(c.workspace, 256)) return fail(TC_EINVAL, "workspace is NULL or not 256-byte aligned");
+    if (workspace_bytes < need) {
+        set_error("the workspace has %lld bytes, %lld are needed", (long long)workspace_bytes, (long long)need);
+        return TC_EINVAL;
+    }
+    Spans spans;
+    for (int32_t k = 0; k < K; ++k) {
+        for (const Vector& v : vectors)
+            if (v.wanted && (v.always || rows[k] > 0)) spans.add(v.p[k], (v.each ? v.each : rows[k]) * v.es, v.name, k, v.written);
+        spans.add(in, k, rows[k], cols, false);
+        if (c.backward) spans.add(out, k, rows[k], cols, true);
+    }
+    spans.add(c.workspace, need, "workspace", 0, true);
+    if (int32_t r = spans.check()) return r;
+    if (int32_t r = check_row_device(K, rows, c.x, "x")) return r;
+    hipError_t e = launch_cross_entropy(c, static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return hip_fail(e, name);
+    return TC_OK;
+}
+
+}  // namespace
+
+TC_API int64_t tc_cross_entropy_workspace(int32_t K, const int64_t* rows, int64_t cols, int64_t classes, int32_t dtype,
+                                          int32_t w_dtype) {
+    clear_error();
+    if (check_loss(K, rows, cols, classes, dtype, w_dtype) != TC_OK) return -1;
+    return cross_entropy_workspace(K, rows, cols, classes, dtype, w_dtype, false, TC_F32);
+}
+
+TC_API int32_t tc_cross_entropy(int32_t K, const int64_t* rows, int64_t cols, int64_t classes, const void* const* x,
+                                int64_t x_ld, int32_t dtype, const void* const* weight, const void* const* bias,
+                                int32_t w_dtype, const int64_t* const* label, float* const* loss, float* const* lse,
+                                void* workspace, int64_t workspace_bytes, void* stream) {
+    clear_error();
+    if (int32_t r = check_loss(K, rows, cols, classes, dtype, w_dtype)) return r;
+    LossCall c;
+    c.K = K;
+    c.rows = rows;
+    c.cols = cols;
+    c.classes = classes;
+    c.x = x;
+    c.x_ld = x_ld;
+    c.dtype = dtype;
+    c.w_dtype = w_dtype;
+    c.weight = weight;
+    c.bias = bias;
+    c.label = label;
+    c.workspace = workspace;
+    c.loss = loss;
+    c.lse = lse;
+    return run_loss(c, workspace_bytes, stream, "tc_cross_entropy launch");
+}
+
+TC_API int64_t tc_cross_entropy_backward_workspace(int32_t K, const int64_t* rows, int64_t cols, int64_t classes,
+                                                   int32_t dtype, int32_t w_dtype, int32_t dw_dtype) {
+    clear_error();
+    if (check_loss(K, rows, cols, classes, dtype, w_dtype) != TC_OK) return -1;
+    if (!elem_size(dw_dtype)) { set_error("unknown dtype %d of dweight and dbias", dw_dtype); return -1; }
+    return cross_entropy_workspace(K, rows, cols, classes, dtype, w_dtype, true, dw_dtype);
+}
+
+TC_API int32_t tc_cross_entropy_backward(int32_t K, const int64_t* rows, int64_t cols, int64_t classes,
+                                         const void* const* x, int64_t x_ld, int32_t dtype, const void* const* weight,
+                                         const void* const* bias, int32_t w_dtype, const int64_t* const* label,
+                                         const float* const* lse, const float* const* dloss, float scale, void* const* dx,
+                                         int64_t dx_ld, void* const* dweight, void* const* dbias, int32_t dw_dtype,
+                                         void* workspace, int64_t workspace_bytes, void* stream) {
+    clear_error();
+    if (int32_t r = check_loss(K, rows, cols, classes, dtype, w_dtype)) return r;
+    if (!elem_size(dw_dtype)) { set_error("unknown dtype %d of dweight and dbias", dw_dtype); return TC_EINVAL; }
+    if (!std::isfinite(scale)) return fail(TC_EINVAL, "scale must be finite");
+    LossCall c;
+    c.K = K;
+    c.rows = rows;
+    c.cols = cols;
+    c.classes = classes;
+    c.x = x;
+    c.x_ld = x_ld;
+    c.dtype = dtype;
+    c.w_dtype = w_dtype;
+    c.weight = weight;
+    c.bias = bias;
+    c.label = label;
+    c.workspace = workspace;
+    c.backward = true;
+    c.lse_in = lse;
+    c.dloss = dloss;
+    c.scale = scale;
+    c.dx = dx;
+    c.dx_ld = dx_ld;
+    c.dweight = dweight;
+    c.dbias = dbias;
+    c.dw_dtype = dw_dtype;
+    return run_loss(c, workspace_bytes, stream, "tc_cross_entropy_backward launch");
 }
 
 // ------------------------------------------------------- orthogonalised update

@@ -172,6 +172,42 @@ hipError_t launch_layernorm_backward(int K, const int64_t* rows, int64_t cols, c
                                      const float* const* mean, const float* const* rstd, void* const* dx, int64_t dx_ld,
                                      void* const* dw, void* const* db, int w_dtype, void* workspace, hipStream_t stream);
 
+// Dropout of K workers' rows (r null: no residual), threshold of 16 bits.
+hipError_t launch_dropout(int K, const int64_t* rows, int64_t cols, const void* const* x, int64_t x_ld, int dtype,
+                          const void* const* r, int64_t r_ld, void* const* y, int64_t y_ld, uint32_t threshold,
+                          const int64_t* random, uint32_t site, hipStream_t stream);
+
+// Softmax cross entropy of K workers' rows, or its gradients (row strides in
+// elements).
+struct LossCall {
+    int K = 0;
+    const int64_t* rows = nullptr;
+    int64_t cols = 0, classes = 0;
+    const void* const* x = nullptr;
+    int64_t x_ld = 0;
+    int dtype = TC_F32, w_dtype = TC_F32;
+    const void* const* weight = nullptr;
+    const void* const* bias = nullptr;  // may be null
+    const int64_t* const* label = nullptr;
+    void* workspace = nullptr;
+    bool backward = false;
+    // forward
+    float* const* loss = nullptr;
+    float* const* lse = nullptr;
+    // backward
+    const float* const* lse_in = nullptr;
+    const float* const* dloss = nullptr;  // may be null
+    float scale = 1.0f;
+    void* const* dx = nullptr;
+    int64_t dx_ld = 0;
+    void* const* dweight = nullptr;
+    void* const* dbias = nullptr;  // may be null
+    int dw_dtype = TC_F32;
+};
+int64_t cross_entropy_workspace(int K, const int64_t* rows, int64_t cols, int64_t classes, int dtype, int w_dtype,
+                                bool backward, int dw_dtype);
+hipError_t launch_cross_entropy(const LossCall& c, hipStream_t stream);
+
 // The orthogonalised momentum update: the plan (null and an error on failure),
 // what it needs, whether the coefficients keep the values in range, the call.
 tc_ortho* make_ortho(const tc_group* g, int32_t K, const int64_t* rows, const int64_t* cols, const float* scale,

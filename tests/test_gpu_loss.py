@@ -1,0 +1,377 @@
+"""Softmax cross entropy of K workers' rows and its gradients against the
+formulas in 64 bits.
+
+Bounds, from the arithmetic.  A logit's products are summed in binary32 (each of
+C additions off by at most 2^-24 of what the terms' sizes add up to), and
+binary32 operands are held with 22 bits: dz <= (2^-21 [binary32] + (C + 16)
+2^-24) sum |x w| + 2^-23 |b|.  Twice that is what the exponentials are off by,
+next to their own rounding (an ulp, and 2^-23 of the exponent); their sum in
+binary32 has at most 64 + V / 128 + 32 additions in a row.  g is held with 11
+bits (a bfloat16 result) or 22; so are the operands it meets, which a bfloat16
+operand needs 8 of.  A result is rounded once, half a step."""
+
+import itertools
+
+import pytest
+import torch
+
+import paper_1801_03855_amd as tc
+
+pytestmark = pytest.mark.gpu
+
+F32, BF16 = torch.float32, torch.bfloat16
+LEFT_OUT = -100
+
+
+def view(t, pad):
+    wide = torch.full((t.shape[0], t.shape[1] + pad), float("nan"), dtype=t.dtype, device=t.device)
+    wide[:, : t.shape[1]] = t
+    return wide[:, : t.shape[1]]
+
+
+def flat_views(ts, offset):
+    """The tensors as pieces of one flat buffer that starts `offset` elements off."""
+    flat = torch.empty(offset + sum(t.numel() for t in ts) + 8, dtype=ts[0].dtype, device="cuda")
+    out, at = [], offset
+    for t in ts:
+        out.append(flat[at : at + t.numel()].view(t.shape).copy_(t))
+        at += t.numel()
+    return out
+
+
+class Case:
+    def __init__(self, rows, cols, classes, x=F32, w=F32, dw=F32, bias=False, pad=0, weighted=False, out=0.0, offset=0, seed=0, scale=0.25):
+        gen = torch.Generator(device="cuda").manual_seed(seed)
+        r = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
+        self.rows, self.cols, self.classes, self.dw_type, self.scale = list(rows), cols, classes, dw, scale
+        K = len(self.rows)
+        self.w = flat_views([(r(classes, cols) * cols ** -0.5 * 1.5).to(w) for _ in range(K)], offset)
+        self.b = flat_views([r(classes).to(w) for _ in range(K)], offset) if bias else None
+        self.x = [view((r(n, cols) * 1.5).to(x), pad) for n in rows]
+        self.label = [torch.randint(0, classes, (n,), generator=gen, device="cuda") for n in rows]
+        for t in self.label:
+            t[torch.rand(len(t), generator=gen, device="cuda") < out] = LEFT_OUT
+        self.dloss = [torch.rand(n, generator=gen, device="cuda") * 2 - 0.5 for n in rows] if weighted else None
+        self.loss, self.lse = [[torch.full((n,), 7.0, device="cuda") for n in rows] for _ in range(2)]
+        self.dx = [view(torch.full((n, cols), 7.0, dtype=x, device="cuda"), pad) for n in rows]
+        self.dw = flat_views([torch.full((classes, cols), 7.0, dtype=dw, device="cuda") for _ in rows], offset)
+        self.db = flat_views([torch.full((classes,), 7.0, dtype=dw, device="cuda") for _ in rows], offset) if bias else None
+
+    def forward(self, **k):
+        tc.cross_entropy(self.x, self.w, self.b, self.label, self.loss, self.lse, **k)
+
+    def backward(self, **k):
+        tc.cross_entropy_backward(self.x, self.w, self.b, self.label, self.lse, self.dloss, self.dx, self.dw, self.db,
+                                  scale=self.scale, **k)
+
+    def outputs(self):
+        return self.loss + self.lse + self.dx + self.dw + (self.db or [])
+
+
+def eps(dtype):
+    return torch.finfo(dtype).eps / 2
+
+
+def logits(c, k):
+    """The logits, and how far binary32 sums may be from them."""
+    x, w = c.x[k].double(), c.w[k].double()
+    b = c.b[k].double() if c.b else torch.zeros(c.classes, dtype=torch.float64, device="cuda")
+    wide = c.x[k].dtype is F32 or c.w[k].dtype is F32
+    z = x @ w.t() + b
+    size = x.abs() @ w.abs().t()
+    dz = (2.0 ** -21 * wide + (c.cols + 16) * 2.0 ** -24) * size + 2.0 ** -23 * (z.abs() + torch.where(b.isinf(), 0.0, b.abs()))
+    return z, torch.where(z.isinf(), 0.0, dz)
+
+
+def check_forward(c):
+    for k, n in enumerate(c.rows):
+        if not n:
+            continue
+        z, dz = logits(c, k)
+        lse = torch.logsumexp(z, 1)
+        far = (lse[:, None] - torch.where(z.isinf(), lse[:, None], z)).amax(1)
+        off = 2 * dz.amax(1) + lse.abs() * 2.0 ** -22 + (100 + c.classes / 128) * 2.0 ** -23 + far * 2.0 ** -22
+        assert bool(((c.lse[k].double() - lse).abs() <= off).all()), ("lse", k, ((c.lse[k].double() - lse).abs() / off).max())
+        there = (c.label[k] >= 0) & (c.label[k] < c.classes)
+        own = z.gather(1, torch.where(there, c.label[k], 0)[:, None])[:, 0]
+        want = torch.where(there, lse - own, 0.0)
+        off = off + 2 * dz.amax(1) + own.abs() * 2.0 ** -23 + want.abs() * 2.0 ** -23
+        same = torch.where(want.isinf(), c.loss[k].double() == want, (c.loss[k].double() - want).abs() <= off)
+        assert bool(same.all()), ("loss", k, ((c.loss[k].double() - want).abs() / off).max())
+        assert bool((c.loss[k][~there] == 0).all())
+
+
+def check_backward(c):
+    for k, n in enumerate(c.rows):
+        if not n:
+            assert not c.dw[k].any() and (c.db is None or not c.db[k].any())
+            continue
+        x, w, lse = c.x[k].double(), c.w[k].double(), c.lse[k].double()[:, None]
+        z, dz = logits(c, k)
+        there = (c.label[k] >= 0) & (c.label[k] < c.classes)
+        f = c.scale * there.double()
+        if c.dloss is not None:
+            f = f * c.dloss[k].double()
+        f = f[:, None]
+        p = torch.exp(z - lse)
+        g = p.clone()
+        g[torch.arange(n, device="cuda"), torch.where(there, c.label[k], 0)] -= 1.0
+        t = torch.where(z.isinf(), 0.0, (z - lse).abs())
+        dg = p * (2 * dz + (t + lse.abs() + 4) * 2.0 ** -22) + g.abs() * 2.0 ** -24 + 2.0 ** -38
+        bits = lambda dtype: 2.0 ** -12 if dtype is BF16 else 2.0 ** -21  # noqa: E731
+
+        def bound(dg, size, held, operand, terms, dtype, want):
+            # (an operand of 8 bits is whole)
+            return dg + size * ((held if operand is BF16 else 2 * held) + held + (terms + 64) * 2.0 ** -24) + want.abs() * eps(dtype) + 1e-30
+
+        want = f * (g @ w)
+        held = bits(c.x[k].dtype)
+        off = bound(f.abs() * (dg @ w.abs()), f.abs() * (g.abs() @ w.abs()), held, c.w[k].dtype, c.classes, c.x[k].dtype, want)
+        got = c.dx[k].double()
+        assert bool(((got - want).abs() <= off).all()), ("dx", k, ((got - want).abs() / off).max())
+        assert bool((got[~there] == 0).all())
+        held = bits(c.dw_type)
+        fg, fdg = f * g, f.abs() * dg
+        want = fg.t() @ x
+        off = bound(fdg.t() @ x.abs(), fg.abs().t() @ x.abs(), held, c.x[k].dtype, n, c.dw_type, want)
+        got = c.dw[k].double()
+        assert bool(((got - want).abs() <= off).all()), ("dw", k, ((got - want).abs() / off).max())
+        if c.db is not None:
+            want = fg.sum(0)
+            off = fdg.sum(0) + fg.abs().sum(0) * (held + (n + 64) * 2.0 ** -24) + want.abs() * eps(c.dw_type) + 1e-30
+            got = c.db[k].double()
+            assert bool(((got - want).abs() <= off).all()), ("db", k, ((got - want).abs() / off).max())
+
+
+def check(c):
+    c.forward()
+    torch.cuda.synchronize()
+    check_forward(c)
+    c.backward()
+    torch.cuda.synchronize()
+    check_backward(c)
+
+
+SIZES = [([1], 1, 1), ([1], 64, 2), ([3, 0, 5], 7, 127), ([1, 1], 512, 1000), ([32] * 3, 200, 1000), ([64, 65], 65, 129), ([17], 128, 4099),
+         ([129, 1], 96, 257), ([300, 257, 2], 320, 515), ([513], 1003, 1031), ([16], 2048, 1000)]
+
+
+@pytest.mark.parametrize("rows,cols,classes", SIZES, ids=str)
+@pytest.mark.parametrize("x,w,dw", [(F32, F32, F32), (BF16, BF16, BF16), (BF16, F32, F32)], ids=["f32", "bf16", "mixed"])
+def test_sizes(rows, cols, classes, x, w, dw):
+    check(Case(rows, cols, classes, x, w, dw, bias=True, out=0.1))
+
+
+@pytest.mark.parametrize("x,w,dw", list(itertools.product((F32, BF16), repeat=3)), ids=str)
+@pytest.mark.parametrize("bias,weighted", [(False, True), (True, False)])
+def test_types(x, w, dw, bias, weighted):
+    check(Case([40, 70], 96, 300, x, w, dw, bias=bias, weighted=weighted, pad=3, out=0.2, seed=1))
+
+
+@pytest.mark.parametrize("x,w", [(F32, F32), (BF16, BF16)], ids=["f32", "bf16"])
+@pytest.mark.parametrize("pad,offset", [(8, 8), (1, 1), (0, 3)])
+@pytest.mark.parametrize("rows", [[5, 9], [130, 90]], ids=str)
+def test_strides_and_alignment(rows, x, w, pad, offset):
+    check(Case(rows, 128, 333, x, w, w, bias=True, pad=pad, offset=offset, seed=2))
+
+
+@pytest.mark.parametrize("x,w,dw", [(F32, F32, F32), (BF16, BF16, BF16)], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows", [[6, 4], [140, 70]], ids=str)
+def test_what_is_left_out_may_hold_anything(rows, x, w, dw):
+    """Rows without a label, or with a factor of zero, that hold infinities, NaN and the largest values: the
+    others' results are as if they held zeros, and theirs are zero."""
+    results = []
+    for bad in (0.0, float("nan"), float("inf"), 3e38):
+        c = Case(rows, 96, 300, x, w, dw, bias=True, weighted=True, seed=3)
+        for t, label, dloss in zip(c.x, c.label, c.dloss):
+            label[1] = LEFT_OUT
+            label[2] = c.classes
+            dloss[3] = 0.0
+            dloss[1] = float("nan")
+            t[1:4] = bad
+        c.forward()
+        c.backward()
+        torch.cuda.synchronize()
+        for k in range(2):
+            assert bool((c.loss[k][1:3] == 0).all()) and not c.dx[k][1:4].any()
+        keep = [torch.cat([v[:1], v[4:]]) for v in c.loss + c.lse]
+        results.append(keep + c.dx + c.dw + c.db)
+    for other in results[1:]:
+        for a, b in zip(results[0], other):
+            assert torch.equal(a, b)
+
+
+def test_a_row_that_is_not_finite_reaches_its_own_results_alone():
+    for x in (F32, BF16):
+        good, c = [Case([140], 96, 300, x, x, x, seed=4) for _ in range(2)]
+        c.x[0][7, 5] = float("inf")
+        c.x[0][9] = float("nan")
+        for q in (good, c):
+            q.forward()
+            q.backward()
+        rest = [r for r in range(140) if r not in (7, 9)]
+        assert c.loss[0][[7, 9]].isnan().all() and c.dx[0][[7, 9]].isnan().all()
+        assert torch.equal(good.loss[0][rest], c.loss[0][rest]) and torch.equal(good.dx[0][rest], c.dx[0][rest])
+        assert c.dw[0].isnan().any()
+
+
+@pytest.mark.parametrize("x", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows", [[5], [150]], ids=str)
+def test_classes_that_a_bias_takes_out(rows, x):
+    c = Case(rows, 96, 300, x, x, x, bias=True, seed=5)
+    c.b[0][10:200] = float("-inf")
+    c.label[0].fill_(250)
+    c.label[0][0] = 11  # (its loss is infinite)
+    c.dloss = [torch.ones(rows[0], device="cuda")]
+    c.forward()
+    torch.cuda.synchronize()
+    check_forward(c)
+    assert c.loss[0][0] == float("inf") and bool(c.loss[0][1:].isfinite().all())
+    c.backward()
+    torch.cuda.synchronize()
+    check_backward(c)
+    others = [v for v in range(10, 200) if v != 11]
+    assert not c.dw[0][others].any() and not c.db[0][others].any()
+
+
+def test_every_class_taken_out():
+    c = Case([3, 200], 64, 130, bias=True, seed=6)
+    for b in c.b:
+        b.fill_(float("-inf"))
+    c.forward()
+    torch.cuda.synchronize()
+    for k in range(2):
+        assert bool((c.lse[k] == float("-inf")).all()) and bool(c.loss[k].isnan().all())
+
+
+@pytest.mark.parametrize("big,small", [(1e30, 1e-30), (3e38, 1.0), (1e-38, 1e-3), (1.0, 1e-37)])
+def test_values_of_any_size(big, small):
+    """Rows and weights of very different sizes: each result next to its own terms."""
+    c = Case([70], 80, 200, seed=7)
+    c.x[0].mul_(0.1)
+    c.x[0][::2] *= 1e-3
+    c.x[0].mul_(min(big, 1e37))
+    c.w[0].mul_(min(1.0 / min(big, 1e37), 1e37))
+    c.x[0][5] *= small if small < 1 else 1.0
+    check(c)
+
+
+def test_a_certain_row():
+    """The label's own probability rounds to one: its gradient does not."""
+    c = Case([4, 140], 64, 100, seed=8)
+    for x, w, label in zip(c.x, c.w, c.label):
+        x.copy_(w[label] * 12.0)
+    check(c)
+
+
+def test_many_rows_and_pieces():
+    """Rows enough for several pieces of the classes, which dx adds up."""
+    for x in (F32, BF16):
+        rows, cols, classes = 70000, 72, 5003
+        c = Case([rows], cols, classes, x, x, F32, bias=True, out=0.05, seed=9, scale=1.0 / 64)
+        check(c)
+
+
+def test_few_rows_and_many_classes():
+    for x in (F32, BF16):
+        check(Case([3, 1], 264, 40009, x, x, x, out=0.0, seed=10))
+
+
+def test_the_same_bits_and_any_stream():
+    c = Case([40, 200], 136, 1001, BF16, F32, F32, bias=True, weighted=True, seed=11)
+    c.forward()
+    c.backward()
+    torch.cuda.synchronize()
+    first = [t.clone() for t in c.outputs()]
+    for t in c.outputs():
+        t.zero_()
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    c.forward(stream=s)
+    c.backward(stream=s)
+    s.synchronize()
+    for a, b in zip(first, c.outputs()):
+        assert torch.equal(a, b)
+
+
+def test_two_captured_graphs_and_one_workspace():
+    cases = [Case([33, 150], 128, 700, x, w, F32, bias=True, seed=12) for x, w in ((F32, F32), (BF16, BF16))]
+    need = 0
+    for c in cases:
+        x, w = c.x[0].dtype, c.w[0].dtype
+        need = max(need, tc.cross_entropy_workspace(c.rows, c.cols, c.classes, x, w),
+                   tc.cross_entropy_backward_workspace(c.rows, c.cols, c.classes, x, w, F32))
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    want = []
+    for c in cases:
+        c.forward(workspace=ws)
+        c.backward(workspace=ws)
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in c.outputs()])
+    graphs = []
+    for c in cases:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            c.forward(workspace=ws)
+            c.backward(workspace=ws)
+        graphs.append(g)
+    for turn in range(3):
+        for c in cases:
+            for t in c.outputs():
+                t.fill_(7.0)
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for c, ts in zip(cases, want):
+            for a, b in zip(ts, c.outputs()):
+                assert torch.equal(a, b), turn
+        ws.random_(0, 255)  # the program's own work between the replays
+        torch.cuda.synchronize()
+
+
+def test_rows_behind_the_views_stay():
+    c = Case([5, 140], 100, 257, pad=5, seed=13)
+    wide = [t._base if t._base is not None else t for t in c.dx]
+    for t in wide:
+        t.fill_(3.0)
+    c.forward()
+    c.backward()
+    torch.cuda.synchronize()
+    for t in wide:
+        assert bool((t[:, 100:] == 3.0).all())
+
+
+def test_dx_in_the_place_of_x():
+    for x in (F32, BF16):
+        a, b = [Case([9, 140], 128, 300, x, x, x, seed=14) for _ in range(2)]
+        a.forward()
+        b.forward()
+        a.backward()
+        b.dx = b.x
+        b.backward()
+        torch.cuda.synchronize()
+        for p, q in zip(a.dx + a.dw, b.x + b.dw):
+            assert torch.equal(p, q)
+
+
+def test_gradients_against_differences():
+    """(L(t + h d) - L(t - h d)) / 2h along a direction d.  The sum of the losses is off by at most 2^-21 of itself and the
+    third derivative's part is under h^2 times the direction's size cubed."""
+    c = Case([24], 48, 90, bias=True, seed=15, scale=1.0)
+    c.forward()
+    c.backward()
+    torch.cuda.synchronize()
+    gen = torch.Generator(device="cuda").manual_seed(16)
+    for t, g in ((c.x[0], c.dx[0]), (c.w[0], c.dw[0]), (c.b[0], c.db[0])):
+        d = torch.randn(t.shape, generator=gen, device="cuda")
+        d /= d.norm()
+        start, h, sums = t.clone(), 2.0 ** -5, []
+        for sign in (1.0, -1.0):
+            t.copy_(start + sign * h * d)
+            c.forward()
+            torch.cuda.synchronize()
+            sums.append(float(c.loss[0].double().sum()))
+        t.copy_(start)
+        want = float((g.double() * d.double()).sum())
+        tol = abs(sums[0]) * 2.0 ** -21 / h + 24 * h * h * 4.0
+        assert abs((sums[0] - sums[1]) / (2 * h) - want) <= tol
