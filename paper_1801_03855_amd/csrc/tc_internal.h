@@ -207,6 +207,11 @@ struct LossCall {
 int64_t cross_entropy_workspace(int K, const int64_t* rows, int64_t cols, int64_t classes, int dtype, int w_dtype,
                                 bool backward, int dw_dtype);
 hipError_t launch_cross_entropy(const LossCall& c, hipStream_t stream);
+// The same where a worker's rows or the classes are few; list: the workers with rows.
+bool few_fits(int K, const int64_t* rows, int64_t classes);
+int64_t few_workspace(int K, const int64_t* rows, int64_t cols, int64_t classes, int dtype, int w_dtype, bool backward,
+                      int dw_dtype);
+hipError_t launch_few(const LossCall& c, const int* list, int count, hipStream_t stream);
 
 // The orthogonalised momentum update: the plan (null and an error on failure),
 // what it needs, whether the coefficients keep the values in range, the call.

@@ -930,6 +930,7 @@ int runs_of(int left, int right, Side& l, Side& r) {
 
 int64_t cross_entropy_workspace(int K, const int64_t* rows, int64_t cols, int64_t classes, int dtype, int w_dtype,
                                 bool backward, int dw_dtype) {
+    if (few_fits(K, rows, classes)) return few_workspace(K, rows, cols, classes, dtype, w_dtype, backward, dw_dtype);
     const Plan p = plan_of(K, rows, cols, classes, dtype, w_dtype, backward, dw_dtype);
     return p.batch * p.stride;
 }
@@ -949,7 +950,6 @@ void run_logits(const LogitArgs& a, bool bf, int n, hipStream_t s) {
 
 hipError_t launch_cross_entropy(const LossCall& c, hipStream_t s) {
     const bool back = c.backward;
-    const Plan p = plan_of(c.K, c.rows, c.cols, c.classes, c.dtype, c.w_dtype, back, c.dw_dtype);
     const int x_bf = c.dtype == TC_BF16, w_bf = c.w_dtype == TC_BF16, dw_bf = c.dw_dtype == TC_BF16;
     const int we = w_bf ? 2 : 4, dwe = dw_bf ? 2 : 4;
     const int64_t cols = c.cols, classes = c.classes;
@@ -966,6 +966,8 @@ hipError_t launch_cross_entropy(const LossCall& c, hipStream_t s) {
             if (hipError_t e = hipGetLastError()) return e;
         }
     }
+    if (few_fits(c.K, c.rows, classes)) return launch_few(c, list, count, s);
+    const Plan p = plan_of(c.K, c.rows, cols, classes, c.dtype, c.w_dtype, back, c.dw_dtype);
     for (int k0 = 0; k0 < count; k0 += p.batch) {
         const int n = std::min(p.batch, count - k0);
         const int* who = list + k0;

@@ -1,0 +1,844 @@
+// Softmax cross entropy and its gradients where one side is short: at most 64
+// rows a worker (a small batch, the last tokens of a few sequences), or at most
+// 64 classes.  The formulas are the large path's; what differs is what bounds
+// them: the long side (the weight, or the rows) is read once a pass, and its
+// products with the short side are few.  So nothing is laid out anew.
+//
+// "Stream" is the long side (n x cols), "side" the short one (up to 64 x cols).
+//   few_logit   a workgroup takes 32 or so rows of the stream: the logits, with
+//               the sum over columns cut among its waves and joined in LDS; then
+//               forward what a row needs of them, backward g, and with it at once
+//               the stream's own gradient, g side, a sum over the short side
+//   few_sum     the side's gradient, g^T stream: a sum over the stream, which is
+//               read again, cut among waves and workgroups
+//   few_finish  adds the workgroups' sums up in a fixed order
+//
+// Operands go from memory to registers and to the matrix cores as bfloat16
+// pieces: a bfloat16 element is one, a binary32 element three that hold its 24
+// bits (cut off, not rounded, so that the largest value does not overflow).  Of
+// the pieces' products those under 2^-24 of a term are left out; of g, whose
+// results are rounded to bfloat16, two pieces are taken.
+//
+// A matrix instruction sums over 32 elements, of which a lane has eight.  For
+// the logits they are neighbours in a row.  For the other two products the sum
+// runs over rows: a lane takes 16 bytes of the same columns of eight rows, and
+// each column of them is an operand of a product of its own, so nothing is
+// transposed in memory or in LDS.
+#include <algorithm>
+#include <type_traits>
+
+#include "tc_lane.h"
+
+namespace tc {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kWorkers = 16;  // of one launch
+constexpr int kShort = 64;    // rows of the short side
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+// --------------------------------------------------------------------- operands
+
+// Eight elements as bfloat16 pieces, the largest first.
+template <int P>
+struct Pieces {
+    u32x4 p[P];
+};
+
+__device__ __forceinline__ uint32_t high_halves(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }
+
+// P pieces of eight binary32 values, cut off.
+template <int P>
+__device__ __forceinline__ Pieces<P> cut(const float* f) {
+    Pieces<P> r;
+    float rest[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) rest[e] = f[e];
+#pragma unroll
+    for (int n = 0; n < P; ++n) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.p[n][i] = high_halves(__float_as_uint(rest[2 * i]), __float_as_uint(rest[2 * i + 1]));
+        if (n + 1 < P)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) rest[e] -= __uint_as_float(__float_as_uint(rest[e]) & 0xffff0000u);
+    }
+    return r;
+}
+
+template <int PA, int PB>
+__device__ __forceinline__ f32x4 multiply(const Pieces<PA>& a, const Pieces<PB>& b, f32x4 c) {
+    constexpr int kMost = (PA > PB ? PA : PB) - 1;  // products of pieces i and j, i + j <= kMost, small ones first
+#pragma unroll
+    for (int s = kMost; s >= 0; --s)
+#pragma unroll
+        for (int i = 0; i < PA; ++i) {
+            const int j = s - i;
+            if (j < 0 || j >= PB) continue;
+            c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a.p[i]), __builtin_bit_cast(bf16x8, b.p[j]), c, 0, 0, 0);
+        }
+    return c;
+}
+
+// Eight neighbouring elements of a row as they lie, and as pieces.
+template <bool BF>
+struct Eight {
+    u32x4 v[BF ? 1 : 2];
+};
+// WHOLE: they are in the row; otherwise zeros past its end.
+template <bool BF, bool WHOLE>
+__device__ __forceinline__ Eight<BF> load_eight(uintptr_t row, int c, int cols) {
+    Eight<BF> r;
+    constexpr int V = BF ? 8 : 4;
+    using T = std::conditional_t<BF, __bf16, float>;
+#pragma unroll
+    for (int h = 0; h < (BF ? 1 : 2); ++h)
+        r.v[h] = WHOLE ? gld_u<u32x4>(row + (c / V + h) * 16) : load_vec<T, true>(row, c / V + h, cols);
+    return r;
+}
+template <bool BF>
+__device__ __forceinline__ Pieces<BF ? 1 : 3> pieces(const Eight<BF>& e) {
+    if constexpr (BF) {
+        return {{e.v[0]}};
+    } else {
+        float f[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(e.v[i / 4][i % 4]);
+        return cut<3>(f);
+    }
+}
+
+// Lane l's 16 bytes of a block of columns: the products' results then lie so
+// that neighbouring groups of 16 lanes store neighbouring columns.
+__device__ __forceinline__ int chunk_of(int lane) { return (lane % 4) * 4 + lane % 16 / 4; }
+
+// The operands of one block of columns from eight rows: kTiles of them (4 of
+// binary32, 8 of bfloat16), one for each column of a lane's 16 bytes.
+template <bool BF>
+struct Columns {
+    static constexpr int kTiles = BF ? 8 : 4, kBlock = 16 * kTiles;  // columns of a block
+    u32x4 v[8];                                                      // one row each
+    // only rows whose bit is set: the others count as zeros, whatever they hold
+    __device__ __forceinline__ void keep(uint32_t rows) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[j][i] = rows >> j & 1 ? v[j][i] : 0u;
+    }
+    // column t of the lane's, over the eight rows
+    template <int P>
+    __device__ __forceinline__ Pieces<P> get(int t) const {
+        if constexpr (BF) {
+            Pieces<P> r;
+            const uint32_t select = t % 2 ? 0x07060302u : 0x05040100u;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r.p[0][i] = __builtin_amdgcn_perm(v[2 * i + 1][t / 2], v[2 * i][t / 2], select);
+            return r;
+        } else {
+            float f[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(v[j][t]);
+            return cut<P>(f);
+        }
+    }
+};
+
+// 16 bytes of a row at column c; zeros past its end.
+template <bool BF, bool WHOLE>
+__device__ __forceinline__ u32x4 load_sixteen(uintptr_t row, int c, int cols) {
+    using T = std::conditional_t<BF, __bf16, float>;
+    return WHOLE ? gld_u<u32x4>(row + c / (BF ? 8 : 4) * 16) : load_vec<T, true>(row, c / (BF ? 8 : 4), cols);
+}
+
+// ----------------------------------------------------------------------- logits
+
+struct FewArgs {
+    const void* x[kWorkers];
+    const void* w[kWorkers];
+    const void* bias[kWorkers];
+    const int64_t* label[kWorkers];
+    float* lse[kWorkers];   // written forward, read backward
+    float* loss[kWorkers];  // forward
+    const float* dloss[kWorkers];
+    void* out[kWorkers];  // the stream's gradient
+    void* db[kWorkers];   // dbias
+    int64_t rows[kWorkers];
+    char* work;
+    int64_t stride;            // of the workspace, from worker to worker
+    int64_t at_pairs, at_own;  // forward, stream of classes: (largest, sum) [row][workgroup]; the label's logit
+    int64_t at_g, plane_g;     // backward: g [piece][row of the side][row of the stream], bfloat16
+    int64_t padded;            // rows of the stream in g
+    int64_t at_f;              // stream of rows: their factors
+    int64_t at_db;             // and partial sums of dbias [workgroup][class]
+    int64_t x_ld, out_ld;      // elements
+    int64_t classes;
+    int32_t cols, tiles, w_bf, out_bf, db_bf, has_dloss;
+    int32_t pieces_g;  // of g as it is stored
+    int32_t store_g, store_out;
+    float scale;
+};
+
+enum Mode { kForward, kBackward };
+
+__device__ __forceinline__ float load_any(const void* p, int64_t i, int bf) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+    return bf ? Lane<__bf16>::get(a + i * 2) : Lane<float>::get(a + i * 4);
+}
+__device__ __forceinline__ void store_any(void* p, int64_t i, int bf, float v) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+    if (bf)
+        Lane<__bf16>::put(a + i * 2, v);
+    else
+        Lane<float>::put(a + i * 4, v);
+}
+
+// The factor of a row without `scale`: 0 of a row that is left out.
+__device__ __forceinline__ float factor_of(const int64_t* label, const float* dloss, int64_t row, int64_t classes) {
+    const int64_t l = label[row];
+    return l >= 0 && l < classes ? (dloss ? dloss[row] : 1.0f) : 0.0f;
+}
+
+__device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
+    const float top = fmaxf(m, m2);
+    const float a = m == top ? s : s * __builtin_amdgcn_exp2f((m - top) * kLog2e);
+    const float b = m2 == top ? s2 : s2 * __builtin_amdgcn_exp2f((m2 - top) * kLog2e);
+    m = top;
+    s = a + b;
+}
+
+// SB, TB: stream and side are bfloat16.  MT: the side's rows in 16's; CT: the
+// stream's rows of a workgroup in 16's.  ROWS: the stream is the rows, the side
+// the classes.  PG: pieces of g in the stream's gradient.
+template <bool SB, bool TB, int MT, int CT, bool ROWS, Mode MODE, int PG>
+__global__ void __launch_bounds__(256) few_logit_kernel(const FewArgs a) {
+    constexpr int kS = CT * 16, kT = MT * 16;  // rows of the stream and the side
+    constexpr int kPitch = kS + 4;
+    constexpr int kGPitch = kT + 8;  // elements of a row of g's pieces
+    constexpr int kLdsZ = 4 * kT * kPitch * 4, kLdsG = MODE == kBackward ? PG * kS * (MT > 2 ? kT + 8 : 40) * 2 : 0;
+    constexpr int kGP = MT > 2 ? kGPitch : 40;
+    __shared__ __attribute__((aligned(16))) char lds[kLdsZ > kLdsG ? kLdsZ : kLdsG];
+    __shared__ float factors[ROWS ? kS : kT];
+    const int k = blockIdx.y, tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+    const int64_t rows = a.rows[k];
+    const int64_t n_s = ROWS ? rows : a.classes;
+    const int n_t = static_cast<int>(ROWS ? a.classes : rows);
+    const int64_t s0 = static_cast<int64_t>(blockIdx.x) * kS;
+    if (s0 >= n_s) return;
+    const int cols = a.cols;
+    constexpr int se = SB ? 2 : 4, te = TB ? 2 : 4;
+    const uintptr_t stream = reinterpret_cast<uintptr_t>(ROWS ? a.x[k] : a.w[k]);
+    const uintptr_t side = reinterpret_cast<uintptr_t>(ROWS ? a.w[k] : a.x[k]);
+    const int64_t s_ld = (ROWS ? a.x_ld : cols) * se, t_ld = (ROWS ? cols : a.x_ld) * te;
+    // ---- the logits: each wave takes every fourth 32 columns
+    f32x4 acc[CT][MT] = {};
+    {
+        uintptr_t sp[CT], tp[MT];
+#pragma unroll
+        for (int i = 0; i < CT; ++i) sp[i] = stream + std::min<int64_t>(s0 + i * 16 + lane % 16, n_s - 1) * s_ld;
+#pragma unroll
+        for (int j = 0; j < MT; ++j) tp[j] = side + std::min(j * 16 + lane % 16, n_t - 1) * t_ld;
+        Eight<SB> s[2][CT];
+        Eight<TB> t[2][MT];
+        auto fetch = [&](auto whole, int to, int c) {
+#pragma unroll
+            for (int i = 0; i < CT; ++i) s[to][i] = load_eight<SB, decltype(whole)::value>(sp[i], c, cols);
+#pragma unroll
+            for (int j = 0; j < MT; ++j) t[to][j] = load_eight<TB, decltype(whole)::value>(tp[j], c, cols);
+        };
+        auto step = [&](int from) {
+            Pieces<SB ? 1 : 3> ps[CT];
+#pragma unroll
+            for (int i = 0; i < CT; ++i) ps[i] = pieces<SB>(s[from][i]);
+#pragma unroll
+            for (int j = 0; j < MT; ++j) {
+                const Pieces<TB ? 1 : 3> pt = pieces<TB>(t[from][j]);
+#pragma unroll
+                for (int i = 0; i < CT; ++i) acc[i][j] = multiply(ps[i], pt, acc[i][j]);
+            }
+        };
+        const int own = lane / 16 * 8, full = cols / 32 * 32;
+        int c = wave * 32;
+        if (c < full) fetch(std::true_type{}, 0, c + own);
+        while (c < full) {
+            if (c + 128 < full) fetch(std::true_type{}, 1, c + 128 + own);
+            step(0);
+            c += 128;
+            if (c >= full) break;
+            if (c + 128 < full) fetch(std::true_type{}, 0, c + 128 + own);
+            step(1);
+            c += 128;
+        }
+        if (c < cols) {
+            fetch(std::false_type{}, 0, c + own);
+            step(0);
+        }
+    }
+    float* z = reinterpret_cast<float*>(lds);
+    auto at_z = [&](int t, int s) -> float& { return z[t * kPitch + s]; };
+#pragma unroll
+    for (int i = 0; i < CT; ++i)
+#pragma unroll
+        for (int j = 0; j < MT; ++j)
+            *reinterpret_cast<f32x4*>(z + (wave * kT + j * 16 + lane % 16) * kPitch + i * 16 + lane / 16 * 4) = acc[i][j];
+    const float* dloss = a.has_dloss ? a.dloss[k] : nullptr;
+    if (MODE == kBackward && tid < (ROWS ? kS : kT)) {
+        const int64_t row = ROWS ? s0 + tid : tid;
+        factors[tid] = row < rows ? factor_of(a.label[k], dloss, row, a.classes) : 0.0f;
+    }
+    __syncthreads();
+    // the sum of the four waves' parts, with the bias; classes that are none are -infinity
+    for (int n = tid; n < kT * kS; n += 256) {
+        const int t = n / kS, s = n % kS;
+        const int64_t v = ROWS ? t : s0 + s;
+        float b = v < a.classes ? 0.0f : -INFINITY;
+        if (a.bias[k] && v < a.classes) b = load_any(a.bias[k], v, a.w_bf);
+        const float q = (at_z(t, s) + at_z(kT + t, s)) + (at_z(2 * kT + t, s) + at_z(3 * kT + t, s));
+        at_z(t, s) = q + b;
+    }
+    __syncthreads();
+    char* work = a.work + k * a.stride;
+    if constexpr (MODE == kForward) {
+        // the largest and the sum: of a side's row over the workgroup's classes,
+        // or of a stream's row over all of them
+        constexpr int kRows = ROWS ? kS : kT, kOver = ROWS ? kT : kS, kLanes = 256 / kRows;
+        const int r = tid / kLanes, sub = tid % kLanes;
+        auto get = [&](int o) { return ROWS ? at_z(o, r) : at_z(r, o); };
+        float top = -INFINITY, sum = 0.0f;
+        for (int o = sub; o < kOver; o += kLanes) top = fmaxf(top, get(o));
+        const float from = top > -INFINITY ? top : 0.0f;
+        for (int o = sub; o < kOver; o += kLanes) sum += __builtin_amdgcn_exp2f((get(o) - from) * kLog2e);
+#pragma unroll
+        for (int m = kLanes / 2; m > 0; m >>= 1) join(top, sum, __shfl_xor(top, m, 64), __shfl_xor(sum, m, 64));
+        const int64_t row = ROWS ? s0 + r : r;
+        if (sub || row >= rows) return;
+        const int64_t label = a.label[k][row];
+        const bool counts = label >= 0 && label < a.classes;
+        if constexpr (ROWS) {
+            const float lse = top + log2f(sum) * kLn2;
+            a.lse[k][row] = lse;
+            a.loss[k][row] = counts ? lse - get(static_cast<int>(label)) : 0.0f;
+        } else {
+            reinterpret_cast<float2*>(work + a.at_pairs)[row * a.tiles + blockIdx.x] = make_float2(top, sum);
+            if (counts && label >= s0 && label < s0 + kS) reinterpret_cast<float*>(work + a.at_own)[row] = get(static_cast<int>(label - s0));
+        }
+    } else {
+        // g in the place of the logits, and stored for the side's gradient
+        // (there with the factor if the sum runs over the rows)
+        constexpr int kLanes = 256 / kT, kEach = kS / kLanes;  // lanes of a side's row, and their elements
+        const int t = tid / kLanes, first = tid % kLanes * kEach;
+        float g[kEach];
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+            const int s = first + e;
+            const int64_t row = ROWS ? s0 + s : t, v = ROWS ? t : s0 + s;
+            const float f = factors[ROWS ? s : t];
+            g[e] = 0.0f;
+            if (f != 0.0f && v < a.classes) {
+                const float p = __builtin_amdgcn_exp2f((at_z(t, s) - a.lse[k][row]) * kLog2e);
+                g[e] = a.label[k][row] == v ? p - 1.0f : p;
+            }
+            at_z(t, s) = g[e] * f;
+            if (ROWS) g[e] *= f;
+        }
+        for (int n = 0; n < (a.store_g ? a.pieces_g : 0); ++n) {
+            char* to = work + a.at_g + n * a.plane_g + (t * a.padded + s0 + first) * 2;
+#pragma unroll
+            for (int e = 0; e < kEach; e += 2) {
+                *reinterpret_cast<uint32_t*>(to + e * 2) = high_halves(__float_as_uint(g[e]), __float_as_uint(g[e + 1]));
+                g[e] -= __uint_as_float(__float_as_uint(g[e]) & 0xffff0000u);
+                g[e + 1] -= __uint_as_float(__float_as_uint(g[e + 1]) & 0xffff0000u);
+            }
+        }
+        if (ROWS && a.store_g && tid < kS && s0 + tid < rows) reinterpret_cast<float*>(work + a.at_f)[s0 + tid] = factors[tid];
+        __syncthreads();
+        // dbias: sums over the rows
+        if (a.db[k] && a.store_g) {
+            if constexpr (ROWS) {
+                if (tid < kT) {
+                    float sum = 0.0f;
+                    for (int s = 0; s < kS; ++s) sum += at_z(tid, s);
+                    reinterpret_cast<float*>(work + a.at_db)[blockIdx.x * kShort + tid] = sum;
+                }
+            } else if (tid < kS && s0 + tid < a.classes) {
+                float sum = 0.0f;
+                for (int r = 0; r < kT; ++r) sum += at_z(r, tid);
+                store_any(a.db[k], s0 + tid, a.db_bf, sum * a.scale);
+            }
+        }
+        if (!a.store_out) return;
+        // f g as pieces [row of the stream][row of the side], in the place of the logits
+        constexpr int kKs = MT > 2 ? 2 : 1;  // sums of 32
+        constexpr int kEntries = kS * kKs * 32;
+        float fg[kEntries / 256];
+#pragma unroll
+        for (int i = 0; i < kEntries / 256; ++i) {
+            const int n = i * 256 + tid, q = n % (kKs * 32);
+            fg[i] = q < kT ? at_z(q, n / (kKs * 32)) : 0.0f;
+        }
+        __syncthreads();
+        uint16_t* pg = reinterpret_cast<uint16_t*>(lds);
+#pragma unroll
+        for (int i = 0; i < kEntries / 256; ++i) {
+            const int n = i * 256 + tid, s = n / (kKs * 32), q = n % (kKs * 32);
+#pragma unroll
+            for (int p = 0; p < PG; ++p) {
+                const uint32_t h = __float_as_uint(fg[i]);
+                pg[(p * kS + s) * kGP + q] = static_cast<uint16_t>(h >> 16);
+                fg[i] -= __uint_as_float(h & 0xffff0000u);
+            }
+        }
+        __syncthreads();
+        // ---- the stream's gradient: its rows' f g times the side, a block of columns a wave
+        Pieces<PG> b[CT][kKs];
+#pragma unroll
+        for (int i = 0; i < CT; ++i)
+#pragma unroll
+            for (int h = 0; h < kKs; ++h)
+#pragma unroll
+                for (int p = 0; p < PG; ++p)
+                    b[i][h].p[p] = *reinterpret_cast<const u32x4*>(pg + (p * kS + i * 16 + lane % 16) * kGP + h * 32 + lane / 16 * 8);
+        constexpr int kPT = TB ? 1 : PG;
+        using Col = Columns<TB>;
+        uint32_t there[kKs];  // the rows that are not left out
+#pragma unroll
+        for (int h = 0; h < kKs; ++h) {
+            there[h] = 0;
+            if constexpr (!ROWS)
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int r = h * 32 + lane / 16 * 8 + j;
+                    if (r < kT && factors[r < kT ? r : 0] != 0.0f) there[h] |= 1u << j;
+                }
+        }
+        for (int c0 = wave * Col::kBlock; c0 < cols; c0 += 4 * Col::kBlock) {
+            const int c = c0 + chunk_of(lane) * Col::kTiles;
+            Col x[kKs];
+            auto fetch = [&](auto whole) {
+#pragma unroll
+                for (int h = 0; h < kKs; ++h)
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        x[h].v[j] = load_sixteen<TB, decltype(whole)::value>(
+                            side + std::min(h * 32 + lane / 16 * 8 + j, n_t - 1) * t_ld, c, cols);
+            };
+            if (c0 + Col::kBlock <= cols)
+                fetch(std::true_type{});
+            else
+                fetch(std::false_type{});
+            if (!ROWS)
+#pragma unroll
+                for (int h = 0; h < kKs; ++h) x[h].keep(there[h]);
+            f32x4 d[CT][Col::kTiles] = {};
+#pragma unroll
+            for (int q = 0; q < Col::kTiles; ++q)
+#pragma unroll
+                for (int h = 0; h < kKs; ++h) {
+                    const Pieces<kPT> px = x[h].template get<kPT>(q);
+#pragma unroll
+                    for (int i = 0; i < CT; ++i) d[i][q] = multiply(px, b[i][h], d[i][q]);
+                }
+            // lane: row lane % 16 of the stream, columns e * 4 + lane / 16 of 16 bytes of the side
+#pragma unroll
+            for (int i = 0; i < CT; ++i) {
+                const int64_t s = s0 + i * 16 + lane % 16;
+                if (s >= n_s) continue;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const int at = c0 + (e * 4 + lane / 16) * Col::kTiles;
+                    float v[8];
+#pragma unroll
+                    for (int q = 0; q < Col::kTiles; ++q) v[q] = d[i][q][e] * a.scale;
+                    const uintptr_t out = reinterpret_cast<uintptr_t>(a.out[k]) + s * a.out_ld * (a.out_bf ? 2 : 4);
+                    if (a.out_bf) {
+                        if constexpr (TB) {
+                            store_vec<__bf16, true>(out, at / 8, cols, v);
+                        } else {
+                            if (at + 4 <= cols) {
+                                v[4] = v[5] = v[6] = v[7] = 0.0f;
+                                const u32x4 h = Lane<__bf16>::narrow(v);
+                                gst_u<u32x2>(out + at * 2, u32x2{h[0], h[1]});
+                            } else {
+#pragma unroll
+                                for (int q = 0; q < 4; ++q)
+                                    if (at + q < cols) Lane<__bf16>::put(out + (at + q) * 2, v[q]);
+                            }
+                        }
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < Col::kTiles / 4; ++h) store_vec<float, true>(out, at / 4 + h, cols, v + 4 * h);
+                    }
+                }
+            }
+        }
+    }
+}
+
+// Joins the workgroups' pairs of a row.
+__global__ void __launch_bounds__(256) few_join_kernel(const FewArgs a) {
+    __shared__ float2 lds[4];
+    const int k = blockIdx.y;
+    const int64_t row = blockIdx.x;
+    if (row >= a.rows[k]) return;
+    const char* work = a.work + k * a.stride;
+    const float2* pairs = reinterpret_cast<const float2*>(work + a.at_pairs) + row * a.tiles;
+    float top = -INFINITY, sum = 0.0f;
+    for (int t = threadIdx.x; t < a.tiles; t += 256) join(top, sum, pairs[t].x, pairs[t].y);
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) join(top, sum, __shfl_xor(top, m, 64), __shfl_xor(sum, m, 64));
+    if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = make_float2(top, sum);
+    __syncthreads();
+    if (threadIdx.x) return;
+    for (int w = 1; w < 4; ++w) join(top, sum, lds[w].x, lds[w].y);
+    const float lse = top + log2f(sum) * kLn2;
+    a.lse[k][row] = lse;
+    const int64_t label = a.label[k][row];
+    a.loss[k][row] = label >= 0 && label < a.classes ? lse - reinterpret_cast<const float*>(work + a.at_own)[row] : 0.0f;
+}
+
+// ------------------------------------------------------- the sum over the stream
+
+struct SumArgs {
+    const void* stream[kWorkers];
+    const int64_t* label[kWorkers];
+    const float* dloss[kWorkers];
+    void* out[kWorkers];  // the side's gradient
+    void* db[kWorkers];
+    int64_t rows[kWorkers];
+    char* work;
+    int64_t stride, at_g, plane_g, padded, at_f, at_sums, sums_stride, at_db;
+    int64_t ld, out_ld;  // elements
+    int64_t classes;
+    int32_t cols, cols_p, splits, out_bf, db_bf, has_dloss, groups, is_rows;
+    float scale;
+};
+
+// A workgroup takes a block of columns and a part of the stream's rows, 32 at a
+// time a wave.
+template <bool SB, int MT, bool ROWS, int PG>
+__global__ void __launch_bounds__(256) few_sum_kernel(const SumArgs a) {
+    using Col = Columns<SB>;
+    constexpr int kT = MT * 16, kB = Col::kBlock, kPS = SB ? 1 : PG;
+    __shared__ __attribute__((aligned(16))) float lds[2][kT][kB + 4];
+    const int k = blockIdx.z, tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+    const int64_t rows = a.rows[k], n_s = ROWS ? rows : a.classes;
+    const int n_t = static_cast<int>(ROWS ? a.classes : rows);
+    const int cols = a.cols, c0 = blockIdx.x * kB, c = c0 + chunk_of(lane) * Col::kTiles;
+    const int64_t steps = (n_s + 31) / 32;  // of which this workgroup has
+    const int64_t from = steps * blockIdx.y / a.splits, to = steps * (blockIdx.y + 1) / a.splits;
+    char* work = a.work + k * a.stride;
+    const uintptr_t stream = reinterpret_cast<uintptr_t>(a.stream[k]);
+    const int64_t ld = a.ld * (SB ? 2 : 4);
+    const char* g0 = work + a.at_g + lane % 16 * a.padded * 2 + lane / 16 * 16;
+    const float* f0 = reinterpret_cast<const float*>(work + a.at_f);
+    struct Step {
+        Col x;
+        Pieces<PG> g[MT];
+        uint32_t there;
+    } st[2];
+    const bool whole = c0 + kB <= cols;
+    auto fetch = [&](Step& q, int64_t step) {
+        const int64_t s = step * 32 + lane / 16 * 8;
+        auto rows_of = [&](auto whole) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                q.x.v[j] = load_sixteen<SB, decltype(whole)::value>(stream + std::min(s + j, n_s - 1) * ld, c, cols);
+        };
+        if (whole)
+            rows_of(std::true_type{});
+        else
+            rows_of(std::false_type{});
+        if (ROWS) {
+            // rows that are left out (g is zero there, and the rows may hold anything)
+            q.there = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) q.there |= f0[std::min(s + j, n_s - 1)] != 0.0f ? 1u << j : 0u;
+        }
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int p = 0; p < PG; ++p)
+                q.g[m].p[p] = *reinterpret_cast<const u32x4*>(g0 + p * a.plane_g + m * 16 * a.padded * 2 + step * 64);
+    };
+    f32x4 acc[Col::kTiles][MT] = {};
+    auto use = [&](Step& q) {
+        if (ROWS) q.x.keep(q.there);
+#pragma unroll
+        for (int t = 0; t < Col::kTiles; ++t) {
+            const Pieces<kPS> x = q.x.template get<kPS>(t);
+#pragma unroll
+            for (int m = 0; m < MT; ++m) acc[t][m] = multiply(x, q.g[m], acc[t][m]);
+        }
+    };
+    int64_t at = from + wave;
+    if (at < to) fetch(st[0], at);
+    while (at < to) {
+        if (at + 4 < to) fetch(st[1], at + 4);
+        use(st[0]);
+        at += 4;
+        if (at >= to) break;
+        if (at + 4 < to) fetch(st[0], at + 4);
+        use(st[1]);
+        at += 4;
+    }
+    // the four waves' sums, two at a time
+    auto place = [&](int half, int m, int e) -> float* { return &lds[half][m * 16 + lane % 16][(e * 4 + lane / 16) * Col::kTiles]; };
+#pragma unroll
+    for (int turn = 0; turn < 2; ++turn) {
+        if (wave / 2 == 1 - turn)
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float* p = place(wave % 2, m, e);
+#pragma unroll
+                    for (int t = 0; t < Col::kTiles; ++t) p[t] = turn ? p[t] + acc[t][m][e] : acc[t][m][e];
+                }
+        __syncthreads();
+    }
+    float* out = reinterpret_cast<float*>(work + a.at_sums + blockIdx.y * a.sums_stride);
+    for (int n = tid; n < kT * kB / 4; n += 256) {
+        const int t = n / (kB / 4), q = n % (kB / 4) * 4;
+        if (t >= n_t) break;
+        const f32x4 v = *reinterpret_cast<const f32x4*>(&lds[0][t][q]) + *reinterpret_cast<const f32x4*>(&lds[1][t][q]);
+        *reinterpret_cast<f32x4*>(out + static_cast<int64_t>(t) * a.cols_p + c0 + q) = v;
+    }
+}
+
+// The side's gradient from the workgroups' sums; dbias where the side is the
+// classes.
+__global__ void __launch_bounds__(256) few_finish_kernel(const SumArgs a) {
+    const int k = blockIdx.z, t = blockIdx.y;
+    const int64_t rows = a.rows[k];
+    const int n_t = static_cast<int>(a.is_rows ? a.classes : rows);
+    if (t >= n_t) return;
+    const char* work = a.work + k * a.stride;
+    if (blockIdx.x == gridDim.x - 1) {  // the last one has no columns
+        if (!a.is_rows || !a.db[k]) return;
+        __shared__ float lds[256];
+        float s = 0.0f;
+        const int64_t groups = (rows + a.groups - 1) / a.groups;
+        for (int64_t g = threadIdx.x; g < groups; g += 256) s += reinterpret_cast<const float*>(work + a.at_db)[g * kShort + t];
+        lds[threadIdx.x] = s;
+        __syncthreads();
+        for (int m = 128; m > 0; m >>= 1) {
+            if (threadIdx.x < m) lds[threadIdx.x] += lds[threadIdx.x + m];
+            __syncthreads();
+        }
+        if (threadIdx.x == 0) store_any(a.db[k], t, a.db_bf, lds[0] * a.scale);
+        return;
+    }
+    const int c = (blockIdx.x * 256 + threadIdx.x) * 4;
+    if (c >= a.cols) return;
+    const char* from = work + a.at_sums + (static_cast<int64_t>(t) * a.cols_p + c) * 4;
+    f32x4 v = *reinterpret_cast<const f32x4*>(from);
+    for (int s = 1; s < a.splits; ++s) v += *reinterpret_cast<const f32x4*>(from + s * a.sums_stride);
+    const float f = a.is_rows ? 1.0f : factor_of(a.label[k], a.has_dloss ? a.dloss[k] : nullptr, t, a.classes);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (c + e < a.cols) store_any(a.out[k], t * a.out_ld + c + e, a.out_bf, f == 0.0f ? 0.0f : v[e] * (f * a.scale));
+}
+
+// --------------------------------------------------------------------- dispatch
+
+// What a call takes, from its sizes and types alone.
+struct FewPlan {
+    bool rows_stream;  // the stream is the rows
+    int mt, batch, tiles, groups, splits, cols_p, blocks, pieces;
+    int64_t n_s, padded, stride, at_pairs, at_own, at_g, plane_g, at_f, at_db, at_sums, sums_stride;
+};
+
+constexpr int kCt = 2;  // rows of the stream of a workgroup, in 16's
+
+FewPlan few_plan(int K, const int64_t* rows, int64_t cols, int64_t classes, int dtype, int w_dtype, bool backward, int dw_dtype) {
+    FewPlan p{};
+    int64_t most = 0;
+    int with = 0;
+    for (int k = 0; k < K; ++k) {
+        most = std::max(most, rows[k]);
+        with += rows[k] > 0;
+    }
+    p.rows_stream = classes < most;
+    const int64_t n_t = p.rows_stream ? classes : most;
+    p.n_s = p.rows_stream ? most : classes;
+    p.mt = n_t <= 16 ? 1 : n_t <= 32 ? 2 : 4;
+    p.groups = kCt * 16;
+    p.tiles = static_cast<int>((p.n_s + p.groups - 1) / p.groups);
+    p.batch = std::max(1, std::min(with, kWorkers));
+    int64_t at = 0;
+    auto take = [&](int64_t bytes) {
+        const int64_t here = at;
+        at += (bytes + 255) / 256 * 256;
+        return here;
+    };
+    if (!backward) {
+        if (!p.rows_stream) {
+            p.at_pairs = take(n_t * p.tiles * 8);
+            p.at_own = take(n_t * 4);
+        }
+    } else {
+        const bool side_bf = (p.rows_stream ? dw_dtype : dtype) == TC_BF16;
+        const bool stream_bf = (p.rows_stream ? dtype : w_dtype) == TC_BF16;
+        p.pieces = side_bf ? 2 : 3;
+        p.padded = (static_cast<int64_t>(p.tiles) * p.groups + 31) / 32 * 32;
+        p.plane_g = p.mt * 16 * p.padded * 2;
+        p.at_g = take(p.pieces * p.plane_g);
+        const int block = stream_bf ? 128 : 64;
+        p.blocks = static_cast<int>((cols + block - 1) / block);
+        p.cols_p = p.blocks * block;
+        // workgroups enough to fill the chip four times, of at least 128 rows of
+        // the stream
+        p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(1024 / (p.blocks * p.batch), (p.n_s + 127) / 128)));
+        p.sums_stride = n_t * p.cols_p * 4;
+        p.at_sums = take(p.splits * p.sums_stride);
+        if (p.rows_stream) {
+            p.at_f = take(p.padded * 4);
+            p.at_db = take(static_cast<int64_t>(p.tiles) * kShort * 4);
+        }
+    }
+    p.stride = std::max<int64_t>(at, 256);
+    return p;
+}
+
+template <bool SB, bool TB, int MT, bool ROWS>
+void run_logit(const FewArgs& a, bool backward, bool fine, dim3 grid, hipStream_t s) {
+    if (!backward)
+        few_logit_kernel<SB, TB, MT, kCt, ROWS, kForward, 1><<<grid, 256, 0, s>>>(a);
+    else if (fine)
+        few_logit_kernel<SB, TB, MT, kCt, ROWS, kBackward, 3><<<grid, 256, 0, s>>>(a);
+    else
+        few_logit_kernel<SB, TB, MT, kCt, ROWS, kBackward, 2><<<grid, 256, 0, s>>>(a);
+}
+template <bool SB, bool TB, bool ROWS>
+void run_logit(const FewArgs& a, int mt, bool backward, bool fine, dim3 grid, hipStream_t s) {
+    if (mt == 1)
+        run_logit<SB, TB, 1, ROWS>(a, backward, fine, grid, s);
+    else if (mt == 2)
+        run_logit<SB, TB, 2, ROWS>(a, backward, fine, grid, s);
+    else
+        run_logit<SB, TB, 4, ROWS>(a, backward, fine, grid, s);
+}
+template <bool SB, bool ROWS, int PG>
+void run_sum(const SumArgs& a, int mt, dim3 grid, hipStream_t s) {
+    if (mt == 1)
+        few_sum_kernel<SB, 1, ROWS, PG><<<grid, 256, 0, s>>>(a);
+    else if (mt == 2)
+        few_sum_kernel<SB, 2, ROWS, PG><<<grid, 256, 0, s>>>(a);
+    else
+        few_sum_kernel<SB, 4, ROWS, PG><<<grid, 256, 0, s>>>(a);
+}
+
+}  // namespace
+
+bool few_fits(int K, const int64_t* rows, int64_t classes) {
+    int64_t most = 0;
+    for (int k = 0; k < K; ++k) most = std::max(most, rows[k]);
+    return most <= kShort || classes <= kShort;
+}
+
+int64_t few_workspace(int K, const int64_t* rows, int64_t cols, int64_t classes, int dtype, int w_dtype, bool backward, int dw_dtype) {
+    const FewPlan p = few_plan(K, rows, cols, classes, dtype, w_dtype, backward, dw_dtype);
+    return p.batch * p.stride;
+}
+
+hipError_t launch_few(const LossCall& c, const int* list, int count, hipStream_t s) {
+    const FewPlan p = few_plan(c.K, c.rows, c.cols, c.classes, c.dtype, c.w_dtype, c.backward, c.dw_dtype);
+    const bool x_bf = c.dtype == TC_BF16, w_bf = c.w_dtype == TC_BF16, dw_bf = c.dw_dtype == TC_BF16;
+    for (int k0 = 0; k0 < count; k0 += p.batch) {
+        const int n = std::min(p.batch, count - k0);
+        FewArgs a{};
+        SumArgs m{};
+        for (int i = 0; i < n; ++i) {
+            const int k = list[k0 + i];
+            a.x[i] = c.x[k];
+            a.w[i] = c.weight[k];
+            a.bias[i] = c.bias ? c.bias[k] : nullptr;
+            a.label[i] = m.label[i] = c.label[k];
+            a.rows[i] = m.rows[i] = c.rows[k];
+            if (c.backward) {
+                a.lse[i] = const_cast<float*>(c.lse_in[k]);
+                a.dloss[i] = m.dloss[i] = c.dloss ? c.dloss[k] : nullptr;
+                a.db[i] = m.db[i] = c.dbias ? c.dbias[k] : nullptr;
+                a.out[i] = p.rows_stream ? c.dx[k] : c.dweight[k];
+                m.out[i] = p.rows_stream ? c.dweight[k] : c.dx[k];
+                m.stream[i] = p.rows_stream ? c.x[k] : c.weight[k];
+            } else {
+                a.lse[i] = c.lse[k];
+                a.loss[i] = c.loss[k];
+            }
+        }
+        a.work = m.work = static_cast<char*>(c.workspace);
+        a.stride = m.stride = p.stride;
+        a.at_pairs = p.at_pairs;
+        a.at_own = p.at_own;
+        a.at_g = m.at_g = p.at_g;
+        a.plane_g = m.plane_g = p.plane_g;
+        a.padded = m.padded = p.padded;
+        a.at_f = m.at_f = p.at_f;
+        a.at_db = m.at_db = p.at_db;
+        a.x_ld = c.x_ld;
+        a.out_ld = p.rows_stream ? c.dx_ld : c.cols;
+        a.classes = m.classes = c.classes;
+        a.cols = m.cols = static_cast<int32_t>(c.cols);
+        a.tiles = p.tiles;
+        a.w_bf = w_bf;
+        a.out_bf = p.rows_stream ? x_bf : dw_bf;
+        a.db_bf = m.db_bf = dw_bf;
+        a.has_dloss = m.has_dloss = c.dloss != nullptr;
+        a.pieces_g = p.pieces;
+        a.scale = m.scale = c.scale;
+        const dim3 grid(p.tiles, n);
+        const bool fine = !a.out_bf;
+        // a stream of rows whose gradient takes its place: that is written last,
+        // with the logits made once more
+        bool in_place = false;
+        if (c.backward && p.rows_stream)
+            for (int i = 0; i < n; ++i) in_place = in_place || a.x[i] == a.out[i];
+        a.store_g = 1;
+        a.store_out = !in_place;
+        auto logits = [&] {
+            if (p.rows_stream)
+                x_bf ? (w_bf ? run_logit<true, true, true>(a, p.mt, c.backward, fine, grid, s) : run_logit<true, false, true>(a, p.mt, c.backward, fine, grid, s))
+                     : (w_bf ? run_logit<false, true, true>(a, p.mt, c.backward, fine, grid, s) : run_logit<false, false, true>(a, p.mt, c.backward, fine, grid, s));
+            else
+                w_bf ? (x_bf ? run_logit<true, true, false>(a, p.mt, c.backward, fine, grid, s) : run_logit<true, false, false>(a, p.mt, c.backward, fine, grid, s))
+                     : (x_bf ? run_logit<false, true, false>(a, p.mt, c.backward, fine, grid, s) : run_logit<false, false, false>(a, p.mt, c.backward, fine, grid, s));
+            return hipGetLastError();
+        };
+        if (hipError_t e = logits()) return e;
+        if (!c.backward) {
+            if (!p.rows_stream) few_join_kernel<<<dim3(static_cast<uint32_t>(p.mt * 16), n), 256, 0, s>>>(a);
+            if (hipError_t e = hipGetLastError()) return e;
+            continue;
+        }
+        m.at_sums = p.at_sums;
+        m.sums_stride = p.sums_stride;
+        m.ld = p.rows_stream ? c.x_ld : c.cols;
+        m.out_ld = p.rows_stream ? c.cols : c.dx_ld;
+        m.cols_p = p.cols_p;
+        m.splits = p.splits;
+        m.out_bf = p.rows_stream ? dw_bf : x_bf;
+        m.groups = p.groups;
+        m.is_rows = p.rows_stream;
+        const dim3 grid2(p.blocks, p.splits, n);
+        const bool sb = p.rows_stream ? x_bf : w_bf, three = p.pieces == 3;
+        if (p.rows_stream)
+            sb ? (three ? run_sum<true, true, 3>(m, p.mt, grid2, s) : run_sum<true, true, 2>(m, p.mt, grid2, s))
+               : (three ? run_sum<false, true, 3>(m, p.mt, grid2, s) : run_sum<false, true, 2>(m, p.mt, grid2, s));
+        else
+            sb ? (three ? run_sum<true, false, 3>(m, p.mt, grid2, s) : run_sum<true, false, 2>(m, p.mt, grid2, s))
+               : (three ? run_sum<false, false, 3>(m, p.mt, grid2, s) : run_sum<false, false, 2>(m, p.mt, grid2, s));
+        if (hipError_t e = hipGetLastError()) return e;
+        const int64_t n_t = p.rows_stream ? c.classes : p.mt * 16;
+        few_finish_kernel<<<dim3(static_cast<uint32_t>((c.cols + 1023) / 1024 + 1), static_cast<uint32_t>(n_t), n), 256, 0, s>>>(m);
+        if (hipError_t e = hipGetLastError()) return e;
+        if (in_place) {
+            a.store_g = 0;
+            a.store_out = 1;
+            if (hipError_t e = logits()) return e;
+        }
+    }
+    return hipSuccess;
+}
+
+}  // namespace tc

@@ -153,7 +153,8 @@ def check(c):
 
 
 SIZES = [([1], 1, 1), ([1], 64, 2), ([3, 0, 5], 7, 127), ([1, 1], 512, 1000), ([32] * 3, 200, 1000), ([64, 65], 65, 129), ([17], 128, 4099),
-         ([129, 1], 96, 257), ([300, 257, 2], 320, 515), ([513], 1003, 1031), ([16], 2048, 1000)]
+         ([129, 1], 96, 257), ([300, 257, 2], 320, 515), ([513], 1003, 1031), ([16], 2048, 1000),
+         ([200, 3], 96, 10), ([1500, 0, 700], 130, 64), ([70], 1003, 49), ([5000], 64, 1), ([66], 40, 33)]
 
 
 @pytest.mark.parametrize("rows,cols,classes", SIZES, ids=str)
@@ -164,25 +165,26 @@ def test_sizes(rows, cols, classes, x, w, dw):
 
 @pytest.mark.parametrize("x,w,dw", list(itertools.product((F32, BF16), repeat=3)), ids=str)
 @pytest.mark.parametrize("bias,weighted", [(False, True), (True, False)])
-def test_types(x, w, dw, bias, weighted):
-    check(Case([40, 70], 96, 300, x, w, dw, bias=bias, weighted=weighted, pad=3, out=0.2, seed=1))
+@pytest.mark.parametrize("rows,classes", [([40, 70], 300), ([40, 64], 300), ([12, 3], 300), ([25], 100), ([400, 90], 40)], ids=str)
+def test_types(rows, classes, x, w, dw, bias, weighted):
+    check(Case(rows, 96, classes, x, w, dw, bias=bias, weighted=weighted, pad=3, out=0.2, seed=1))
 
 
 @pytest.mark.parametrize("x,w", [(F32, F32), (BF16, BF16)], ids=["f32", "bf16"])
 @pytest.mark.parametrize("pad,offset", [(8, 8), (1, 1), (0, 3)])
-@pytest.mark.parametrize("rows", [[5, 9], [130, 90]], ids=str)
-def test_strides_and_alignment(rows, x, w, pad, offset):
-    check(Case(rows, 128, 333, x, w, w, bias=True, pad=pad, offset=offset, seed=2))
+@pytest.mark.parametrize("rows,classes", [([5, 9], 333), ([130, 90], 333), ([130, 90], 33)], ids=str)
+def test_strides_and_alignment(rows, classes, x, w, pad, offset):
+    check(Case(rows, 128, classes, x, w, w, bias=True, pad=pad, offset=offset, seed=2))
 
 
 @pytest.mark.parametrize("x,w,dw", [(F32, F32, F32), (BF16, BF16, BF16)], ids=["f32", "bf16"])
-@pytest.mark.parametrize("rows", [[6, 4], [140, 70]], ids=str)
-def test_what_is_left_out_may_hold_anything(rows, x, w, dw):
+@pytest.mark.parametrize("rows,classes", [([6, 4], 300), ([60, 50], 300), ([140, 70], 300), ([140, 70], 30)], ids=str)
+def test_what_is_left_out_may_hold_anything(rows, classes, x, w, dw):
     """Rows without a label, or with a factor of zero, that hold infinities, NaN and the largest values: the
     others' results are as if they held zeros, and theirs are zero."""
     results = []
     for bad in (0.0, float("nan"), float("inf"), 3e38):
-        c = Case(rows, 96, 300, x, w, dw, bias=True, weighted=True, seed=3)
+        c = Case(rows, 96, classes, x, w, dw, bias=True, weighted=True, seed=3)
         for t, label, dloss in zip(c.x, c.label, c.dloss):
             label[1] = LEFT_OUT
             label[2] = c.classes
@@ -201,15 +203,17 @@ def test_what_is_left_out_may_hold_anything(rows, x, w, dw):
             assert torch.equal(a, b)
 
 
-def test_a_row_that_is_not_finite_reaches_its_own_results_alone():
+@pytest.mark.parametrize("classes", [300, 30])
+@pytest.mark.parametrize("rows", [30, 140])
+def test_a_row_that_is_not_finite_reaches_its_own_results_alone(rows, classes):
     for x in (F32, BF16):
-        good, c = [Case([140], 96, 300, x, x, x, seed=4) for _ in range(2)]
+        good, c = [Case([rows], 96, classes, x, x, x, seed=4) for _ in range(2)]
         c.x[0][7, 5] = float("inf")
         c.x[0][9] = float("nan")
         for q in (good, c):
             q.forward()
             q.backward()
-        rest = [r for r in range(140) if r not in (7, 9)]
+        rest = [r for r in range(rows) if r not in (7, 9)]
         assert c.loss[0][[7, 9]].isnan().all() and c.dx[0][[7, 9]].isnan().all()
         assert torch.equal(good.loss[0][rest], c.loss[0][rest]) and torch.equal(good.dx[0][rest], c.dx[0][rest])
         assert c.dw[0].isnan().any()
@@ -278,7 +282,11 @@ def test_few_rows_and_many_classes():
 
 
 def test_the_same_bits_and_any_stream():
-    c = Case([40, 200], 136, 1001, BF16, F32, F32, bias=True, weighted=True, seed=11)
+    for rows, classes in (([40, 200], 1001), ([40, 20], 1001), ([400, 200], 50)):
+        same_bits(Case(rows, 136, classes, BF16, F32, F32, bias=True, weighted=True, seed=11))
+
+
+def same_bits(c):
     c.forward()
     c.backward()
     torch.cuda.synchronize()
@@ -295,7 +303,7 @@ def test_the_same_bits_and_any_stream():
 
 
 def test_two_captured_graphs_and_one_workspace():
-    cases = [Case([33, 150], 128, 700, x, w, F32, bias=True, seed=12) for x, w in ((F32, F32), (BF16, BF16))]
+    cases = [Case(rows, 128, 700, x, w, F32, bias=True, seed=12) for rows, x, w in (([33, 150], F32, F32), ([33, 15], F32, F32), ([33, 150], BF16, BF16))]
     need = 0
     for c in cases:
         x, w = c.x[0].dtype, c.w[0].dtype
@@ -330,7 +338,11 @@ def test_two_captured_graphs_and_one_workspace():
 
 
 def test_rows_behind_the_views_stay():
-    c = Case([5, 140], 100, 257, pad=5, seed=13)
+    for rows, classes in (([5, 140], 257), ([5, 14], 257), ([5, 140], 25)):
+        rows_behind(Case(rows, 100, classes, pad=5, seed=13))
+
+
+def rows_behind(c):
     wide = [t._base if t._base is not None else t for t in c.dx]
     for t in wide:
         t.fill_(3.0)
@@ -341,17 +353,18 @@ def test_rows_behind_the_views_stay():
         assert bool((t[:, 100:] == 3.0).all())
 
 
-def test_dx_in_the_place_of_x():
-    for x in (F32, BF16):
-        a, b = [Case([9, 140], 128, 300, x, x, x, seed=14) for _ in range(2)]
-        a.forward()
-        b.forward()
-        a.backward()
-        b.dx = b.x
-        b.backward()
-        torch.cuda.synchronize()
-        for p, q in zip(a.dx + a.dw, b.x + b.dw):
-            assert torch.equal(p, q)
+@pytest.mark.parametrize("rows,classes", [([9, 40], 300), ([9, 140], 300), ([300, 140], 30)], ids=str)
+@pytest.mark.parametrize("x", [F32, BF16], ids=["f32", "bf16"])
+def test_dx_in_the_place_of_x(rows, classes, x):
+    a, b = [Case(rows, 128, classes, x, x, x, bias=True, seed=14) for _ in range(2)]
+    a.forward()
+    b.forward()
+    a.backward()
+    b.dx = b.x
+    b.backward()
+    torch.cuda.synchronize()
+    for p, q in zip(a.dx + a.dw + a.db, b.x + b.dw + b.db):
+        assert torch.equal(p, q)
 
 
 def test_gradients_against_differences():
