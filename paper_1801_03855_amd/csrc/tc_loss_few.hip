@@ -5,13 +5,14 @@
 // products with the short side are few.  So nothing is laid out anew.
 //
 // "Stream" is the long side (n x cols), "side" the short one (up to 64 x cols).
-//   few_logit   a workgroup takes 32 or so rows of the stream: the logits, with
-//               the sum over columns cut among its waves and joined in LDS; then
-//               forward what a row needs of them, backward g, and with it at once
-//               the stream's own gradient, g side, a sum over the short side
+//   few_logit   a workgroup takes 32 rows of the stream: the logits, with the sum
+//               over columns cut among its waves and joined in LDS; then forward
+//               what a row needs of them, backward g, stored both ways
 //   few_sum     the side's gradient, g^T stream: a sum over the stream, which is
 //               read again, cut among waves and workgroups
 //   few_finish  adds the workgroups' sums up in a fixed order
+//   few_outer   the stream's gradient, g side: a sum over the short side, bound
+//               by what it writes
 //
 // Operands go from memory to registers and to the matrix cores as bfloat16
 // pieces: a bfloat16 element is one, a binary32 element three that hold its 24
@@ -37,6 +38,8 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kWorkers = 16;  // of one launch
 constexpr int kShort = 64;    // rows of the short side
+constexpr int kTurn = 5;      // steps from one workgroup's beginning to the next one's
+constexpr int kCt = 2;        // rows of the stream of a workgroup of the logits, in 16's
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // --------------------------------------------------------------------- operands
@@ -113,18 +116,36 @@ __device__ __forceinline__ Pieces<BF ? 1 : 3> pieces(const Eight<BF>& e) {
 // that neighbouring groups of 16 lanes store neighbouring columns.
 __device__ __forceinline__ int chunk_of(int lane) { return (lane % 4) * 4 + lane % 16 / 4; }
 
-// The operands of one block of columns from eight rows: kTiles of them (4 of
-// binary32, 8 of bfloat16), one for each column of a lane's 16 bytes.
-template <bool BF>
+// The operands of one block of columns from eight rows: one for each of the
+// TILES columns that a lane has, 16 bytes of a row (8 of bfloat16, 4 of
+// binary32) or 8 (4 of bfloat16).
+template <bool BF, int TILES = BF ? 8 : 4>
 struct Columns {
-    static constexpr int kTiles = BF ? 8 : 4, kBlock = 16 * kTiles;  // columns of a block
-    u32x4 v[8];                                                      // one row each
+    static constexpr int kTiles = TILES, kBlock = 16 * TILES;  // columns of a block
+    static constexpr int kWords = TILES * (BF ? 2 : 4) / 4;
+    typedef uint32_t Row __attribute__((ext_vector_type(kWords)));
+    Row v[8];
+    // of a row, at column c; WHOLE: they are in the row; otherwise zeros past its end
+    template <bool WHOLE>
+    static __device__ __forceinline__ Row load(uintptr_t row, int c, int cols) {
+        if constexpr (WHOLE) {
+            return gld_u<Row>(row + c * (BF ? 2 : 4));
+        } else if constexpr (kWords == 4) {
+            return load_vec<std::conditional_t<BF, __bf16, float>, true>(row, c / TILES, cols);
+        } else {
+            Row r = {};
+#pragma unroll
+            for (int i = 0; i < TILES; ++i)
+                if (c + i < cols) r[i / 2] |= static_cast<uint32_t>(gld<uint16_t>(row + (c + i) * 2)) << i % 2 * 16;
+            return r;
+        }
+    }
     // only rows whose bit is set: the others count as zeros, whatever they hold
     __device__ __forceinline__ void keep(uint32_t rows) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[j][i] = rows >> j & 1 ? v[j][i] : 0u;
+            for (int i = 0; i < kWords; ++i) v[j][i] = rows >> j & 1 ? v[j][i] : 0u;
     }
     // column t of the lane's, over the eight rows
     template <int P>
@@ -144,13 +165,6 @@ struct Columns {
     }
 };
 
-// 16 bytes of a row at column c; zeros past its end.
-template <bool BF, bool WHOLE>
-__device__ __forceinline__ u32x4 load_sixteen(uintptr_t row, int c, int cols) {
-    using T = std::conditional_t<BF, __bf16, float>;
-    return WHOLE ? gld_u<u32x4>(row + c / (BF ? 8 : 4) * 16) : load_vec<T, true>(row, c / (BF ? 8 : 4), cols);
-}
-
 // ----------------------------------------------------------------------- logits
 
 struct FewArgs {
@@ -161,21 +175,20 @@ struct FewArgs {
     float* lse[kWorkers];   // written forward, read backward
     float* loss[kWorkers];  // forward
     const float* dloss[kWorkers];
-    void* out[kWorkers];  // the stream's gradient
-    void* db[kWorkers];   // dbias
+    void* db[kWorkers];  // dbias
     int64_t rows[kWorkers];
     char* work;
     int64_t stride;            // of the workspace, from worker to worker
     int64_t at_pairs, at_own;  // forward, stream of classes: (largest, sum) [row][workgroup]; the label's logit
     int64_t at_g, plane_g;     // backward: g [piece][row of the side][row of the stream], bfloat16
+    int64_t at_fg, plane_fg;   // f g [piece][row of the stream][row of the side]
     int64_t padded;            // rows of the stream in g
     int64_t at_f;              // stream of rows: their factors
     int64_t at_db;             // and partial sums of dbias [workgroup][class]
-    int64_t x_ld, out_ld;      // elements
+    int64_t x_ld;              // elements
     int64_t classes;
-    int32_t cols, tiles, w_bf, out_bf, db_bf, has_dloss;
-    int32_t pieces_g;  // of g as it is stored
-    int32_t store_g, store_out;
+    int32_t cols, tiles, w_bf, db_bf, has_dloss;
+    int32_t pieces_g, pieces_fg;
     float scale;
 };
 
@@ -207,17 +220,14 @@ __device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
     s = a + b;
 }
 
-// SB, TB: stream and side are bfloat16.  MT: the side's rows in 16's; CT: the
-// stream's rows of a workgroup in 16's.  ROWS: the stream is the rows, the side
-// the classes.  PG: pieces of g in the stream's gradient.
-template <bool SB, bool TB, int MT, int CT, bool ROWS, Mode MODE, int PG>
-__global__ void __launch_bounds__(256) few_logit_kernel(const FewArgs a) {
-    constexpr int kS = CT * 16, kT = MT * 16;  // rows of the stream and the side
+// SB, TB: stream and side are bfloat16.  MT: the side's rows in 16's.  ROWS: the
+// stream is the rows, the side the classes.  W: waves, among which the sum is
+// cut, 64 columns at a time.
+template <bool SB, bool TB, int MT, int W, bool ROWS, Mode MODE>
+__global__ void __launch_bounds__(W * 64) few_logit_kernel(const FewArgs a) {
+    constexpr int CT = kCt, kS = CT * 16, kT = MT * 16, kThreads = W * 64;  // rows of the stream and the side
     constexpr int kPitch = kS + 4;
-    constexpr int kGPitch = kT + 8;  // elements of a row of g's pieces
-    constexpr int kLdsZ = 4 * kT * kPitch * 4, kLdsG = MODE == kBackward ? PG * kS * (MT > 2 ? kT + 8 : 40) * 2 : 0;
-    constexpr int kGP = MT > 2 ? kGPitch : 40;
-    __shared__ __attribute__((aligned(16))) char lds[kLdsZ > kLdsG ? kLdsZ : kLdsG];
+    __shared__ __attribute__((aligned(16))) float z[W * kT * kPitch];
     __shared__ float factors[ROWS ? kS : kT];
     const int k = blockIdx.y, tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
     const int64_t rows = a.rows[k];
@@ -230,7 +240,7 @@ __global__ void __launch_bounds__(256) few_logit_kernel(const FewArgs a) {
     const uintptr_t stream = reinterpret_cast<uintptr_t>(ROWS ? a.x[k] : a.w[k]);
     const uintptr_t side = reinterpret_cast<uintptr_t>(ROWS ? a.w[k] : a.x[k]);
     const int64_t s_ld = (ROWS ? a.x_ld : cols) * se, t_ld = (ROWS ? cols : a.x_ld) * te;
-    // ---- the logits: each wave takes every fourth 32 columns
+    // ---- the logits
     f32x4 acc[CT][MT] = {};
     {
         uintptr_t sp[CT], tp[MT];
@@ -238,8 +248,10 @@ __global__ void __launch_bounds__(256) few_logit_kernel(const FewArgs a) {
         for (int i = 0; i < CT; ++i) sp[i] = stream + std::min<int64_t>(s0 + i * 16 + lane % 16, n_s - 1) * s_ld;
 #pragma unroll
         for (int j = 0; j < MT; ++j) tp[j] = side + std::min(j * 16 + lane % 16, n_t - 1) * t_ld;
-        Eight<SB> s[2][CT];
-        Eight<TB> t[2][MT];
+        // steps ahead: what the registers hold
+        constexpr int kAhead = MT == 4 ? 2 : 3;
+        Eight<SB> s[kAhead][CT];
+        Eight<TB> t[kAhead][MT];
         auto fetch = [&](auto whole, int to, int c) {
 #pragma unroll
             for (int i = 0; i < CT; ++i) s[to][i] = load_eight<SB, decltype(whole)::value>(sp[i], c, cols);
@@ -257,24 +269,35 @@ __global__ void __launch_bounds__(256) few_logit_kernel(const FewArgs a) {
                 for (int i = 0; i < CT; ++i) acc[i][j] = multiply(ps[i], pt, acc[i][j]);
             }
         };
+        // The wave's step n: its 64 columns of every 64 W, 32 at a time.  The
+        // workgroups begin at different ones, or the rows' equal distances would
+        // have all of them at the same channels of the memory at a time.
         const int own = lane / 16 * 8, full = cols / 32 * 32;
-        int c = wave * 32;
-        if (c < full) fetch(std::true_type{}, 0, c + own);
-        while (c < full) {
-            if (c + 128 < full) fetch(std::true_type{}, 1, c + 128 + own);
-            step(0);
-            c += 128;
-            if (c >= full) break;
-            if (c + 128 < full) fetch(std::true_type{}, 0, c + 128 + own);
-            step(1);
-            c += 128;
+        auto column = [&](int n) { return n / 2 * (64 * W) + n % 2 * 32 + wave * 64; };
+        const int steps = full / (64 * W) * 2 + std::clamp((full % (64 * W) - wave * 64) / 32, 0, 2);
+        int n = 0, ahead = steps > 0 ? static_cast<int>(blockIdx.x * kTurn % steps) : 0, asked = 0;
+        auto next = [&](int to) {
+            if (asked == steps) return;
+            fetch(std::true_type{}, to, column(ahead) + own);
+            ++asked;
+            if (++ahead == steps) ahead = 0;
+        };
+#pragma unroll
+        for (int q = 0; q < kAhead - 1; ++q) next(q);
+        while (n < steps) {
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q) {
+                if (n == steps) break;
+                next((q + kAhead - 1) % kAhead);
+                step(q);
+                ++n;
+            }
         }
-        if (c < cols) {
-            fetch(std::false_type{}, 0, c + own);
+        if (column(steps) == full && full < cols) {
+            fetch(std::false_type{}, 0, full + own);
             step(0);
         }
     }
-    float* z = reinterpret_cast<float*>(lds);
     auto at_z = [&](int t, int s) -> float& { return z[t * kPitch + s]; };
 #pragma unroll
     for (int i = 0; i < CT; ++i)
@@ -287,13 +310,15 @@ __global__ void __launch_bounds__(256) few_logit_kernel(const FewArgs a) {
         factors[tid] = row < rows ? factor_of(a.label[k], dloss, row, a.classes) : 0.0f;
     }
     __syncthreads();
-    // the sum of the four waves' parts, with the bias; classes that are none are -infinity
-    for (int n = tid; n < kT * kS; n += 256) {
+    // the sum of the waves' parts, with the bias; classes that are none are -infinity
+    for (int n = tid; n < kT * kS; n += kThreads) {
         const int t = n / kS, s = n % kS;
         const int64_t v = ROWS ? t : s0 + s;
         float b = v < a.classes ? 0.0f : -INFINITY;
         if (a.bias[k] && v < a.classes) b = load_any(a.bias[k], v, a.w_bf);
-        const float q = (at_z(t, s) + at_z(kT + t, s)) + (at_z(2 * kT + t, s) + at_z(3 * kT + t, s));
+        float q = 0.0f;
+#pragma unroll
+        for (int w = 0; w < W; w += 2) q += at_z(w * kT + t, s) + at_z(w * kT + kT + t, s);
         at_z(t, s) = q + b;
     }
     __syncthreads();
@@ -301,7 +326,7 @@ __global__ void __launch_bounds__(256) few_logit_kernel(const FewArgs a) {
     if constexpr (MODE == kForward) {
         // the largest and the sum: of a side's row over the workgroup's classes,
         // or of a stream's row over all of them
-        constexpr int kRows = ROWS ? kS : kT, kOver = ROWS ? kT : kS, kLanes = 256 / kRows;
+        constexpr int kRows = ROWS ? kS : kT, kOver = ROWS ? kT : kS, kLanes = kThreads / kRows < 64 ? kThreads / kRows : 64;
         const int r = tid / kLanes, sub = tid % kLanes;
         auto get = [&](int o) { return ROWS ? at_z(o, r) : at_z(r, o); };
         float top = -INFINITY, sum = 0.0f;
@@ -311,7 +336,7 @@ __global__ void __launch_bounds__(256) few_logit_kernel(const FewArgs a) {
 #pragma unroll
         for (int m = kLanes / 2; m > 0; m >>= 1) join(top, sum, __shfl_xor(top, m, 64), __shfl_xor(sum, m, 64));
         const int64_t row = ROWS ? s0 + r : r;
-        if (sub || row >= rows) return;
+        if (sub || r >= kRows || row >= rows) return;
         const int64_t label = a.label[k][row];
         const bool counts = label >= 0 && label < a.classes;
         if constexpr (ROWS) {
@@ -323,153 +348,53 @@ __global__ void __launch_bounds__(256) few_logit_kernel(const FewArgs a) {
             if (counts && label >= s0 && label < s0 + kS) reinterpret_cast<float*>(work + a.at_own)[row] = get(static_cast<int>(label - s0));
         }
     } else {
-        // g in the place of the logits, and stored for the side's gradient
-        // (there with the factor if the sum runs over the rows)
-        constexpr int kLanes = 256 / kT, kEach = kS / kLanes;  // lanes of a side's row, and their elements
-        const int t = tid / kLanes, first = tid % kLanes * kEach;
-        float g[kEach];
-#pragma unroll
-        for (int e = 0; e < kEach; ++e) {
-            const int s = first + e;
-            const int64_t row = ROWS ? s0 + s : t, v = ROWS ? t : s0 + s;
-            const float f = factors[ROWS ? s : t];
-            g[e] = 0.0f;
-            if (f != 0.0f && v < a.classes) {
-                const float p = __builtin_amdgcn_exp2f((at_z(t, s) - a.lse[k][row]) * kLog2e);
-                g[e] = a.label[k][row] == v ? p - 1.0f : p;
+        // g, stored for the side's gradient (with the factor if its sum runs over
+        // the rows), and f g for the stream's: two elements at a time
+        auto store = [&](char* to, int64_t plane, int pieces, float g0, float g1) {
+            for (int n = 0; n < pieces; ++n) {
+                *reinterpret_cast<uint32_t*>(to + n * plane) = high_halves(__float_as_uint(g0), __float_as_uint(g1));
+                g0 -= __uint_as_float(__float_as_uint(g0) & 0xffff0000u);
+                g1 -= __uint_as_float(__float_as_uint(g1) & 0xffff0000u);
             }
-            at_z(t, s) = g[e] * f;
-            if (ROWS) g[e] *= f;
-        }
-        for (int n = 0; n < (a.store_g ? a.pieces_g : 0); ++n) {
-            char* to = work + a.at_g + n * a.plane_g + (t * a.padded + s0 + first) * 2;
+        };
+        for (int n = tid; n < kT * kS / 2; n += kThreads) {
+            const int t = n / (kS / 2), s = n % (kS / 2) * 2;
+            float g[2];
 #pragma unroll
-            for (int e = 0; e < kEach; e += 2) {
-                *reinterpret_cast<uint32_t*>(to + e * 2) = high_halves(__float_as_uint(g[e]), __float_as_uint(g[e + 1]));
-                g[e] -= __uint_as_float(__float_as_uint(g[e]) & 0xffff0000u);
-                g[e + 1] -= __uint_as_float(__float_as_uint(g[e + 1]) & 0xffff0000u);
+            for (int e = 0; e < 2; ++e) {
+                const int64_t row = ROWS ? s0 + s + e : t, v = ROWS ? t : s0 + s + e;
+                const float f = factors[ROWS ? s + e : t];
+                g[e] = 0.0f;
+                if (f != 0.0f && v < a.classes) {
+                    const float p = __builtin_amdgcn_exp2f((at_z(t, s + e) - a.lse[k][row]) * kLog2e);
+                    g[e] = a.label[k][row] == v ? p - 1.0f : p;
+                }
+                at_z(t, s + e) = g[e] * f;
+                if (ROWS) g[e] *= f;
             }
+            store(work + a.at_g + (t * a.padded + s0 + s) * 2, a.plane_g, a.pieces_g, g[0], g[1]);
         }
-        if (ROWS && a.store_g && tid < kS && s0 + tid < rows) reinterpret_cast<float*>(work + a.at_f)[s0 + tid] = factors[tid];
+        if (ROWS && tid < kS && s0 + tid < rows) reinterpret_cast<float*>(work + a.at_f)[s0 + tid] = factors[tid];
         __syncthreads();
+        constexpr int kSide = MT > 2 ? 64 : 32;  // rows of the side in f g, with zeros
+        for (int n = tid; n < kS * kSide / 2; n += kThreads) {
+            const int s = n / (kSide / 2), t = n % (kSide / 2) * 2;
+            const bool in = t < kT;
+            store(work + a.at_fg + ((s0 + s) * kSide + t) * 2, a.plane_fg, a.pieces_fg, in ? at_z(in ? t : 0, s) : 0.0f,
+                  in ? at_z(in ? t + 1 : 0, s) : 0.0f);
+        }
         // dbias: sums over the rows
-        if (a.db[k] && a.store_g) {
-            if constexpr (ROWS) {
-                if (tid < kT) {
-                    float sum = 0.0f;
-                    for (int s = 0; s < kS; ++s) sum += at_z(tid, s);
-                    reinterpret_cast<float*>(work + a.at_db)[blockIdx.x * kShort + tid] = sum;
-                }
-            } else if (tid < kS && s0 + tid < a.classes) {
+        if (!a.db[k]) return;
+        if constexpr (ROWS) {
+            if (tid < kT) {
                 float sum = 0.0f;
-                for (int r = 0; r < kT; ++r) sum += at_z(r, tid);
-                store_any(a.db[k], s0 + tid, a.db_bf, sum * a.scale);
+                for (int s = 0; s < kS; ++s) sum += at_z(tid, s);
+                reinterpret_cast<float*>(work + a.at_db)[static_cast<int64_t>(blockIdx.x) * kShort + tid] = sum;
             }
-        }
-        if (!a.store_out) return;
-        // f g as pieces [row of the stream][row of the side], in the place of the logits
-        constexpr int kKs = MT > 2 ? 2 : 1;  // sums of 32
-        constexpr int kEntries = kS * kKs * 32;
-        float fg[kEntries / 256];
-#pragma unroll
-        for (int i = 0; i < kEntries / 256; ++i) {
-            const int n = i * 256 + tid, q = n % (kKs * 32);
-            fg[i] = q < kT ? at_z(q, n / (kKs * 32)) : 0.0f;
-        }
-        __syncthreads();
-        uint16_t* pg = reinterpret_cast<uint16_t*>(lds);
-#pragma unroll
-        for (int i = 0; i < kEntries / 256; ++i) {
-            const int n = i * 256 + tid, s = n / (kKs * 32), q = n % (kKs * 32);
-#pragma unroll
-            for (int p = 0; p < PG; ++p) {
-                const uint32_t h = __float_as_uint(fg[i]);
-                pg[(p * kS + s) * kGP + q] = static_cast<uint16_t>(h >> 16);
-                fg[i] -= __uint_as_float(h & 0xffff0000u);
-            }
-        }
-        __syncthreads();
-        // ---- the stream's gradient: its rows' f g times the side, a block of columns a wave
-        Pieces<PG> b[CT][kKs];
-#pragma unroll
-        for (int i = 0; i < CT; ++i)
-#pragma unroll
-            for (int h = 0; h < kKs; ++h)
-#pragma unroll
-                for (int p = 0; p < PG; ++p)
-                    b[i][h].p[p] = *reinterpret_cast<const u32x4*>(pg + (p * kS + i * 16 + lane % 16) * kGP + h * 32 + lane / 16 * 8);
-        constexpr int kPT = TB ? 1 : PG;
-        using Col = Columns<TB>;
-        uint32_t there[kKs];  // the rows that are not left out
-#pragma unroll
-        for (int h = 0; h < kKs; ++h) {
-            there[h] = 0;
-            if constexpr (!ROWS)
-#pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int r = h * 32 + lane / 16 * 8 + j;
-                    if (r < kT && factors[r < kT ? r : 0] != 0.0f) there[h] |= 1u << j;
-                }
-        }
-        for (int c0 = wave * Col::kBlock; c0 < cols; c0 += 4 * Col::kBlock) {
-            const int c = c0 + chunk_of(lane) * Col::kTiles;
-            Col x[kKs];
-            auto fetch = [&](auto whole) {
-#pragma unroll
-                for (int h = 0; h < kKs; ++h)
-#pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        x[h].v[j] = load_sixteen<TB, decltype(whole)::value>(
-                            side + std::min(h * 32 + lane / 16 * 8 + j, n_t - 1) * t_ld, c, cols);
-            };
-            if (c0 + Col::kBlock <= cols)
-                fetch(std::true_type{});
-            else
-                fetch(std::false_type{});
-            if (!ROWS)
-#pragma unroll
-                for (int h = 0; h < kKs; ++h) x[h].keep(there[h]);
-            f32x4 d[CT][Col::kTiles] = {};
-#pragma unroll
-            for (int q = 0; q < Col::kTiles; ++q)
-#pragma unroll
-                for (int h = 0; h < kKs; ++h) {
-                    const Pieces<kPT> px = x[h].template get<kPT>(q);
-#pragma unroll
-                    for (int i = 0; i < CT; ++i) d[i][q] = multiply(px, b[i][h], d[i][q]);
-                }
-            // lane: row lane % 16 of the stream, columns e * 4 + lane / 16 of 16 bytes of the side
-#pragma unroll
-            for (int i = 0; i < CT; ++i) {
-                const int64_t s = s0 + i * 16 + lane % 16;
-                if (s >= n_s) continue;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const int at = c0 + (e * 4 + lane / 16) * Col::kTiles;
-                    float v[8];
-#pragma unroll
-                    for (int q = 0; q < Col::kTiles; ++q) v[q] = d[i][q][e] * a.scale;
-                    const uintptr_t out = reinterpret_cast<uintptr_t>(a.out[k]) + s * a.out_ld * (a.out_bf ? 2 : 4);
-                    if (a.out_bf) {
-                        if constexpr (TB) {
-                            store_vec<__bf16, true>(out, at / 8, cols, v);
-                        } else {
-                            if (at + 4 <= cols) {
-                                v[4] = v[5] = v[6] = v[7] = 0.0f;
-                                const u32x4 h = Lane<__bf16>::narrow(v);
-                                gst_u<u32x2>(out + at * 2, u32x2{h[0], h[1]});
-                            } else {
-#pragma unroll
-                                for (int q = 0; q < 4; ++q)
-                                    if (at + q < cols) Lane<__bf16>::put(out + (at + q) * 2, v[q]);
-                            }
-                        }
-                    } else {
-#pragma unroll
-                        for (int h = 0; h < Col::kTiles / 4; ++h) store_vec<float, true>(out, at / 4 + h, cols, v + 4 * h);
-                    }
-                }
-            }
+        } else if (tid < kS && s0 + tid < a.classes) {
+            float sum = 0.0f;
+            for (int r = 0; r < kT; ++r) sum += at_z(r, tid);
+            store_any(a.db[k], s0 + tid, a.db_bf, sum * a.scale);
         }
     }
 }
@@ -517,7 +442,7 @@ struct SumArgs {
 // time a wave.
 template <bool SB, int MT, bool ROWS, int PG>
 __global__ void __launch_bounds__(256) few_sum_kernel(const SumArgs a) {
-    using Col = Columns<SB>;
+    using Col = Columns<SB, SB && MT < 4 ? 8 : 4>;  // (with more the sums would not fit the registers)
     constexpr int kT = MT * 16, kB = Col::kBlock, kPS = SB ? 1 : PG;
     __shared__ __attribute__((aligned(16))) float lds[2][kT][kB + 4];
     const int k = blockIdx.z, tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
@@ -542,7 +467,7 @@ __global__ void __launch_bounds__(256) few_sum_kernel(const SumArgs a) {
         auto rows_of = [&](auto whole) {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-                q.x.v[j] = load_sixteen<SB, decltype(whole)::value>(stream + std::min(s + j, n_s - 1) * ld, c, cols);
+                q.x.v[j] = Col::template load<decltype(whole)::value>(stream + std::min(s + j, n_s - 1) * ld, c, cols);
         };
         if (whole)
             rows_of(std::true_type{});
@@ -639,16 +564,118 @@ __global__ void __launch_bounds__(256) few_finish_kernel(const SumArgs a) {
         if (c + e < a.cols) store_any(a.out[k], t * a.out_ld + c + e, a.out_bf, f == 0.0f ? 0.0f : v[e] * (f * a.scale));
 }
 
+// ----------------------------------------------------------- the stream's gradient
+
+struct OuterArgs {
+    const void* side[kWorkers];
+    const int64_t* label[kWorkers];
+    const float* dloss[kWorkers];
+    void* out[kWorkers];
+    int64_t rows[kWorkers];
+    char* work;
+    int64_t stride, at_fg, plane_fg;
+    int64_t ld, out_ld;  // elements
+    int64_t classes;
+    int32_t cols, out_bf, has_dloss, chunk;  // rows of the stream of a workgroup
+    float scale;
+};
+
+// A wave holds its block of columns of the side as pieces, and takes its rows of
+// the stream 16 at a time.
+template <bool TB, int KS, bool ROWS, int PG>
+__global__ void __launch_bounds__(256) few_outer_kernel(const OuterArgs a) {
+    using Col = Columns<TB>;
+    constexpr int kSide = KS * 32, kPT = TB ? 1 : PG;
+    const int k = blockIdx.z, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int64_t rows = a.rows[k], n_s = ROWS ? rows : a.classes;
+    const int n_t = static_cast<int>(ROWS ? a.classes : rows);
+    const int cols = a.cols, c0 = (blockIdx.x * 4 + wave) * Col::kBlock;
+    if (c0 >= cols) return;
+    const int c = c0 + chunk_of(lane) * Col::kTiles;
+    const uintptr_t side = reinterpret_cast<uintptr_t>(a.side[k]);
+    const int64_t t_ld = a.ld * (TB ? 2 : 4);
+    Pieces<kPT> x[KS][Col::kTiles];
+#pragma unroll
+    for (int h = 0; h < KS; ++h) {
+        Col v;
+        auto fetch = [&](auto whole) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                v.v[j] = Col::template load<decltype(whole)::value>(side + std::min(h * 32 + lane / 16 * 8 + j, n_t - 1) * t_ld, c, cols);
+        };
+        if (c0 + Col::kBlock <= cols)
+            fetch(std::true_type{});
+        else
+            fetch(std::false_type{});
+        if constexpr (!ROWS) {
+            uint32_t there = 0;  // the rows that are not left out
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int r = h * 32 + lane / 16 * 8 + j;
+                if (r < n_t && factor_of(a.label[k], a.has_dloss ? a.dloss[k] : nullptr, r, a.classes) != 0.0f) there |= 1u << j;
+            }
+            v.keep(there);
+        }
+#pragma unroll
+        for (int q = 0; q < Col::kTiles; ++q) x[h][q] = v.template get<kPT>(q);
+    }
+    const char* fg = a.work + k * a.stride + a.at_fg + lane % 16 * (kSide * 2) + lane / 16 * 16;
+    const int64_t first = static_cast<int64_t>(blockIdx.y) * a.chunk, end = std::min<int64_t>(first + a.chunk, n_s);
+    struct Factors {
+        Pieces<PG> b[KS];
+    } now, next;
+    auto fetch = [&](Factors& f, int64_t s) {
+#pragma unroll
+        for (int h = 0; h < KS; ++h)
+#pragma unroll
+            for (int p = 0; p < PG; ++p) f.b[h].p[p] = *reinterpret_cast<const u32x4*>(fg + p * a.plane_fg + s * (kSide * 2) + h * 64);
+    };
+    if (first < end) fetch(now, first);
+    for (int64_t s0 = first; s0 < end; s0 += 16) {
+        if (s0 + 16 < end) fetch(next, s0 + 16);
+        f32x4 d[Col::kTiles] = {};
+#pragma unroll
+        for (int q = 0; q < Col::kTiles; ++q)
+#pragma unroll
+            for (int h = 0; h < KS; ++h) d[q] = multiply(x[h][q], now.b[h], d[q]);
+        now = next;
+        // lane: row lane % 16 of the stream, columns e * 4 + lane / 16 of 16 bytes of the side
+        const int64_t s = s0 + lane % 16;
+        if (s >= n_s) continue;
+        const uintptr_t out = reinterpret_cast<uintptr_t>(a.out[k]) + s * a.out_ld * (a.out_bf ? 2 : 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int at = c0 + (e * 4 + lane / 16) * Col::kTiles;
+            float v[8] = {};
+#pragma unroll
+            for (int q = 0; q < Col::kTiles; ++q) v[q] = d[q][e] * a.scale;
+            if (a.out_bf) {
+                if constexpr (TB) {
+                    store_vec<__bf16, true>(out, at / 8, cols, v);
+                } else if (at + 4 <= cols) {
+                    const u32x4 h = Lane<__bf16>::narrow(v);
+                    gst_u<u32x2>(out + at * 2, u32x2{h[0], h[1]});
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (at + q < cols) Lane<__bf16>::put(out + (at + q) * 2, v[q]);
+                }
+            } else {
+#pragma unroll
+                for (int h = 0; h < Col::kTiles / 4; ++h) store_vec<float, true>(out, at / 4 + h, cols, v + 4 * h);
+            }
+        }
+    }
+}
+
 // --------------------------------------------------------------------- dispatch
 
 // What a call takes, from its sizes and types alone.
 struct FewPlan {
     bool rows_stream;  // the stream is the rows
-    int mt, batch, tiles, groups, splits, cols_p, blocks, pieces;
-    int64_t n_s, padded, stride, at_pairs, at_own, at_g, plane_g, at_f, at_db, at_sums, sums_stride;
+    int mt, batch, tiles, groups, splits, cols_p, blocks, pieces, pieces_fg;
+    int64_t n_s, padded, stride, at_pairs, at_own, at_g, plane_g, at_fg, plane_fg, at_f, at_db, at_sums, sums_stride;
 };
-
-constexpr int kCt = 2;  // rows of the stream of a workgroup, in 16's
 
 FewPlan few_plan(int K, const int64_t* rows, int64_t cols, int64_t classes, int dtype, int w_dtype, bool backward, int dw_dtype) {
     FewPlan p{};
@@ -683,7 +710,10 @@ FewPlan few_plan(int K, const int64_t* rows, int64_t cols, int64_t classes, int 
         p.padded = (static_cast<int64_t>(p.tiles) * p.groups + 31) / 32 * 32;
         p.plane_g = p.mt * 16 * p.padded * 2;
         p.at_g = take(p.pieces * p.plane_g);
-        const int block = stream_bf ? 128 : 64;
+        p.pieces_fg = (p.rows_stream ? dtype : dw_dtype) == TC_BF16 ? 2 : 3;
+        p.plane_fg = p.padded * (p.mt > 2 ? 64 : 32) * 2;
+        p.at_fg = take(p.pieces_fg * p.plane_fg);
+        const int block = stream_bf && p.mt < 4 ? 128 : 64;
         p.blocks = static_cast<int>((cols + block - 1) / block);
         p.cols_p = p.blocks * block;
         // workgroups enough to fill the chip four times, of at least 128 rows of
@@ -701,22 +731,38 @@ FewPlan few_plan(int K, const int64_t* rows, int64_t cols, int64_t classes, int 
 }
 
 template <bool SB, bool TB, int MT, bool ROWS>
-void run_logit(const FewArgs& a, bool backward, bool fine, dim3 grid, hipStream_t s) {
-    if (!backward)
-        few_logit_kernel<SB, TB, MT, kCt, ROWS, kForward, 1><<<grid, 256, 0, s>>>(a);
-    else if (fine)
-        few_logit_kernel<SB, TB, MT, kCt, ROWS, kBackward, 3><<<grid, 256, 0, s>>>(a);
+void run_logit(const FewArgs& a, bool backward, dim3 grid, hipStream_t s) {
+    // eight waves where the workgroups leave CUs idle
+    const bool eight = grid.x * grid.y <= 512;
+    if (eight)
+        backward ? few_logit_kernel<SB, TB, MT, 8, ROWS, kBackward><<<grid, 512, 0, s>>>(a)
+                 : few_logit_kernel<SB, TB, MT, 8, ROWS, kForward><<<grid, 512, 0, s>>>(a);
     else
-        few_logit_kernel<SB, TB, MT, kCt, ROWS, kBackward, 2><<<grid, 256, 0, s>>>(a);
+        backward ? few_logit_kernel<SB, TB, MT, 4, ROWS, kBackward><<<grid, 256, 0, s>>>(a)
+                 : few_logit_kernel<SB, TB, MT, 4, ROWS, kForward><<<grid, 256, 0, s>>>(a);
 }
 template <bool SB, bool TB, bool ROWS>
-void run_logit(const FewArgs& a, int mt, bool backward, bool fine, dim3 grid, hipStream_t s) {
+void run_logit(const FewArgs& a, int mt, bool backward, dim3 grid, hipStream_t s) {
     if (mt == 1)
-        run_logit<SB, TB, 1, ROWS>(a, backward, fine, grid, s);
+        run_logit<SB, TB, 1, ROWS>(a, backward, grid, s);
     else if (mt == 2)
-        run_logit<SB, TB, 2, ROWS>(a, backward, fine, grid, s);
+        run_logit<SB, TB, 2, ROWS>(a, backward, grid, s);
     else
-        run_logit<SB, TB, 4, ROWS>(a, backward, fine, grid, s);
+        run_logit<SB, TB, 4, ROWS>(a, backward, grid, s);
+}
+template <bool ROWS>
+void run_logit(const FewArgs& a, bool sb, bool tb, int mt, bool backward, dim3 grid, hipStream_t s) {
+    if (sb)
+        tb ? run_logit<true, true, ROWS>(a, mt, backward, grid, s) : run_logit<true, false, ROWS>(a, mt, backward, grid, s);
+    else
+        tb ? run_logit<false, true, ROWS>(a, mt, backward, grid, s) : run_logit<false, false, ROWS>(a, mt, backward, grid, s);
+}
+template <bool TB, bool ROWS>
+void run_outer(const OuterArgs& a, int mt, int pieces, dim3 grid, hipStream_t s) {
+    if (mt > 2)
+        pieces == 3 ? few_outer_kernel<TB, 2, ROWS, 3><<<grid, 256, 0, s>>>(a) : few_outer_kernel<TB, 2, ROWS, 2><<<grid, 256, 0, s>>>(a);
+    else
+        pieces == 3 ? few_outer_kernel<TB, 1, ROWS, 3><<<grid, 256, 0, s>>>(a) : few_outer_kernel<TB, 1, ROWS, 2><<<grid, 256, 0, s>>>(a);
 }
 template <bool SB, bool ROWS, int PG>
 void run_sum(const SumArgs& a, int mt, dim3 grid, hipStream_t s) {
@@ -744,73 +790,63 @@ int64_t few_workspace(int K, const int64_t* rows, int64_t cols, int64_t classes,
 hipError_t launch_few(const LossCall& c, const int* list, int count, hipStream_t s) {
     const FewPlan p = few_plan(c.K, c.rows, c.cols, c.classes, c.dtype, c.w_dtype, c.backward, c.dw_dtype);
     const bool x_bf = c.dtype == TC_BF16, w_bf = c.w_dtype == TC_BF16, dw_bf = c.dw_dtype == TC_BF16;
+    const bool sb = p.rows_stream ? x_bf : w_bf, tb = p.rows_stream ? w_bf : x_bf;
+    const int32_t cols = static_cast<int32_t>(c.cols), has_dloss = c.dloss != nullptr;
     for (int k0 = 0; k0 < count; k0 += p.batch) {
         const int n = std::min(p.batch, count - k0);
         FewArgs a{};
         SumArgs m{};
+        OuterArgs o{};
         for (int i = 0; i < n; ++i) {
             const int k = list[k0 + i];
             a.x[i] = c.x[k];
             a.w[i] = c.weight[k];
             a.bias[i] = c.bias ? c.bias[k] : nullptr;
-            a.label[i] = m.label[i] = c.label[k];
-            a.rows[i] = m.rows[i] = c.rows[k];
+            a.label[i] = m.label[i] = o.label[i] = c.label[k];
+            a.rows[i] = m.rows[i] = o.rows[i] = c.rows[k];
             if (c.backward) {
                 a.lse[i] = const_cast<float*>(c.lse_in[k]);
-                a.dloss[i] = m.dloss[i] = c.dloss ? c.dloss[k] : nullptr;
+                a.dloss[i] = m.dloss[i] = o.dloss[i] = c.dloss ? c.dloss[k] : nullptr;
                 a.db[i] = m.db[i] = c.dbias ? c.dbias[k] : nullptr;
-                a.out[i] = p.rows_stream ? c.dx[k] : c.dweight[k];
-                m.out[i] = p.rows_stream ? c.dweight[k] : c.dx[k];
+                o.side[i] = p.rows_stream ? c.weight[k] : c.x[k];
+                o.out[i] = p.rows_stream ? c.dx[k] : c.dweight[k];
                 m.stream[i] = p.rows_stream ? c.x[k] : c.weight[k];
+                m.out[i] = p.rows_stream ? c.dweight[k] : c.dx[k];
             } else {
                 a.lse[i] = c.lse[k];
                 a.loss[i] = c.loss[k];
             }
         }
-        a.work = m.work = static_cast<char*>(c.workspace);
-        a.stride = m.stride = p.stride;
+        a.work = m.work = o.work = static_cast<char*>(c.workspace);
+        a.stride = m.stride = o.stride = p.stride;
         a.at_pairs = p.at_pairs;
         a.at_own = p.at_own;
         a.at_g = m.at_g = p.at_g;
         a.plane_g = m.plane_g = p.plane_g;
+        a.at_fg = o.at_fg = p.at_fg;
+        a.plane_fg = o.plane_fg = p.plane_fg;
         a.padded = m.padded = p.padded;
         a.at_f = m.at_f = p.at_f;
         a.at_db = m.at_db = p.at_db;
         a.x_ld = c.x_ld;
-        a.out_ld = p.rows_stream ? c.dx_ld : c.cols;
-        a.classes = m.classes = c.classes;
-        a.cols = m.cols = static_cast<int32_t>(c.cols);
+        a.classes = m.classes = o.classes = c.classes;
+        a.cols = m.cols = o.cols = cols;
         a.tiles = p.tiles;
         a.w_bf = w_bf;
-        a.out_bf = p.rows_stream ? x_bf : dw_bf;
         a.db_bf = m.db_bf = dw_bf;
-        a.has_dloss = m.has_dloss = c.dloss != nullptr;
+        a.has_dloss = m.has_dloss = o.has_dloss = has_dloss;
         a.pieces_g = p.pieces;
-        a.scale = m.scale = c.scale;
+        a.pieces_fg = p.pieces_fg;
+        a.scale = m.scale = o.scale = c.scale;
         const dim3 grid(p.tiles, n);
-        const bool fine = !a.out_bf;
-        // a stream of rows whose gradient takes its place: that is written last,
-        // with the logits made once more
-        bool in_place = false;
-        if (c.backward && p.rows_stream)
-            for (int i = 0; i < n; ++i) in_place = in_place || a.x[i] == a.out[i];
-        a.store_g = 1;
-        a.store_out = !in_place;
-        auto logits = [&] {
-            if (p.rows_stream)
-                x_bf ? (w_bf ? run_logit<true, true, true>(a, p.mt, c.backward, fine, grid, s) : run_logit<true, false, true>(a, p.mt, c.backward, fine, grid, s))
-                     : (w_bf ? run_logit<false, true, true>(a, p.mt, c.backward, fine, grid, s) : run_logit<false, false, true>(a, p.mt, c.backward, fine, grid, s));
-            else
-                w_bf ? (x_bf ? run_logit<true, true, false>(a, p.mt, c.backward, fine, grid, s) : run_logit<true, false, false>(a, p.mt, c.backward, fine, grid, s))
-                     : (x_bf ? run_logit<false, true, false>(a, p.mt, c.backward, fine, grid, s) : run_logit<false, false, false>(a, p.mt, c.backward, fine, grid, s));
-            return hipGetLastError();
-        };
-        if (hipError_t e = logits()) return e;
+        p.rows_stream ? run_logit<true>(a, sb, tb, p.mt, c.backward, grid, s) : run_logit<false>(a, sb, tb, p.mt, c.backward, grid, s);
+        if (hipError_t e = hipGetLastError()) return e;
         if (!c.backward) {
             if (!p.rows_stream) few_join_kernel<<<dim3(static_cast<uint32_t>(p.mt * 16), n), 256, 0, s>>>(a);
             if (hipError_t e = hipGetLastError()) return e;
             continue;
         }
+        // the side's gradient first: the stream's may take the place of the rows
         m.at_sums = p.at_sums;
         m.sums_stride = p.sums_stride;
         m.ld = p.rows_stream ? c.x_ld : c.cols;
@@ -821,7 +857,7 @@ hipError_t launch_few(const LossCall& c, const int* list, int count, hipStream_t
         m.groups = p.groups;
         m.is_rows = p.rows_stream;
         const dim3 grid2(p.blocks, p.splits, n);
-        const bool sb = p.rows_stream ? x_bf : w_bf, three = p.pieces == 3;
+        const bool three = p.pieces == 3;
         if (p.rows_stream)
             sb ? (three ? run_sum<true, true, 3>(m, p.mt, grid2, s) : run_sum<true, true, 2>(m, p.mt, grid2, s))
                : (three ? run_sum<false, true, 3>(m, p.mt, grid2, s) : run_sum<false, true, 2>(m, p.mt, grid2, s));
@@ -829,14 +865,23 @@ hipError_t launch_few(const LossCall& c, const int* list, int count, hipStream_t
             sb ? (three ? run_sum<true, false, 3>(m, p.mt, grid2, s) : run_sum<true, false, 2>(m, p.mt, grid2, s))
                : (three ? run_sum<false, false, 3>(m, p.mt, grid2, s) : run_sum<false, false, 2>(m, p.mt, grid2, s));
         if (hipError_t e = hipGetLastError()) return e;
+        o.ld = p.rows_stream ? c.cols : c.x_ld;
+        o.out_ld = p.rows_stream ? c.dx_ld : c.cols;
+        o.out_bf = p.rows_stream ? x_bf : dw_bf;
+        const int64_t across = (c.cols + (tb ? 512 : 256) - 1) / (tb ? 512 : 256);
+        // rows of a workgroup: 256, or as many as leave 1,024 workgroups
+        int64_t chunk = p.n_s * across * n / 1024 / 16 * 16;
+        o.chunk = static_cast<int32_t>(std::max<int64_t>(32, std::min<int64_t>(256, chunk)));
+        if ((p.n_s + o.chunk - 1) / o.chunk > 65535) o.chunk = static_cast<int32_t>((p.n_s / 65535 + 16) / 16 * 16);
+        const dim3 grid3(static_cast<uint32_t>(across), static_cast<uint32_t>((p.n_s + o.chunk - 1) / o.chunk), n);
+        if (p.rows_stream)
+            tb ? run_outer<true, true>(o, p.mt, p.pieces_fg, grid3, s) : run_outer<false, true>(o, p.mt, p.pieces_fg, grid3, s);
+        else
+            tb ? run_outer<true, false>(o, p.mt, p.pieces_fg, grid3, s) : run_outer<false, false>(o, p.mt, p.pieces_fg, grid3, s);
+        if (hipError_t e = hipGetLastError()) return e;
         const int64_t n_t = p.rows_stream ? c.classes : p.mt * 16;
         few_finish_kernel<<<dim3(static_cast<uint32_t>((c.cols + 1023) / 1024 + 1), static_cast<uint32_t>(n_t), n), 256, 0, s>>>(m);
         if (hipError_t e = hipGetLastError()) return e;
-        if (in_place) {
-            a.store_g = 0;
-            a.store_out = 1;
-            if (hipError_t e = logits()) return e;
-        }
     }
     return hipSuccess;
 }
