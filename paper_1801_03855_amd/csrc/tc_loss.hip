@@ -21,11 +21,14 @@
 // at a sixteenth).  g is within [-1, 1] and is held times 2^14: one binary16
 // value where the result is bfloat16, hi and lo where it is binary32.
 //
-// Layout.  An operand in the workspace is a panel: for every 64 elements of the
-// summed axis, one line of 128 bytes a row, all rows next to each other, so that
-// a stage of a tile is one block of memory.  Padded with zeros to 64 elements
-// and 256 rows, so the products have no edges.
+// Layout.  An operand in the workspace is a panel: for every 32 elements of the
+// summed axis, one line of 64 bytes a row, all rows next to each other, so that a
+// stage of a tile is one block of memory.  (Loaded from where they lie instead,
+// rows of 8 KB have a stage's lines at a few of the memory's channels: 8,192 rows
+// of 4,096 over 131,072 classes in bfloat16 16.5 ms.)  The summed axis is padded
+// with zeros to 64 elements.
 #include <algorithm>
+#include <type_traits>
 
 #include "tc_lane.h"
 
@@ -41,7 +44,7 @@ typedef __attribute__((address_space(3))) char lds_char;
 typedef __attribute__((address_space(1))) const char global_char;
 
 constexpr int kBatch = 8;      // workers of one launch
-constexpr int kRow = 128;      // bytes of a panel's row: 64 elements of the summed axis
+constexpr int kLine = 64;      // bytes of a panel's row: 32 elements of the summed axis
 constexpr int kParts = 256;    // partial maxima of an operand
 constexpr int kUnitBits = 14;  // g is held times 2^14
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
@@ -181,7 +184,7 @@ __device__ __forceinline__ int exponent_of(const float* parts) {
 struct Panels {
     const void* p[kBatch];
     int64_t rows[kBatch];      // of the operand, from `first` on
-    int64_t at, at_t;          // of the panels in a worker's workspace; -1: not wanted
+    int64_t at, at_t;          // of the panels in a worker's workspace; at_t -1: not wanted
     int64_t plane, plane_t;    // from hi to lo
     int64_t padded, padded_t;  // rows of the panels
     int64_t ld;                // elements
@@ -241,8 +244,8 @@ __global__ void __launch_bounds__(256) loss_panel_kernel(const PanelArgs a) {
                 Lane<float>::widen(load_vec<float, true>(at, c / 4 + 1, a.cols), v + 4);
             }
         }
-        if (o.at >= 0) {
-            char* to = ws + o.at + (c0 / 64 * o.padded + row) * kRow + piece * 16;
+        {
+            char* to = ws + o.at + ((c0 / 32 + piece / 4) * o.padded + row) * kLine + piece % 4 * 16;
             if (o.raw) {
                 *reinterpret_cast<u32x4*>(to) = Lane<__bf16>::narrow(v);
             } else {
@@ -269,7 +272,7 @@ __global__ void __launch_bounds__(256) loss_panel_kernel(const PanelArgs a) {
         for (int e = 0; e < 8; ++e) v[e] = lds[piece * 8 + e][c];
         u16x8 hi, lo;
         split(v, whole, hi, lo);
-        char* to = ws + o.at_t + (r0 / 64 * o.padded_t + c0 + c) * kRow + piece * 16;
+        char* to = ws + o.at_t + ((r0 / 32 + piece / 4) * o.padded_t + c0 + c) * kLine + piece % 4 * 16;
         *reinterpret_cast<u16x8*>(to) = hi;
         if (o.planes_t > 1) *reinterpret_cast<u16x8*>(to + o.plane_t) = lo;
     }
@@ -279,10 +282,9 @@ __global__ void __launch_bounds__(256) loss_panel_kernel(const PanelArgs a) {
 
 // Rows of one operand of a product.
 struct Side {
-    int64_t step;    // bytes from one 64 elements of the sum to the next
-    int64_t plane;   // from hi to lo
-    uint32_t pitch;  // from row to row
-    uint32_t planes; // bit n: plane of the n-th run over the sum
+    int64_t step;     // bytes from one 32 elements of the sum to the next
+    int64_t plane;    // from hi to lo
+    uint32_t planes;  // bit n: plane of the n-th run over the sum
 };
 
 template <bool BF>
@@ -294,48 +296,57 @@ __device__ __forceinline__ f32x16 multiply(u32x4 a, u32x4 b, f32x16 c) {
 }
 
 // One tile of left right^T, TILE x TILE, of four waves with a quarter each, as
-// 32 x 32 x 16 products.  A stage is 128 bytes of each of the 2 TILE rows; two
-// stages are in LDS, one loaded straight from memory while the other is
-// multiplied.  A row's 128 bytes are eight 16-byte pieces; piece p of row r lies
-// at p ^ (r / 2 % 8), so that 16 lanes reading one piece each of 16 rows touch
-// all 64 banks once.  Left and right: the tile's first rows, of which there are
-// `rows` (the last one stands for those behind it).  The sum runs over the
-// steps [first, end) of 64 elements `runs` times, over other planes each time.
+// 32 x 32 x 16 products.  A stage is 32 elements (64 bytes) of each of the 2 TILE
+// rows; kStages of them are in LDS, loaded straight from memory while others are
+// multiplied.  A row's 64 bytes are four 16-byte pieces; piece p of row r lies at
+// p ^ (r / 4 % 4), so that 16 lanes reading one piece each of 16 rows touch all
+// 64 banks once.  Left and right: the tile's first rows, of which there are
+// `rows` (the last one stands for those behind it).  The sum runs over the steps
+// [first, end) of 32 elements `runs` times, over other planes each time.
+//
+// A SIMD has one wave (or two), so nothing but the order of the instructions
+// covers for what is not a product: every product is followed by at most one
+// read from LDS or load.
 //
 // acc[i][j], lane l, element e: row i * 32 + e / 4 * 8 + l / 32 * 4 + e % 4 of
 // the wave's quarter of left, row j * 32 + l % 32 of its quarter of right.
+constexpr int kStages = 4;
+
 template <int TILE, bool BF>
 __device__ __forceinline__ void product(char* lds, const char* left, const Side& ls, int left_rows, const char* right,
                                         const Side& rs, int right_rows, int first, int end, int runs,
                                         f32x16 (&acc)[TILE / 64][TILE / 64]) {
-    constexpr int kHalf = TILE * kRow, kStage = 2 * kHalf, kSide = TILE / 64, kLoads = TILE / 32;
+    constexpr int kHalf = TILE * kLine, kStage = 2 * kHalf, kSide = TILE / 64, kLoads = TILE / 64;
     const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const int wr = wave / 2 * (TILE / 2), wc = wave % 2 * (TILE / 2);
-    // this wave's 1,024-byte pieces of a stage: eight rows each
+    // this wave's 1,024-byte pieces of a stage: sixteen rows each
     uint32_t off_l[kLoads], off_r[kLoads];
 #pragma unroll
     for (int q = 0; q < kLoads; ++q) {
-        const int r = (wave * kLoads + q) * 8 + lane / 8, p = (lane % 8) ^ (r / 2 % 8);
-        off_l[q] = static_cast<uint32_t>(min(r, left_rows - 1)) * ls.pitch + static_cast<uint32_t>(p * 16);
-        off_r[q] = static_cast<uint32_t>(min(r, right_rows - 1)) * rs.pitch + static_cast<uint32_t>(p * 16);
+        const int r = (wave * kLoads + q) * 16 + lane / 4, p = (lane % 4) ^ (r / 4 % 4);
+        off_l[q] = static_cast<uint32_t>(min(r, left_rows - 1) * kLine + p * 16);
+        off_r[q] = static_cast<uint32_t>(min(r, right_rows - 1) * kLine + p * 16);
     }
-    // the stage that is loaded next
-    int at = first, run = 0;
+    // the stage that is loaded next, and the one behind the last
+    const int stages = (end - first) * runs;
+    int asked = 0, at = first, run = 0;
     const char *pl, *pr;
     auto seek = [&] {
-        pl = left + at * ls.step + (ls.planes >> run & 1) * ls.plane;
-        pr = right + at * rs.step + (rs.planes >> run & 1) * rs.plane;
+        pl = left + first * ls.step + (ls.planes >> run & 1) * ls.plane;
+        pr = right + first * rs.step + (rs.planes >> run & 1) * rs.plane;
     };
     seek();
-    auto fetch = [&](int buf, int from, int to) {
+    // load n of a stage's 2 kLoads
+    auto load = [&](int buf, int n) {
         char* dst = lds + buf * kStage + wave * kLoads * 1024;
-#pragma unroll
-        for (int q = from; q < to; ++q) {
+        const int q = n / 2;
+        if (n % 2 == 0)
             __builtin_amdgcn_global_load_lds((global_char*)(pl + off_l[q]), (lds_char*)(dst + q * 1024), 16, 0, 0);
+        else
             __builtin_amdgcn_global_load_lds((global_char*)(pr + off_r[q]), (lds_char*)(dst + kHalf + q * 1024), 16, 0, 0);
-        }
     };
     auto advance = [&] {
+        ++asked;
         pl += ls.step;
         pr += rs.step;
         if (++at == end) {
@@ -347,55 +358,75 @@ __device__ __forceinline__ void product(char* lds, const char* left, const Side&
     struct Operands {
         u32x4 a[kSide], b[kSide];
     } now, next;
-    const int ra = (wr + lane % 32) * kRow, rb = kHalf + (wc + lane % 32) * kRow, turn = lane / 2 % 8;
-    auto read = [&](Operands& f, int buf, int step) {
-        const char* p = lds + buf * kStage;
-        const int piece = ((step * 2 + lane / 32) ^ turn) * 16;
-#pragma unroll
-        for (int i = 0; i < kSide; ++i) {
-            f.a[i] = *reinterpret_cast<const u32x4*>(p + ra + i * 32 * kRow + piece);
-            f.b[i] = *reinterpret_cast<const u32x4*>(p + rb + i * 32 * kRow + piece);
-        }
+    const int ra = (wr + lane % 32) * kLine, rb = kHalf + (wc + lane % 32) * kLine, turn = lane / 4 % 4;
+    const int piece[2] = {((lane / 32) ^ turn) * 16, ((2 + lane / 32) ^ turn) * 16};
+    // operand n of 2 kSide: those of the first products first
+    auto read = [&](Operands& f, int buf, int step, int n) {
+        const char* p = lds + buf * kStage + piece[step];
+        if (n == 0)
+            f.a[0] = *reinterpret_cast<const u32x4*>(p + ra);
+        else if (n <= kSide)
+            f.b[n - 1] = *reinterpret_cast<const u32x4*>(p + rb + (n - 1) * 32 * kLine);
+        else
+            f.a[n - kSide] = *reinterpret_cast<const u32x4*>(p + ra + (n - kSide) * 32 * kLine);
     };
-    constexpr int kAll = kSide * kSide, kFirst = kAll / 4;
-    auto products = [&](const Operands& f, int from, int to) {
-#pragma unroll
-        for (int n = from; n < to; ++n) acc[n / kSide][n % kSide] = multiply<BF>(f.a[n / kSide], f.b[n % kSide], acc[n / kSide][n % kSide]);
+    constexpr int kAll = kSide * kSide, kReads = 2 * kSide, kAsks = 2 * kLoads;
+    auto one = [&](const Operands& f, int n) {
+        acc[n / kSide][n % kSide] = multiply<BF>(f.a[n / kSide], f.b[n % kSide], acc[n / kSide][n % kSide]);
     };
-    // The stage under way is there, in every wave, and every wave has its
-    // operands of the one before, whose buffer is loaded next.
-    auto arrive = [&] {
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    for (int n = 0; n < kStages - 1 && n < stages; ++n) {
+#pragma unroll
+        for (int q = 0; q < kAsks; ++q) load(n, q);
+        advance();
+    }
+    // The stage after the one under way is there, in every wave, and every wave
+    // has its operands of the one under way, whose buffer is loaded next.
+    // `full`: the stages after it are all asked for.
+    auto arrive = [&](bool full) {
+        if (full)
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kStages - 2) * kAsks) : "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    const int stages = (end - first) * runs;
-    fetch(0, 0, kLoads);
-    arrive();
-    read(now, 0, 0);
+    arrive(stages >= kStages - 1);
+#pragma unroll
+    for (int q = 0; q < kReads; ++q) read(now, 0, 0, q);
     int buf = 0;
     for (int st = 0; st < stages; ++st) {
-        const bool more = st + 1 < stages;
-        if (more) advance();
+        const int then = buf + 1 == kStages ? 0 : buf + 1, before = buf == 0 ? kStages - 1 : buf - 1;
+        const bool more = asked < stages;
+        // the first 16 elements; the next 16 are read, a stage is asked for
 #pragma unroll
-        for (int s = 0; s < 4; ++s) {
-            Operands& f = s % 2 ? next : now;
-            Operands& g = s % 2 ? now : next;
-            // the next stage's loads are asked for in the first half of this one
-            if (s < 2 && more) fetch(buf ^ 1, s * kLoads / 2, (s + 1) * kLoads / 2);
-            products(f, 0, kFirst);
+        for (int n = 0; n < kAll; ++n) {
+            one(now, n);
             __builtin_amdgcn_sched_barrier(0);
-            if (s < 3) {
-                read(g, buf, s + 1);
-            } else if (more) {
-                arrive();
-                read(g, buf ^ 1, 0);
-            }
-            __builtin_amdgcn_sched_barrier(0);
-            products(f, kFirst, kAll);
+#pragma unroll
+            for (int q = n * kReads / kAll; q < (n + 1) * kReads / kAll; ++q) read(next, buf, 1, q);
+#pragma unroll
+            for (int q = n * kAsks / kAll; q < (n + 1) * kAsks / kAll; ++q)
+                if (more) load(before, q);
             __builtin_amdgcn_sched_barrier(0);
         }
-        buf ^= 1;
+        if (more) advance();
+        constexpr int kFirst = kAll / 4;
+#pragma unroll
+        for (int n = 0; n < kFirst; ++n) one(next, n);
+        __builtin_amdgcn_sched_barrier(0);
+        const bool last = st + 1 == stages;
+        if (!last) arrive(more);
+#pragma unroll
+        for (int n = kFirst; n < kAll; ++n) {
+            // (past the end of the last stage they are operands of nothing)
+#pragma unroll
+            for (int q = (n - kFirst) * kReads / (kAll - kFirst); q < (n - kFirst + 1) * kReads / (kAll - kFirst); ++q)
+                read(now, then, 0, q);
+            __builtin_amdgcn_sched_barrier(0);
+            one(next, n);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        buf = then;
     }
 }
 
@@ -415,8 +446,6 @@ __device__ __forceinline__ Place place_of(uint32_t b, uint32_t n, int down, int 
 
 // The logits of one piece of the classes.
 struct LogitArgs {
-    const char* w[kBatch];  // the piece's first class
-    const char* x[kBatch];
     const void* bias[kBatch];
     const int64_t* label[kBatch];
     const float* lse[kBatch];
@@ -425,6 +454,7 @@ struct LogitArgs {
     char* work;
     int64_t stride;                 // of the workspace, from worker to worker
     int64_t at_rows, at_parts;
+    int64_t at_w, at_x;             // panels
     int64_t at_g, at_gt;            // g as [row][class] and [class][row]
     int64_t plane_g, plane_gt;
     int64_t at_pairs, at_own;       // (largest, sum) of every tile and row; the label's logit
@@ -453,7 +483,7 @@ __device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
 template <int TILE, bool BF, bool GRAD>
 __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) loss_logit_kernel(const LogitArgs a) {
     constexpr int kSide = TILE / 64;
-    __shared__ __attribute__((aligned(16))) char lds[4 * TILE * kRow];
+    __shared__ __attribute__((aligned(16))) char lds[kStages * 2 * TILE * kLine];
     __shared__ __attribute__((aligned(16))) float extra[TILE + (GRAD ? 0 : 2 * TILE)];
     const int k = blockIdx.y;
     const int64_t rows = a.rows[k];
@@ -462,12 +492,12 @@ __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) loss_logit_kernel(co
     const int v0 = at.i * TILE;
     const int64_t r0 = static_cast<int64_t>(at.j) * TILE;
     if (r0 >= rows) return;
+    char* work = a.work + k * a.stride;
     f32x16 acc[kSide][kSide] = {};
-    product<TILE, BF>(lds, a.w[k] + static_cast<int64_t>(v0) * a.ws.pitch, a.ws, a.count - v0, a.x[k] + r0 * a.xs.pitch, a.xs,
+    product<TILE, BF>(lds, work + a.at_w + static_cast<int64_t>(v0) * kLine, a.ws, a.count - v0, work + a.at_x + r0 * kLine, a.xs,
                       static_cast<int>(min(static_cast<int64_t>(TILE), rows - r0)), 0, a.steps, a.runs, acc);
     const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
     const int wr = wave / 2 * (TILE / 2), wc = wave % 2 * (TILE / 2);
-    char* work = a.work + k * a.stride;
     // the tile's biases; classes behind the last one have -infinity
     for (int v = tid; v < TILE; v += 256)
         extra[v] = v0 + v < a.count ? (a.bias[k] ? load_as(a.bias[k], a.first + v0 + v, a.w_bf) : 0.0f) : -INFINITY;
@@ -574,20 +604,20 @@ __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) loss_logit_kernel(co
         auto put_g = [&](int plane) {
             char* g = work + a.at_g + plane * a.plane_g;
             for (int n = tid; n < TILE * kPieces; n += 256) {
-                const int block = n / (TILE * 8), r = n / 8 % TILE, p = n % 8;  // of 64 classes
-                *reinterpret_cast<u32x4*>(g + ((v0 / 64 + block) * a.padded_r + r0 + r) * kRow + p * 16) =
-                    *reinterpret_cast<const u32x4*>(piece_at(r, block * 8 + p));
+                const int block = n / (TILE * 4), r = n / 4 % TILE, p = n % 4;  // of 32 classes
+                *reinterpret_cast<u32x4*>(g + ((v0 / 32 + block) * a.padded_r + r0 + r) * kLine + p * 16) =
+                    *reinterpret_cast<const u32x4*>(piece_at(r, block * 4 + p));
             }
         };
         auto put_gt = [&](int plane) {
             char* g = work + a.at_gt + plane * a.plane_gt;
             for (int n = tid; n < TILE * kPieces; n += 256) {
-                const int block = n / (TILE * 8), v = n / 8 % TILE, p = n % 8;  // of 64 rows
-                if (r0 + block * 64 >= left_k) break;
+                const int block = n / (TILE * 4), v = n / 4 % TILE, p = n % 4;  // of 32 rows
+                if (r0 + block * 32 >= left_k) break;
                 u16x8 h;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) h[e] = *reinterpret_cast<const uint16_t*>(piece_at(block * 64 + p * 8 + e, v / 8) + v % 8 * 2);
-                *reinterpret_cast<u16x8*>(g + ((r0 / 64 + block) * a.padded + v0 + v) * kRow + p * 16) = h;
+                for (int e = 0; e < 8; ++e) h[e] = *reinterpret_cast<const uint16_t*>(piece_at(block * 32 + p * 8 + e, v / 8) + v % 8 * 2);
+                *reinterpret_cast<u16x8*>(g + ((r0 / 32 + block) * a.padded + v0 + v) * kLine + p * 16) = h;
             }
         };
         for (int pass = 0; pass < 4; ++pass) {
@@ -667,7 +697,7 @@ struct GradArgs {
 template <int TILE>
 __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) loss_grad_kernel(const GradArgs a) {
     constexpr int kSide = TILE / 64;
-    __shared__ __attribute__((aligned(16))) char lds[4 * TILE * kRow];
+    __shared__ __attribute__((aligned(16))) char lds[kStages * 2 * TILE * kLine];
     const int k = blockIdx.y;
     const bool second = static_cast<int>(blockIdx.x) >= a.job[1].first;
     const GradJob& o = a.job[second];
@@ -677,14 +707,14 @@ __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) loss_grad_kernel(con
     const int64_t rows = o.rows[k], n0 = static_cast<int64_t>(at.j) * TILE;
     if (n0 >= rows) return;
     const int m0 = at.i * TILE;
-    const int steps = o.by_rows ? static_cast<int>(round_up(a.x_rows[k], 64) / 64) : o.steps;
+    const int steps = o.by_rows ? static_cast<int>(round_up(a.x_rows[k], 64) / 32) : o.steps;
     const int from = static_cast<int>(static_cast<int64_t>(steps) * part / o.splits);
     const int to = static_cast<int>(static_cast<int64_t>(steps) * (part + 1) / o.splits);
     char* work = a.work + k * a.stride;
     f32x16 acc[kSide][kSide] = {};
     if (to > from)
-        product<TILE, false>(lds, work + o.at_left + static_cast<int64_t>(m0) * kRow, o.left, TILE,
-                             work + o.at_right + n0 * kRow, o.right, TILE, from, to, o.runs, acc);
+        product<TILE, false>(lds, work + o.at_left + static_cast<int64_t>(m0) * kLine, o.left, TILE,
+                             work + o.at_right + n0 * kLine, o.right, TILE, from, to, o.runs, acc);
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int wr = wave / 2 * (TILE / 2), wc = wave % 2 * (TILE / 2);
     const Parts* parts = reinterpret_cast<const Parts*>(work + a.at_parts);
@@ -796,7 +826,7 @@ __global__ void __launch_bounds__(256) loss_bias_kernel(const BiasArgs a) {
     float s = 0.0f;
     for (int64_t b = 0; b < round_up(a.rows[k], 64) / 64; ++b)
         for (int p = 0; p < a.planes; ++p) {
-            const f16x8 h = *reinterpret_cast<const f16x8*>(work + a.at_gt + p * a.plane_gt + (b * a.padded + v) * kRow + piece * 16);
+            const f16x8 h = *reinterpret_cast<const f16x8*>(work + a.at_gt + p * a.plane_gt + ((b * 2 + piece / 4) * a.padded + v) * kLine + piece % 4 * 16);
 #pragma unroll
             for (int i = 0; i < 8; ++i) s += static_cast<float>(h[i]);
         }
@@ -829,7 +859,7 @@ struct Plan {
     int planes_x, planes_w;    // of the logits' operands
     int planes_g, planes_wt;   // of dx's
     int planes_gt, planes_xt;  // of dweight's
-    int64_t rows, rows_p, cols_p, steps;  // most rows of a worker, padded to 256, columns to 256, 64's
+    int64_t rows, rows_p, cols_p, steps;  // most rows of a worker, padded to 256, columns to 256, 32's
     int64_t piece, pieces;     // classes at a time
     int batch;                 // workers at a time
     int splits;                // of the sum of dx
@@ -855,11 +885,11 @@ Plan plan_of(int K, const int64_t* rows, int64_t cols, int64_t classes, int dtyp
     for (int k = 0; k < K; ++k) p.rows = std::max(p.rows, rows[k]);
     p.rows_p = round_up(p.rows, 256);
     p.cols_p = round_up(cols, 256);
-    p.steps = round_up(cols, 64) / 64;
+    p.steps = round_up(cols, 64) / 32;
     // classes of a piece by the bytes that one takes, most of them the panels of
     // g and of the weight
     const int64_t all = round_up(classes, 256);
-    int64_t each = 2 * p.steps * 64 * p.planes_w;
+    int64_t each = p.steps * kLine * p.planes_w;
     if (backward) each += 2 * p.rows_p * (p.planes_g + p.planes_gt) + 2 * p.cols_p * p.planes_wt;
     p.piece = std::min(all, std::max<int64_t>(1024, kRoom / each / 256 * 256));
     p.pieces = (all + p.piece - 1) / p.piece;
@@ -886,26 +916,20 @@ Plan plan_of(int K, const int64_t* rows, int64_t cols, int64_t classes, int dtyp
         p.at_own = take(p.rows_p * 4);
         p.at_pairs = take((p.piece * p.pieces / kTilesPair) * p.rows_p * 8);
     }
-    p.at_xz = take(p.steps * p.rows_p * kRow * p.planes_x);
-    p.at_wz = take(p.steps * p.piece * kRow * p.planes_w);
+    p.at_xz = take(p.steps * p.rows_p * kLine * p.planes_x);
+    p.at_wz = take(p.steps * p.piece * kLine * p.planes_w);
     if (backward) {
-        const int64_t rows_k = round_up(p.rows, 64) / 64;
-        p.at_xt = take(rows_k * p.cols_p * kRow * p.planes_xt);
-        p.at_wt = take(p.piece / 64 * p.cols_p * kRow * p.planes_wt);
-        p.at_g = take(p.piece / 64 * p.rows_p * kRow * p.planes_g);
-        p.at_gt = take(rows_k * p.piece * kRow * p.planes_gt);
+        const int64_t rows_k = round_up(p.rows, 64) / 32;
+        p.at_xt = take(rows_k * p.cols_p * kLine * p.planes_xt);
+        p.at_wt = take(p.piece / 32 * p.cols_p * kLine * p.planes_wt);
+        p.at_g = take(p.piece / 32 * p.rows_p * kLine * p.planes_g);
+        p.at_gt = take(rows_k * p.piece * kLine * p.planes_gt);
         p.at_sums = take(p.splits * p.rows_p * p.cols_p * 4);
         if (p.splits_w) p.at_sums_w = take(p.splits_w * p.piece * p.cols_p * 4);
     }
     p.stride = round_up(at, 4096);
     p.batch = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({K, kBatch, 2 * kRoom / p.stride})));
     return p;
-}
-
-// An operand that is multiplied where it lies: bfloat16 rows of whole lines at
-// 16-byte addresses.
-bool lies_right(const void* p, int64_t ld, int64_t cols) {
-    return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0 && ld < (1 << 21) && cols % 64 == 0;
 }
 
 // The side of the tiles of a down x across result, of n such results: the one
@@ -971,14 +995,9 @@ hipError_t launch_cross_entropy(const LossCall& c, hipStream_t s) {
     for (int k0 = 0; k0 < count; k0 += p.batch) {
         const int n = std::min(p.batch, count - k0);
         const int* who = list + k0;
-        bool x_right = p.bf, w_right = p.bf;
         int64_t most = 0;
-        for (int i = 0; i < n; ++i) {
-            x_right = x_right && lies_right(c.x[who[i]], c.x_ld, cols);
-            w_right = w_right && lies_right(c.weight[who[i]], cols, cols);
-            most = std::max(most, c.rows[who[i]]);
-        }
-        const int64_t piece = w_right && !back ? round_up(classes, 256) : p.piece;
+        for (int i = 0; i < n; ++i) most = std::max(most, c.rows[who[i]]);
+        const int64_t piece = p.piece;
         if (back || !p.bf) {
             TopArgs t{};
             for (int i = 0; i < n; ++i) {
@@ -1019,21 +1038,21 @@ hipError_t launch_cross_entropy(const LossCall& c, hipStream_t s) {
             a.at_rows = p.at_rows;
             a.at_parts = p.at_parts;
             a.cols = static_cast<int32_t>(cols);
-            const int32_t tiles_c = static_cast<int32_t>(p.steps);
-            x.at = x_right ? -1 : p.at_xz;
+            const int32_t tiles_c = static_cast<int32_t>(p.steps / 2);
+            x.at = p.at_xz;
             x.at_t = back ? p.at_xt : -1;
-            x.plane = p.steps * p.rows_p * kRow;
-            x.plane_t = round_up(p.rows, 64) / 64 * p.cols_p * kRow;
+            x.plane = p.steps * p.rows_p * kLine;
+            x.plane_t = round_up(p.rows, 64) / 32 * p.cols_p * kLine;
             x.padded = p.rows_p;
             x.ld = c.x_ld;
             x.planes = p.planes_x;
             x.planes_t = p.planes_xt;
             x.bf = x_bf;
             x.by_rows = 1;
-            w.at = w_right ? -1 : p.at_wz;
+            w.at = p.at_wz;
             w.at_t = back ? p.at_wt : -1;
-            w.plane = p.steps * p.piece * kRow;
-            w.plane_t = p.piece / 64 * p.cols_p * kRow;
+            w.plane = p.steps * p.piece * kLine;
+            w.plane_t = p.piece / 32 * p.cols_p * kLine;
             w.padded = p.piece;
             w.ld = cols;
             w.planes = p.planes_w;
@@ -1042,27 +1061,22 @@ hipError_t launch_cross_entropy(const LossCall& c, hipStream_t s) {
             x.raw = w.raw = p.bf;
             x.padded_t = w.padded_t = p.cols_p;
             x.tiles_c = w.tiles_c = tiles_c;
-            const bool x_wanted = v0 == 0 && (x.at >= 0 || x.at_t >= 0), w_wanted = w.at >= 0 || w.at_t >= 0;
-            w.first = x_wanted ? static_cast<int32_t>((most + 63) / 64) * tiles_c : 0;
-            const int32_t blocks = w.first + (w_wanted ? static_cast<int32_t>((here + 63) / 64) * tiles_c : 0);
-            if (blocks) {
-                loss_panel_kernel<<<dim3(blocks, n), 256, 0, s>>>(a);
-                if (hipError_t e = hipGetLastError()) return e;
-            }
+            w.first = v0 == 0 ? static_cast<int32_t>((most + 63) / 64) * tiles_c : 0;
+            loss_panel_kernel<<<dim3(w.first + static_cast<int32_t>((here + 63) / 64) * tiles_c, n), 256, 0, s>>>(a);
+            if (hipError_t e = hipGetLastError()) return e;
             // the logits
             LogitArgs l{};
             for (int i = 0; i < n; ++i) {
                 const int k = who[i];
-                char* own = work + i * p.stride;
-                l.w[i] = w_right ? static_cast<const char*>(w.p[i]) : own + p.at_wz;
-                l.x[i] = x_right ? static_cast<const char*>(c.x[k]) : own + p.at_xz;
                 l.bias[i] = c.bias ? c.bias[k] : nullptr;
                 l.label[i] = c.label[k];
                 l.lse[i] = back ? c.lse_in[k] : nullptr;
                 l.rows[i] = c.rows[k];
             }
-            l.ws = w_right ? Side{kRow, 0, static_cast<uint32_t>(cols * 2), 0} : Side{p.piece * kRow, w.plane, kRow, 0};
-            l.xs = x_right ? Side{kRow, 0, static_cast<uint32_t>(c.x_ld * 2), 0} : Side{p.rows_p * kRow, x.plane, kRow, 0};
+            l.at_w = p.at_wz;
+            l.at_x = p.at_xz;
+            l.ws = {p.piece * kLine, w.plane, 0};
+            l.xs = {p.rows_p * kLine, x.plane, 0};
             l.runs = runs_of(p.planes_w, p.planes_x, l.ws, l.xs);
             l.work = work;
             l.stride = p.stride;
@@ -1070,7 +1084,7 @@ hipError_t launch_cross_entropy(const LossCall& c, hipStream_t s) {
             l.at_parts = p.at_parts;
             l.at_g = p.at_g;
             l.at_gt = p.at_gt;
-            const int64_t plane_g = p.piece / 64 * p.rows_p * kRow, plane_gt = round_up(p.rows, 64) / 64 * p.piece * kRow;
+            const int64_t plane_g = p.piece / 32 * p.rows_p * kLine, plane_gt = round_up(p.rows, 64) / 32 * p.piece * kLine;
             l.plane_g = plane_g;
             l.plane_gt = plane_gt;
             l.at_pairs = p.at_pairs;
@@ -1080,7 +1094,7 @@ hipError_t launch_cross_entropy(const LossCall& c, hipStream_t s) {
             l.first = v0;
             l.classes = static_cast<int32_t>(classes);
             l.count = static_cast<int32_t>(here);
-            l.steps = tiles_c;
+            l.steps = static_cast<int32_t>(p.steps);
             l.scaled = !p.bf;
             l.w_bf = w_bf;
             l.planes_g = p.planes_g;
@@ -1143,19 +1157,19 @@ hipError_t launch_cross_entropy(const LossCall& c, hipStream_t s) {
             const int32_t down = static_cast<int32_t>((cols + tile2 - 1) / tile2);
             dx.at_left = p.at_wt;
             dx.at_right = p.at_g;
-            dx.left = {p.cols_p * kRow, w.plane_t, kRow, 0};
-            dx.right = {p.rows_p * kRow, plane_g, kRow, 0};
+            dx.left = {p.cols_p * kLine, w.plane_t, 0};
+            dx.right = {p.rows_p * kLine, plane_g, 0};
             dx.runs = runs_of(p.planes_wt, p.planes_g, dx.left, dx.right);
             dx.at_sums = p.at_sums;
             dx.sums_stride = p.rows_p * p.cols_p * 4;
             dx.across = static_cast<int32_t>((most + tile2 - 1) / tile2);
             dx.splits = p.splits;
-            dx.steps = static_cast<int32_t>((here + 63) / 64);
+            dx.steps = static_cast<int32_t>((here + 63) / 64 * 2);
             dx.add = v0 > 0;
             dw.at_left = p.at_xt;
             dw.at_right = p.at_gt;
-            dw.left = {p.cols_p * kRow, x.plane_t, kRow, 0};
-            dw.right = {p.piece * kRow, plane_gt, kRow, 0};
+            dw.left = {p.cols_p * kLine, x.plane_t, 0};
+            dw.right = {p.piece * kLine, plane_gt, 0};
             dw.runs = runs_of(p.planes_xt, p.planes_gt, dw.left, dw.right);
             dw.at_sums = p.splits_w ? p.at_sums_w : -1;
             dw.sums_stride = p.piece * p.cols_p * 4;
