@@ -45,7 +45,7 @@ typedef __attribute__((address_space(1))) const char global_char;
 
 constexpr int kBatch = 8;      // workers of one launch
 constexpr int kLine = 64;      // bytes of a panel's row: 32 elements of the summed axis
-constexpr int kParts = 256;    // partial maxima of an operand
+constexpr int kParts = 512;    // partial maxima of an operand
 constexpr int kUnitBits = 14;  // g is held times 2^14
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
@@ -107,16 +107,29 @@ __global__ void __launch_bounds__(256) loss_top_kernel(const TopArgs a) {
         float top = 0.0f;
         const int64_t n = a.w_size / 8;
         const uintptr_t w = reinterpret_cast<uintptr_t>(a.w[k]);
-        for (int64_t v = part * 256 + threadIdx.x; v < n; v += kParts * 256) {
-            float f[8];
-            if (a.w_bf) {
-                Lane<__bf16>::widen(gld_u<u32x4>(w + v * 16), f);
-            } else {
-                Lane<float>::widen(gld_u<u32x4>(w + v * 32), f);
-                Lane<float>::widen(gld_u<u32x4>(w + v * 32 + 16), f + 4);
+        // four at a time: with one the loads' latency is what bounds it (131,072 x
+        // 4,096 bfloat16 560 us)
+        constexpr int kAhead = 4;
+        for (int64_t v = part * 256 + threadIdx.x; v < n; v += kAhead * kParts * 256) {
+            u32x4 q[kAhead][2];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int64_t at = std::min(v + i * kParts * 256, n - 1);
+                q[i][0] = gld_u<u32x4>(w + at * (a.w_bf ? 16 : 32));
+                if (!a.w_bf) q[i][1] = gld_u<u32x4>(w + at * 32 + 16);
             }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) top = fmaxf(top, finite_abs(f[e]));
+            for (int i = 0; i < kAhead; ++i) {
+                float f[8];
+                if (a.w_bf) {
+                    Lane<__bf16>::widen(q[i][0], f);
+                } else {
+                    Lane<float>::widen(q[i][0], f);
+                    Lane<float>::widen(q[i][1], f + 4);
+                }
+#pragma unroll
+                for (int e = 0; e < 8; ++e) top = fmaxf(top, finite_abs(f[e]));
+            }
         }
         if (part == 0 && threadIdx.x < a.w_size - n * 8) top = fmaxf(top, finite_abs(load_as(a.w[k], n * 8 + threadIdx.x, a.w_bf)));
         top = wave_max(top);
@@ -467,6 +480,8 @@ struct LogitArgs {
     int32_t scaled;                 // operands have exponents
     int32_t w_bf;                   // of the bias
     int32_t planes_g, planes_gt, has_dloss;
+    int64_t at_acc;                 // sums of a part of the columns [part][tile][register][lane]
+    int32_t splits;
 };
 
 // Joins (m, s) and (m2, s2): the largest, and the sum of exp(z - largest).  A
@@ -478,9 +493,13 @@ __device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
     s = a + b;
 }
 
+// What a launch does of a tile: all; where tiles are few, the sums over parts of
+// the columns; what comes after them.
+enum Part { kWhole, kSums, kRest };
+
 // Rows of left are classes, rows of right are workers' rows: a lane has one row's
 // logits of 16 classes of each 32 x 32 product.
-template <int TILE, bool BF, bool GRAD>
+template <int TILE, bool BF, bool GRAD, Part PART>
 __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) loss_logit_kernel(const LogitArgs a) {
     constexpr int kSide = TILE / 64;
     __shared__ __attribute__((aligned(16))) char lds[kStages * 2 * TILE * kLine];
@@ -494,8 +513,34 @@ __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) loss_logit_kernel(co
     if (r0 >= rows) return;
     char* work = a.work + k * a.stride;
     f32x16 acc[kSide][kSide] = {};
-    product<TILE, BF>(lds, work + a.at_w + static_cast<int64_t>(v0) * kLine, a.ws, a.count - v0, work + a.at_x + r0 * kLine, a.xs,
-                      static_cast<int>(min(static_cast<int64_t>(TILE), rows - r0)), 0, a.steps, a.runs, acc);
+    // (in the order of the registers, 16 bytes a lane)
+    f32x4* sums = reinterpret_cast<f32x4*>(work + a.at_acc) + (static_cast<int64_t>(at.i) * a.tiles_r + at.j) * (TILE * TILE / 4) + threadIdx.x;
+    const int64_t all = static_cast<int64_t>(a.tiles_v) * a.tiles_r * (TILE * TILE / 4);
+    if constexpr (PART != kRest) {
+        const int from = PART == kSums ? a.steps * static_cast<int>(blockIdx.z) / a.splits : 0;
+        const int to = PART == kSums ? a.steps * (static_cast<int>(blockIdx.z) + 1) / a.splits : a.steps;
+        product<TILE, BF>(lds, work + a.at_w + static_cast<int64_t>(v0) * kLine, a.ws, a.count - v0, work + a.at_x + r0 * kLine, a.xs,
+                          static_cast<int>(min(static_cast<int64_t>(TILE), rows - r0)), from, to, a.runs, acc);
+    }
+    if constexpr (PART != kWhole)
+#pragma unroll
+        for (int i = 0; i < kSide; ++i)
+#pragma unroll
+            for (int j = 0; j < kSide; ++j)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    f32x4* place = sums + ((i * kSide + j) * 4 + q) * 256;
+                    f32x4 v = {acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
+                    if constexpr (PART == kSums) {
+                        place[all * blockIdx.z] = v;
+                    } else {
+                        v = *place;
+                        for (int p = 1; p < a.splits; ++p) v += place[all * p];
+#pragma unroll
+                        for (int n = 0; n < 4; ++n) acc[i][j][q * 4 + n] = v[n];
+                    }
+                }
+    if constexpr (PART == kSums) return;
     const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
     const int wr = wave / 2 * (TILE / 2), wc = wave % 2 * (TILE / 2);
     // the tile's biases; classes behind the last one have -infinity
@@ -862,10 +907,12 @@ struct Plan {
     int64_t rows, rows_p, cols_p, steps;  // most rows of a worker, padded to 256, columns to 256, 32's
     int64_t piece, pieces;     // classes at a time
     int batch;                 // workers at a time
+    int tile, cuts;            // of the logits; parts of their sum
+    int tile_g;                // of the gradients' products
     int splits;                // of the sum of dx
     int splits_w;              // and of dweight; 0: it is written as it is computed
     // offsets in a worker's part of the workspace
-    int64_t at_rows, at_parts, at_own, at_pairs, at_xz, at_wz, at_xt, at_wt, at_g, at_gt, at_sums, at_sums_w, stride;
+    int64_t at_rows, at_parts, at_own, at_pairs, at_xz, at_wz, at_xt, at_wt, at_g, at_gt, at_sums, at_sums_w, at_acc, stride;
 };
 
 // Workspace of a batch of workers: enough for a piece whose products fill the
@@ -891,18 +938,35 @@ Plan plan_of(int K, const int64_t* rows, int64_t cols, int64_t classes, int dtyp
     const int64_t all = round_up(classes, 256);
     int64_t each = p.steps * kLine * p.planes_w;
     if (backward) each += 2 * p.rows_p * (p.planes_g + p.planes_gt) + 2 * p.cols_p * p.planes_wt;
-    p.piece = std::min(all, std::max<int64_t>(1024, kRoom / each / 256 * 256));
+    // forward, what stays in the last-level cache, unless that is too few tiles
+    int64_t room = kRoom;
+    if (!backward) room = std::min(kRoom, std::max(kRoom / 16, each * 256 * (1024 / std::max<int64_t>(1, p.rows_p / 256))));
+    p.piece = std::min(all, std::max<int64_t>(1024, room / each / 256 * 256));
     p.pieces = (all + p.piece - 1) / p.piece;
     p.piece = round_up((all + p.pieces - 1) / p.pieces, 256);
+    // Tiles: the side whose tiles multiply less (of 128 a CU makes 0.72 of what it
+    // makes of 256), the smaller one where the larger would leave CUs idle; and
+    // where tiles are few their sums are cut, so that every CU has two.
+    int64_t with = 0;
+    for (int k = 0; k < K; ++k) with += rows[k] > 0;
+    with = std::max<int64_t>(1, std::min<int64_t>(with, kBatch));
+    auto tiles = [](int64_t t, int64_t down, int64_t across) { return (down + t - 1) / t * ((across + t - 1) / t); };
+    const int64_t here = std::min(p.piece, classes);
+    const int64_t large = tiles(256, here, p.rows), small = tiles(128, here, p.rows);
+    p.tile = large * with >= 256 && large * 4 * 0.72 <= small ? 256 : 128;
+    p.cuts = 1;
+    if (p.tile == 128)
+        p.cuts = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({512 / (small * with), p.steps * (p.planes_w + p.planes_x - 1) / 8, p.steps, 16})));
     if (backward) {
-        // a sum over many classes and few tiles of dx is cut, and so is one over
-        // many rows and few tiles of dweight
-        auto cut = [](int64_t tiles, int64_t steps) {
-            return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({512 / std::max<int64_t>(1, tiles), steps / 8, 32})));
-        };
-        p.splits = cut(p.rows_p / 128 * (p.cols_p / 128), p.piece / 64);
-        p.splits_w = cut(p.piece / 128 * (p.cols_p / 128), round_up(p.rows, 64) / 64);
-        if (p.splits_w == 1) p.splits_w = 0;
+        const int64_t sx = round_up(here, 64) / 32 * (p.planes_g + p.planes_wt - 1), sw = round_up(p.rows, 64) / 32 * (p.planes_gt + p.planes_xt - 1);
+        auto work = [&](int64_t t) { return tiles(t, p.rows, cols) * sx + tiles(t, here, cols) * sw; };
+        const int64_t most = tiles(256, p.rows, cols) + tiles(256, here, cols);
+        p.tile_g = most * with >= 256 && work(256) * 4 * 0.72 <= work(128) ? 256 : 128;
+        const int64_t each = std::max<int64_t>(16, work(p.tile_g) * with / (p.tile_g == 256 ? 512 : 1024));
+        p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({(sx + each - 1) / each, round_up(here, 64) / 64, 32})));
+        // (sums of dweight that are cut are written and read once more)
+        p.splits_w = static_cast<int>(std::min<int64_t>({sw / (2 * each), round_up(p.rows, 64) / 64, 32}));
+        if (p.splits_w < 2) p.splits_w = 0;
     }
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
@@ -916,6 +980,7 @@ Plan plan_of(int K, const int64_t* rows, int64_t cols, int64_t classes, int dtyp
         p.at_own = take(p.rows_p * 4);
         p.at_pairs = take((p.piece * p.pieces / kTilesPair) * p.rows_p * 8);
     }
+    if (p.cuts > 1) p.at_acc = take(p.cuts * small * 128 * 128 * 4);
     p.at_xz = take(p.steps * p.rows_p * kLine * p.planes_x);
     p.at_wz = take(p.steps * p.piece * kLine * p.planes_w);
     if (backward) {
@@ -930,15 +995,6 @@ Plan plan_of(int K, const int64_t* rows, int64_t cols, int64_t classes, int dtyp
     p.stride = round_up(at, 4096);
     p.batch = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({K, kBatch, 2 * kRoom / p.stride})));
     return p;
-}
-
-// The side of the tiles of a down x across result, of n such results: the one
-// whose tiles take fewer turns of the chip.  A CU holds one of 256 x 256 or two
-// of 128 x 128.
-int tile_for(int64_t down, int64_t across, int64_t n) {
-    auto tiles = [&](int64_t t) { return (down + t - 1) / t * ((across + t - 1) / t) * n; };
-    const int64_t large = (tiles(256) + 255) / 256 * 3, small = (tiles(128) + 511) / 512 * 2;
-    return large <= small ? 256 : 128;
 }
 
 // Runs over the sum, and each one's planes: lo hi, hi lo, hi hi.
@@ -961,13 +1017,26 @@ int64_t cross_entropy_workspace(int K, const int64_t* rows, int64_t cols, int64_
 
 namespace {
 
-template <int TILE, bool GRAD>
+template <int TILE, bool GRAD, Part PART>
 void run_logits(const LogitArgs& a, bool bf, int n, hipStream_t s) {
-    const dim3 grid(static_cast<uint32_t>(a.tiles_v) * a.tiles_r, n);
+    const dim3 grid(static_cast<uint32_t>(a.tiles_v) * a.tiles_r, n, PART == kSums ? a.splits : 1);
     if (bf)
-        loss_logit_kernel<TILE, true, GRAD><<<grid, 256, 0, s>>>(a);
+        loss_logit_kernel<TILE, true, GRAD, PART><<<grid, 256, 0, s>>>(a);
     else
-        loss_logit_kernel<TILE, false, GRAD><<<grid, 256, 0, s>>>(a);
+        loss_logit_kernel<TILE, false, GRAD, PART><<<grid, 256, 0, s>>>(a);
+}
+template <bool GRAD>
+hipError_t run_logits(const LogitArgs& a, int tile, bool bf, int n, hipStream_t s) {
+    if (tile == 256) {
+        run_logits<256, GRAD, kWhole>(a, bf, n, s);
+    } else if (a.splits == 1) {
+        run_logits<128, GRAD, kWhole>(a, bf, n, s);
+    } else {
+        run_logits<128, false, kSums>(a, bf, n, s);
+        if (hipError_t e = hipGetLastError()) return e;
+        run_logits<128, GRAD, kRest>(a, bf, n, s);
+    }
+    return hipGetLastError();
 }
 
 }  // namespace
@@ -1100,15 +1169,13 @@ hipError_t launch_cross_entropy(const LossCall& c, hipStream_t s) {
             l.planes_g = p.planes_g;
             l.planes_gt = p.planes_gt;
             l.has_dloss = has_dloss;
-            const int tile = tile_for(here, most, n);
+            const int tile = p.tile;
             l.pair_tile = v0 / tile;
             l.tiles_v = static_cast<int32_t>((here + tile - 1) / tile);
             l.tiles_r = static_cast<int32_t>((most + tile - 1) / tile);
-            if (tile == 256)
-                back ? run_logits<256, true>(l, p.bf, n, s) : run_logits<256, false>(l, p.bf, n, s);
-            else
-                back ? run_logits<128, true>(l, p.bf, n, s) : run_logits<128, false>(l, p.bf, n, s);
-            if (hipError_t e = hipGetLastError()) return e;
+            l.at_acc = p.at_acc;
+            l.splits = p.cuts;
+            if (hipError_t e = back ? run_logits<true>(l, tile, p.bf, n, s) : run_logits<false>(l, tile, p.bf, n, s)) return e;
             if (!back) {
                 if (v0 + piece < classes) continue;
                 LossArgs o{};
@@ -1153,7 +1220,7 @@ hipError_t launch_cross_entropy(const LossCall& c, hipStream_t s) {
             // both products of g: dx adds the pieces up, dweight is the piece's own
             GradArgs g{};
             GradJob &dx = g.job[0], &dw = g.job[1];
-            const int tile2 = tile_for(std::max(here, most), cols, n * (p.splits + 1));
+            const int tile2 = p.tile_g;
             const int32_t down = static_cast<int32_t>((cols + tile2 - 1) / tile2);
             dx.at_left = p.at_wt;
             dx.at_right = p.at_g;
