@@ -523,23 +523,22 @@ __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) loss_logit_kernel(co
                           static_cast<int>(min(static_cast<int64_t>(TILE), rows - r0)), from, to, a.runs, acc);
     }
     if constexpr (PART != kWhole)
+        for (int p = 0; p < (PART == kSums ? 1 : a.splits); ++p)
 #pragma unroll
-        for (int i = 0; i < kSide; ++i)
+            for (int i = 0; i < kSide; ++i)
 #pragma unroll
-            for (int j = 0; j < kSide; ++j)
+                for (int j = 0; j < kSide; ++j)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    f32x4* place = sums + ((i * kSide + j) * 4 + q) * 256;
-                    f32x4 v = {acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
-                    if constexpr (PART == kSums) {
-                        place[all * blockIdx.z] = v;
-                    } else {
-                        v = *place;
-                        for (int p = 1; p < a.splits; ++p) v += place[all * p];
+                    for (int q = 0; q < 4; ++q) {
+                        f32x4* place = sums + ((i * kSide + j) * 4 + q) * 256 + all * (PART == kSums ? static_cast<int>(blockIdx.z) : p);
+                        if constexpr (PART == kSums) {
+                            *place = {acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
+                        } else {
+                            const f32x4 v = *place;
 #pragma unroll
-                        for (int n = 0; n < 4; ++n) acc[i][j][q * 4 + n] = v[n];
+                            for (int n = 0; n < 4; ++n) acc[i][j][q * 4 + n] += v[n];
+                        }
                     }
-                }
     if constexpr (PART == kSums) return;
     const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
     const int wr = wave / 2 * (TILE / 2), wc = wave % 2 * (TILE / 2);
@@ -722,6 +721,7 @@ struct GradJob {
     int64_t at_sums, sums_stride;  // partial sums [split][row of right][column], or
     void* out[kBatch];             // (at_sums < 0) results of `bf` with rows of cols
     int64_t rows[kBatch];          // of right
+    int64_t out_ld;                // elements
     int32_t down, across, splits, steps, runs;
     int32_t padded;                // columns of the partial sums
     int32_t add;                   // to the sums that are there
@@ -733,7 +733,7 @@ struct GradJob {
 struct GradArgs {
     GradJob job[2];
     char* work;
-    int64_t stride, at_parts;
+    int64_t stride, at_rows, at_parts;
     int64_t x_rows[kBatch];
     float scale;
     int32_t cols, has_dloss;
@@ -763,11 +763,19 @@ __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) loss_grad_kernel(con
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int wr = wave / 2 * (TILE / 2), wc = wave % 2 * (TILE / 2);
     const Parts* parts = reinterpret_cast<const Parts*>(work + a.at_parts);
-    const int e = o.at_sums >= 0 ? 0 : -(exponent_of(parts->x) + kUnitBits + (a.has_dloss ? exponent_of(parts->f) - 15 : 0));
+    const int e = o.at_sums >= 0 ? 0
+                  : o.by_rows    ? -(exponent_of(parts->x) + kUnitBits + (a.has_dloss ? exponent_of(parts->f) - 15 : 0))
+                                 : -(exponent_of(parts->w) + kUnitBits);
+    const float* factors = reinterpret_cast<const float*>(work + a.at_rows) + round_up(a.x_rows[k], 256);
+    // (through LDS, in whole lines, it took longer: 2 x 7,511 classes, 206 rows of
+    // 2,585 bfloat16 112 us so and 119, 6 x 165 classes, 3,815 rows of 3,136 238
+    // and 280)
 #pragma unroll
     for (int j = 0; j < kSide; ++j) {
         const int64_t row = n0 + wc + j * 32 + lane % 32;
         if (row >= rows) continue;
+        // (dx: a row that is left out is 0, whatever the sums hold)
+        const float f = o.by_rows || o.at_sums >= 0 ? 1.0f : factors[row];
 #pragma unroll
         for (int i = 0; i < kSide; ++i)
 #pragma unroll
@@ -775,14 +783,14 @@ __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) loss_grad_kernel(con
                 const int c = m0 + wr + i * 32 + q * 8 + lane / 32 * 4;
                 f32x4 v = {acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
                 if (o.at_sums >= 0) {
-                    f32x4* to_sums = reinterpret_cast<f32x4*>(work + o.at_sums + part * o.sums_stride + (row * o.padded + c) * 4);
-                    if (o.add) v += *to_sums;
-                    *to_sums = v;
+                    f32x4* sums = reinterpret_cast<f32x4*>(work + o.at_sums + part * o.sums_stride + (row * o.padded + c) * 4);
+                    if (o.add) v += *sums;
+                    *sums = v;
                     continue;
                 }
 #pragma unroll
-                for (int x = 0; x < 4; ++x) v[x] = ldexpf(v[x], e) * a.scale;
-                const uintptr_t out = reinterpret_cast<uintptr_t>(o.out[k]) + (row * a.cols + c) * (o.bf ? 2 : 4);
+                for (int x = 0; x < 4; ++x) v[x] = f == 0.0f ? 0.0f : ldexpf(v[x], e) * (f * a.scale);
+                const uintptr_t out = reinterpret_cast<uintptr_t>(o.out[k]) + (row * o.out_ld + c) * (o.bf ? 2 : 4);
                 if (c + 4 <= a.cols) {
                     if (o.bf) {
                         typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
@@ -862,14 +870,18 @@ struct BiasArgs {
     float scale;
 };
 
-// dbias of a piece's classes: sums over the rows of f g, 32 classes a workgroup.
-__global__ void __launch_bounds__(256) loss_bias_kernel(const BiasArgs a) {
-    const int k = blockIdx.y, v = blockIdx.x * 32 + threadIdx.x / 8, piece = threadIdx.x % 8;
+// dbias of a piece's classes: sums over the rows of f g, 8 classes a workgroup,
+// whose waves take the rows 64 at a time in turn.
+__global__ void __launch_bounds__(512) loss_bias_kernel(const BiasArgs a) {
+    __shared__ float lds[8][8];
+    const int k = blockIdx.y, wave = threadIdx.x / 64, lane = threadIdx.x % 64, piece = lane % 8;
+    const int v = blockIdx.x * 8 + lane / 8;
     const char* work = a.work + k * a.stride;
     const Parts* parts = reinterpret_cast<const Parts*>(work + a.at_parts);
     const int e = -(kUnitBits + (a.has_dloss ? exponent_of(parts->f) - 15 : 0));
     float s = 0.0f;
-    for (int64_t b = 0; b < round_up(a.rows[k], 64) / 64; ++b)
+    const int64_t blocks = round_up(a.rows[k], 64) / 64;
+    for (int64_t b = wave; b < blocks; b += 8)
         for (int p = 0; p < a.planes; ++p) {
             const f16x8 h = *reinterpret_cast<const f16x8*>(work + a.at_gt + p * a.plane_gt + ((b * 2 + piece / 4) * a.padded + v) * kLine + piece % 4 * 16);
 #pragma unroll
@@ -877,7 +889,10 @@ __global__ void __launch_bounds__(256) loss_bias_kernel(const BiasArgs a) {
         }
 #pragma unroll
     for (int m = 4; m > 0; m >>= 1) s += __shfl_xor(s, m, 64);
-    if (piece || v >= a.count) return;
+    if (piece == 0) lds[wave][lane / 8] = s;
+    __syncthreads();
+    if (wave || piece || v >= a.count) return;
+    for (int w = 1; w < 8; ++w) s += lds[w][lane / 8];
     const uintptr_t out = reinterpret_cast<uintptr_t>(a.out[k]) + (a.first + v) * (a.bf ? 2 : 4);
     s = ldexpf(s, e) * a.scale;
     if (a.bf)
@@ -910,6 +925,7 @@ struct Plan {
     int tile, cuts;            // of the logits; parts of their sum
     int tile_g;                // of the gradients' products
     int splits;                // of the sum of dx
+    bool sums_dx;              // which is added up before it is rounded
     int splits_w;              // and of dweight; 0: it is written as it is computed
     // offsets in a worker's part of the workspace
     int64_t at_rows, at_parts, at_own, at_pairs, at_xz, at_wz, at_xt, at_wt, at_g, at_gt, at_sums, at_sums_w, at_acc, stride;
@@ -967,6 +983,7 @@ Plan plan_of(int K, const int64_t* rows, int64_t cols, int64_t classes, int dtyp
         // (sums of dweight that are cut are written and read once more)
         p.splits_w = static_cast<int>(std::min<int64_t>({sw / (2 * each), round_up(p.rows, 64) / 64, 32}));
         if (p.splits_w < 2) p.splits_w = 0;
+        p.sums_dx = p.splits > 1 || p.pieces > 1;
     }
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
@@ -989,7 +1006,7 @@ Plan plan_of(int K, const int64_t* rows, int64_t cols, int64_t classes, int dtyp
         p.at_wt = take(p.piece / 32 * p.cols_p * kLine * p.planes_wt);
         p.at_g = take(p.piece / 32 * p.rows_p * kLine * p.planes_g);
         p.at_gt = take(rows_k * p.piece * kLine * p.planes_gt);
-        p.at_sums = take(p.splits * p.rows_p * p.cols_p * 4);
+        if (p.sums_dx) p.at_sums = take(p.splits * p.rows_p * p.cols_p * 4);
         if (p.splits_w) p.at_sums_w = take(p.splits_w * p.piece * p.cols_p * 4);
     }
     p.stride = round_up(at, 4096);
@@ -1214,7 +1231,7 @@ hipError_t launch_cross_entropy(const LossCall& c, hipStream_t s) {
                 b.bf = dw_bf;
                 b.has_dloss = has_dloss;
                 b.scale = c.scale;
-                loss_bias_kernel<<<dim3(static_cast<uint32_t>((here + 31) / 32), n), 256, 0, s>>>(b);
+                loss_bias_kernel<<<dim3(static_cast<uint32_t>((here + 7) / 8), n), 512, 0, s>>>(b);
                 if (hipError_t e = hipGetLastError()) return e;
             }
             // both products of g: dx adds the pieces up, dweight is the piece's own
@@ -1227,7 +1244,10 @@ hipError_t launch_cross_entropy(const LossCall& c, hipStream_t s) {
             dx.left = {p.cols_p * kLine, w.plane_t, 0};
             dx.right = {p.rows_p * kLine, plane_g, 0};
             dx.runs = runs_of(p.planes_wt, p.planes_g, dx.left, dx.right);
-            dx.at_sums = p.at_sums;
+            dx.at_sums = p.sums_dx ? p.at_sums : -1;
+            dx.bf = x_bf;
+            dx.out_ld = c.dx_ld;
+            dw.out_ld = cols;
             dx.sums_stride = p.rows_p * p.cols_p * 4;
             dx.across = static_cast<int32_t>((most + tile2 - 1) / tile2);
             dx.splits = p.splits;
@@ -1246,6 +1266,7 @@ hipError_t launch_cross_entropy(const LossCall& c, hipStream_t s) {
             dw.bf = dw_bf;
             for (int i = 0; i < n; ++i) {
                 g.x_rows[i] = dx.rows[i] = c.rows[who[i]];
+                dx.out[i] = c.dx[who[i]];
                 dw.out[i] = static_cast<char*>(c.dweight[who[i]]) + v0 * cols * dwe;
                 dw.rows[i] = here;
             }
@@ -1255,6 +1276,7 @@ hipError_t launch_cross_entropy(const LossCall& c, hipStream_t s) {
             g.work = work;
             g.stride = p.stride;
             g.at_parts = p.at_parts;
+            g.at_rows = p.at_rows;
             g.scale = c.scale;
             g.cols = static_cast<int32_t>(cols);
             g.has_dloss = has_dloss;
@@ -1266,7 +1288,7 @@ hipError_t launch_cross_entropy(const LossCall& c, hipStream_t s) {
             if (hipError_t e = hipGetLastError()) return e;
             // results from the partial sums
             for (int which = 0; which < 2; ++which) {
-                if (which ? v0 + piece < classes : !p.splits_w) continue;
+                if (which ? v0 + piece < classes || !p.sums_dx : !p.splits_w) continue;
                 FinishArgs f{};
                 for (int i = 0; i < n; ++i) {
                     f.out[i] = which ? c.dx[who[i]] : dw.out[i];

@@ -165,6 +165,10 @@ struct Columns {
     }
 };
 
+// Loads stay on this side: the compiler would move them down to where they are
+// needed.
+__device__ __forceinline__ void loads_first() { asm volatile("" ::: "memory"); }
+
 // ----------------------------------------------------------------------- logits
 
 struct FewArgs {
@@ -229,7 +233,7 @@ __global__ void __launch_bounds__(W * 64) few_logit_kernel(const FewArgs a) {
     constexpr int kPitch = kS + 4;
     __shared__ __attribute__((aligned(16))) float z[W * kT * kPitch];
     __shared__ float factors[ROWS ? kS : kT];
-    const int k = blockIdx.y, tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+    const int k = blockIdx.y, tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const int64_t rows = a.rows[k];
     const int64_t n_s = ROWS ? rows : a.classes;
     const int n_t = static_cast<int>(ROWS ? a.classes : rows);
@@ -275,22 +279,32 @@ __global__ void __launch_bounds__(W * 64) few_logit_kernel(const FewArgs a) {
         const int own = lane / 16 * 8, full = cols / 32 * 32;
         auto column = [&](int n) { return n / 2 * (64 * W) + n % 2 * 32 + wave * 64; };
         const int steps = full / (64 * W) * 2 + std::clamp((full % (64 * W) - wave * 64) / 32, 0, 2);
-        int n = 0, ahead = steps > 0 ? static_cast<int>(blockIdx.x * kTurn % steps) : 0, asked = 0;
+        // (past the last step it is loaded again: were the loads left out, the
+        // counts of loads under way would differ, and all would be waited for)
+        int ahead = steps > 0 ? static_cast<int>(blockIdx.x * kTurn % steps) : 0, asked = 0;
         auto next = [&](int to) {
-            if (asked == steps) return;
             fetch(std::true_type{}, to, column(ahead) + own);
-            ++asked;
-            if (++ahead == steps) ahead = 0;
+            loads_first();
+            if (asked + 1 < steps) {
+                ++asked;
+                if (++ahead == steps) ahead = 0;
+            }
         };
+        if (steps > 0) {
 #pragma unroll
-        for (int q = 0; q < kAhead - 1; ++q) next(q);
-        while (n < steps) {
+            for (int q = 0; q < kAhead - 1; ++q) next(q);
+            for (int n = 0;;) {
+                bool more = true;
 #pragma unroll
-            for (int q = 0; q < kAhead; ++q) {
-                if (n == steps) break;
-                next((q + kAhead - 1) % kAhead);
-                step(q);
-                ++n;
+                for (int q = 0; q < kAhead; ++q) {
+                    next((q + kAhead - 1) % kAhead);
+                    step(q);
+                    if (++n == steps) {
+                        more = false;
+                        break;
+                    }
+                }
+                if (!more) break;
             }
         }
         if (column(steps) == full && full < cols) {
@@ -445,7 +459,7 @@ __global__ void __launch_bounds__(256) few_sum_kernel(const SumArgs a) {
     using Col = Columns<SB, SB && MT < 4 ? 8 : 4>;  // (with more the sums would not fit the registers)
     constexpr int kT = MT * 16, kB = Col::kBlock, kPS = SB ? 1 : PG;
     __shared__ __attribute__((aligned(16))) float lds[2][kT][kB + 4];
-    const int k = blockIdx.z, tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+    const int k = blockIdx.z, tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const int64_t rows = a.rows[k], n_s = ROWS ? rows : a.classes;
     const int n_t = static_cast<int>(ROWS ? a.classes : rows);
     const int cols = a.cols, c0 = blockIdx.x * kB, c = c0 + chunk_of(lane) * Col::kTiles;
@@ -484,6 +498,7 @@ __global__ void __launch_bounds__(256) few_sum_kernel(const SumArgs a) {
 #pragma unroll
             for (int p = 0; p < PG; ++p)
                 q.g[m].p[p] = *reinterpret_cast<const u32x4*>(g0 + p * a.plane_g + m * 16 * a.padded * 2 + step * 64);
+        loads_first();
     };
     f32x4 acc[Col::kTiles][MT] = {};
     auto use = [&](Step& q) {
@@ -495,16 +510,21 @@ __global__ void __launch_bounds__(256) few_sum_kernel(const SumArgs a) {
             for (int m = 0; m < MT; ++m) acc[t][m] = multiply(x, q.g[m], acc[t][m]);
         }
     };
+    // (past the last step it is loaded again: were the loads left out, the counts
+    // of loads under way would differ, and all would be waited for)
+    const int64_t last = to - 1 - (to - 1 - from - wave) % 4;
     int64_t at = from + wave;
-    if (at < to) fetch(st[0], at);
-    while (at < to) {
-        if (at + 4 < to) fetch(st[1], at + 4);
-        use(st[0]);
-        at += 4;
-        if (at >= to) break;
-        if (at + 4 < to) fetch(st[0], at + 4);
-        use(st[1]);
-        at += 4;
+    if (at < to) {
+        fetch(st[0], at);
+        for (;;) {
+            fetch(st[1], std::min(at + 4, last));
+            use(st[0]);
+            if (at == last) break;
+            fetch(st[0], std::min(at + 8, last));
+            use(st[1]);
+            if (at + 4 == last) break;
+            at += 8;
+        }
     }
     // the four waves' sums, two at a time
     auto place = [&](int half, int m, int e) -> float* { return &lds[half][m * 16 + lane % 16][(e * 4 + lane / 16) * Col::kTiles]; };
@@ -586,7 +606,7 @@ template <bool TB, int KS, bool ROWS, int PG>
 __global__ void __launch_bounds__(256) few_outer_kernel(const OuterArgs a) {
     using Col = Columns<TB>;
     constexpr int kSide = KS * 32, kPT = TB ? 1 : PG;
-    const int k = blockIdx.z, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+    const int k = blockIdx.z, lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int64_t rows = a.rows[k], n_s = ROWS ? rows : a.classes;
     const int n_t = static_cast<int>(ROWS ? a.classes : rows);
     const int cols = a.cols, c0 = (blockIdx.x * 4 + wave) * Col::kBlock;
@@ -629,10 +649,13 @@ __global__ void __launch_bounds__(256) few_outer_kernel(const OuterArgs a) {
         for (int h = 0; h < KS; ++h)
 #pragma unroll
             for (int p = 0; p < PG; ++p) f.b[h].p[p] = *reinterpret_cast<const u32x4*>(fg + p * a.plane_fg + s * (kSide * 2) + h * 64);
+        loads_first();
     };
-    if (first < end) fetch(now, first);
+    if (first >= end) return;
+    const int64_t last = first + (end - 1 - first) / 16 * 16;
+    fetch(now, first);
     for (int64_t s0 = first; s0 < end; s0 += 16) {
-        if (s0 + 16 < end) fetch(next, s0 + 16);
+        fetch(next, std::min(s0 + 16, last));
         f32x4 d[Col::kTiles] = {};
 #pragma unroll
         for (int q = 0; q < Col::kTiles; ++q)
