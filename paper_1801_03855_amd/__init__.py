@@ -656,33 +656,35 @@ def cross_entropy_backward_workspace(rows: Sequence[int], cols: int, classes: in
                                                              _DTYPES[dtype], _DTYPES[w_dtype], _DTYPES[dw_dtype]))
 
 
-def _matrices(ts, K: int, shape, dtypes, device: int, what: str):
-    """Device pointers of the K workers' contiguous tensors of one shape, or None."""
+def _exactly(ts, shapes, dtype: torch.dtype, device: int, what: str):
+    """Device pointers of the K workers' contiguous tensors of these shapes (one without rows needs none), or None."""
     if ts is None:
         return None
-    if len(ts) != K:
-        raise ValueError(f"need {K} tensors as {what}, got {len(ts)}")
-    for k, t in enumerate(ts):
-        if tuple(t.shape) != shape:
-            raise ValueError(f"{what}[{k}] has shape {tuple(t.shape)}, expected {shape}")
-    n = 1
-    for s in shape:
-        n *= s
-    return _ptr_array([_dev_ptr(t, n, dtypes, f"{what}[{k}]", device) for k, t in enumerate(ts)])
+    if len(ts) != len(shapes):
+        raise ValueError(f"need {len(shapes)} tensors as {what}, got {len(ts)}")
+    ptrs = []
+    for t, shape in zip(ts, shapes):
+        if t.shape != shape or t.dtype is not dtype or t.get_device() != device or not t.is_contiguous():
+            if t.shape != shape:
+                raise ValueError(f"{what}[{len(ptrs)}] has shape {tuple(t.shape)}, expected {shape}")
+            _dev_ptr(t, t.numel(), (dtype,), f"{what}[{len(ptrs)}]", device)  # says what is wrong
+        ptrs.append(t.data_ptr() if shape[0] else None)
+    return (ctypes.c_void_p * len(ptrs))(*ptrs)
 
 
 def _loss_args(xs, weights, biases, labels):
-    """(workers, row counts, columns, classes, types, device, the shared arguments' pointers)."""
+    """(row counts, as an array too, columns, classes, types, device, the rows' shapes, the shared arguments)."""
     arr, rows, cols, dt = _norm_rows(xs)
     dev = xs[0].get_device()
     if len(weights) != len(rows) or weights[0].dim() != 2:
         raise ValueError("need one [classes, columns] weight per worker")
     classes, wdt = weights[0].shape[0], _gdt(weights)
+    each = [(r,) for r in rows]
     xp, x_ld = _row_ptrs(xs, rows, cols, dt, dev, "x")
-    wp = _matrices(weights, len(rows), (classes, cols), (wdt,), dev, "weight")
-    bp = _matrices(biases, len(rows), (classes,), (wdt,), dev, "bias")
-    return arr, rows, cols, classes, dt, wdt, dev, (xp, x_ld, _DTYPES[dt], wp, bp, _DTYPES[wdt],
-                                                    _row_vectors(labels, rows, (torch.int64,), dev, "label"))
+    wp = _exactly(weights, [(classes, cols)] * len(rows), wdt, dev, "weight")
+    bp = _exactly(biases, [(classes,)] * len(rows), wdt, dev, "bias")
+    return arr, rows, cols, classes, dt, wdt, dev, each, (xp, x_ld, _DTYPES[dt], wp, bp, _DTYPES[wdt],
+                                                          _exactly(labels, each, torch.int64, dev, "label"))
 
 
 def _loss_scratch(workspace, need: int, dev: int, device, stream) -> torch.Tensor:
@@ -701,13 +703,12 @@ def cross_entropy(xs: Sequence[torch.Tensor], weights: Sequence[torch.Tensor], b
     the sums for the backward pass.  labels: int64; a row whose label is outside
     [0, classes) is left out, with a loss of 0.  The logits are never kept
     (tc_cross_entropy)."""
-    arr, rows, cols, classes, dt, wdt, dev, shared = _loss_args(xs, weights, biases, labels)
-    f32 = (torch.float32,)
-    need = lib().tc_cross_entropy_workspace(len(rows), arr, cols, classes, _DTYPES[dt], _DTYPES[wdt])
+    arr, rows, cols, classes, dt, wdt, dev, each, shared = _loss_args(xs, weights, biases, labels)
+    L = lib()
+    need = L.tc_cross_entropy_workspace(len(rows), arr, cols, classes, _DTYPES[dt], _DTYPES[wdt])
     ws = _loss_scratch(workspace, need, dev, xs[0].device, stream)
-    _check(lib().tc_cross_entropy(len(rows), arr, cols, classes, *shared, _row_vectors(losses, rows, f32, dev, "loss"),
-                                  _row_vectors(lses, rows, f32, dev, "lse"), ws.data_ptr(), ws.numel() * ws.element_size(),
-                                  _stream(stream)))
+    _check(L.tc_cross_entropy(len(rows), arr, cols, classes, *shared, _exactly(losses, each, torch.float32, dev, "loss"),
+                              _exactly(lses, each, torch.float32, dev, "lse"), ws.data_ptr(), ws.nbytes, _stream(stream)))
 
 
 def cross_entropy_backward(xs: Sequence[torch.Tensor], weights: Sequence[torch.Tensor], biases, labels, lses, dlosses,
@@ -717,17 +718,17 @@ def cross_entropy_backward(xs: Sequence[torch.Tensor], weights: Sequence[torch.T
     (None: ones): dxs[k] of worker k's rows, dweights[k] and dbiases[k] (None: not
     wanted; binary32 or bfloat16) of its weight and bias.  lses: as cross_entropy
     wrote them (tc_cross_entropy_backward)."""
-    arr, rows, cols, classes, dt, wdt, dev, shared = _loss_args(xs, weights, biases, labels)
-    f32, gdt = (torch.float32,), _gdt(dweights)
+    arr, rows, cols, classes, dt, wdt, dev, each, shared = _loss_args(xs, weights, biases, labels)
+    L, gdt = lib(), _gdt(dweights)
     dxp, dx_ld = _row_ptrs(dxs, rows, cols, dt, dev, "dx")
-    need = lib().tc_cross_entropy_backward_workspace(len(rows), arr, cols, classes, _DTYPES[dt], _DTYPES[wdt], _DTYPES[gdt])
+    need = L.tc_cross_entropy_backward_workspace(len(rows), arr, cols, classes, _DTYPES[dt], _DTYPES[wdt], _DTYPES[gdt])
     ws = _loss_scratch(workspace, need, dev, xs[0].device, stream)
-    _check(lib().tc_cross_entropy_backward(
-        len(rows), arr, cols, classes, *shared, _row_vectors(lses, rows, f32, dev, "lse"),
-        _row_vectors(dlosses, rows, f32, dev, "dloss"), float(scale), dxp, dx_ld,
-        _matrices(dweights, len(rows), (classes, cols), (gdt,), dev, "dweight"),
-        _matrices(dbiases, len(rows), (classes,), (gdt,), dev, "dbias"), _DTYPES[gdt], ws.data_ptr(),
-        ws.numel() * ws.element_size(), _stream(stream)))
+    _check(L.tc_cross_entropy_backward(
+        len(rows), arr, cols, classes, *shared, _exactly(lses, each, torch.float32, dev, "lse"),
+        _exactly(dlosses, each, torch.float32, dev, "dloss"), float(scale), dxp, dx_ld,
+        _exactly(dweights, [(classes, cols)] * len(rows), gdt, dev, "dweight"),
+        _exactly(dbiases, [(classes,)] * len(rows), gdt, dev, "dbias"), _DTYPES[gdt], ws.data_ptr(), ws.nbytes,
+        _stream(stream)))
 
 
 # ------------------------------------------------------- orthogonalised update

@@ -5,9 +5,11 @@
 // products with the short side are few.  So nothing is laid out anew.
 //
 // "Stream" is the long side (n x cols), "side" the short one (up to 64 x cols).
-//   few_logit   a workgroup takes 32 rows of the stream: the logits, with the sum
-//               over columns cut among its waves and joined in LDS; then forward
-//               what a row needs of them, backward g, stored both ways
+//   few_side    the short side as operands of the logits, in their order (not
+//               for the smallest calls)
+//   few_logit   a workgroup takes 16 or 32 rows of the stream: the logits, with
+//               the sum over columns cut among its waves and joined in LDS; then
+//               forward what a row needs of them, backward g, stored both ways
 //   few_sum     the side's gradient, g^T stream: a sum over the stream, which is
 //               read again, cut among waves and workgroups
 //   few_finish  adds the workgroups' sums up in a fixed order
@@ -39,7 +41,6 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 constexpr int kWorkers = 16;  // of one launch
 constexpr int kShort = 64;    // rows of the short side
 constexpr int kTurn = 5;      // steps from one workgroup's beginning to the next one's
-constexpr int kCt = 2;        // rows of the stream of a workgroup of the logits, in 16's
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // --------------------------------------------------------------------- operands
@@ -84,41 +85,57 @@ __device__ __forceinline__ f32x4 multiply(const Pieces<PA>& a, const Pieces<PB>&
     return c;
 }
 
+// What the rows of an operand are: binary32, bfloat16 at addresses of whole
+// words, or bfloat16 at any.
+enum Kind { kF32, kBf16, kOdd };
+
 // Eight neighbouring elements of a row as they lie, and as pieces.
-template <bool BF>
+template <Kind KIND>
 struct Eight {
-    u32x4 v[BF ? 1 : 2];
+    u32x4 v[KIND == kF32 ? 2 : 1];
+    uint32_t more;  // kOdd: the word behind
 };
-// WHOLE: they are in the row; otherwise zeros past its end.
-template <bool BF, bool WHOLE>
-__device__ __forceinline__ Eight<BF> load_eight(uintptr_t row, int c, int cols) {
-    Eight<BF> r;
-    constexpr int V = BF ? 8 : 4;
-    using T = std::conditional_t<BF, __bf16, float>;
+// WHOLE: they are in the row; otherwise zeros past its end.  (Where rows begin
+// between words, 16 bytes at such an address take more than twice the time: 48
+// rows of 2,417 over 17,610 classes 104 us, of 2,418 43.  So whole words are
+// loaded, each of which has an element of the row, and moved down.)
+template <Kind KIND, bool WHOLE>
+__device__ __forceinline__ Eight<KIND> load_eight(uintptr_t row, int c, int cols) {
+    Eight<KIND> r;
+    if constexpr (KIND == kF32) {
 #pragma unroll
-    for (int h = 0; h < (BF ? 1 : 2); ++h)
-        r.v[h] = WHOLE ? gld_u<u32x4>(row + (c / V + h) * 16) : load_vec<T, true>(row, c / V + h, cols);
+        for (int h = 0; h < 2; ++h) r.v[h] = WHOLE ? gld_u<u32x4>(row + c * 4 + h * 16) : load_vec<float, true>(row, c / 4 + h, cols);
+    } else if constexpr (KIND == kBf16 || !WHOLE) {
+        r.v[0] = WHOLE ? gld_u<u32x4>(row + c * 2) : load_vec<__bf16, true>(row, c / 8, cols);
+    } else {
+        const uintptr_t at = row + c * 2;
+        r.v[0] = gld_u<u32x4>(at & ~uintptr_t{3});
+        r.more = gld<uint32_t>((at & ~uintptr_t{3}) + 12 + (at & 2) * 2);
+    }
     return r;
 }
-template <bool BF>
-__device__ __forceinline__ Pieces<BF ? 1 : 3> pieces(const Eight<BF>& e) {
-    if constexpr (BF) {
-        return {{e.v[0]}};
-    } else {
+template <Kind KIND, bool WHOLE>
+__device__ __forceinline__ Pieces<KIND == kF32 ? 3 : 1> pieces(const Eight<KIND>& e, uintptr_t row) {
+    if constexpr (KIND == kF32) {
         float f[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(e.v[i / 4][i % 4]);
         return cut<3>(f);
+    } else if constexpr (KIND == kBf16 || !WHOLE) {
+        return {{e.v[0]}};
+    } else {
+        const uint32_t by = (row & 2) * 8;  // bits
+        Pieces<1> r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.p[0][i] = __builtin_amdgcn_alignbit(i < 3 ? e.v[0][i + 1] : e.more, e.v[0][i], by);
+        return r;
     }
 }
 
-// Lane l's 16 bytes of a block of columns: the products' results then lie so
-// that neighbouring groups of 16 lanes store neighbouring columns.
-__device__ __forceinline__ int chunk_of(int lane) { return (lane % 4) * 4 + lane % 16 / 4; }
-
 // The operands of one block of columns from eight rows: one for each of the
 // TILES columns that a lane has, 16 bytes of a row (8 of bfloat16, 4 of
-// binary32) or 8 (4 of bfloat16).
+// binary32) or 8 (4 of bfloat16).  As right operands: the results' rows are the
+// other operand's, and 16 lanes have neighbouring columns of a row.
 template <bool BF, int TILES = BF ? 8 : 4>
 struct Columns {
     static constexpr int kTiles = TILES, kBlock = 16 * TILES;  // columns of a block
@@ -184,19 +201,17 @@ struct FewArgs {
     char* work;
     int64_t stride;            // of the workspace, from worker to worker
     int64_t at_pairs, at_own;  // forward, stream of classes: (largest, sum) [row][workgroup]; the label's logit
-    int64_t at_g, plane_g;     // backward: g [piece][row of the side][row of the stream], bfloat16
-    int64_t at_fg, plane_fg;   // f g [piece][row of the stream][row of the side]
-    int64_t padded;            // rows of the stream in g
+    int64_t at_side;           // the side as operands: [32 columns][16 rows][piece][lane]
+    int64_t at_g;              // backward: g as operands: [32 rows of the stream][16 of the side][piece][lane]
+    int64_t at_fg;             // f g: [16 rows of the stream][32 of the side][piece][lane]
     int64_t at_f;              // stream of rows: their factors
     int64_t at_db;             // and partial sums of dbias [workgroup][class]
     int64_t x_ld;              // elements
     int64_t classes;
-    int32_t cols, tiles, w_bf, db_bf, has_dloss;
+    int32_t cols, tiles, w_bf, db_bf, has_dloss, backward;
     int32_t pieces_g, pieces_fg;
     float scale;
 };
-
-enum Mode { kForward, kBackward };
 
 __device__ __forceinline__ float load_any(const void* p, int64_t i, int bf) {
     const uintptr_t a = reinterpret_cast<uintptr_t>(p);
@@ -224,51 +239,91 @@ __device__ __forceinline__ void join(float& m, float& s, float m2, float s2) {
     s = a + b;
 }
 
-// SB, TB: stream and side are bfloat16.  MT: the side's rows in 16's.  ROWS: the
-// stream is the rows, the side the classes.  W: waves, among which the sum is
-// cut, 64 columns at a time.
-template <bool SB, bool TB, int MT, int W, bool ROWS, Mode MODE>
-__global__ void __launch_bounds__(W * 64) few_logit_kernel(const FewArgs a) {
-    constexpr int CT = kCt, kS = CT * 16, kT = MT * 16, kThreads = W * 64;  // rows of the stream and the side
-    constexpr int kPitch = kS + 4;
+// The side's operands of the logits: a lane's eight elements of one row, in
+// pieces, as a wave loads them; zeros where there are no rows or columns.
+template <bool TB, bool ROWS>
+__global__ void __launch_bounds__(256) few_side_kernel(const FewArgs a, int mt) {
+    constexpr int P = TB ? 1 : 3;
+    const int k = blockIdx.y, unit = blockIdx.x * 4 + threadIdx.x / 64, lane = threadIdx.x % 64;
+    const int steps = (a.cols + 31) / 32, c = unit / mt * 32 + lane / 16 * 8, t = unit % mt * 16 + lane % 16;
+    if (unit >= steps * mt) return;
+    const int64_t n_t = ROWS ? a.classes : a.rows[k];
+    const uintptr_t side = reinterpret_cast<uintptr_t>(ROWS ? a.w[k] : a.x[k]);
+    const uintptr_t row = side + t * (ROWS ? a.cols : a.x_ld) * (TB ? 2 : 4);
+    constexpr Kind kKind = TB ? kBf16 : kF32;
+    Eight<kKind> e{};
+    if (t < n_t && c < a.cols) e = load_eight<kKind, false>(row, c, a.cols);
+    const Pieces<P> p = pieces<kKind, false>(e, row);
+    u32x4* to = reinterpret_cast<u32x4*>(a.work + k * a.stride + a.at_side) + unit * (P * 64) + lane;
+#pragma unroll
+    for (int n = 0; n < P; ++n) to[n * 64] = p.p[n];
+}
+
+// STREAM, TB: what the stream's rows are, and whether the side is bfloat16.  MT,
+// CT: the side's rows, and the stream's of a workgroup, in 16's.  PRE: few_side
+// has laid out the side.  ROWS: the stream is the rows, the side the classes.
+// Eight waves; W of them have the same rows of the stream, and the sum is cut
+// among these, 64 columns at a time.
+template <Kind STREAM, bool TB, int MT, int CT, int W, bool PRE, bool ROWS>
+__global__ void __launch_bounds__(512) few_logit_kernel(const FewArgs a) {
+    constexpr int kThreads = 512, kS = CT * 16 * (8 / W), kT = MT * 16;  // rows of the stream and the side
+    constexpr int kPitch = kS + 4, PT = TB ? 1 : 3;
     __shared__ __attribute__((aligned(16))) float z[W * kT * kPitch];
     __shared__ float factors[ROWS ? kS : kT];
     const int k = blockIdx.y, tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const int64_t rows = a.rows[k];
     const int64_t n_s = ROWS ? rows : a.classes;
     const int n_t = static_cast<int>(ROWS ? a.classes : rows);
+    const int part = wave % W, group = wave / W * (CT * 16);
     const int64_t s0 = static_cast<int64_t>(blockIdx.x) * kS;
-    if (s0 >= n_s) return;
+    if (s0 >= (n_s + 63) / 64 * 64) return;
     const int cols = a.cols;
-    constexpr int se = SB ? 2 : 4, te = TB ? 2 : 4;
+    constexpr int se = STREAM == kF32 ? 4 : 2, te = TB ? 2 : 4;
     const uintptr_t stream = reinterpret_cast<uintptr_t>(ROWS ? a.x[k] : a.w[k]);
     const uintptr_t side = reinterpret_cast<uintptr_t>(ROWS ? a.w[k] : a.x[k]);
     const int64_t s_ld = (ROWS ? a.x_ld : cols) * se, t_ld = (ROWS ? cols : a.x_ld) * te;
+    char* work = a.work + k * a.stride;
     // ---- the logits
     f32x4 acc[CT][MT] = {};
     {
-        uintptr_t sp[CT], tp[MT];
+        constexpr Kind kSide = TB ? kBf16 : kF32;
+        uintptr_t sp[CT], tp[PRE ? 1 : MT];
 #pragma unroll
-        for (int i = 0; i < CT; ++i) sp[i] = stream + std::min<int64_t>(s0 + i * 16 + lane % 16, n_s - 1) * s_ld;
+        for (int i = 0; i < CT; ++i) sp[i] = stream + std::min<int64_t>(s0 + group + i * 16 + lane % 16, n_s - 1) * s_ld;
+        if constexpr (PRE)
+            tp[0] = reinterpret_cast<uintptr_t>(work + a.at_side) + lane * 16;
+        else
 #pragma unroll
-        for (int j = 0; j < MT; ++j) tp[j] = side + std::min(j * 16 + lane % 16, n_t - 1) * t_ld;
-        // steps ahead: what the registers hold
-        constexpr int kAhead = MT == 4 ? 2 : 3;
-        Eight<SB> s[kAhead][CT];
-        Eight<TB> t[kAhead][MT];
-        auto fetch = [&](auto whole, int to, int c) {
+            for (int j = 0; j < MT; ++j) tp[j] = side + std::min(j * 16 + lane % 16, n_t - 1) * t_ld;
+        constexpr int kAhead = 2;
+        struct Step {
+            Eight<STREAM> s[CT];
+            Eight<kSide> t[PRE ? 1 : MT];
+            Pieces<PT> p[PRE ? MT : 1];
+        } st[kAhead];
+        const int own = lane / 16 * 8, full = cols / 32 * 32;
+        auto fetch = [&](auto whole, Step& q, int c) {
+            constexpr bool kWhole = decltype(whole)::value;
 #pragma unroll
-            for (int i = 0; i < CT; ++i) s[to][i] = load_eight<SB, decltype(whole)::value>(sp[i], c, cols);
+            for (int i = 0; i < CT; ++i) q.s[i] = load_eight<STREAM, kWhole>(sp[i], c + own, cols);
+            if constexpr (PRE) {
 #pragma unroll
-            for (int j = 0; j < MT; ++j) t[to][j] = load_eight<TB, decltype(whole)::value>(tp[j], c, cols);
+                for (int j = 0; j < MT; ++j)
+#pragma unroll
+                    for (int p = 0; p < PT; ++p) q.p[j].p[p] = gld<u32x4>(tp[0] + ((c / 32 * MT + j) * PT + p) * 1024);
+            } else {
+#pragma unroll
+                for (int j = 0; j < MT; ++j) q.t[j] = load_eight<kSide, kWhole>(tp[j], c + own, cols);
+            }
         };
-        auto step = [&](int from) {
-            Pieces<SB ? 1 : 3> ps[CT];
+        auto step = [&](auto whole, const Step& q) {
+            constexpr bool kWhole = decltype(whole)::value;
+            Pieces<STREAM == kF32 ? 3 : 1> ps[CT];
 #pragma unroll
-            for (int i = 0; i < CT; ++i) ps[i] = pieces<SB>(s[from][i]);
+            for (int i = 0; i < CT; ++i) ps[i] = pieces<STREAM, kWhole>(q.s[i], sp[i]);
 #pragma unroll
             for (int j = 0; j < MT; ++j) {
-                const Pieces<TB ? 1 : 3> pt = pieces<TB>(t[from][j]);
+                const Pieces<PT> pt = PRE ? q.p[PRE ? j : 0] : pieces<kSide, kWhole>(q.t[PRE ? 0 : j], tp[PRE ? 0 : j]);
 #pragma unroll
                 for (int i = 0; i < CT; ++i) acc[i][j] = multiply(ps[i], pt, acc[i][j]);
             }
@@ -276,14 +331,13 @@ __global__ void __launch_bounds__(W * 64) few_logit_kernel(const FewArgs a) {
         // The wave's step n: its 64 columns of every 64 W, 32 at a time.  The
         // workgroups begin at different ones, or the rows' equal distances would
         // have all of them at the same channels of the memory at a time.
-        const int own = lane / 16 * 8, full = cols / 32 * 32;
-        auto column = [&](int n) { return n / 2 * (64 * W) + n % 2 * 32 + wave * 64; };
-        const int steps = full / (64 * W) * 2 + std::clamp((full % (64 * W) - wave * 64) / 32, 0, 2);
+        auto column = [&](int n) { return n / 2 * (64 * W) + n % 2 * 32 + part * 64; };
+        const int steps = full / (64 * W) * 2 + std::clamp((full % (64 * W) - part * 64) / 32, 0, 2);
         // (past the last step it is loaded again: were the loads left out, the
         // counts of loads under way would differ, and all would be waited for)
         int ahead = steps > 0 ? static_cast<int>(blockIdx.x * kTurn % steps) : 0, asked = 0;
-        auto next = [&](int to) {
-            fetch(std::true_type{}, to, column(ahead) + own);
+        auto next = [&](Step& to) {
+            fetch(std::true_type{}, to, column(ahead));
             loads_first();
             if (asked + 1 < steps) {
                 ++asked;
@@ -292,13 +346,13 @@ __global__ void __launch_bounds__(W * 64) few_logit_kernel(const FewArgs a) {
         };
         if (steps > 0) {
 #pragma unroll
-            for (int q = 0; q < kAhead - 1; ++q) next(q);
+            for (int q = 0; q < kAhead - 1; ++q) next(st[q]);
             for (int n = 0;;) {
                 bool more = true;
 #pragma unroll
                 for (int q = 0; q < kAhead; ++q) {
-                    next((q + kAhead - 1) % kAhead);
-                    step(q);
+                    next(st[(q + kAhead - 1) % kAhead]);
+                    step(std::true_type{}, st[q]);
                     if (++n == steps) {
                         more = false;
                         break;
@@ -308,8 +362,8 @@ __global__ void __launch_bounds__(W * 64) few_logit_kernel(const FewArgs a) {
             }
         }
         if (column(steps) == full && full < cols) {
-            fetch(std::false_type{}, 0, full + own);
-            step(0);
+            fetch(std::false_type{}, st[0], full);
+            step(std::false_type{}, st[0]);
         }
     }
     auto at_z = [&](int t, int s) -> float& { return z[t * kPitch + s]; };
@@ -317,9 +371,9 @@ __global__ void __launch_bounds__(W * 64) few_logit_kernel(const FewArgs a) {
     for (int i = 0; i < CT; ++i)
 #pragma unroll
         for (int j = 0; j < MT; ++j)
-            *reinterpret_cast<f32x4*>(z + (wave * kT + j * 16 + lane % 16) * kPitch + i * 16 + lane / 16 * 4) = acc[i][j];
+            *reinterpret_cast<f32x4*>(z + (part * kT + j * 16 + lane % 16) * kPitch + group + i * 16 + lane / 16 * 4) = acc[i][j];
     const float* dloss = a.has_dloss ? a.dloss[k] : nullptr;
-    if (MODE == kBackward && tid < (ROWS ? kS : kT)) {
+    if (a.backward && tid < (ROWS ? kS : kT)) {
         const int64_t row = ROWS ? s0 + tid : tid;
         factors[tid] = row < rows ? factor_of(a.label[k], dloss, row, a.classes) : 0.0f;
     }
@@ -336,8 +390,7 @@ __global__ void __launch_bounds__(W * 64) few_logit_kernel(const FewArgs a) {
         at_z(t, s) = q + b;
     }
     __syncthreads();
-    char* work = a.work + k * a.stride;
-    if constexpr (MODE == kForward) {
+    if (!a.backward) {
         // the largest and the sum: of a side's row over the workgroup's classes,
         // or of a stream's row over all of them
         constexpr int kRows = ROWS ? kS : kT, kOver = ROWS ? kT : kS, kLanes = kThreads / kRows < 64 ? kThreads / kRows : 64;
@@ -363,10 +416,11 @@ __global__ void __launch_bounds__(W * 64) few_logit_kernel(const FewArgs a) {
         }
     } else {
         // g, stored for the side's gradient (with the factor if its sum runs over
-        // the rows), and f g for the stream's: two elements at a time
-        auto store = [&](char* to, int64_t plane, int pieces, float g0, float g1) {
+        // the rows), and f g for the stream's: two elements at a time, as pieces
+        // 1,024 bytes from each other
+        auto store = [&](char* to, int pieces, float g0, float g1) {
             for (int n = 0; n < pieces; ++n) {
-                *reinterpret_cast<uint32_t*>(to + n * plane) = high_halves(__float_as_uint(g0), __float_as_uint(g1));
+                *reinterpret_cast<uint32_t*>(to + n * 1024) = high_halves(__float_as_uint(g0), __float_as_uint(g1));
                 g0 -= __uint_as_float(__float_as_uint(g0) & 0xffff0000u);
                 g1 -= __uint_as_float(__float_as_uint(g1) & 0xffff0000u);
             }
@@ -386,16 +440,17 @@ __global__ void __launch_bounds__(W * 64) few_logit_kernel(const FewArgs a) {
                 at_z(t, s + e) = g[e] * f;
                 if (ROWS) g[e] *= f;
             }
-            store(work + a.at_g + (t * a.padded + s0 + s) * 2, a.plane_g, a.pieces_g, g[0], g[1]);
+            const int64_t at = s0 + s;
+            store(work + a.at_g + (at / 32 * MT + t / 16) * a.pieces_g * 1024 + ((at % 32 / 8) * 16 + t % 16) * 16 + at % 8 * 2, a.pieces_g, g[0], g[1]);
         }
         if (ROWS && tid < kS && s0 + tid < rows) reinterpret_cast<float*>(work + a.at_f)[s0 + tid] = factors[tid];
         __syncthreads();
-        constexpr int kSide = MT > 2 ? 64 : 32;  // rows of the side in f g, with zeros
+        constexpr int kKs = MT > 2 ? 2 : 1, kSide = kKs * 32;  // rows of the side in f g, with zeros
         for (int n = tid; n < kS * kSide / 2; n += kThreads) {
             const int s = n / (kSide / 2), t = n % (kSide / 2) * 2;
             const bool in = t < kT;
-            store(work + a.at_fg + ((s0 + s) * kSide + t) * 2, a.plane_fg, a.pieces_fg, in ? at_z(in ? t : 0, s) : 0.0f,
-                  in ? at_z(in ? t + 1 : 0, s) : 0.0f);
+            store(work + a.at_fg + ((s0 + s) / 16 * kKs + t / 32) * a.pieces_fg * 1024 + ((t % 32 / 8) * 16 + s % 16) * 16 + t % 8 * 2,
+                  a.pieces_fg, in ? at_z(in ? t : 0, s) : 0.0f, in ? at_z(in ? t + 1 : 0, s) : 0.0f);
         }
         // dbias: sums over the rows
         if (!a.db[k]) return;
@@ -414,21 +469,21 @@ __global__ void __launch_bounds__(W * 64) few_logit_kernel(const FewArgs a) {
 }
 
 // Joins the workgroups' pairs of a row.
-__global__ void __launch_bounds__(256) few_join_kernel(const FewArgs a) {
-    __shared__ float2 lds[4];
+__global__ void __launch_bounds__(1024) few_join_kernel(const FewArgs a) {
+    __shared__ float2 lds[16];
     const int k = blockIdx.y;
     const int64_t row = blockIdx.x;
     if (row >= a.rows[k]) return;
     const char* work = a.work + k * a.stride;
     const float2* pairs = reinterpret_cast<const float2*>(work + a.at_pairs) + row * a.tiles;
     float top = -INFINITY, sum = 0.0f;
-    for (int t = threadIdx.x; t < a.tiles; t += 256) join(top, sum, pairs[t].x, pairs[t].y);
+    for (int t = threadIdx.x; t < a.tiles; t += blockDim.x) join(top, sum, pairs[t].x, pairs[t].y);
 #pragma unroll
     for (int m = 32; m > 0; m >>= 1) join(top, sum, __shfl_xor(top, m, 64), __shfl_xor(sum, m, 64));
     if (threadIdx.x % 64 == 0) lds[threadIdx.x / 64] = make_float2(top, sum);
     __syncthreads();
     if (threadIdx.x) return;
-    for (int w = 1; w < 4; ++w) join(top, sum, lds[w].x, lds[w].y);
+    for (int w = 1; w < static_cast<int>(blockDim.x / 64); ++w) join(top, sum, lds[w].x, lds[w].y);
     const float lse = top + log2f(sum) * kLn2;
     a.lse[k][row] = lse;
     const int64_t label = a.label[k][row];
@@ -445,7 +500,7 @@ struct SumArgs {
     void* db[kWorkers];
     int64_t rows[kWorkers];
     char* work;
-    int64_t stride, at_g, plane_g, padded, at_f, at_sums, sums_stride, at_db;
+    int64_t stride, at_g, at_f, at_sums, sums_stride, at_db;
     int64_t ld, out_ld;  // elements
     int64_t classes;
     int32_t cols, cols_p, splits, out_bf, db_bf, has_dloss, groups, is_rows;
@@ -462,13 +517,13 @@ __global__ void __launch_bounds__(256) few_sum_kernel(const SumArgs a) {
     const int k = blockIdx.z, tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const int64_t rows = a.rows[k], n_s = ROWS ? rows : a.classes;
     const int n_t = static_cast<int>(ROWS ? a.classes : rows);
-    const int cols = a.cols, c0 = blockIdx.x * kB, c = c0 + chunk_of(lane) * Col::kTiles;
+    const int cols = a.cols, c0 = blockIdx.x * kB, c = c0 + lane % 16 * Col::kTiles;
     const int64_t steps = (n_s + 31) / 32;  // of which this workgroup has
     const int64_t from = steps * blockIdx.y / a.splits, to = steps * (blockIdx.y + 1) / a.splits;
     char* work = a.work + k * a.stride;
     const uintptr_t stream = reinterpret_cast<uintptr_t>(a.stream[k]);
     const int64_t ld = a.ld * (SB ? 2 : 4);
-    const char* g0 = work + a.at_g + lane % 16 * a.padded * 2 + lane / 16 * 16;
+    const char* g0 = work + a.at_g + lane * 16;
     const float* f0 = reinterpret_cast<const float*>(work + a.at_f);
     struct Step {
         Col x;
@@ -497,7 +552,7 @@ __global__ void __launch_bounds__(256) few_sum_kernel(const SumArgs a) {
         for (int m = 0; m < MT; ++m)
 #pragma unroll
             for (int p = 0; p < PG; ++p)
-                q.g[m].p[p] = *reinterpret_cast<const u32x4*>(g0 + p * a.plane_g + m * 16 * a.padded * 2 + step * 64);
+                q.g[m].p[p] = *reinterpret_cast<const u32x4*>(g0 + ((step * MT + m) * PG + p) * 1024);
         loads_first();
     };
     f32x4 acc[Col::kTiles][MT] = {};
@@ -507,7 +562,7 @@ __global__ void __launch_bounds__(256) few_sum_kernel(const SumArgs a) {
         for (int t = 0; t < Col::kTiles; ++t) {
             const Pieces<kPS> x = q.x.template get<kPS>(t);
 #pragma unroll
-            for (int m = 0; m < MT; ++m) acc[t][m] = multiply(x, q.g[m], acc[t][m]);
+            for (int m = 0; m < MT; ++m) acc[t][m] = multiply(q.g[m], x, acc[t][m]);
         }
     };
     // (past the last step it is loaded again: were the loads left out, the counts
@@ -527,7 +582,7 @@ __global__ void __launch_bounds__(256) few_sum_kernel(const SumArgs a) {
         }
     }
     // the four waves' sums, two at a time
-    auto place = [&](int half, int m, int e) -> float* { return &lds[half][m * 16 + lane % 16][(e * 4 + lane / 16) * Col::kTiles]; };
+    auto place = [&](int half, int m, int e) -> float* { return &lds[half][m * 16 + lane / 16 * 4 + e][lane % 16 * Col::kTiles]; };
 #pragma unroll
     for (int turn = 0; turn < 2; ++turn) {
         if (wave / 2 == 1 - turn)
@@ -573,11 +628,18 @@ __global__ void __launch_bounds__(256) few_finish_kernel(const SumArgs a) {
         if (threadIdx.x == 0) store_any(a.db[k], t, a.db_bf, lds[0] * a.scale);
         return;
     }
-    const int c = (blockIdx.x * 256 + threadIdx.x) * 4;
-    if (c >= a.cols) return;
+    // 64 lanes of four columns; the waves take the parts in turn
+    __shared__ f32x4 sums[4][64];
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = (blockIdx.x * 64 + lane) * 4;
     const char* from = work + a.at_sums + (static_cast<int64_t>(t) * a.cols_p + c) * 4;
-    f32x4 v = *reinterpret_cast<const f32x4*>(from);
-    for (int s = 1; s < a.splits; ++s) v += *reinterpret_cast<const f32x4*>(from + s * a.sums_stride);
+    f32x4 v = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (c < a.cols)
+#pragma unroll 4
+        for (int s = wave; s < a.splits; s += 4) v += *reinterpret_cast<const f32x4*>(from + s * a.sums_stride);
+    sums[wave][lane] = v;
+    __syncthreads();
+    if (wave || c >= a.cols) return;
+    v = (v + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
     const float f = a.is_rows ? 1.0f : factor_of(a.label[k], a.has_dloss ? a.dloss[k] : nullptr, t, a.classes);
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -593,7 +655,7 @@ struct OuterArgs {
     void* out[kWorkers];
     int64_t rows[kWorkers];
     char* work;
-    int64_t stride, at_fg, plane_fg;
+    int64_t stride, at_fg;
     int64_t ld, out_ld;  // elements
     int64_t classes;
     int32_t cols, out_bf, has_dloss, chunk;  // rows of the stream of a workgroup
@@ -605,13 +667,13 @@ struct OuterArgs {
 template <bool TB, int KS, bool ROWS, int PG>
 __global__ void __launch_bounds__(256) few_outer_kernel(const OuterArgs a) {
     using Col = Columns<TB>;
-    constexpr int kSide = KS * 32, kPT = TB ? 1 : PG;
+    constexpr int kPT = TB ? 1 : PG;
     const int k = blockIdx.z, lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int64_t rows = a.rows[k], n_s = ROWS ? rows : a.classes;
     const int n_t = static_cast<int>(ROWS ? a.classes : rows);
     const int cols = a.cols, c0 = (blockIdx.x * 4 + wave) * Col::kBlock;
     if (c0 >= cols) return;
-    const int c = c0 + chunk_of(lane) * Col::kTiles;
+    const int c = c0 + lane % 16 * Col::kTiles;
     const uintptr_t side = reinterpret_cast<uintptr_t>(a.side[k]);
     const int64_t t_ld = a.ld * (TB ? 2 : 4);
     Pieces<kPT> x[KS][Col::kTiles];
@@ -639,7 +701,7 @@ __global__ void __launch_bounds__(256) few_outer_kernel(const OuterArgs a) {
 #pragma unroll
         for (int q = 0; q < Col::kTiles; ++q) x[h][q] = v.template get<kPT>(q);
     }
-    const char* fg = a.work + k * a.stride + a.at_fg + lane % 16 * (kSide * 2) + lane / 16 * 16;
+    const char* fg = a.work + k * a.stride + a.at_fg + lane * 16;
     const int64_t first = static_cast<int64_t>(blockIdx.y) * a.chunk, end = std::min<int64_t>(first + a.chunk, n_s);
     struct Factors {
         Pieces<PG> b[KS];
@@ -648,7 +710,7 @@ __global__ void __launch_bounds__(256) few_outer_kernel(const OuterArgs a) {
 #pragma unroll
         for (int h = 0; h < KS; ++h)
 #pragma unroll
-            for (int p = 0; p < PG; ++p) f.b[h].p[p] = *reinterpret_cast<const u32x4*>(fg + p * a.plane_fg + s * (kSide * 2) + h * 64);
+            for (int p = 0; p < PG; ++p) f.b[h].p[p] = *reinterpret_cast<const u32x4*>(fg + ((s / 16 * KS + h) * PG + p) * 1024);
         loads_first();
     };
     if (first >= end) return;
@@ -660,15 +722,15 @@ __global__ void __launch_bounds__(256) few_outer_kernel(const OuterArgs a) {
 #pragma unroll
         for (int q = 0; q < Col::kTiles; ++q)
 #pragma unroll
-            for (int h = 0; h < KS; ++h) d[q] = multiply(x[h][q], now.b[h], d[q]);
+            for (int h = 0; h < KS; ++h) d[q] = multiply(now.b[h], x[h][q], d[q]);
         now = next;
-        // lane: row lane % 16 of the stream, columns e * 4 + lane / 16 of 16 bytes of the side
-        const int64_t s = s0 + lane % 16;
-        if (s >= n_s) continue;
-        const uintptr_t out = reinterpret_cast<uintptr_t>(a.out[k]) + s * a.out_ld * (a.out_bf ? 2 : 4);
+        // lane: rows lane / 16 * 4 + e of the stream, its columns of the side
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const int at = c0 + (e * 4 + lane / 16) * Col::kTiles;
+            const int64_t s = s0 + lane / 16 * 4 + e;
+            if (s >= n_s) continue;
+            const uintptr_t out = reinterpret_cast<uintptr_t>(a.out[k]) + s * a.out_ld * (a.out_bf ? 2 : 4);
+            const int at = c;
             float v[8] = {};
 #pragma unroll
             for (int q = 0; q < Col::kTiles; ++q) v[q] = d[q][e] * a.scale;
@@ -696,9 +758,14 @@ __global__ void __launch_bounds__(256) few_outer_kernel(const OuterArgs a) {
 // What a call takes, from its sizes and types alone.
 struct FewPlan {
     bool rows_stream;  // the stream is the rows
-    int mt, batch, tiles, groups, splits, cols_p, blocks, pieces, pieces_fg;
-    int64_t n_s, padded, stride, at_pairs, at_own, at_g, plane_g, at_fg, plane_fg, at_f, at_db, at_sums, sums_stride;
+    bool pre;          // the side is laid out for the logits
+    int mt, ct, waves, groups, batch, tiles, splits, cols_p, blocks, pieces, pieces_fg;
+    int64_t n_s, stride, at_pairs, at_own, at_side, at_g, at_fg, at_f, at_db, at_sums, sums_stride;
 };
+
+#ifndef TC_FEW_GROUPS
+#define TC_FEW_GROUPS 256
+#endif
 
 FewPlan few_plan(int K, const int64_t* rows, int64_t cols, int64_t classes, int dtype, int w_dtype, bool backward, int dw_dtype) {
     FewPlan p{};
@@ -712,40 +779,50 @@ FewPlan few_plan(int K, const int64_t* rows, int64_t cols, int64_t classes, int 
     const int64_t n_t = p.rows_stream ? classes : most;
     p.n_s = p.rows_stream ? most : classes;
     p.mt = n_t <= 16 ? 1 : n_t <= 32 ? 2 : 4;
-    p.groups = kCt * 16;
-    p.tiles = static_cast<int>((p.n_s + p.groups - 1) / p.groups);
     p.batch = std::max(1, std::min(with, kWorkers));
+    const bool side_bf = (p.rows_stream ? w_dtype : dtype) == TC_BF16;
+    // A side of more than 32 rows (or 16, if the stream is long) is laid out: it is
+    // read by every workgroup.  (4 x 64 rows of 4,096 over 1,000 classes, the
+    // logits: 50 us as it lies, 32 + 5 laid out; 8 x 32 rows of 2,048, 20.5 and
+    // 21.7 + 5.)  Smaller calls save the launch.
+    const int64_t size = p.n_s * cols * p.batch;
+    // Of short rows (up to 256 columns) two waves cut the sum, not eight.
+    p.waves = cols <= 256 ? 2 : 8;
+    p.pre = p.waves == 8 && ((p.mt == 4 && size > (1 << 21)) || (p.mt == 2 && size > (1 << 26)));
+    // Rows of the stream of a workgroup: 64 or 32 where that leaves workgroups
+    // enough (8 rows of 4,096 over 131,072 classes: 280 us with 16, 245, 224)
+    p.ct = p.mt == 1 && (p.n_s + 63) / 64 * p.batch >= 1024 ? 4 : (p.pre || p.mt < 4) && (p.n_s + 31) / 32 * p.batch >= (p.pre ? 512 : 256) ? 2 : 1;
+    if (p.waves == 2) p.ct = 1;
+    const int64_t padded = (p.n_s + 63) / 64 * 64;
+    p.groups = p.ct * 16 * (8 / p.waves);
+    p.tiles = static_cast<int>(padded / p.groups);
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
         const int64_t here = at;
         at += (bytes + 255) / 256 * 256;
         return here;
     };
+    if (p.pre) p.at_side = take((cols + 31) / 32 * p.mt * (side_bf ? 1 : 3) * 1024);
     if (!backward) {
         if (!p.rows_stream) {
             p.at_pairs = take(n_t * p.tiles * 8);
             p.at_own = take(n_t * 4);
         }
     } else {
-        const bool side_bf = (p.rows_stream ? dw_dtype : dtype) == TC_BF16;
-        const bool stream_bf = (p.rows_stream ? dtype : w_dtype) == TC_BF16;
-        p.pieces = side_bf ? 2 : 3;
-        p.padded = (static_cast<int64_t>(p.tiles) * p.groups + 31) / 32 * 32;
-        p.plane_g = p.mt * 16 * p.padded * 2;
-        p.at_g = take(p.pieces * p.plane_g);
+        p.pieces = (p.rows_stream ? dw_dtype : dtype) == TC_BF16 ? 2 : 3;
         p.pieces_fg = (p.rows_stream ? dtype : dw_dtype) == TC_BF16 ? 2 : 3;
-        p.plane_fg = p.padded * (p.mt > 2 ? 64 : 32) * 2;
-        p.at_fg = take(p.pieces_fg * p.plane_fg);
+        p.at_g = take(padded / 32 * p.mt * p.pieces * 1024);
+        p.at_fg = take(padded / 16 * (p.mt > 2 ? 2 : 1) * p.pieces_fg * 1024);
+        const bool stream_bf = (p.rows_stream ? dtype : w_dtype) == TC_BF16;
         const int block = stream_bf && p.mt < 4 ? 128 : 64;
         p.blocks = static_cast<int>((cols + block - 1) / block);
         p.cols_p = p.blocks * block;
-        // workgroups enough to fill the chip four times, of at least 128 rows of
-        // the stream
-        p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(1024 / (p.blocks * p.batch), (p.n_s + 127) / 128)));
+        // workgroups enough to fill the chip, of at least 128 rows of the stream
+        p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(TC_FEW_GROUPS / (p.blocks * p.batch), (p.n_s + 127) / 128)));
         p.sums_stride = n_t * p.cols_p * 4;
         p.at_sums = take(p.splits * p.sums_stride);
         if (p.rows_stream) {
-            p.at_f = take(p.padded * 4);
+            p.at_f = take(padded * 4);
             p.at_db = take(static_cast<int64_t>(p.tiles) * kShort * 4);
         }
     }
@@ -753,32 +830,47 @@ FewPlan few_plan(int K, const int64_t* rows, int64_t cols, int64_t classes, int 
     return p;
 }
 
-template <bool SB, bool TB, int MT, bool ROWS>
-void run_logit(const FewArgs& a, bool backward, dim3 grid, hipStream_t s) {
-    // eight waves where the workgroups leave CUs idle
-    const bool eight = grid.x * grid.y <= 512;
-    if (eight)
-        backward ? few_logit_kernel<SB, TB, MT, 8, ROWS, kBackward><<<grid, 512, 0, s>>>(a)
-                 : few_logit_kernel<SB, TB, MT, 8, ROWS, kForward><<<grid, 512, 0, s>>>(a);
-    else
-        backward ? few_logit_kernel<SB, TB, MT, 4, ROWS, kBackward><<<grid, 256, 0, s>>>(a)
-                 : few_logit_kernel<SB, TB, MT, 4, ROWS, kForward><<<grid, 256, 0, s>>>(a);
+template <Kind STREAM, bool TB, int MT, bool ROWS>
+void run_logit(const FewArgs& a, const FewPlan& p, dim3 grid, hipStream_t s) {
+    if (p.waves == 2) {
+        few_logit_kernel<STREAM, TB, MT, 1, 2, false, ROWS><<<grid, 512, 0, s>>>(a);
+    } else if (MT > 1 && p.pre) {
+        if (p.ct == 1)
+            few_logit_kernel<STREAM, TB, MT, 1, 8, MT != 1, ROWS><<<grid, 512, 0, s>>>(a);
+        else
+            few_logit_kernel<STREAM, TB, MT, 2, 8, MT != 1, ROWS><<<grid, 512, 0, s>>>(a);
+    } else if (MT == 4 || p.ct == 1) {
+        few_logit_kernel<STREAM, TB, MT, 1, 8, false, ROWS><<<grid, 512, 0, s>>>(a);
+    } else if (MT == 1 && p.ct == 4) {
+        few_logit_kernel<STREAM, TB, MT, MT == 1 ? 4 : 1, 8, false, ROWS><<<grid, 512, 0, s>>>(a);
+    } else {
+        few_logit_kernel<STREAM, TB, MT, MT < 4 ? 2 : 1, 8, false, ROWS><<<grid, 512, 0, s>>>(a);
+    }
 }
-template <bool SB, bool TB, bool ROWS>
-void run_logit(const FewArgs& a, int mt, bool backward, dim3 grid, hipStream_t s) {
-    if (mt == 1)
-        run_logit<SB, TB, 1, ROWS>(a, backward, grid, s);
-    else if (mt == 2)
-        run_logit<SB, TB, 2, ROWS>(a, backward, grid, s);
+template <Kind STREAM, bool TB, bool ROWS>
+void run_logit(const FewArgs& a, const FewPlan& p, dim3 grid, hipStream_t s) {
+    if (p.mt == 1)
+        run_logit<STREAM, TB, 1, ROWS>(a, p, grid, s);
+    else if (p.mt == 2)
+        run_logit<STREAM, TB, 2, ROWS>(a, p, grid, s);
     else
-        run_logit<SB, TB, 4, ROWS>(a, backward, grid, s);
+        run_logit<STREAM, TB, 4, ROWS>(a, p, grid, s);
 }
-template <bool ROWS>
-void run_logit(const FewArgs& a, bool sb, bool tb, int mt, bool backward, dim3 grid, hipStream_t s) {
-    if (sb)
-        tb ? run_logit<true, true, ROWS>(a, mt, backward, grid, s) : run_logit<true, false, ROWS>(a, mt, backward, grid, s);
+template <bool TB, bool ROWS>
+hipError_t run_logit(const FewArgs& a, const FewPlan& p, Kind stream, int n, hipStream_t s) {
+    if (p.pre) {
+        const int units = (a.cols + 31) / 32 * p.mt;
+        few_side_kernel<TB, ROWS><<<dim3((units + 3) / 4, n), 256, 0, s>>>(a, p.mt);
+        if (hipError_t e = hipGetLastError()) return e;
+    }
+    const dim3 grid(p.tiles, n);
+    if (stream == kF32)
+        run_logit<kF32, TB, ROWS>(a, p, grid, s);
+    else if (stream == kBf16)
+        run_logit<kBf16, TB, ROWS>(a, p, grid, s);
     else
-        tb ? run_logit<false, true, ROWS>(a, mt, backward, grid, s) : run_logit<false, false, ROWS>(a, mt, backward, grid, s);
+        run_logit<kOdd, TB, ROWS>(a, p, grid, s);
+    return hipGetLastError();
 }
 template <bool TB, bool ROWS>
 void run_outer(const OuterArgs& a, int mt, int pieces, dim3 grid, hipStream_t s) {
@@ -844,11 +936,9 @@ hipError_t launch_few(const LossCall& c, const int* list, int count, hipStream_t
         a.stride = m.stride = o.stride = p.stride;
         a.at_pairs = p.at_pairs;
         a.at_own = p.at_own;
+        a.at_side = p.at_side;
         a.at_g = m.at_g = p.at_g;
-        a.plane_g = m.plane_g = p.plane_g;
         a.at_fg = o.at_fg = p.at_fg;
-        a.plane_fg = o.plane_fg = p.plane_fg;
-        a.padded = m.padded = p.padded;
         a.at_f = m.at_f = p.at_f;
         a.at_db = m.at_db = p.at_db;
         a.x_ld = c.x_ld;
@@ -861,11 +951,16 @@ hipError_t launch_few(const LossCall& c, const int* list, int count, hipStream_t
         a.pieces_g = p.pieces;
         a.pieces_fg = p.pieces_fg;
         a.scale = m.scale = o.scale = c.scale;
-        const dim3 grid(p.tiles, n);
-        p.rows_stream ? run_logit<true>(a, sb, tb, p.mt, c.backward, grid, s) : run_logit<false>(a, sb, tb, p.mt, c.backward, grid, s);
-        if (hipError_t e = hipGetLastError()) return e;
+        a.backward = c.backward;
+        // rows of the stream that begin between words
+        bool odd = sb && p.n_s > 1 && (p.rows_stream ? c.x_ld : c.cols) % 2;
+        for (int i = 0; sb && i < n; ++i) odd = odd || reinterpret_cast<uintptr_t>(p.rows_stream ? a.x[i] : a.w[i]) % 4;
+        const Kind stream = !sb ? kF32 : odd ? kOdd : kBf16;
+        hipError_t e = p.rows_stream ? (tb ? run_logit<true, true>(a, p, stream, n, s) : run_logit<false, true>(a, p, stream, n, s))
+                                     : (tb ? run_logit<true, false>(a, p, stream, n, s) : run_logit<false, false>(a, p, stream, n, s));
+        if (e != hipSuccess) return e;
         if (!c.backward) {
-            if (!p.rows_stream) few_join_kernel<<<dim3(static_cast<uint32_t>(p.mt * 16), n), 256, 0, s>>>(a);
+            if (!p.rows_stream) few_join_kernel<<<dim3(static_cast<uint32_t>(p.mt * 16), n), p.tiles > 512 ? 1024 : 256, 0, s>>>(a);
             if (hipError_t e = hipGetLastError()) return e;
             continue;
         }
@@ -903,7 +998,7 @@ hipError_t launch_few(const LossCall& c, const int* list, int count, hipStream_t
             tb ? run_outer<true, false>(o, p.mt, p.pieces_fg, grid3, s) : run_outer<false, false>(o, p.mt, p.pieces_fg, grid3, s);
         if (hipError_t e = hipGetLastError()) return e;
         const int64_t n_t = p.rows_stream ? c.classes : p.mt * 16;
-        few_finish_kernel<<<dim3(static_cast<uint32_t>((c.cols + 1023) / 1024 + 1), static_cast<uint32_t>(n_t), n), 256, 0, s>>>(m);
+        few_finish_kernel<<<dim3(static_cast<uint32_t>((c.cols + 255) / 256 + 1), static_cast<uint32_t>(n_t), n), 256, 0, s>>>(m);
         if (hipError_t e = hipGetLastError()) return e;
     }
     return hipSuccess;
