@@ -88,6 +88,17 @@ __device__ __forceinline__ void gst_u(uintptr_t a, V v) {
     *reinterpret_cast<TC_GLOBAL Vu*>(a) = v;
 }
 
+template <typename V>
+__device__ __forceinline__ V gld_u_nt(uintptr_t a) {
+    typedef V Vu __attribute__((aligned(1)));
+    return __builtin_nontemporal_load(reinterpret_cast<const TC_GLOBAL Vu*>(a));
+}
+template <typename V>
+__device__ __forceinline__ void gst_u_nt(uintptr_t a, V v) {
+    typedef V Vu __attribute__((aligned(1)));
+    __builtin_nontemporal_store(v, reinterpret_cast<TC_GLOBAL Vu*>(a));
+}
+
 // Workgroup w of a launch runs on XCD w % 8, and each of the 8 XCDs has its
 // own L2 cache and address-translation caches.  tile_of<R> renumbers the
 // workgroups so that, within every 8R consecutive tiles, each XCD takes R

@@ -80,13 +80,15 @@ __device__ __forceinline__ u32x4 load_vec(uintptr_t a, int v, int cols) {
 // (12,764 rows of 8,513 bfloat16, forward: 188 us by elements, 109 so; two
 // workers' 22,424 rows of 722, backward: 59 and 50).  Not for the long rows'
 // kernels, whose lanes may have stored over the elements before by then.
-template <typename T, bool EDGE>
+// NT: past the caches.
+template <typename T, bool EDGE, bool NT = false>
 __device__ __forceinline__ u32x4 load_ahead(uintptr_t a, int v, int cols) {
     constexpr int V = Lane<T>::kVec;
-    if (!EDGE || cols < V) return load_vec<T, EDGE>(a, v, cols);
+    if ((!EDGE && !NT) || cols < V) return load_vec<T, EDGE>(a, v, cols);
     const int c = v * V;
     u32x4 r = {0, 0, 0, 0};
-    if (c < cols) r = gld_u<u32x4>(a + static_cast<uintptr_t>(c + V <= cols ? c : cols - V) * sizeof(T));
+    const uintptr_t at = a + static_cast<uintptr_t>(c + V <= cols ? c : cols - V) * sizeof(T);
+    if (c < cols) r = NT ? gld_u_nt<u32x4>(at) : gld_u<u32x4>(at);
     return r;
 }
 template <typename T, bool EDGE>
@@ -101,12 +103,15 @@ __device__ __forceinline__ void settle(float* f, int v, int cols) {
             for (int e = 0; e < V; ++e) f[e] = e + m < V ? f[e + m] : 0.0f;
 }
 
-template <typename T, bool EDGE>
+template <typename T, bool EDGE, bool NT = false>
 __device__ __forceinline__ void store_vec(uintptr_t a, int v, int cols, const float* f) {
     constexpr int V = Lane<T>::kVec;
     const int left = cols - v * V;
     if (left >= V) {
-        gst_u<u32x4>(a + static_cast<uintptr_t>(v) * 16, Lane<T>::narrow(f));
+        if (NT)
+            gst_u_nt<u32x4>(a + static_cast<uintptr_t>(v) * 16, Lane<T>::narrow(f));
+        else
+            gst_u<u32x4>(a + static_cast<uintptr_t>(v) * 16, Lane<T>::narrow(f));
     } else if (EDGE) {
 #pragma unroll
         for (int i = 0; i < V; ++i)

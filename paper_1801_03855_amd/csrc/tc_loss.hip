@@ -480,6 +480,7 @@ struct LogitArgs {
     int32_t scaled;                 // operands have exponents
     int32_t w_bf;                   // of the bias
     int32_t planes_g, planes_gt, has_dloss;
+    int64_t at_db;                  // sums of f g over a wave's rows [wave][class]; -1: not wanted
     int64_t at_acc;                 // sums of a part of the columns [part][tile][register][lane]
     int32_t splits;
 };
@@ -612,6 +613,35 @@ __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) loss_logit_kernel(co
             out[r] = make_float2(top, sum);
         }
     } else {
+        if (a.at_db >= 0) {
+            // f g summed over the wave's rows: in the lane, then over 32 lanes, of which
+            // each step leaves half of the classes to either half
+            float sum[16 * kSide] = {};
+#pragma unroll
+            for (int j = 0; j < kSide; ++j) {
+                const float f = factors[std::min<int64_t>(r0 + wc + j * 32 + lane % 32, rows - 1)];
+#pragma unroll
+                for (int i = 0; i < kSide; ++i)
+#pragma unroll
+                    for (int q = 0; q < 16; ++q) sum[i * 16 + q] = acc[i][j][q] == 0.0f ? sum[i * 16 + q] : fmaf(acc[i][j][q], f, sum[i * 16 + q]);
+            }
+#pragma unroll
+            for (int m = 16; m > 0; m >>= 1) {
+                const bool upper = lane & m;
+                const int half = 8 * kSide * m / 16;
+#pragma unroll
+                for (int h = 0; h < half; ++h) {
+                    const float keep = upper ? sum[h + half] : sum[h], send = upper ? sum[h] : sum[h + half];
+                    sum[h] = keep + __shfl_xor(send, m, 64);
+                }
+            }
+            float* out = reinterpret_cast<float*>(work + a.at_db) + (at.j * 2 + wave % 2) * a.padded + v0;
+#pragma unroll
+            for (int h = 0; h < kSide / 2; ++h) {
+                const int n = lane % 32 * (kSide / 2) + h;  // i, e / 4, e % 4
+                out[wr + n / 16 * 32 + n / 4 % 4 * 8 + lane / 32 * 4 + n % 4] = sum[h];
+            }
+        }
         // g leaves through LDS, as [row][class] with 16-byte pieces turned, a
         // plane at a time, in both orders.
         constexpr int kPieces = TILE / 8;
@@ -645,23 +675,50 @@ __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) loss_logit_kernel(co
             }
             __syncthreads();
         };
+        // (a SIMD has one wave, which waits for what it reads: several at a time)
+        constexpr int kAtOnce = 8;
         auto put_g = [&](int plane) {
             char* g = work + a.at_g + plane * a.plane_g;
-            for (int n = tid; n < TILE * kPieces; n += 256) {
-                const int block = n / (TILE * 4), r = n / 4 % TILE, p = n % 4;  // of 32 classes
-                *reinterpret_cast<u32x4*>(g + ((v0 / 32 + block) * a.padded_r + r0 + r) * kLine + p * 16) =
-                    *reinterpret_cast<const u32x4*>(piece_at(r, block * 4 + p));
+            for (int n0 = tid; n0 < TILE * kPieces; n0 += 256 * kAtOnce) {
+                u32x4 h[kAtOnce];
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u) {
+                    const int n = n0 + u * 256, block = n / (TILE * 4), r = n / 4 % TILE, p = n % 4;  // of 32 classes
+                    h[u] = *reinterpret_cast<const u32x4*>(piece_at(r, block * 4 + p));
+                }
+#pragma unroll
+                for (int u = 0; u < kAtOnce; ++u) {
+                    const int n = n0 + u * 256, block = n / (TILE * 4), r = n / 4 % TILE, p = n % 4;
+                    *reinterpret_cast<u32x4*>(g + ((v0 / 32 + block) * a.padded_r + r0 + r) * kLine + p * 16) = h[u];
+                }
             }
         };
+        // two classes of eight rows
         auto put_gt = [&](int plane) {
             char* g = work + a.at_gt + plane * a.plane_gt;
-            for (int n = tid; n < TILE * kPieces; n += 256) {
-                const int block = n / (TILE * 4), v = n / 4 % TILE, p = n % 4;  // of 32 rows
-                if (r0 + block * 32 >= left_k) break;
-                u16x8 h;
+            constexpr int kPairs = kAtOnce / 2;
+            for (int n0 = tid; n0 < TILE * kPieces / 2; n0 += 256 * kPairs) {
+                uint32_t h[kPairs][8];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) h[e] = *reinterpret_cast<const uint16_t*>(piece_at(block * 32 + p * 8 + e, v / 8) + v % 8 * 2);
-                *reinterpret_cast<u16x8*>(g + ((r0 / 32 + block) * a.padded + v0 + v) * kLine + p * 16) = h;
+                for (int u = 0; u < kPairs; ++u) {
+                    const int n = n0 + u * 256, block = n / (TILE * 2), v = n / 4 % (TILE / 2) * 2, p = n % 4;  // of 32 rows
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) h[u][e] = *reinterpret_cast<const uint32_t*>(piece_at(block * 32 + p * 8 + e, v / 8) + v % 8 * 2);
+                }
+#pragma unroll
+                for (int u = 0; u < kPairs; ++u) {
+                    const int n = n0 + u * 256, block = n / (TILE * 2), v = n / 4 % (TILE / 2) * 2, p = n % 4;
+                    if (r0 + block * 32 >= left_k) continue;
+                    char* to = g + ((r0 / 32 + block) * a.padded + v0 + v) * kLine + p * 16;
+                    u32x4 first, second;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        first[i] = __builtin_amdgcn_perm(h[u][2 * i + 1], h[u][2 * i], 0x05040100u);
+                        second[i] = __builtin_amdgcn_perm(h[u][2 * i + 1], h[u][2 * i], 0x07060302u);
+                    }
+                    *reinterpret_cast<u32x4*>(to) = first;
+                    *reinterpret_cast<u32x4*>(to + kLine) = second;
+                }
             }
         };
         for (int pass = 0; pass < 4; ++pass) {
@@ -864,41 +921,26 @@ struct BiasArgs {
     void* out[kBatch];
     int64_t rows[kBatch];
     char* work;
-    int64_t stride, at_gt, plane_gt, at_parts;
-    int64_t padded, first;  // classes of the panel; first class of the piece
-    int32_t count, planes, bf, has_dloss;
+    int64_t stride, at_db;
+    int64_t padded, first;  // classes of a part; first class of the piece
+    int32_t count, tile, bf;
     float scale;
 };
 
-// dbias of a piece's classes: sums over the rows of f g, 8 classes a workgroup,
-// whose waves take the rows 64 at a time in turn.
-__global__ void __launch_bounds__(512) loss_bias_kernel(const BiasArgs a) {
-    __shared__ float lds[8][8];
-    const int k = blockIdx.y, wave = threadIdx.x / 64, lane = threadIdx.x % 64, piece = lane % 8;
-    const int v = blockIdx.x * 8 + lane / 8;
-    const char* work = a.work + k * a.stride;
-    const Parts* parts = reinterpret_cast<const Parts*>(work + a.at_parts);
-    const int e = -(kUnitBits + (a.has_dloss ? exponent_of(parts->f) - 15 : 0));
+// dbias of a piece's classes from the waves' sums, in a fixed order.
+__global__ void __launch_bounds__(256) loss_bias_kernel(const BiasArgs a) {
+    const int k = blockIdx.y, v = blockIdx.x * 256 + threadIdx.x;
+    if (v >= a.count) return;
+    const float* parts = reinterpret_cast<const float*>(a.work + k * a.stride + a.at_db) + v;
+    const int n = static_cast<int>((a.rows[k] + a.tile - 1) / a.tile * 2);
     float s = 0.0f;
-    const int64_t blocks = round_up(a.rows[k], 64) / 64;
-    for (int64_t b = wave; b < blocks; b += 8)
-        for (int p = 0; p < a.planes; ++p) {
-            const f16x8 h = *reinterpret_cast<const f16x8*>(work + a.at_gt + p * a.plane_gt + ((b * 2 + piece / 4) * a.padded + v) * kLine + piece % 4 * 16);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) s += static_cast<float>(h[i]);
-        }
-#pragma unroll
-    for (int m = 4; m > 0; m >>= 1) s += __shfl_xor(s, m, 64);
-    if (piece == 0) lds[wave][lane / 8] = s;
-    __syncthreads();
-    if (wave || piece || v >= a.count) return;
-    for (int w = 1; w < 8; ++w) s += lds[w][lane / 8];
+#pragma unroll 4
+    for (int p = 0; p < n; ++p) s += parts[p * a.padded];
     const uintptr_t out = reinterpret_cast<uintptr_t>(a.out[k]) + (a.first + v) * (a.bf ? 2 : 4);
-    s = ldexpf(s, e) * a.scale;
     if (a.bf)
-        Lane<__bf16>::put(out, s);
+        Lane<__bf16>::put(out, s * a.scale);
     else
-        Lane<float>::put(out, s);
+        Lane<float>::put(out, s * a.scale);
 }
 
 // A worker without rows has gradients of zero.
@@ -928,7 +970,7 @@ struct Plan {
     bool sums_dx;              // which is added up before it is rounded
     int splits_w;              // and of dweight; 0: it is written as it is computed
     // offsets in a worker's part of the workspace
-    int64_t at_rows, at_parts, at_own, at_pairs, at_xz, at_wz, at_xt, at_wt, at_g, at_gt, at_sums, at_sums_w, at_acc, stride;
+    int64_t at_rows, at_parts, at_own, at_pairs, at_xz, at_wz, at_xt, at_wt, at_g, at_gt, at_sums, at_sums_w, at_acc, at_db, stride;
 };
 
 // Workspace of a batch of workers: enough for a piece whose products fill the
@@ -960,16 +1002,23 @@ Plan plan_of(int K, const int64_t* rows, int64_t cols, int64_t classes, int dtyp
     p.piece = std::min(all, std::max<int64_t>(1024, room / each / 256 * 256));
     p.pieces = (all + p.piece - 1) / p.piece;
     p.piece = round_up((all + p.pieces - 1) / p.pieces, 256);
-    // Tiles: the side whose tiles multiply less (of 128 a CU makes 0.72 of what it
-    // makes of 256), the smaller one where the larger would leave CUs idle; and
-    // where tiles are few their sums are cut, so that every CU has two.
+    // Tiles of 256 or 128.  A CU makes about as much of two small ones (0.9) as of
+    // a large one, whose operands are read less often, but the padding of the
+    // sides differs; and two workgroups cover for each other's beginnings and
+    // ends, which count where sums are short (stages: 8,192 rows of 4,096 over
+    // 131,072 classes, 128 of them, 7.65 ms with 256 and 8.6 with 128; 7,158 of 307
+    // over 12,827, 20, 1,055 us and 1,020; backward, where ends are longer, 901 of
+    // 1,003 over 30,011, 64, 974 and 951).  128 also where larger ones would leave
+    // CUs idle; and where tiles are few their sums are cut, so that every CU has
+    // two.
     int64_t with = 0;
     for (int k = 0; k < K; ++k) with += rows[k] > 0;
     with = std::max<int64_t>(1, std::min<int64_t>(with, kBatch));
     auto tiles = [](int64_t t, int64_t down, int64_t across) { return (down + t - 1) / t * ((across + t - 1) / t); };
     const int64_t here = std::min(p.piece, classes);
     const int64_t large = tiles(256, here, p.rows), small = tiles(128, here, p.rows);
-    p.tile = large * with >= 256 && large * 4 * 0.72 <= small ? 256 : 128;
+    const int64_t stages = p.steps * (p.planes_w + p.planes_x - 1);
+    p.tile = large * with >= 256 && large * 4 * 0.9 <= small && stages >= (backward ? 100 : 32) ? 256 : 128;
     p.cuts = 1;
     if (p.tile == 128)
         p.cuts = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({512 / (small * with), p.steps * (p.planes_w + p.planes_x - 1) / 8, p.steps, 16})));
@@ -977,7 +1026,10 @@ Plan plan_of(int K, const int64_t* rows, int64_t cols, int64_t classes, int dtyp
         const int64_t sx = round_up(here, 64) / 32 * (p.planes_g + p.planes_wt - 1), sw = round_up(p.rows, 64) / 32 * (p.planes_gt + p.planes_xt - 1);
         auto work = [&](int64_t t) { return tiles(t, p.rows, cols) * sx + tiles(t, here, cols) * sw; };
         const int64_t most = tiles(256, p.rows, cols) + tiles(256, here, cols);
-        p.tile_g = most * with >= 256 && work(256) * 4 * 0.72 <= work(128) ? 256 : 128;
+        // (206 rows of 2,585 over 7,511 classes, 14 stages on average, 269 us with 256
+        // and 226 with 128; 531 of 1,088 over 16,853, 55, 288 and 246; 901 of 1,003
+        // over 30,011, 86, the products alone, 369 and 407)
+        p.tile_g = most * with >= 256 && work(256) >= 80 * most && work(256) * 4 * 0.9 <= work(128) ? 256 : 128;
         const int64_t each = std::max<int64_t>(16, work(p.tile_g) * with / (p.tile_g == 256 ? 512 : 1024));
         p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({(sx + each - 1) / each, round_up(here, 64) / 64, 32})));
         // (sums of dweight that are cut are written and read once more)
@@ -1002,6 +1054,7 @@ Plan plan_of(int K, const int64_t* rows, int64_t cols, int64_t classes, int dtyp
     p.at_wz = take(p.steps * p.piece * kLine * p.planes_w);
     if (backward) {
         const int64_t rows_k = round_up(p.rows, 64) / 32;
+        p.at_db = take(p.rows_p / 128 * 2 * p.piece * 4);
         p.at_xt = take(rows_k * p.cols_p * kLine * p.planes_xt);
         p.at_wt = take(p.piece / 32 * p.cols_p * kLine * p.planes_wt);
         p.at_g = take(p.piece / 32 * p.rows_p * kLine * p.planes_g);
@@ -1191,6 +1244,7 @@ hipError_t launch_cross_entropy(const LossCall& c, hipStream_t s) {
             l.tiles_v = static_cast<int32_t>((here + tile - 1) / tile);
             l.tiles_r = static_cast<int32_t>((most + tile - 1) / tile);
             l.at_acc = p.at_acc;
+            l.at_db = c.dbias ? p.at_db : -1;
             l.splits = p.cuts;
             if (hipError_t e = back ? run_logits<true>(l, tile, p.bf, n, s) : run_logits<false>(l, tile, p.bf, n, s)) return e;
             if (!back) {
@@ -1221,17 +1275,14 @@ hipError_t launch_cross_entropy(const LossCall& c, hipStream_t s) {
                 }
                 b.work = work;
                 b.stride = p.stride;
-                b.at_gt = p.at_gt;
-                b.plane_gt = plane_gt;
-                b.at_parts = p.at_parts;
+                b.at_db = p.at_db;
                 b.padded = p.piece;
                 b.first = v0;
                 b.count = l.count;
-                b.planes = p.planes_gt;
+                b.tile = tile;
                 b.bf = dw_bf;
-                b.has_dloss = has_dloss;
                 b.scale = c.scale;
-                loss_bias_kernel<<<dim3(static_cast<uint32_t>((here + 7) / 8), n), 512, 0, s>>>(b);
+                loss_bias_kernel<<<dim3(static_cast<uint32_t>((here + 255) / 256), n), 256, 0, s>>>(b);
                 if (hipError_t e = hipGetLastError()) return e;
             }
             // both products of g: dx adds the pieces up, dweight is the piece's own

@@ -791,7 +791,7 @@ FewPlan few_plan(int K, const int64_t* rows, int64_t cols, int64_t classes, int 
     p.pre = p.waves == 8 && ((p.mt == 4 && size > (1 << 21)) || (p.mt == 2 && size > (1 << 26)));
     // Rows of the stream of a workgroup: 64 or 32 where that leaves workgroups
     // enough (8 rows of 4,096 over 131,072 classes: 280 us with 16, 245, 224)
-    p.ct = p.mt == 1 && (p.n_s + 63) / 64 * p.batch >= 1024 ? 4 : (p.pre || p.mt < 4) && (p.n_s + 31) / 32 * p.batch >= (p.pre ? 512 : 256) ? 2 : 1;
+    p.ct = p.mt == 1 && (p.n_s + 63) / 64 * p.batch >= 384 ? 4 : (p.pre || p.mt < 4) && (p.n_s + 31) / 32 * p.batch >= (p.pre ? 512 : 256) ? 2 : 1;
     if (p.waves == 2) p.ct = 1;
     const int64_t padded = (p.n_s + 63) / 64 * 64;
     p.groups = p.ct * 16 * (8 / p.waves);
@@ -987,8 +987,9 @@ hipError_t launch_few(const LossCall& c, const int* list, int count, hipStream_t
         o.out_ld = p.rows_stream ? c.dx_ld : c.cols;
         o.out_bf = p.rows_stream ? x_bf : dw_bf;
         const int64_t across = (c.cols + (tb ? 512 : 256) - 1) / (tb ? 512 : 256);
-        // rows of a workgroup: 256, or as many as leave 1,024 workgroups
-        int64_t chunk = p.n_s * across * n / 1024 / 16 * 16;
+        // rows of a workgroup: 256, or as many as leave 256 workgroups (4 x 64 rows of
+        // 4,096 over 1,000 classes, all: 84 us, with 1,024 89, 2,048 93)
+        int64_t chunk = p.n_s * across * n / 256 / 16 * 16;
         o.chunk = static_cast<int32_t>(std::max<int64_t>(32, std::min<int64_t>(256, chunk)));
         if ((p.n_s + o.chunk - 1) / o.chunk > 65535) o.chunk = static_cast<int32_t>((p.n_s / 65535 + 16) / 16 * 16);
         const dim3 grid3(static_cast<uint32_t>(across), static_cast<uint32_t>((p.n_s + o.chunk - 1) / o.chunk), n);
