@@ -28,6 +28,7 @@
 // of 4,096 over 131,072 classes in bfloat16 16.5 ms.)  The summed axis is padded
 // with zeros to 64 elements.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "tc_lane.h"
@@ -503,8 +504,10 @@ enum Part { kWhole, kSums, kRest };
 template <int TILE, bool BF, bool GRAD, Part PART>
 __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) loss_logit_kernel(const LogitArgs a) {
     constexpr int kSide = TILE / 64;
-    __shared__ __attribute__((aligned(16))) char lds[kStages * 2 * TILE * kLine];
-    __shared__ __attribute__((aligned(16))) float extra[TILE + (GRAD ? 0 : 2 * TILE)];
+    // (the stages of the product; then a tile of g)
+    constexpr int kLds = kStages * 2 * TILE * kLine, kTileG = TILE * TILE * 2;
+    __shared__ __attribute__((aligned(16))) char lds[GRAD && kTileG > kLds ? kTileG : kLds];
+    float* const extra = reinterpret_cast<float*>(lds);  // after the product: biases; forward, pairs of the upper waves
     const int k = blockIdx.y;
     const int64_t rows = a.rows[k];
     // (workers with fewer rows leave the tiles behind them)
@@ -523,6 +526,28 @@ __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) loss_logit_kernel(co
         product<TILE, BF>(lds, work + a.at_w + static_cast<int64_t>(v0) * kLine, a.ws, a.count - v0, work + a.at_x + r0 * kLine, a.xs,
                           static_cast<int>(min(static_cast<int64_t>(TILE), rows - r0)), from, to, a.runs, acc);
     }
+    // What the lane's rows have, asked for at once.
+    const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+    const int wr = wave / 2 * (TILE / 2), wc = wave % 2 * (TILE / 2);
+    const int32_t* exponents = reinterpret_cast<const int32_t*>(work + a.at_rows);
+    const float* factors = reinterpret_cast<const float*>(exponents + round_up(rows, 256));
+    const Parts* parts = reinterpret_cast<const Parts*>(work + a.at_parts);
+    int64_t label[kSide];
+    float lses[kSide], factor[kSide];
+    int exponent[kSide];
+    int ew = 0;
+    auto ask = [&] {
+#pragma unroll
+        for (int j = 0; j < kSide; ++j) {
+            const int64_t row = std::min<int64_t>(r0 + wc + j * 32 + lane % 32, rows - 1);
+            label[j] = a.label[k][row];
+            lses[j] = GRAD ? a.lse[k][row] : 0.0f;
+            factor[j] = GRAD ? factors[row] : 1.0f;
+            exponent[j] = a.scaled ? exponents[row] : 0;
+        }
+        if (a.scaled) ew = exponent_of(parts->w);
+    };
+    if constexpr (PART == kRest) ask();
     if constexpr (PART != kWhole)
         for (int p = 0; p < (PART == kSums ? 1 : a.splits); ++p)
 #pragma unroll
@@ -541,26 +566,20 @@ __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) loss_logit_kernel(co
                         }
                     }
     if constexpr (PART == kSums) return;
-    const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
-    const int wr = wave / 2 * (TILE / 2), wc = wave % 2 * (TILE / 2);
+    if constexpr (PART == kWhole) ask();
     // the tile's biases; classes behind the last one have -infinity
+    __syncthreads();
     for (int v = tid; v < TILE; v += 256)
         extra[v] = v0 + v < a.count ? (a.bias[k] ? load_as(a.bias[k], a.first + v0 + v, a.w_bf) : 0.0f) : -INFINITY;
     __syncthreads();
-    const int32_t* exponents = reinterpret_cast<const int32_t*>(work + a.at_rows);
-    const float* factors = reinterpret_cast<const float*>(exponents + round_up(rows, 256));
-    const Parts* parts = reinterpret_cast<const Parts*>(work + a.at_parts);
-    const int ew = a.scaled ? exponent_of(parts->w) : 0;
 #pragma unroll
     for (int j = 0; j < kSide; ++j) {
         const int64_t row = r0 + wc + j * 32 + lane % 32;
-        const bool there = row < rows;
-        const int64_t label = there ? a.label[k][row] : -1;
         // (backward, a factor of 0 leaves a row out as well)
-        const bool counts = label >= 0 && label < a.classes && (!GRAD || factors[row] != 0.0f);
-        const int own = counts && label >= a.first + v0 && label < a.first + v0 + TILE ? static_cast<int>(label - a.first) - v0 : -1;
-        const int e = a.scaled && there ? -(ew + exponents[row]) : 0;
-        const float lse = GRAD && counts ? a.lse[k][row] : 0.0f;
+        const bool counts = row < rows && label[j] >= 0 && label[j] < a.classes && (!GRAD || factor[j] != 0.0f);
+        const int own = counts && label[j] >= a.first + v0 && label[j] < a.first + v0 + TILE ? static_cast<int>(label[j] - a.first) - v0 : -1;
+        const int e = -(ew + exponent[j]);
+        const float lse = lses[j];
         float top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < kSide; ++i)
@@ -619,7 +638,7 @@ __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) loss_logit_kernel(co
             float sum[16 * kSide] = {};
 #pragma unroll
             for (int j = 0; j < kSide; ++j) {
-                const float f = factors[std::min<int64_t>(r0 + wc + j * 32 + lane % 32, rows - 1)];
+                const float f = factor[j];
 #pragma unroll
                 for (int i = 0; i < kSide; ++i)
 #pragma unroll
@@ -656,7 +675,7 @@ __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) loss_logit_kernel(co
 #pragma unroll
             for (int j = 0; j < kSide; ++j) {
                 const int r = wc + j * 32 + lane % 32 + turn;
-                const float unit = factored ? ldexpf(factors[min(r0 + r, rows - 1)], ef + bits) : static_cast<float>(1 << kUnitBits);
+                const float unit = factored ? ldexpf(factor[j], ef + bits) : static_cast<float>(1 << kUnitBits);
 #pragma unroll
                 for (int i = 0; i < kSide; ++i)
 #pragma unroll
@@ -1019,9 +1038,11 @@ Plan plan_of(int K, const int64_t* rows, int64_t cols, int64_t classes, int dtyp
     const int64_t large = tiles(256, here, p.rows), small = tiles(128, here, p.rows);
     const int64_t stages = p.steps * (p.planes_w + p.planes_x - 1);
     p.tile = large * with >= 256 && large * 4 * 0.9 <= small && stages >= (backward ? 100 : 32) ? 256 : 128;
+    // A part's sums are 64 KB of a tile, which the rest reads at about the time of
+    // three stages: as many parts as leave both alike.
     p.cuts = 1;
     if (p.tile == 128)
-        p.cuts = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({512 / (small * with), p.steps * (p.planes_w + p.planes_x - 1) / 8, p.steps, 16})));
+        p.cuts = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>({512 / (small * with), static_cast<int64_t>(std::sqrt(0.3 * stages)), p.steps, 16})));
     if (backward) {
         const int64_t sx = round_up(here, 64) / 32 * (p.planes_g + p.planes_wt - 1), sw = round_up(p.rows, 64) / 32 * (p.planes_gt + p.planes_xt - 1);
         auto work = [&](int64_t t) { return tiles(t, p.rows, cols) * sx + tiles(t, here, cols) * sw; };
