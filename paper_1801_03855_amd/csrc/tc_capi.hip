@@ -935,6 +935,11 @@ int32_t check_loss(int32_t K, const int64_t* rows, int64_t cols, int64_t classes
     }
     for (int32_t k = 0; k < K; ++k)
         if (rows[k] > TC_MAX_CE_ROWS) { set_error("rows[%d] = %lld is more than %d", k, (long long)rows[k], TC_MAX_CE_ROWS); return TC_EINVAL; }
+    for (int32_t k = -1; k < K; ++k)
+        if ((k < 0 ? classes : rows[k]) > TC_MAX_CE_SIZE / cols) {
+            set_error(k < 0 ? "the weight has more than 2^36 elements" : "rows[%d] * cols is more than 2^36", k);
+            return TC_EINVAL;
+        }
     if (!elem_size(w_dtype)) { set_error("unknown dtype %d of weight and bias", w_dtype); return TC_EINVAL; }
     return TC_OK;
 }
