@@ -12,7 +12,8 @@
 //               forward what a row needs of them, backward g, stored both ways
 //   few_sum     the side's gradient, g^T stream: a sum over the stream, which is
 //               read again, cut among waves and workgroups
-//   few_finish  adds the workgroups' sums up in a fixed order
+//   few_finish  adds the workgroups' sums up in a fixed order, if there are more
+//               than one
 //   few_outer   the stream's gradient, g side: a sum over the short side, bound
 //               by what it writes
 //
@@ -252,7 +253,7 @@ __global__ void __launch_bounds__(256) few_side_kernel(const FewArgs a, int mt) 
     const uintptr_t row = side + t * (ROWS ? a.cols : a.x_ld) * (TB ? 2 : 4);
     constexpr Kind kKind = TB ? kBf16 : kF32;
     Eight<kKind> e{};
-    if (t < n_t && c < a.cols) e = load_eight<kKind, false>(row, c, a.cols);
+    if (t < n_t) e = c + 8 <= a.cols ? load_eight<kKind, true>(row, c, a.cols) : load_eight<kKind, false>(row, c, a.cols);
     const Pieces<P> p = pieces<kKind, false>(e, row);
     u32x4* to = reinterpret_cast<u32x4*>(a.work + k * a.stride + a.at_side) + unit * (P * 64) + lane;
 #pragma unroll
@@ -507,6 +508,14 @@ struct SumArgs {
     float scale;
 };
 
+// Four columns of the side's gradient.
+__device__ __forceinline__ void side_gradient(const SumArgs& a, int k, int t, int c, f32x4 v) {
+    const float f = a.is_rows ? 1.0f : factor_of(a.label[k], a.has_dloss ? a.dloss[k] : nullptr, t, a.classes);
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+        if (c + e < a.cols) store_any(a.out[k], t * a.out_ld + c + e, a.out_bf, f == 0.0f ? 0.0f : v[e] * (f * a.scale));
+}
+
 // A workgroup takes a block of columns and a part of the stream's rows, 32 at a
 // time a wave.
 template <bool SB, int MT, bool ROWS, int PG>
@@ -596,12 +605,14 @@ __global__ void __launch_bounds__(256) few_sum_kernel(const SumArgs a) {
                 }
         __syncthreads();
     }
-    float* out = reinterpret_cast<float*>(work + a.at_sums + blockIdx.y * a.sums_stride);
     for (int n = tid; n < kT * kB / 4; n += 256) {
         const int t = n / (kB / 4), q = n % (kB / 4) * 4;
         if (t >= n_t) break;
         const f32x4 v = *reinterpret_cast<const f32x4*>(&lds[0][t][q]) + *reinterpret_cast<const f32x4*>(&lds[1][t][q]);
-        *reinterpret_cast<f32x4*>(out + static_cast<int64_t>(t) * a.cols_p + c0 + q) = v;
+        if (a.splits > 1)
+            *reinterpret_cast<f32x4*>(work + a.at_sums + blockIdx.y * a.sums_stride + (static_cast<int64_t>(t) * a.cols_p + c0 + q) * 4) = v;
+        else
+            side_gradient(a, k, t, c0 + q, v);
     }
 }
 
@@ -628,6 +639,7 @@ __global__ void __launch_bounds__(256) few_finish_kernel(const SumArgs a) {
         if (threadIdx.x == 0) store_any(a.db[k], t, a.db_bf, lds[0] * a.scale);
         return;
     }
+    if (a.splits == 1) return;
     // 64 lanes of four columns; the waves take the parts in turn
     __shared__ f32x4 sums[4][64];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = (blockIdx.x * 64 + lane) * 4;
@@ -639,11 +651,7 @@ __global__ void __launch_bounds__(256) few_finish_kernel(const SumArgs a) {
     sums[wave][lane] = v;
     __syncthreads();
     if (wave || c >= a.cols) return;
-    v = (v + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
-    const float f = a.is_rows ? 1.0f : factor_of(a.label[k], a.has_dloss ? a.dloss[k] : nullptr, t, a.classes);
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-        if (c + e < a.cols) store_any(a.out[k], t * a.out_ld + c + e, a.out_bf, f == 0.0f ? 0.0f : v[e] * (f * a.scale));
+    side_gradient(a, k, t, c, (v + sums[1][lane]) + (sums[2][lane] + sums[3][lane]));
 }
 
 // ----------------------------------------------------------- the stream's gradient
@@ -820,7 +828,7 @@ FewPlan few_plan(int K, const int64_t* rows, int64_t cols, int64_t classes, int 
         // workgroups enough to fill the chip, of at least 128 rows of the stream
         p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(TC_FEW_GROUPS / (p.blocks * p.batch), (p.n_s + 127) / 128)));
         p.sums_stride = n_t * p.cols_p * 4;
-        p.at_sums = take(p.splits * p.sums_stride);
+        if (p.splits > 1) p.at_sums = take(p.splits * p.sums_stride);
         if (p.rows_stream) {
             p.at_f = take(padded * 4);
             p.at_db = take(static_cast<int64_t>(p.tiles) * kShort * 4);
@@ -999,6 +1007,7 @@ hipError_t launch_few(const LossCall& c, const int* list, int count, hipStream_t
             tb ? run_outer<true, false>(o, p.mt, p.pieces_fg, grid3, s) : run_outer<false, false>(o, p.mt, p.pieces_fg, grid3, s);
         if (hipError_t e = hipGetLastError()) return e;
         const int64_t n_t = p.rows_stream ? c.classes : p.mt * 16;
+        if (p.splits == 1 && !(p.rows_stream && c.dbias)) continue;
         few_finish_kernel<<<dim3(static_cast<uint32_t>((c.cols + 255) / 256 + 1), static_cast<uint32_t>(n_t), n), 256, 0, s>>>(m);
         if (hipError_t e = hipGetLastError()) return e;
     }
