@@ -40,6 +40,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef _Float16 f16x4 __attribute__((ext_vector_type(4)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint16_t u16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) char lds_char;
 typedef __attribute__((address_space(1))) const char global_char;
@@ -320,11 +321,20 @@ __device__ __forceinline__ f32x16 multiply(u32x4 a, u32x4 b, f32x16 c) {
 //
 // A SIMD has one wave (or two), so nothing but the order of the instructions
 // covers for what is not a product: every product is followed by at most one
-// read from LDS or load.
+// read from LDS or load.  8,192 rows of 4,096 over 131,072 classes in bfloat16:
+// the logits run at 1,180 TFLOP/s, their ends included, the gradients' products at
+// 1,160, the matrix cores busy 58% of the time at 1.92 GHz (the library's 8,192^3
+// product: 1,420).  With stages of 64 elements, loads and reads asked for between
+// groups of products, it was 970 and 1,125.
+//
+// Stages of tiles of 256: with two the forward pass takes 9.3 ms, with three, four
+// or five 7.6.  Of 128: with three a CU has room for three workgroups (206 rows of
+// 2,585 over 7,511 classes, backward: 204 us with four, 193).
 //
 // acc[i][j], lane l, element e: row i * 32 + e / 4 * 8 + l / 32 * 4 + e % 4 of
 // the wave's quarter of left, row j * 32 + l % 32 of its quarter of right.
-constexpr int kStages = 4;
+template <int TILE>
+constexpr int kStages = TILE == 256 ? 4 : 3;
 
 template <int TILE, bool BF>
 __device__ __forceinline__ void product(char* lds, const char* left, const Side& ls, int left_rows, const char* right,
@@ -388,7 +398,7 @@ __device__ __forceinline__ void product(char* lds, const char* left, const Side&
     auto one = [&](const Operands& f, int n) {
         acc[n / kSide][n % kSide] = multiply<BF>(f.a[n / kSide], f.b[n % kSide], acc[n / kSide][n % kSide]);
     };
-    for (int n = 0; n < kStages - 1 && n < stages; ++n) {
+    for (int n = 0; n < kStages<TILE> - 1 && n < stages; ++n) {
 #pragma unroll
         for (int q = 0; q < kAsks; ++q) load(n, q);
         advance();
@@ -398,18 +408,18 @@ __device__ __forceinline__ void product(char* lds, const char* left, const Side&
     // `full`: the stages after it are all asked for.
     auto arrive = [&](bool full) {
         if (full)
-            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kStages - 2) * kAsks) : "memory");
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"((kStages<TILE> - 2) * kAsks) : "memory");
         else
             asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
     };
-    arrive(stages >= kStages - 1);
+    arrive(stages >= kStages<TILE> - 1);
 #pragma unroll
     for (int q = 0; q < kReads; ++q) read(now, 0, 0, q);
     int buf = 0;
     for (int st = 0; st < stages; ++st) {
-        const int then = buf + 1 == kStages ? 0 : buf + 1, before = buf == 0 ? kStages - 1 : buf - 1;
+        const int then = buf + 1 == kStages<TILE> ? 0 : buf + 1, before = buf == 0 ? kStages<TILE> - 1 : buf - 1;
         const bool more = asked < stages;
         // the first 16 elements; the next 16 are read, a stage is asked for
 #pragma unroll
@@ -505,7 +515,7 @@ template <int TILE, bool BF, bool GRAD, Part PART>
 __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) loss_logit_kernel(const LogitArgs a) {
     constexpr int kSide = TILE / 64;
     // (the stages of the product; then a tile of g)
-    constexpr int kLds = kStages * 2 * TILE * kLine, kTileG = TILE * TILE * 2;
+    constexpr int kLds = kStages<TILE> * 2 * TILE * kLine, kTileG = TILE * TILE * 2;
     __shared__ __attribute__((aligned(16))) char lds[GRAD && kTileG > kLds ? kTileG : kLds];
     float* const extra = reinterpret_cast<float*>(lds);  // after the product: biases; forward, pairs of the upper waves
     const int k = blockIdx.y;
@@ -818,7 +828,7 @@ struct GradArgs {
 template <int TILE>
 __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) loss_grad_kernel(const GradArgs a) {
     constexpr int kSide = TILE / 64;
-    __shared__ __attribute__((aligned(16))) char lds[kStages * 2 * TILE * kLine];
+    __shared__ __attribute__((aligned(16))) char lds[kStages<TILE> * 2 * TILE * kLine];
     const int k = blockIdx.y;
     const bool second = static_cast<int>(blockIdx.x) >= a.job[1].first;
     const GradJob& o = a.job[second];
@@ -843,51 +853,84 @@ __global__ void __launch_bounds__(256, TILE == 256 ? 1 : 2) loss_grad_kernel(con
                   : o.by_rows    ? -(exponent_of(parts->x) + kUnitBits + (a.has_dloss ? exponent_of(parts->f) - 15 : 0))
                                  : -(exponent_of(parts->w) + kUnitBits);
     const float* factors = reinterpret_cast<const float*>(work + a.at_rows) + round_up(a.x_rows[k], 256);
-    // (through LDS, in whole lines, it took longer: 2 x 7,511 classes, 206 rows of
-    // 2,585 bfloat16 112 us so and 119, 6 x 165 classes, 3,815 rows of 3,136 238
-    // and 280)
+    if (o.at_sums >= 0) {
 #pragma unroll
-    for (int j = 0; j < kSide; ++j) {
-        const int64_t row = n0 + wc + j * 32 + lane % 32;
-        if (row >= rows) continue;
-        // (dx: a row that is left out is 0, whatever the sums hold)
-        const float f = o.by_rows || o.at_sums >= 0 ? 1.0f : factors[row];
+        for (int j = 0; j < kSide; ++j) {
+            const int64_t row = n0 + wc + j * 32 + lane % 32;
+            if (row >= rows) continue;
 #pragma unroll
-        for (int i = 0; i < kSide; ++i)
+            for (int i = 0; i < kSide; ++i)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int c = m0 + wr + i * 32 + q * 8 + lane / 32 * 4;
-                f32x4 v = {acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
-                if (o.at_sums >= 0) {
+                for (int q = 0; q < 4; ++q) {
+                    const int c = m0 + wr + i * 32 + q * 8 + lane / 32 * 4;
+                    f32x4 v = {acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
                     f32x4* sums = reinterpret_cast<f32x4*>(work + o.at_sums + part * o.sums_stride + (row * o.padded + c) * 4);
                     if (o.add) v += *sums;
                     *sums = v;
-                    continue;
                 }
+        }
+        return;
+    }
+    // The result leaves through LDS in two halves of the tile's rows, so that
+    // whole lines are stored, past the caches: a row's columns as 16-byte pieces,
+    // piece p of row r at p ^ (r % 32).  (2 x 206 rows of 2,585 over 7,511 classes,
+    // the whole gradient, 222 us from the registers, 220 so, 203 past the caches.)
+    constexpr int kHalfRows = TILE / 2, kPieces = TILE / 4, kRowsAtOnce = 256 / kPieces, kAtOnce = 8;
+    static_assert(kHalfRows * TILE * 4 <= kStages<TILE> * 2 * TILE * kLine, "half a tile fits");
+    const int tid = threadIdx.x, p = tid % kPieces, c = m0 + p * 4;
+    auto piece_at = [&](int r, int at) { return reinterpret_cast<f32x4*>(lds + (r * kPieces + (at ^ (r % 32))) * 16); };
 #pragma unroll
-                for (int x = 0; x < 4; ++x) v[x] = f == 0.0f ? 0.0f : ldexpf(v[x], e) * (f * a.scale);
+    for (int half = 0; half < 2; ++half) {
+        __syncthreads();
+        if (wave % 2 == half)
+#pragma unroll
+            for (int j = 0; j < kSide; ++j)
+#pragma unroll
+                for (int i = 0; i < kSide; ++i)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        *piece_at(j * 32 + lane % 32, (wr + i * 32 + q * 8) / 4 + lane / 32) =
+                            f32x4{acc[i][j][q * 4], acc[i][j][q * 4 + 1], acc[i][j][q * 4 + 2], acc[i][j][q * 4 + 3]};
+        __syncthreads();
+        for (int first = tid / kPieces; first < kHalfRows; first += kRowsAtOnce * kAtOnce) {
+            f32x4 v[kAtOnce];
+            float f[kAtOnce];
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+                const int64_t row = n0 + half * kHalfRows + first + u * kRowsAtOnce;
+                v[u] = *piece_at(first + u * kRowsAtOnce, p);
+                // (dx: a row that is left out is 0, whatever the sums hold)
+                f[u] = o.by_rows ? 1.0f : factors[std::min<int64_t>(row, rows - 1)];
+            }
+#pragma unroll
+            for (int u = 0; u < kAtOnce; ++u) {
+                const int64_t row = n0 + half * kHalfRows + first + u * kRowsAtOnce;
+                if (row >= rows || c >= a.cols) break;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) v[u][x] = f[u] == 0.0f ? 0.0f : ldexpf(v[u][x], e) * (f[u] * a.scale);
                 const uintptr_t out = reinterpret_cast<uintptr_t>(o.out[k]) + (row * o.out_ld + c) * (o.bf ? 2 : 4);
                 if (c + 4 <= a.cols) {
                     if (o.bf) {
                         typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
                         bf16x4 h;
 #pragma unroll
-                        for (int x = 0; x < 4; ++x) h[x] = static_cast<__bf16>(v[x]);
-                        gst_u(out, h);
+                        for (int x = 0; x < 4; ++x) h[x] = static_cast<__bf16>(v[u][x]);
+                        gst_u_nt(out, __builtin_bit_cast(u32x2, h));
                     } else {
-                        gst_u(out, v);
+                        gst_u_nt(out, v[u]);
                     }
                 } else {
 #pragma unroll
                     for (int x = 0; x < 3; ++x)
                         if (c + x < a.cols) {
                             if (o.bf)
-                                Lane<__bf16>::put(out + x * 2, v[x]);
+                                Lane<__bf16>::put(out + x * 2, v[u][x]);
                             else
-                                Lane<float>::put(out + x * 4, v[x]);
+                                Lane<float>::put(out + x * 4, v[u][x]);
                         }
                 }
             }
+        }
     }
 }
 

@@ -671,7 +671,9 @@ struct OuterArgs {
 };
 
 // A wave holds its block of columns of the side as pieces, and takes its rows of
-// the stream 16 at a time.
+// the stream 16 at a time.  Its stores pass the caches by, which hold the stream
+// (16 rows of 4,096 over 32,000 classes in bfloat16, the whole gradient: 194 us,
+// so 149; 3 x 13 rows of 4,224 over 5,426 in float 213 and 168).
 template <bool TB, int KS, bool ROWS, int PG>
 __global__ void __launch_bounds__(256) few_outer_kernel(const OuterArgs a) {
     using Col = Columns<TB>;
@@ -744,10 +746,10 @@ __global__ void __launch_bounds__(256) few_outer_kernel(const OuterArgs a) {
             for (int q = 0; q < Col::kTiles; ++q) v[q] = d[q][e] * a.scale;
             if (a.out_bf) {
                 if constexpr (TB) {
-                    store_vec<__bf16, true>(out, at / 8, cols, v);
+                    store_vec<__bf16, true, true>(out, at / 8, cols, v);
                 } else if (at + 4 <= cols) {
                     const u32x4 h = Lane<__bf16>::narrow(v);
-                    gst_u<u32x2>(out + at * 2, u32x2{h[0], h[1]});
+                    gst_u_nt(out + at * 2, u32x2{h[0], h[1]});
                 } else {
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
@@ -755,7 +757,7 @@ __global__ void __launch_bounds__(256) few_outer_kernel(const OuterArgs a) {
                 }
             } else {
 #pragma unroll
-                for (int h = 0; h < Col::kTiles / 4; ++h) store_vec<float, true>(out, at / 4 + h, cols, v + 4 * h);
+                for (int h = 0; h < Col::kTiles / 4; ++h) store_vec<float, true, true>(out, at / 4 + h, cols, v + 4 * h);
             }
         }
     }
