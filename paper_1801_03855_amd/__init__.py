@@ -687,8 +687,9 @@ def _loss_args(xs, weights, biases, labels):
                                                           _exactly(labels, each, torch.int64, dev, "label"))
 
 
-def _loss_scratch(workspace, need: int, dev: int, device, stream) -> torch.Tensor:
-    ws = _scratch(workspace, _needed(need), device, stream)
+def _loss_scratch(workspace, need, dev: int, device, stream) -> torch.Tensor:
+    # (of a workspace that is given the call itself checks the size)
+    ws = _scratch(workspace, _needed(need()) if workspace is None else 0, device, stream)
     if ws.get_device() != dev:
         raise _elsewhere(ws, dev, "the workspace")
     return ws
@@ -705,7 +706,7 @@ def cross_entropy(xs: Sequence[torch.Tensor], weights: Sequence[torch.Tensor], b
     (tc_cross_entropy)."""
     arr, rows, cols, classes, dt, wdt, dev, each, shared = _loss_args(xs, weights, biases, labels)
     L = lib()
-    need = L.tc_cross_entropy_workspace(len(rows), arr, cols, classes, _DTYPES[dt], _DTYPES[wdt])
+    need = lambda: L.tc_cross_entropy_workspace(len(rows), arr, cols, classes, _DTYPES[dt], _DTYPES[wdt])  # noqa: E731
     ws = _loss_scratch(workspace, need, dev, xs[0].device, stream)
     _check(L.tc_cross_entropy(len(rows), arr, cols, classes, *shared, _exactly(losses, each, torch.float32, dev, "loss"),
                               _exactly(lses, each, torch.float32, dev, "lse"), ws.data_ptr(), ws.nbytes, _stream(stream)))
@@ -721,7 +722,8 @@ def cross_entropy_backward(xs: Sequence[torch.Tensor], weights: Sequence[torch.T
     arr, rows, cols, classes, dt, wdt, dev, each, shared = _loss_args(xs, weights, biases, labels)
     L, gdt = lib(), _gdt(dweights)
     dxp, dx_ld = _row_ptrs(dxs, rows, cols, dt, dev, "dx")
-    need = L.tc_cross_entropy_backward_workspace(len(rows), arr, cols, classes, _DTYPES[dt], _DTYPES[wdt], _DTYPES[gdt])
+    need = lambda: L.tc_cross_entropy_backward_workspace(  # noqa: E731
+        len(rows), arr, cols, classes, _DTYPES[dt], _DTYPES[wdt], _DTYPES[gdt])
     ws = _loss_scratch(workspace, need, dev, xs[0].device, stream)
     _check(L.tc_cross_entropy_backward(
         len(rows), arr, cols, classes, *shared, _exactly(lses, each, torch.float32, dev, "lse"),
