@@ -490,9 +490,10 @@ int32_t tc_dropout_backward(int32_t K, const int64_t* rows, int64_t cols, const 
  * with each other or with what is read.  A worker without rows needs no
  * pointers.  The rows are on the current device.  cols in [1, TC_MAX_CE_COLS],
  * classes in [1, TC_MAX_CLASSES], rows[k] at most TC_MAX_CE_ROWS, rows[k] * cols
- * and classes * cols at most TC_MAX_CE_SIZE.  A row of x that is not finite makes
- * its own loss and lse NaN, an element of a weight that is not finite all of its
- * worker's.  workspace: at least tc_cross_entropy_workspace bytes of device memory, 256-byte aligned,
+ * and classes * cols at most TC_MAX_CE_SIZE.  What is not finite in a row of x
+ * reaches that row's results, in a weight all of its worker's; they are NaN
+ * unless all that it makes are logits of -infinity.  workspace: at least
+ * tc_cross_entropy_workspace bytes of device memory, 256-byte aligned,
  * that nothing else uses until the call's work is done.
  * ---------------------------------------------------------------------- */
 #define TC_MAX_CE_COLS (1 << 18)
@@ -519,14 +520,16 @@ int64_t tc_cross_entropy_backward_workspace(int32_t K, const int64_t* rows, int6
  *     dx      = f * sum over the classes of g * weight
  *     dweight = sum over the rows of f * g * x,   dbias = sum over the rows of f * g
  * (zeros for a worker without rows; dx of a row that is left out is 0, whatever
- * it holds, and so is a row's with a dloss of 0).  x, weight, bias, label as above; lse: as tc_cross_entropy wrote
- * it.  dloss: K device pointers to rows[k] binary32 values, or NULL for ones.
+ * it holds, and so is a row's with a dloss of 0).  x, weight, bias, label as
+ * above; lse: as tc_cross_entropy wrote it.  dloss: K device pointers to rows[k]
+ * binary32 values, or NULL for ones.
  * dx: rows of dtype every dx_ld elements; dx[k] may be x[k] itself (with the
  * same stride).  dweight (classes x cols), dbias: K device pointers to values
  * of dw_dtype, at any alignment of the type (pieces of a flat gradient buffer);
  * dbias NULL: not wanted.  Sums are kept in binary32, g is held with 11 bits
- * next to 1 (22 where the result it goes to is binary32) or more, and results
- * are rounded once.  The same inputs give the same bits.  workspace: at least
+ * next to 1 (22 where the result it goes to is binary32) or more, for dweight
+ * f g next to the worker's largest |f|, and results are rounded once.  The same
+ * inputs give the same bits.  workspace: at least
  * tc_cross_entropy_backward_workspace bytes, 256-byte aligned, that nothing
  * else uses until the call's work is done.  dx apart from the above, dweight,
  * dbias and the workspace share no byte with each other or with what is

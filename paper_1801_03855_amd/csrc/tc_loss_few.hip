@@ -773,10 +773,6 @@ struct FewPlan {
     int64_t n_s, stride, at_pairs, at_own, at_side, at_g, at_fg, at_f, at_db, at_sums, sums_stride;
 };
 
-#ifndef TC_FEW_GROUPS
-#define TC_FEW_GROUPS 256
-#endif
-
 FewPlan few_plan(int K, const int64_t* rows, int64_t cols, int64_t classes, int dtype, int w_dtype, bool backward, int dw_dtype) {
     FewPlan p{};
     int64_t most = 0;
@@ -828,7 +824,7 @@ FewPlan few_plan(int K, const int64_t* rows, int64_t cols, int64_t classes, int 
         p.blocks = static_cast<int>((cols + block - 1) / block);
         p.cols_p = p.blocks * block;
         // workgroups enough to fill the chip, of at least 128 rows of the stream
-        p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(TC_FEW_GROUPS / (p.blocks * p.batch), (p.n_s + 127) / 128)));
+        p.splits = static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(256 / (p.blocks * p.batch), (p.n_s + 127) / 128)));
         p.sums_stride = n_t * p.cols_p * 4;
         if (p.splits > 1) p.at_sums = take(p.splits * p.sums_stride);
         if (p.rows_stream) {
@@ -974,7 +970,6 @@ hipError_t launch_few(const LossCall& c, const int* list, int count, hipStream_t
             if (hipError_t e = hipGetLastError()) return e;
             continue;
         }
-        // the side's gradient first: the stream's may take the place of the rows
         m.at_sums = p.at_sums;
         m.sums_stride = p.sums_stride;
         m.ld = p.rows_stream ? c.x_ld : c.cols;
@@ -984,15 +979,17 @@ hipError_t launch_few(const LossCall& c, const int* list, int count, hipStream_t
         m.out_bf = p.rows_stream ? dw_bf : x_bf;
         m.groups = p.groups;
         m.is_rows = p.rows_stream;
-        const dim3 grid2(p.blocks, p.splits, n);
-        const bool three = p.pieces == 3;
-        if (p.rows_stream)
-            sb ? (three ? run_sum<true, true, 3>(m, p.mt, grid2, s) : run_sum<true, true, 2>(m, p.mt, grid2, s))
-               : (three ? run_sum<false, true, 3>(m, p.mt, grid2, s) : run_sum<false, true, 2>(m, p.mt, grid2, s));
-        else
-            sb ? (three ? run_sum<true, false, 3>(m, p.mt, grid2, s) : run_sum<true, false, 2>(m, p.mt, grid2, s))
-               : (three ? run_sum<false, false, 3>(m, p.mt, grid2, s) : run_sum<false, false, 2>(m, p.mt, grid2, s));
-        if (hipError_t e = hipGetLastError()) return e;
+        auto sum = [&] {
+            const dim3 grid(p.blocks, p.splits, n);
+            const bool three = p.pieces == 3;
+            if (p.rows_stream)
+                sb ? (three ? run_sum<true, true, 3>(m, p.mt, grid, s) : run_sum<true, true, 2>(m, p.mt, grid, s))
+                   : (three ? run_sum<false, true, 3>(m, p.mt, grid, s) : run_sum<false, true, 2>(m, p.mt, grid, s));
+            else
+                sb ? (three ? run_sum<true, false, 3>(m, p.mt, grid, s) : run_sum<true, false, 2>(m, p.mt, grid, s))
+                   : (three ? run_sum<false, false, 3>(m, p.mt, grid, s) : run_sum<false, false, 2>(m, p.mt, grid, s));
+            return hipGetLastError();
+        };
         o.ld = p.rows_stream ? c.cols : c.x_ld;
         o.out_ld = p.rows_stream ? c.dx_ld : c.cols;
         o.out_bf = p.rows_stream ? x_bf : dw_bf;
@@ -1002,12 +999,22 @@ hipError_t launch_few(const LossCall& c, const int* list, int count, hipStream_t
         int64_t chunk = p.n_s * across * n / 256 / 16 * 16;
         o.chunk = static_cast<int32_t>(std::max<int64_t>(32, std::min<int64_t>(256, chunk)));
         if ((p.n_s + o.chunk - 1) / o.chunk > 65535) o.chunk = static_cast<int32_t>((p.n_s / 65535 + 16) / 16 * 16);
-        const dim3 grid3(static_cast<uint32_t>(across), static_cast<uint32_t>((p.n_s + o.chunk - 1) / o.chunk), n);
-        if (p.rows_stream)
-            tb ? run_outer<true, true>(o, p.mt, p.pieces_fg, grid3, s) : run_outer<false, true>(o, p.mt, p.pieces_fg, grid3, s);
-        else
-            tb ? run_outer<true, false>(o, p.mt, p.pieces_fg, grid3, s) : run_outer<false, false>(o, p.mt, p.pieces_fg, grid3, s);
-        if (hipError_t e = hipGetLastError()) return e;
+        auto outer = [&] {
+            const dim3 grid(static_cast<uint32_t>(across), static_cast<uint32_t>((p.n_s + o.chunk - 1) / o.chunk), n);
+            if (p.rows_stream)
+                tb ? run_outer<true, true>(o, p.mt, p.pieces_fg, grid, s) : run_outer<false, true>(o, p.mt, p.pieces_fg, grid, s);
+            else
+                tb ? run_outer<true, false>(o, p.mt, p.pieces_fg, grid, s) : run_outer<false, false>(o, p.mt, p.pieces_fg, grid, s);
+            return hipGetLastError();
+        };
+        // dweight, which reads the rows, and then dx, which may take their place
+        if (p.rows_stream) {
+            if (hipError_t e = sum()) return e;
+            if (hipError_t e = outer()) return e;
+        } else {
+            if (hipError_t e = outer()) return e;
+            if (hipError_t e = sum()) return e;
+        }
         const int64_t n_t = p.rows_stream ? c.classes : p.mt * 16;
         if (p.splits == 1 && !(p.rows_stream && c.dbias)) continue;
         few_finish_kernel<<<dim3(static_cast<uint32_t>((c.cols + 255) / 256 + 1), static_cast<uint32_t>(n_t), n), 256, 0, s>>>(m);

@@ -367,6 +367,23 @@ def test_dx_in_the_place_of_x(rows, classes, x):
         assert torch.equal(p, q)
 
 
+@pytest.mark.parametrize("rows,cols,classes", [([9, 40], 130, 100), ([60], 136, 128), ([3, 1], 8200, 300)], ids=str)
+@pytest.mark.parametrize("x", [F32, BF16], ids=["f32", "bf16"])
+def test_dx_in_the_place_of_x_where_its_sum_is_not_cut(rows, cols, classes, x):
+    """The sum over the classes is short, or there are columns enough for the whole chip: dx is written by the kernel that
+    sums, and dweight's must have read the rows by then."""
+    c = Case(rows, cols, classes, x, x, x, bias=True, seed=17)
+    c.forward()
+    c.backward()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in c.dx + c.dw + c.db]
+    c.dx = c.x
+    c.backward()
+    torch.cuda.synchronize()
+    for p, q in zip(want, c.x + c.dw + c.db):
+        assert torch.equal(p, q)
+
+
 def test_gradients_against_differences():
     """(L(t + h d) - L(t - h d)) / 2h along a direction d.  The sum of the losses is off by at most 2^-21 of itself and the
     third derivative's part is under h^2 times the direction's size cubed."""
