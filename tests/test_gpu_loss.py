@@ -281,6 +281,44 @@ def test_few_rows_and_many_classes():
         check(Case([3, 1], 264, 40009, x, x, x, out=0.0, seed=10))
 
 
+@pytest.mark.parametrize("rows,classes", [([3 * k % 7 for k in range(19)], 90), ([k * k % 100 for k in range(19)], 70),
+                                          ([80] + [k % 4 for k in range(18)], 21)], ids=["few", "many", "few_classes"])
+def test_more_workers_than_a_launch_has(rows, classes):
+    check(Case(rows, 40, classes, bias=True, weighted=True, seed=18))
+
+
+@pytest.mark.parametrize("x", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("rows,cols,classes", [([3], 40001, 70), ([70], 40001, 70), ([70], 40001, 5), ([2], 1 << 18, 66), ([66], 1 << 18, 66)], ids=str)
+def test_long_rows(rows, cols, classes, x):
+    check(Case(rows, cols, classes, x, x, x, seed=19))
+
+
+@pytest.mark.parametrize("rows,classes", [([40], 200), ([70], 200), ([70], 30)], ids=str)
+def test_rows_far_from_each_other(rows, classes):
+    """Offsets past 32 bits, in bytes or in elements."""
+    check(Case(rows, 96, classes, BF16, BF16, BF16, pad=(1 << 26) - 96, seed=20))
+
+
+@pytest.mark.parametrize("rows", [[6], [70]], ids=str)
+def test_a_weight_of_more_than_32_bits(rows):
+    """Classes that the bias takes out, all but the first and last 500: the results are those of 1,000 classes."""
+    c = Case(rows, 4096, 1000, BF16, BF16, BF16, bias=True, seed=21)
+    V = 1_100_000
+    w, dw = torch.zeros(V, c.cols, dtype=BF16, device="cuda"), torch.full((V, c.cols), 7.0, dtype=BF16, device="cuda")
+    b, db = torch.full((V,), float("-inf"), dtype=BF16, device="cuda"), torch.full((V,), 7.0, dtype=BF16, device="cuda")
+    for big, small in ((w, c.w[0]), (b, c.b[0])):
+        big[:500], big[-500:] = small[:500], small[500:]
+    label = [torch.where(c.label[0] < 500, c.label[0], c.label[0] + (V - 1000))]
+    tc.cross_entropy(c.x, [w], [b], label, c.loss, c.lse)
+    tc.cross_entropy_backward(c.x, [w], [b], label, c.lse, None, c.dx, [dw], [db], scale=c.scale)
+    torch.cuda.synchronize()
+    for big, small in ((dw, c.dw[0]), (db, c.db[0])):
+        small[:500], small[500:] = big[:500], big[-500:]
+        assert not big[500:-500].any()
+    check_forward(c)
+    check_backward(c)
+
+
 def test_the_same_bits_and_any_stream():
     for rows, classes in (([40, 200], 1001), ([40, 20], 1001), ([400, 200], 50)):
         same_bits(Case(rows, 136, classes, BF16, F32, F32, bias=True, weighted=True, seed=11))
