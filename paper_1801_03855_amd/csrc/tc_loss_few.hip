@@ -7,9 +7,10 @@
 // "Stream" is the long side (n x cols), "side" the short one (up to 64 x cols).
 //   few_side    the short side as operands of the logits, in their order (not
 //               for the smallest calls)
-//   few_logit   a workgroup takes 16 or 32 rows of the stream: the logits, with
+//   few_logit   a workgroup takes 16 to 64 rows of the stream: the logits, with
 //               the sum over columns cut among its waves and joined in LDS; then
 //               forward what a row needs of them, backward g, stored both ways
+//   few_rest    does the latter where several workgroups share the columns
 //   few_sum     the side's gradient, g^T stream: a sum over the stream, which is
 //               read again, cut among waves and workgroups
 //   few_finish  adds the workgroups' sums up in a fixed order, if there are more
@@ -207,9 +208,10 @@ struct FewArgs {
     int64_t at_fg;             // f g: [16 rows of the stream][32 of the side][piece][lane]
     int64_t at_f;              // stream of rows: their factors
     int64_t at_db;             // and partial sums of dbias [workgroup][class]
+    int64_t at_z;              // sums over a part of the columns [part][workgroup][row of the side][of the stream]
     int64_t x_ld;              // elements
     int64_t classes;
-    int32_t cols, tiles, w_bf, db_bf, has_dloss, backward;
+    int32_t cols, tiles, cuts, w_bf, db_bf, has_dloss, backward;
     int32_t pieces_g, pieces_fg;
     float scale;
 };
@@ -260,137 +262,34 @@ __global__ void __launch_bounds__(256) few_side_kernel(const FewArgs a, int mt) 
     for (int n = 0; n < P; ++n) to[n * 64] = p.p[n];
 }
 
-// STREAM, TB: what the stream's rows are, and whether the side is bfloat16.  MT,
-// CT: the side's rows, and the stream's of a workgroup, in 16's.  PRE: few_side
-// has laid out the side.  ROWS: the stream is the rows, the side the classes.
-// Eight waves; W of them have the same rows of the stream, and the sum is cut
-// among these, 64 columns at a time.
-template <Kind STREAM, bool TB, int MT, int CT, int W, bool PRE, bool ROWS>
-__global__ void __launch_bounds__(512) few_logit_kernel(const FewArgs a) {
-    constexpr int kThreads = 512, kS = CT * 16 * (8 / W), kT = MT * 16;  // rows of the stream and the side
-    constexpr int kPitch = kS + 4, PT = TB ? 1 : 3;
-    __shared__ __attribute__((aligned(16))) float z[W * kT * kPitch];
-    __shared__ float factors[ROWS ? kS : kT];
-    const int k = blockIdx.y, tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+constexpr int kLogitThreads = 512;
+
+// The factors of the rows that a workgroup has (backward).
+template <int kS, int MT, bool ROWS>
+__device__ __forceinline__ void few_factors(const FewArgs& a, int k, int64_t s0, float* factors) {
+    constexpr int kT = MT * 16;
+    const int tid = threadIdx.x;
     const int64_t rows = a.rows[k];
-    const int64_t n_s = ROWS ? rows : a.classes;
-    const int n_t = static_cast<int>(ROWS ? a.classes : rows);
-    const int part = wave % W, group = wave / W * (CT * 16);
-    const int64_t s0 = static_cast<int64_t>(blockIdx.x) * kS;
-    if (s0 >= (n_s + 63) / 64 * 64) return;
-    const int cols = a.cols;
-    constexpr int se = STREAM == kF32 ? 4 : 2, te = TB ? 2 : 4;
-    const uintptr_t stream = reinterpret_cast<uintptr_t>(ROWS ? a.x[k] : a.w[k]);
-    const uintptr_t side = reinterpret_cast<uintptr_t>(ROWS ? a.w[k] : a.x[k]);
-    const int64_t s_ld = (ROWS ? a.x_ld : cols) * se, t_ld = (ROWS ? cols : a.x_ld) * te;
-    char* work = a.work + k * a.stride;
-    // ---- the logits
-    f32x4 acc[CT][MT] = {};
-    {
-        constexpr Kind kSide = TB ? kBf16 : kF32;
-        uintptr_t sp[CT], tp[PRE ? 1 : MT];
-#pragma unroll
-        for (int i = 0; i < CT; ++i) sp[i] = stream + std::min<int64_t>(s0 + group + i * 16 + lane % 16, n_s - 1) * s_ld;
-        if constexpr (PRE)
-            tp[0] = reinterpret_cast<uintptr_t>(work + a.at_side) + lane * 16;
-        else
-#pragma unroll
-            for (int j = 0; j < MT; ++j) tp[j] = side + std::min(j * 16 + lane % 16, n_t - 1) * t_ld;
-        constexpr int kAhead = 2;
-        struct Step {
-            Eight<STREAM> s[CT];
-            Eight<kSide> t[PRE ? 1 : MT];
-            Pieces<PT> p[PRE ? MT : 1];
-        } st[kAhead];
-        const int own = lane / 16 * 8, full = cols / 32 * 32;
-        auto fetch = [&](auto whole, Step& q, int c) {
-            constexpr bool kWhole = decltype(whole)::value;
-#pragma unroll
-            for (int i = 0; i < CT; ++i) q.s[i] = load_eight<STREAM, kWhole>(sp[i], c + own, cols);
-            if constexpr (PRE) {
-#pragma unroll
-                for (int j = 0; j < MT; ++j)
-#pragma unroll
-                    for (int p = 0; p < PT; ++p) q.p[j].p[p] = gld<u32x4>(tp[0] + ((c / 32 * MT + j) * PT + p) * 1024);
-            } else {
-#pragma unroll
-                for (int j = 0; j < MT; ++j) q.t[j] = load_eight<kSide, kWhole>(tp[j], c + own, cols);
-            }
-        };
-        auto step = [&](auto whole, const Step& q) {
-            constexpr bool kWhole = decltype(whole)::value;
-            Pieces<STREAM == kF32 ? 3 : 1> ps[CT];
-#pragma unroll
-            for (int i = 0; i < CT; ++i) ps[i] = pieces<STREAM, kWhole>(q.s[i], sp[i]);
-#pragma unroll
-            for (int j = 0; j < MT; ++j) {
-                const Pieces<PT> pt = PRE ? q.p[PRE ? j : 0] : pieces<kSide, kWhole>(q.t[PRE ? 0 : j], tp[PRE ? 0 : j]);
-#pragma unroll
-                for (int i = 0; i < CT; ++i) acc[i][j] = multiply(ps[i], pt, acc[i][j]);
-            }
-        };
-        // The wave's step n: its 64 columns of every 64 W, 32 at a time.  The
-        // workgroups begin at different ones, or the rows' equal distances would
-        // have all of them at the same channels of the memory at a time.
-        auto column = [&](int n) { return n / 2 * (64 * W) + n % 2 * 32 + part * 64; };
-        const int steps = full / (64 * W) * 2 + std::clamp((full % (64 * W) - part * 64) / 32, 0, 2);
-        // (past the last step it is loaded again: were the loads left out, the
-        // counts of loads under way would differ, and all would be waited for)
-        int ahead = steps > 0 ? static_cast<int>(blockIdx.x * kTurn % steps) : 0, asked = 0;
-        auto next = [&](Step& to) {
-            fetch(std::true_type{}, to, column(ahead));
-            loads_first();
-            if (asked + 1 < steps) {
-                ++asked;
-                if (++ahead == steps) ahead = 0;
-            }
-        };
-        if (steps > 0) {
-#pragma unroll
-            for (int q = 0; q < kAhead - 1; ++q) next(st[q]);
-            for (int n = 0;;) {
-                bool more = true;
-#pragma unroll
-                for (int q = 0; q < kAhead; ++q) {
-                    next(st[(q + kAhead - 1) % kAhead]);
-                    step(std::true_type{}, st[q]);
-                    if (++n == steps) {
-                        more = false;
-                        break;
-                    }
-                }
-                if (!more) break;
-            }
-        }
-        if (column(steps) == full && full < cols) {
-            fetch(std::false_type{}, st[0], full);
-            step(std::false_type{}, st[0]);
-        }
-    }
-    auto at_z = [&](int t, int s) -> float& { return z[t * kPitch + s]; };
-#pragma unroll
-    for (int i = 0; i < CT; ++i)
-#pragma unroll
-        for (int j = 0; j < MT; ++j)
-            *reinterpret_cast<f32x4*>(z + (part * kT + j * 16 + lane % 16) * kPitch + group + i * 16 + lane / 16 * 4) = acc[i][j];
     const float* dloss = a.has_dloss ? a.dloss[k] : nullptr;
     if (a.backward && tid < (ROWS ? kS : kT)) {
         const int64_t row = ROWS ? s0 + tid : tid;
         factors[tid] = row < rows ? factor_of(a.label[k], dloss, row, a.classes) : 0.0f;
     }
-    __syncthreads();
-    // the sum of the waves' parts, with the bias; classes that are none are -infinity
-    for (int n = tid; n < kT * kS; n += kThreads) {
-        const int t = n / kS, s = n % kS;
-        const int64_t v = ROWS ? t : s0 + s;
-        float b = v < a.classes ? 0.0f : -INFINITY;
-        if (a.bias[k] && v < a.classes) b = load_any(a.bias[k], v, a.w_bf);
-        float q = 0.0f;
-#pragma unroll
-        for (int w = 0; w < W; w += 2) q += at_z(w * kT + t, s) + at_z(w * kT + kT + t, s);
-        at_z(t, s) = q + b;
-    }
-    __syncthreads();
+}
+
+// A class's bias; classes that are none have -infinity.
+__device__ __forceinline__ float few_bias(const FewArgs& a, int k, int64_t v) {
+    return v >= a.classes ? -INFINITY : a.bias[k] ? load_any(a.bias[k], v, a.w_bf) : 0.0f;
+}
+
+// What comes of the logits z [row of the side][of the stream].
+template <int kS, int MT, bool ROWS>
+__device__ __forceinline__ void few_results(const FewArgs& a, int k, int64_t s0, float* z, const float* factors) {
+    constexpr int kThreads = kLogitThreads, kT = MT * 16, kPitch = kS + 4;
+    const int tid = threadIdx.x;
+    const int64_t rows = a.rows[k];
+    char* work = a.work + k * a.stride;
+    auto at_z = [&](int t, int s) -> float& { return z[t * kPitch + s]; };
     if (!a.backward) {
         // the largest and the sum: of a side's row over the workgroup's classes,
         // or of a stream's row over all of them
@@ -467,6 +366,164 @@ __global__ void __launch_bounds__(512) few_logit_kernel(const FewArgs a) {
             store_any(a.db[k], s0 + tid, a.db_bf, sum * a.scale);
         }
     }
+}
+
+// STREAM, TB: what the stream's rows are, and whether the side is bfloat16.  MT,
+// CT: the side's rows, and the stream's of a workgroup, in 16's.  PRE: few_side
+// has laid out the side.  ROWS: the stream is the rows, the side the classes.
+// Eight waves; W of them have the same rows of the stream, and the sum is cut
+// among these, 64 columns at a time, and among a.cuts workgroups.
+template <Kind STREAM, bool TB, int MT, int CT, int W, bool PRE, bool ROWS>
+__global__ void __launch_bounds__(kLogitThreads) few_logit_kernel(const FewArgs a) {
+    constexpr int kS = CT * 16 * (8 / W), kT = MT * 16;  // rows of the stream and the side
+    constexpr int kPitch = kS + 4, PT = TB ? 1 : 3;
+    __shared__ __attribute__((aligned(16))) float z[W * kT * kPitch];
+    __shared__ float factors[ROWS ? kS : kT];
+    const int k = blockIdx.y, tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+    const int64_t rows = a.rows[k];
+    const int64_t n_s = ROWS ? rows : a.classes;
+    const int n_t = static_cast<int>(ROWS ? a.classes : rows);
+    const int part = wave % W, group = wave / W * (CT * 16);
+    // with the other workgroups of the same rows
+    const int parts = W * a.cuts, own_part = static_cast<int>(blockIdx.z) * W + part;
+    const int64_t s0 = static_cast<int64_t>(blockIdx.x) * kS;
+    if (s0 >= (n_s + 63) / 64 * 64) return;
+    const int cols = a.cols;
+    constexpr int se = STREAM == kF32 ? 4 : 2, te = TB ? 2 : 4;
+    const uintptr_t stream = reinterpret_cast<uintptr_t>(ROWS ? a.x[k] : a.w[k]);
+    const uintptr_t side = reinterpret_cast<uintptr_t>(ROWS ? a.w[k] : a.x[k]);
+    const int64_t s_ld = (ROWS ? a.x_ld : cols) * se, t_ld = (ROWS ? cols : a.x_ld) * te;
+    char* work = a.work + k * a.stride;
+    // ---- the logits
+    f32x4 acc[CT][MT] = {};
+    {
+        constexpr Kind kSide = TB ? kBf16 : kF32;
+        uintptr_t sp[CT], tp[PRE ? 1 : MT];
+#pragma unroll
+        for (int i = 0; i < CT; ++i) sp[i] = stream + std::min<int64_t>(s0 + group + i * 16 + lane % 16, n_s - 1) * s_ld;
+        if constexpr (PRE)
+            tp[0] = reinterpret_cast<uintptr_t>(work + a.at_side) + lane * 16;
+        else
+#pragma unroll
+            for (int j = 0; j < MT; ++j) tp[j] = side + std::min(j * 16 + lane % 16, n_t - 1) * t_ld;
+        constexpr int kAhead = 2;
+        struct Step {
+            Eight<STREAM> s[CT];
+            Eight<kSide> t[PRE ? 1 : MT];
+            Pieces<PT> p[PRE ? MT : 1];
+        } st[kAhead];
+        const int own = lane / 16 * 8, full = cols / 32 * 32;
+        auto fetch = [&](auto whole, Step& q, int c) {
+            constexpr bool kWhole = decltype(whole)::value;
+#pragma unroll
+            for (int i = 0; i < CT; ++i) q.s[i] = load_eight<STREAM, kWhole>(sp[i], c + own, cols);
+            if constexpr (PRE) {
+#pragma unroll
+                for (int j = 0; j < MT; ++j)
+#pragma unroll
+                    for (int p = 0; p < PT; ++p) q.p[j].p[p] = gld<u32x4>(tp[0] + ((c / 32 * MT + j) * PT + p) * 1024);
+            } else {
+#pragma unroll
+                for (int j = 0; j < MT; ++j) q.t[j] = load_eight<kSide, kWhole>(tp[j], c + own, cols);
+            }
+        };
+        auto step = [&](auto whole, const Step& q) {
+            constexpr bool kWhole = decltype(whole)::value;
+            Pieces<STREAM == kF32 ? 3 : 1> ps[CT];
+#pragma unroll
+            for (int i = 0; i < CT; ++i) ps[i] = pieces<STREAM, kWhole>(q.s[i], sp[i]);
+#pragma unroll
+            for (int j = 0; j < MT; ++j) {
+                const Pieces<PT> pt = PRE ? q.p[PRE ? j : 0] : pieces<kSide, kWhole>(q.t[PRE ? 0 : j], tp[PRE ? 0 : j]);
+#pragma unroll
+                for (int i = 0; i < CT; ++i) acc[i][j] = multiply(ps[i], pt, acc[i][j]);
+            }
+        };
+        // The wave's step n: its 64 columns of every 64 `parts`, 32 at a time.  The
+        // workgroups begin at different ones, or the rows' equal distances would
+        // have all of them at the same channels of the memory at a time.
+        auto column = [&](int n) { return n / 2 * (64 * parts) + n % 2 * 32 + own_part * 64; };
+        const int steps = full / (64 * parts) * 2 + std::clamp((full % (64 * parts) - own_part * 64) / 32, 0, 2);
+        // (past the last step it is loaded again: were the loads left out, the
+        // counts of loads under way would differ, and all would be waited for)
+        int ahead = steps > 0 ? static_cast<int>(blockIdx.x * kTurn % steps) : 0, asked = 0;
+        auto next = [&](Step& to) {
+            fetch(std::true_type{}, to, column(ahead));
+            loads_first();
+            if (asked + 1 < steps) {
+                ++asked;
+                if (++ahead == steps) ahead = 0;
+            }
+        };
+        if (steps > 0) {
+#pragma unroll
+            for (int q = 0; q < kAhead - 1; ++q) next(st[q]);
+            for (int n = 0;;) {
+                bool more = true;
+#pragma unroll
+                for (int q = 0; q < kAhead; ++q) {
+                    next(st[(q + kAhead - 1) % kAhead]);
+                    step(std::true_type{}, st[q]);
+                    if (++n == steps) {
+                        more = false;
+                        break;
+                    }
+                }
+                if (!more) break;
+            }
+        }
+        if (column(steps) == full && full < cols) {
+            fetch(std::false_type{}, st[0], full);
+            step(std::false_type{}, st[0]);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < CT; ++i)
+#pragma unroll
+        for (int j = 0; j < MT; ++j)
+            *reinterpret_cast<f32x4*>(z + (part * kT + j * 16 + lane % 16) * kPitch + group + i * 16 + lane / 16 * 4) = acc[i][j];
+    if (a.cuts == 1) few_factors<kS, MT, ROWS>(a, k, s0, factors);
+    __syncthreads();
+    // the sum of the waves' parts
+    auto sum = [&](int t, int s) {
+        float q = 0.0f;
+#pragma unroll
+        for (int w = 0; w < W; w += 2) q += z[(w * kT + t) * kPitch + s] + z[(w * kT + kT + t) * kPitch + s];
+        return q;
+    };
+    if (a.cuts > 1) {
+        float* out = reinterpret_cast<float*>(work + a.at_z) + (static_cast<int64_t>(blockIdx.z) * a.tiles + blockIdx.x) * (kT * kS);
+        for (int n = tid; n < kT * kS; n += kLogitThreads) out[n] = sum(n / kS, n % kS);
+        return;
+    }
+    for (int n = tid; n < kT * kS; n += kLogitThreads) {
+        const int t = n / kS, s = n % kS;
+        z[t * kPitch + s] = sum(t, s) + few_bias(a, k, ROWS ? t : s0 + s);
+    }
+    __syncthreads();
+    few_results<kS, MT, ROWS>(a, k, s0, z, factors);
+}
+
+// The same from the sums of the workgroups that shared the columns.
+template <int kS, int MT, bool ROWS>
+__global__ void __launch_bounds__(kLogitThreads) few_rest_kernel(const FewArgs a) {
+    constexpr int kT = MT * 16, kPitch = kS + 4;
+    __shared__ __attribute__((aligned(16))) float z[kT * kPitch];
+    __shared__ float factors[ROWS ? kS : kT];
+    const int k = blockIdx.y;
+    const int64_t n_s = ROWS ? a.rows[k] : a.classes, s0 = static_cast<int64_t>(blockIdx.x) * kS;
+    if (s0 >= (n_s + 63) / 64 * 64) return;
+    few_factors<kS, MT, ROWS>(a, k, s0, factors);
+    const float* sums = reinterpret_cast<const float*>(a.work + k * a.stride + a.at_z) + static_cast<int64_t>(blockIdx.x) * (kT * kS);
+    for (int n = threadIdx.x; n < kT * kS; n += kLogitThreads) {
+        const int t = n / kS, s = n % kS;
+        float q = few_bias(a, k, ROWS ? t : s0 + s);
+#pragma unroll 4
+        for (int c = 0; c < a.cuts; ++c) q += sums[static_cast<int64_t>(c) * a.tiles * (kT * kS) + n];
+        z[t * kPitch + s] = q;
+    }
+    __syncthreads();
+    few_results<kS, MT, ROWS>(a, k, s0, z, factors);
 }
 
 // Joins the workgroups' pairs of a row.
@@ -769,8 +826,8 @@ __global__ void __launch_bounds__(256) few_outer_kernel(const OuterArgs a) {
 struct FewPlan {
     bool rows_stream;  // the stream is the rows
     bool pre;          // the side is laid out for the logits
-    int mt, ct, waves, groups, batch, tiles, splits, cols_p, blocks, pieces, pieces_fg;
-    int64_t n_s, stride, at_pairs, at_own, at_side, at_g, at_fg, at_f, at_db, at_sums, sums_stride;
+    int mt, ct, waves, groups, batch, tiles, cuts, splits, cols_p, blocks, pieces, pieces_fg;
+    int64_t n_s, stride, at_pairs, at_own, at_side, at_g, at_fg, at_f, at_db, at_z, at_sums, sums_stride;
 };
 
 FewPlan few_plan(int K, const int64_t* rows, int64_t cols, int64_t classes, int dtype, int w_dtype, bool backward, int dw_dtype) {
@@ -799,15 +856,27 @@ FewPlan few_plan(int K, const int64_t* rows, int64_t cols, int64_t classes, int 
     // enough (8 rows of 4,096 over 131,072 classes: 280 us with 16, 245, 224)
     p.ct = p.mt == 1 && (p.n_s + 63) / 64 * p.batch >= 384 ? 4 : (p.pre || p.mt < 4) && (p.n_s + 31) / 32 * p.batch >= (p.pre ? 512 : 256) ? 2 : 1;
     if (p.waves == 2) p.ct = 1;
+    // 32 also where the columns can be cut (below) and the side is three pieces,
+    // which every workgroup reads from L2 (60 rows of 8,192 over 4,000 classes in
+    // float: 55 us with 16, 48)
+    if (p.pre && !side_bf && (p.n_s + 31) / 32 * p.batch * std::min<int64_t>(8, cols / 1024) >= 256) p.ct = 2;
     const int64_t padded = (p.n_s + 63) / 64 * 64;
     p.groups = p.ct * 16 * (8 / p.waves);
     p.tiles = static_cast<int>(padded / p.groups);
+    // Where workgroups are too few for the chip, several share the columns, 1,024
+    // and more each, and another kernel adds their sums up (one worker: 32 rows of
+    // 4,096 over 1,000 classes in float, forward, 29 us, 16.5 with four; 60 of
+    // 8,192 52 and 28).  Up to 16 rows are small calls, which two do not pay for
+    // (2 x 1 row of 4,096 16 and 19 us).
+    p.cuts = static_cast<int>(std::min<int64_t>({256 / (static_cast<int64_t>(p.tiles) * p.batch), cols / 1024, 8}));
+    if (p.cuts < (p.mt == 1 ? 3 : 2)) p.cuts = 1;
     int64_t at = 0;
     auto take = [&](int64_t bytes) {
         const int64_t here = at;
         at += (bytes + 255) / 256 * 256;
         return here;
     };
+    if (p.cuts > 1) p.at_z = take(static_cast<int64_t>(p.cuts) * p.tiles * (p.mt * 16) * p.groups * 4);
     if (p.pre) p.at_side = take((cols + 31) / 32 * p.mt * (side_bf ? 1 : 3) * 1024);
     if (!backward) {
         if (!p.rows_stream) {
@@ -862,6 +931,15 @@ void run_logit(const FewArgs& a, const FewPlan& p, dim3 grid, hipStream_t s) {
     else
         run_logit<STREAM, TB, 4, ROWS>(a, p, grid, s);
 }
+template <int MT, bool ROWS>
+void run_rest(const FewArgs& a, const FewPlan& p, dim3 grid, hipStream_t s) {
+    if (p.ct == 1)
+        few_rest_kernel<16, MT, ROWS><<<grid, kLogitThreads, 0, s>>>(a);
+    else if (MT > 1 || p.ct == 2)
+        few_rest_kernel<32, MT, ROWS><<<grid, kLogitThreads, 0, s>>>(a);
+    else
+        few_rest_kernel<64, MT, ROWS><<<grid, kLogitThreads, 0, s>>>(a);
+}
 template <bool TB, bool ROWS>
 hipError_t run_logit(const FewArgs& a, const FewPlan& p, Kind stream, int n, hipStream_t s) {
     if (p.pre) {
@@ -869,13 +947,22 @@ hipError_t run_logit(const FewArgs& a, const FewPlan& p, Kind stream, int n, hip
         few_side_kernel<TB, ROWS><<<dim3((units + 3) / 4, n), 256, 0, s>>>(a, p.mt);
         if (hipError_t e = hipGetLastError()) return e;
     }
-    const dim3 grid(p.tiles, n);
+    const dim3 grid(p.tiles, n, p.cuts);
     if (stream == kF32)
         run_logit<kF32, TB, ROWS>(a, p, grid, s);
     else if (stream == kBf16)
         run_logit<kBf16, TB, ROWS>(a, p, grid, s);
     else
         run_logit<kOdd, TB, ROWS>(a, p, grid, s);
+    if (p.cuts == 1) return hipGetLastError();
+    if (hipError_t e = hipGetLastError()) return e;
+    const dim3 rest(p.tiles, n);
+    if (p.mt == 1)
+        run_rest<1, ROWS>(a, p, rest, s);
+    else if (p.mt == 2)
+        run_rest<2, ROWS>(a, p, rest, s);
+    else
+        run_rest<4, ROWS>(a, p, rest, s);
     return hipGetLastError();
 }
 template <bool TB, bool ROWS>
@@ -951,6 +1038,8 @@ hipError_t launch_few(const LossCall& c, const int* list, int count, hipStream_t
         a.classes = m.classes = o.classes = c.classes;
         a.cols = m.cols = o.cols = cols;
         a.tiles = p.tiles;
+        a.cuts = p.cuts;
+        a.at_z = p.at_z;
         a.w_bf = w_bf;
         a.db_bf = m.db_bf = dw_bf;
         a.has_dloss = m.has_dloss = o.has_dloss = has_dloss;

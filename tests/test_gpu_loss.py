@@ -293,6 +293,13 @@ def test_long_rows(rows, cols, classes, x):
     check(Case(rows, cols, classes, x, x, x, seed=19))
 
 
+@pytest.mark.parametrize("x,w,dw", [(F32, F32, F32), (BF16, BF16, BF16), (BF16, F32, F32)], ids=["f32", "bf16", "mixed"])
+@pytest.mark.parametrize("rows,cols,classes", [([3, 9], 4099, 500), ([20], 4101, 1000), ([31, 0, 2], 2048, 333), ([64], 8190, 777), ([40, 50], 3101, 1001),
+                                               ([300, 7], 5000, 40), ([65], 2100, 20), ([66], 7777, 9), ([61], 4100, 4001)], ids=str)
+def test_few_workgroups_that_share_the_columns(rows, cols, classes, x, w, dw):
+    check(Case(rows, cols, classes, x, w, dw, bias=True, weighted=True, out=0.2, pad=1, seed=22))
+
+
 @pytest.mark.parametrize("rows,classes", [([40], 200), ([70], 200), ([70], 30)], ids=str)
 def test_rows_far_from_each_other(rows, classes):
     """Offsets past 32 bits, in bytes or in elements."""
