@@ -1039,6 +1039,8 @@ struct Plan {
 // chip many times over.
 constexpr int64_t kRoom = int64_t{2} << 30;
 constexpr int kTilesPair = 128;  // classes of the smallest tile of pairs
+constexpr int64_t kChunk = 64;   // rows that count as few
+constexpr int kMostChunks = 8;   // of a worker's rows
 
 Plan plan_of(int K, const int64_t* rows, int64_t cols, int64_t classes, int dtype, int w_dtype, bool backward, int dw_dtype) {
     Plan p{};
@@ -1142,9 +1144,49 @@ int runs_of(int left, int right, Side& l, Side& r) {
 
 }  // namespace
 
+namespace {
+
+// Forward, rows have nothing to do with each other, so somewhat more than few of
+// them are taken as several workers that share their weight, which is read again
+// for each, mostly from the caches.  One worker, 128 rows of 4,096 over 32,000
+// classes 113 us (in tiles 170), over 1,000 20 (31); 256 over 1,000 21 (33), over
+// 32,000 212 (192); 500 over 1,000 31 (34); 500 of 1,024 over 8,000 43 (39); four
+// workers, 256 of 4,096 over 1,000 42 (48), 500 82 (59).  Only bfloat16 rows and
+// weights: of binary32 ones the few rows' pieces do not hold values near the
+// type's smallest, as the tiles' scaled operands do (256 over 1,000 would be 37
+// us, in tiles 55).
+struct Chunks {
+    int K = 0;  // 0: they are not
+    int64_t rows[TC_MAX_K * kMostChunks];
+    int of[TC_MAX_K * kMostChunks];
+};
+
+void chunks_of(Chunks& c, int K, const int64_t* rows, int64_t cols, int64_t classes, int dtype, int w_dtype, bool backward) {
+    if (backward || dtype != TC_BF16 || w_dtype != TC_BF16) return;
+    int64_t most = 0, all = 0, count = 0;
+    for (int k = 0; k < K; ++k) {
+        most = std::max(most, rows[k]);
+        all += rows[k];
+        count += (rows[k] + kChunk - 1) / kChunk;
+    }
+    // (more than 32 would be many launches)
+    const double work = static_cast<double>(all) * classes * cols;
+    if (most > 2 * kChunk && (count > 32 || most > kMostChunks * kChunk || work > (most <= 4 * kChunk ? 0x1p32 : 0x1p31))) return;
+    for (int k = 0; k < K; ++k)
+        for (int64_t r = 0; r < rows[k]; r += kChunk) {
+            c.rows[c.K] = std::min(kChunk, rows[k] - r);
+            c.of[c.K++] = k;
+        }
+}
+
+}  // namespace
+
 int64_t cross_entropy_workspace(int K, const int64_t* rows, int64_t cols, int64_t classes, int dtype, int w_dtype,
                                 bool backward, int dw_dtype) {
     if (few_fits(K, rows, classes)) return few_workspace(K, rows, cols, classes, dtype, w_dtype, backward, dw_dtype);
+    Chunks chunks;
+    chunks_of(chunks, K, rows, cols, classes, dtype, w_dtype, backward);
+    if (chunks.K) return few_workspace(chunks.K, chunks.rows, cols, classes, dtype, w_dtype, backward, dw_dtype);
     const Plan p = plan_of(K, rows, cols, classes, dtype, w_dtype, backward, dw_dtype);
     return p.batch * p.stride;
 }
@@ -1173,6 +1215,36 @@ hipError_t run_logits(const LogitArgs& a, int tile, bool bf, int n, hipStream_t 
     return hipGetLastError();
 }
 
+hipError_t launch_chunks(const LossCall& c, const Chunks& chunks, hipStream_t s) {
+    constexpr int kMost = TC_MAX_K * kMostChunks;
+    const void *x[kMost], *weight[kMost], *bias[kMost];
+    const int64_t* label[kMost];
+    float *loss[kMost], *lse[kMost];
+    int list[kMost];
+    int64_t r = 0;
+    for (int i = 0; i < chunks.K; ++i) {
+        const int k = chunks.of[i];
+        r = i && chunks.of[i - 1] == k ? r + kChunk : 0;
+        x[i] = static_cast<const char*>(c.x[k]) + r * c.x_ld * 2;
+        weight[i] = c.weight[k];
+        bias[i] = c.bias ? c.bias[k] : nullptr;
+        label[i] = c.label[k] + r;
+        loss[i] = c.loss[k] + r;
+        lse[i] = c.lse[k] + r;
+        list[i] = i;
+    }
+    LossCall d = c;
+    d.K = chunks.K;
+    d.rows = chunks.rows;
+    d.x = x;
+    d.weight = weight;
+    if (c.bias) d.bias = bias;
+    d.label = label;
+    d.loss = loss;
+    d.lse = lse;
+    return launch_few(d, list, chunks.K, s);
+}
+
 }  // namespace
 
 hipError_t launch_cross_entropy(const LossCall& c, hipStream_t s) {
@@ -1194,6 +1266,9 @@ hipError_t launch_cross_entropy(const LossCall& c, hipStream_t s) {
         }
     }
     if (few_fits(c.K, c.rows, classes)) return launch_few(c, list, count, s);
+    Chunks chunks;
+    chunks_of(chunks, c.K, c.rows, cols, classes, c.dtype, c.w_dtype, back);
+    if (chunks.K) return launch_chunks(c, chunks, s);
     const Plan p = plan_of(c.K, c.rows, cols, classes, c.dtype, c.w_dtype, back, c.dw_dtype);
     for (int k0 = 0; k0 < count; k0 += p.batch) {
         const int n = std::min(p.batch, count - k0);

@@ -300,6 +300,20 @@ def test_few_workgroups_that_share_the_columns(rows, cols, classes, x, w, dw):
     check(Case(rows, cols, classes, x, w, dw, bias=True, weighted=True, out=0.2, pad=1, seed=22))
 
 
+@pytest.mark.parametrize("x,w", [(F32, F32), (BF16, BF16), (BF16, F32)], ids=["f32", "bf16", "mixed"])
+@pytest.mark.parametrize("rows,cols,classes", [([65], 100, 70), ([128, 64, 1, 0], 1030, 1000), ([129], 333, 5000), ([256, 3, 200], 2050, 700), ([257], 64, 129),
+                                               ([512, 70], 520, 401), ([513], 520, 401), ([320] * 7, 72, 90), ([100] * 21, 40, 80)], ids=str)
+def test_rows_taken_as_several_workers(rows, cols, classes, x, w):
+    """Up to 128 rows in bfloat16, or 512 in small calls, forward, and the sizes next to these."""
+    c = Case(rows, cols, classes, x, w, F32, bias=True, out=0.2, pad=3, offset=1, seed=23)
+    check(c)
+    first = [t.clone() for t in c.loss + c.lse]
+    c.forward(workspace=torch.full((tc.cross_entropy_workspace(rows, cols, classes, x, w),), 255, dtype=torch.uint8, device="cuda"))
+    torch.cuda.synchronize()
+    for a, b in zip(first, c.loss + c.lse):
+        assert torch.equal(a, b)
+
+
 @pytest.mark.parametrize("rows,classes", [([40], 200), ([70], 200), ([70], 30)], ids=str)
 def test_rows_far_from_each_other(rows, classes):
     """Offsets past 32 bits, in bytes or in elements."""
