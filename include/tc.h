@@ -485,8 +485,7 @@ int32_t tc_dropout_backward(int32_t K, const int64_t* rows, int64_t cols, const 
  * integers.  loss, lse: K device pointers to rows[k] binary32 values that
  * receive the rows' losses and logs of sums (the backward pass needs them).
  * Binary32 operands are taken with 22 bits or more next to the operand's
- * largest value (with at most 64 rows a worker, or 64 classes, next to 2^-104 if
- * that is larger), products are summed and exponentials taken in binary32.  The
+ * largest value, products are summed and exponentials taken in binary32.  The
  * same inputs give the same bits.  loss, lse and the workspace share no byte
  * with each other or with what is read.  A worker without rows needs no
  * pointers.  The rows are on the current device.  cols in [1, TC_MAX_CE_COLS],

@@ -20,7 +20,9 @@
 //
 // Operands go from memory to registers and to the matrix cores as bfloat16
 // pieces: a bfloat16 element is one, a binary32 element three that hold its 24
-// bits (cut off, not rounded, so that the largest value does not overflow).  Of
+// bits (cut off, not rounded, so that the largest value does not overflow; for
+// the logits each of the others is scaled to the first one's size and has sums of
+// its own, or the smallest values' pieces would be under bfloat16's).  Of
 // the pieces' products those under 2^-24 of a term are left out; of g, whose
 // results are rounded to bfloat16, two pieces are taken.
 //
@@ -55,8 +57,9 @@ struct Pieces {
 
 __device__ __forceinline__ uint32_t high_halves(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }
 
-// P pieces of eight binary32 values, cut off.
-template <int P>
+// P pieces of eight binary32 values, cut off; UP: piece n times 2^8n, so that it
+// is no smaller than bfloat16's values where the first one is not.
+template <int P, bool UP = false>
 __device__ __forceinline__ Pieces<P> cut(const float* f) {
     Pieces<P> r;
     float rest[8];
@@ -68,10 +71,33 @@ __device__ __forceinline__ Pieces<P> cut(const float* f) {
         for (int i = 0; i < 4; ++i) r.p[n][i] = high_halves(__float_as_uint(rest[2 * i]), __float_as_uint(rest[2 * i + 1]));
         if (n + 1 < P)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) rest[e] -= __uint_as_float(__float_as_uint(rest[e]) & 0xffff0000u);
+            for (int e = 0; e < 8; ++e) {
+                rest[e] -= __uint_as_float(__float_as_uint(rest[e]) & 0xffff0000u);
+                if (UP) rest[e] *= 256.0f;
+            }
     }
     return r;
 }
+
+// Sums of the products of pieces i and j that are times 2^8(i + j).
+template <int PA, int PB>
+struct Sums {
+    static constexpr int kSums = PA > PB ? PA : PB;
+    f32x4 v[kSums];
+    __device__ __forceinline__ void add(const Pieces<PA>& a, const Pieces<PB>& b) {
+#pragma unroll
+        for (int i = 0; i < PA; ++i)
+#pragma unroll
+            for (int j = 0; j < PB; ++j)
+                if (i + j < kSums)
+                    v[i + j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a.p[i]), __builtin_bit_cast(bf16x8, b.p[j]), v[i + j], 0, 0, 0);
+    }
+    __device__ __forceinline__ f32x4 sum() const {
+        f32x4 s = v[0];
+        if constexpr (kSums == 3) s += (v[2] * 0x1p-8f + v[1]) * 0x1p-8f;
+        return s;
+    }
+};
 
 template <int PA, int PB>
 __device__ __forceinline__ f32x4 multiply(const Pieces<PA>& a, const Pieces<PB>& b, f32x4 c) {
@@ -122,7 +148,7 @@ __device__ __forceinline__ Pieces<KIND == kF32 ? 3 : 1> pieces(const Eight<KIND>
         float f[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(e.v[i / 4][i % 4]);
-        return cut<3>(f);
+        return cut<3, true>(f);
     } else if constexpr (KIND == kBf16 || !WHOLE) {
         return {{e.v[0]}};
     } else {
@@ -395,7 +421,7 @@ __global__ void __launch_bounds__(kLogitThreads) few_logit_kernel(const FewArgs 
     const int64_t s_ld = (ROWS ? a.x_ld : cols) * se, t_ld = (ROWS ? cols : a.x_ld) * te;
     char* work = a.work + k * a.stride;
     // ---- the logits
-    f32x4 acc[CT][MT] = {};
+    Sums<STREAM == kF32 ? 3 : 1, PT> acc[CT][MT] = {};
     {
         constexpr Kind kSide = TB ? kBf16 : kF32;
         uintptr_t sp[CT], tp[PRE ? 1 : MT];
@@ -436,7 +462,7 @@ __global__ void __launch_bounds__(kLogitThreads) few_logit_kernel(const FewArgs 
             for (int j = 0; j < MT; ++j) {
                 const Pieces<PT> pt = PRE ? q.p[PRE ? j : 0] : pieces<kSide, kWhole>(q.t[PRE ? 0 : j], tp[PRE ? 0 : j]);
 #pragma unroll
-                for (int i = 0; i < CT; ++i) acc[i][j] = multiply(ps[i], pt, acc[i][j]);
+                for (int i = 0; i < CT; ++i) acc[i][j].add(ps[i], pt);
             }
         };
         // The wave's step n: its 64 columns of every 64 `parts`, 32 at a time.  The
@@ -481,7 +507,7 @@ __global__ void __launch_bounds__(kLogitThreads) few_logit_kernel(const FewArgs 
     for (int i = 0; i < CT; ++i)
 #pragma unroll
         for (int j = 0; j < MT; ++j)
-            *reinterpret_cast<f32x4*>(z + (part * kT + j * 16 + lane % 16) * kPitch + group + i * 16 + lane / 16 * 4) = acc[i][j];
+            *reinterpret_cast<f32x4*>(z + (part * kT + j * 16 + lane % 16) * kPitch + group + i * 16 + lane / 16 * 4) = acc[i][j].sum();
     if (a.cuts == 1) few_factors<kS, MT, ROWS>(a, k, s0, factors);
     __syncthreads();
     // the sum of the waves' parts
@@ -843,7 +869,7 @@ FewPlan few_plan(int K, const int64_t* rows, int64_t cols, int64_t classes, int 
     p.n_s = p.rows_stream ? most : classes;
     p.mt = n_t <= 16 ? 1 : n_t <= 32 ? 2 : 4;
     p.batch = std::max(1, std::min(with, kWorkers));
-    const bool side_bf = (p.rows_stream ? w_dtype : dtype) == TC_BF16;
+    const bool side_bf = (p.rows_stream ? w_dtype : dtype) == TC_BF16, stream_bf = (p.rows_stream ? dtype : w_dtype) == TC_BF16;
     // A side of more than 32 rows (or 16, if the stream is long) is laid out: it is
     // read by every workgroup.  (4 x 64 rows of 4,096 over 1,000 classes, the
     // logits: 50 us as it lies, 32 + 5 laid out; 8 x 32 rows of 2,048, 20.5 and
@@ -853,8 +879,10 @@ FewPlan few_plan(int K, const int64_t* rows, int64_t cols, int64_t classes, int 
     p.waves = cols <= 256 ? 2 : 8;
     p.pre = p.waves == 8 && ((p.mt == 4 && size > (1 << 21)) || (p.mt == 2 && size > (1 << 26)));
     // Rows of the stream of a workgroup: 64 or 32 where that leaves workgroups
-    // enough (8 rows of 4,096 over 131,072 classes: 280 us with 16, 245, 224)
-    p.ct = p.mt == 1 && (p.n_s + 63) / 64 * p.batch >= 384 ? 4 : (p.pre || p.mt < 4) && (p.n_s + 31) / 32 * p.batch >= (p.pre ? 512 : 256) ? 2 : 1;
+    // enough (8 rows of 4,096 over 131,072 classes in bfloat16: 280 us with 16, 245,
+    // 224; in float, whose sums take three times the registers, 5 over 32,000 101 us
+    // with 32 and 120 with 64, of 1,024 38 and 31)
+    p.ct = p.mt == 1 && (stream_bf || cols < 2048) && (p.n_s + 63) / 64 * p.batch >= 384 ? 4 : (p.pre || p.mt < 4) && (p.n_s + 31) / 32 * p.batch >= (p.pre ? 512 : 256) ? 2 : 1;
     if (p.waves == 2) p.ct = 1;
     // 32 also where the columns can be cut (below) and the side is three pieces,
     // which every workgroup reads from L2 (60 rows of 8,192 over 4,000 classes in
@@ -888,7 +916,6 @@ FewPlan few_plan(int K, const int64_t* rows, int64_t cols, int64_t classes, int 
         p.pieces_fg = (p.rows_stream ? dtype : dw_dtype) == TC_BF16 ? 2 : 3;
         p.at_g = take(padded / 32 * p.mt * p.pieces * 1024);
         p.at_fg = take(padded / 16 * (p.mt > 2 ? 2 : 1) * p.pieces_fg * 1024);
-        const bool stream_bf = (p.rows_stream ? dtype : w_dtype) == TC_BF16;
         const int block = stream_bf && p.mt < 4 ? 128 : 64;
         p.blocks = static_cast<int>((cols + block - 1) / block);
         p.cols_p = p.blocks * block;

@@ -260,6 +260,20 @@ def test_values_of_any_size(big, small):
     check(c)
 
 
+@pytest.mark.parametrize("rows,classes", [(5, 200), (40, 300), (400, 30)])
+@pytest.mark.parametrize("big", [1e30, 3e38, 1e-38, 1.0])
+def test_logits_of_values_of_any_size(rows, classes, big):
+    """Few rows or classes: the pieces of values next to the type's smallest count as well."""
+    c = Case([rows], 80, classes, seed=7)
+    c.x[0].mul_(0.1)
+    c.x[0][::2] *= 1e-3
+    c.x[0].mul_(min(big, 1e37))
+    c.w[0].mul_(min(1.0 / min(big, 1e37), 1e37))
+    c.forward()
+    torch.cuda.synchronize()
+    check_forward(c)
+
+
 def test_a_certain_row():
     """The label's own probability rounds to one: its gradient does not."""
     c = Case([4, 140], 64, 100, seed=8)
