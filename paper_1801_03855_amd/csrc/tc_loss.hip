@@ -1149,20 +1149,19 @@ namespace {
 // Forward, rows have nothing to do with each other, so somewhat more than few of
 // them are taken as several workers that share their weight, which is read again
 // for each, mostly from the caches.  One worker, 128 rows of 4,096 over 32,000
-// classes 113 us (in tiles 170), over 1,000 20 (31); 256 over 1,000 21 (33), over
-// 32,000 212 (192); 500 over 1,000 31 (34); 500 of 1,024 over 8,000 43 (39); four
-// workers, 256 of 4,096 over 1,000 42 (48), 500 82 (59).  Only bfloat16 rows and
-// weights: of binary32 ones the few rows' pieces do not hold values near the
-// type's smallest, as the tiles' scaled operands do (256 over 1,000 would be 37
-// us, in tiles 55).
+// classes in bfloat16 113 us (in tiles 170), in float 350 (472), over 1,000 20
+// (31) and 26 (53); 256 over 1,000 21 (33) and 37 (55), over 32,000 212 (192) and
+// 680 (529); 500 over 1,000 31 (34) and 49 (65); 500 of 1,024 over 8,000 43 (39)
+// and 104 (75); four workers, 256 of 4,096 over 1,000 42 (48) and 87 (109), 500
+// 82 (59) and 168 (140).
 struct Chunks {
     int K = 0;  // 0: they are not
     int64_t rows[TC_MAX_K * kMostChunks];
     int of[TC_MAX_K * kMostChunks];
 };
 
-void chunks_of(Chunks& c, int K, const int64_t* rows, int64_t cols, int64_t classes, int dtype, int w_dtype, bool backward) {
-    if (backward || dtype != TC_BF16 || w_dtype != TC_BF16) return;
+void chunks_of(Chunks& c, int K, const int64_t* rows, int64_t cols, int64_t classes, bool backward) {
+    if (backward) return;
     int64_t most = 0, all = 0, count = 0;
     for (int k = 0; k < K; ++k) {
         most = std::max(most, rows[k]);
@@ -1185,7 +1184,7 @@ int64_t cross_entropy_workspace(int K, const int64_t* rows, int64_t cols, int64_
                                 bool backward, int dw_dtype) {
     if (few_fits(K, rows, classes)) return few_workspace(K, rows, cols, classes, dtype, w_dtype, backward, dw_dtype);
     Chunks chunks;
-    chunks_of(chunks, K, rows, cols, classes, dtype, w_dtype, backward);
+    chunks_of(chunks, K, rows, cols, classes, backward);
     if (chunks.K) return few_workspace(chunks.K, chunks.rows, cols, classes, dtype, w_dtype, backward, dw_dtype);
     const Plan p = plan_of(K, rows, cols, classes, dtype, w_dtype, backward, dw_dtype);
     return p.batch * p.stride;
@@ -1225,7 +1224,7 @@ hipError_t launch_chunks(const LossCall& c, const Chunks& chunks, hipStream_t s)
     for (int i = 0; i < chunks.K; ++i) {
         const int k = chunks.of[i];
         r = i && chunks.of[i - 1] == k ? r + kChunk : 0;
-        x[i] = static_cast<const char*>(c.x[k]) + r * c.x_ld * 2;
+        x[i] = static_cast<const char*>(c.x[k]) + r * c.x_ld * (c.dtype == TC_BF16 ? 2 : 4);
         weight[i] = c.weight[k];
         bias[i] = c.bias ? c.bias[k] : nullptr;
         label[i] = c.label[k] + r;
@@ -1267,7 +1266,7 @@ hipError_t launch_cross_entropy(const LossCall& c, hipStream_t s) {
     }
     if (few_fits(c.K, c.rows, classes)) return launch_few(c, list, count, s);
     Chunks chunks;
-    chunks_of(chunks, c.K, c.rows, cols, classes, c.dtype, c.w_dtype, back);
+    chunks_of(chunks, c.K, c.rows, cols, classes, back);
     if (chunks.K) return launch_chunks(c, chunks, s);
     const Plan p = plan_of(c.K, c.rows, cols, classes, c.dtype, c.w_dtype, back, c.dw_dtype);
     for (int k0 = 0; k0 < count; k0 += p.batch) {

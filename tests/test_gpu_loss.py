@@ -318,7 +318,7 @@ def test_few_workgroups_that_share_the_columns(rows, cols, classes, x, w, dw):
 @pytest.mark.parametrize("rows,cols,classes", [([65], 100, 70), ([128, 64, 1, 0], 1030, 1000), ([129], 333, 5000), ([256, 3, 200], 2050, 700), ([257], 64, 129),
                                                ([512, 70], 520, 401), ([513], 520, 401), ([320] * 7, 72, 90), ([100] * 21, 40, 80)], ids=str)
 def test_rows_taken_as_several_workers(rows, cols, classes, x, w):
-    """Up to 128 rows in bfloat16, or 512 in small calls, forward, and the sizes next to these."""
+    """Up to 128 rows, or 512 in small calls, forward, and the sizes next to these."""
     c = Case(rows, cols, classes, x, w, F32, bias=True, out=0.2, pad=3, offset=1, seed=23)
     check(c)
     first = [t.clone() for t in c.loss + c.lse]
