@@ -31,6 +31,7 @@
 #include <cmath>
 #include <type_traits>
 
+#include "tc_grid.h"
 #include "tc_lane.h"
 
 namespace tc {
@@ -228,10 +229,12 @@ __device__ __forceinline__ void split(const float* v, int e, u16x8& hi, u16x8& l
     }
 }
 
-// A workgroup takes 64 x 64 elements of one operand; bound by memory.
+// A workgroup takes 64 x 64 elements of one operand; bound by memory.  2^36
+// elements of each are more workgroups than one dimension takes, so they go on
+// along z (those behind the last tile find no rows).
 __global__ void __launch_bounds__(256) loss_panel_kernel(const PanelArgs a) {
     __shared__ float lds[64][65];
-    const int k = blockIdx.y, b = blockIdx.x, tid = threadIdx.x;
+    const int k = blockIdx.y, b = blockIdx.z * gridDim.x + blockIdx.x, tid = threadIdx.x;
     const bool weight = b >= a.w.first;
     const Panels& o = weight ? a.w : a.x;
     char* ws = a.ws + k * a.ws_stride;
@@ -1339,7 +1342,8 @@ hipError_t launch_cross_entropy(const LossCall& c, hipStream_t s) {
             x.padded_t = w.padded_t = p.cols_p;
             x.tiles_c = w.tiles_c = tiles_c;
             w.first = v0 == 0 ? static_cast<int32_t>((most + 63) / 64) * tiles_c : 0;
-            loss_panel_kernel<<<dim3(w.first + static_cast<int32_t>((here + 63) / 64) * tiles_c, n), 256, 0, s>>>(a);
+            const GridXY panels = grid_of(w.first + (here + 63) / 64 * tiles_c, 256);
+            loss_panel_kernel<<<dim3(panels.x, n, panels.y), 256, 0, s>>>(a);
             if (hipError_t e = hipGetLastError()) return e;
             // the logits
             LogitArgs l{};
