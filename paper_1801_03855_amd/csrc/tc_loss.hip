@@ -488,7 +488,7 @@ struct LogitArgs {
     int64_t padded;                 // classes of the panel of g
     int64_t padded_r;               // rows of the panels
     int64_t first;                  // class of the piece
-    int64_t pair_tile;              // and its first tile
+    int64_t pair_tile;              // and its first tile among those that are joined with it
     int32_t classes, count;         // in all, of the piece
     int32_t tiles_v, tiles_r, steps, runs;
     int32_t scaled;                 // operands have exponents
@@ -774,18 +774,21 @@ struct LossArgs {
     int64_t rows[kBatch];
     char* work;
     int64_t stride, at_pairs, at_own;
+    int64_t at_run;     // the pairs of the classes before these
     int64_t padded_r;
     int32_t tiles, classes;
+    int32_t first, last;
 };
 
 // Joins the tiles' pairs of every row: 64 rows a workgroup, whose 16 waves take
-// the tiles in turn.
+// the tiles in turn.  Where the pairs of all classes would not fit their place
+// they are joined several times, each time with what came of those before.
 __global__ void __launch_bounds__(1024) loss_join_kernel(const LossArgs a) {
     __shared__ float2 lds[16][64];
     const int k = blockIdx.y, lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int64_t rows = a.rows[k], row = static_cast<int64_t>(blockIdx.x) * 64 + lane;
     if (static_cast<int64_t>(blockIdx.x) * 64 >= rows) return;
-    const char* work = a.work + k * a.stride;
+    char* work = a.work + k * a.stride;
     float top = -INFINITY, sum = 0.0f;
     if (row < rows)
         for (int t = wave; t < a.tiles; t += 16) {
@@ -797,6 +800,12 @@ __global__ void __launch_bounds__(1024) loss_join_kernel(const LossArgs a) {
     if (wave || row >= rows) return;
 #pragma unroll
     for (int w = 1; w < 16; ++w) join(top, sum, lds[w][lane].x, lds[w][lane].y);
+    float2* run = reinterpret_cast<float2*>(work + a.at_run) + row;
+    if (!a.first) join(top, sum, run->x, run->y);
+    if (!a.last) {
+        *run = make_float2(top, sum);
+        return;
+    }
     const float lse = top + log2f(sum) * kLn2;
     a.lse[k][row] = lse;
     const int64_t label = a.label[k][row];
@@ -1028,6 +1037,7 @@ struct Plan {
     int planes_gt, planes_xt;  // of dweight's
     int64_t rows, rows_p, cols_p, steps;  // most rows of a worker, padded to 256, columns to 256, 32's
     int64_t piece, pieces;     // classes at a time
+    int64_t joined;            // pieces whose pairs are joined at a time
     int batch;                 // workers at a time
     int tile, cuts;            // of the logits; parts of their sum
     int tile_g;                // of the gradients' products
@@ -1035,13 +1045,17 @@ struct Plan {
     bool sums_dx;              // which is added up before it is rounded
     int splits_w;              // and of dweight; 0: it is written as it is computed
     // offsets in a worker's part of the workspace
-    int64_t at_rows, at_parts, at_own, at_pairs, at_xz, at_wz, at_xt, at_wt, at_g, at_gt, at_sums, at_sums_w, at_acc, at_db, stride;
+    int64_t at_rows, at_parts, at_own, at_pairs, at_run, at_xz, at_wz, at_xt, at_wt, at_g, at_gt, at_sums, at_sums_w, at_acc, at_db, stride;
 };
 
 // Workspace of a batch of workers: enough for a piece whose products fill the
 // chip many times over.
 constexpr int64_t kRoom = int64_t{2} << 30;
 constexpr int kTilesPair = 128;  // classes of the smallest tile of pairs
+// And a worker's of pairs, which would grow with the rows and the classes (2^20
+// rows over 2^18: 16 GiB).  A piece's fit it, so that it has 2^18 tiles at most:
+// HIP takes fewer than 2^24 workgroups of 256 along x.
+constexpr int64_t kPairs = int64_t{256} << 20;
 constexpr int64_t kChunk = 64;   // rows that count as few
 constexpr int kMostChunks = 8;   // of a worker's rows
 
@@ -1067,6 +1081,8 @@ Plan plan_of(int K, const int64_t* rows, int64_t cols, int64_t classes, int dtyp
     int64_t room = kRoom;
     if (!backward) room = std::min(kRoom, std::max(kRoom / 16, each * 256 * (1024 / std::max<int64_t>(1, p.rows_p / 256))));
     p.piece = std::min(all, std::max<int64_t>(1024, room / each / 256 * 256));
+    const int64_t tile_pairs = std::max<int64_t>(256, p.rows_p) * 8;  // bytes
+    if (!backward) p.piece = std::min(p.piece, kPairs / tile_pairs * kTilesPair / 256 * 256);
     p.pieces = (all + p.piece - 1) / p.piece;
     p.piece = round_up((all + p.pieces - 1) / p.pieces, 256);
     // Tiles of 256 or 128.  A CU makes about as much of two small ones (0.9) as of
@@ -1116,7 +1132,9 @@ Plan plan_of(int K, const int64_t* rows, int64_t cols, int64_t classes, int dtyp
     p.at_rows = take(p.rows_p * 8);
     if (!backward) {
         p.at_own = take(p.rows_p * 4);
-        p.at_pairs = take((p.piece * p.pieces / kTilesPair) * p.rows_p * 8);
+        p.joined = std::min(p.pieces, kPairs / (p.piece / kTilesPair * tile_pairs));
+        p.at_pairs = take(p.joined * (p.piece / kTilesPair) * tile_pairs);
+        if (p.joined < p.pieces) p.at_run = take(p.rows_p * 8);
     }
     if (p.cuts > 1) p.at_acc = take(p.cuts * small * 128 * 128 * 4);
     p.at_xz = take(p.steps * p.rows_p * kLine * p.planes_x);
@@ -1382,7 +1400,9 @@ hipError_t launch_cross_entropy(const LossCall& c, hipStream_t s) {
             l.planes_gt = p.planes_gt;
             l.has_dloss = has_dloss;
             const int tile = p.tile;
-            l.pair_tile = v0 / tile;
+            const int64_t index = v0 / piece;
+            const bool last = v0 + piece >= classes;
+            if (!back) l.pair_tile = index % p.joined * (piece / tile);
             l.tiles_v = static_cast<int32_t>((here + tile - 1) / tile);
             l.tiles_r = static_cast<int32_t>((most + tile - 1) / tile);
             l.at_acc = p.at_acc;
@@ -1390,7 +1410,7 @@ hipError_t launch_cross_entropy(const LossCall& c, hipStream_t s) {
             l.splits = p.cuts;
             if (hipError_t e = back ? run_logits<true>(l, tile, p.bf, n, s) : run_logits<false>(l, tile, p.bf, n, s)) return e;
             if (!back) {
-                if (v0 + piece < classes) continue;
+                if (!last && (index + 1) % p.joined) continue;
                 LossArgs o{};
                 for (int i = 0; i < n; ++i) {
                     o.label[i] = c.label[who[i]];
@@ -1402,6 +1422,9 @@ hipError_t launch_cross_entropy(const LossCall& c, hipStream_t s) {
                 o.stride = p.stride;
                 o.at_pairs = p.at_pairs;
                 o.at_own = p.at_own;
+                o.at_run = p.at_run;
+                o.first = index < p.joined;
+                o.last = last;
                 o.padded_r = p.rows_p;
                 o.tiles = static_cast<int32_t>(l.pair_tile) + l.tiles_v;
                 o.classes = l.classes;
@@ -1481,7 +1504,7 @@ hipError_t launch_cross_entropy(const LossCall& c, hipStream_t s) {
             if (hipError_t e = hipGetLastError()) return e;
             // results from the partial sums
             for (int which = 0; which < 2; ++which) {
-                if (which ? v0 + piece < classes || !p.sums_dx : !p.splits_w) continue;
+                if (which ? !last || !p.sums_dx : !p.splits_w) continue;
                 FinishArgs f{};
                 for (int i = 0; i < n; ++i) {
                     f.out[i] = which ? c.dx[who[i]] : dw.out[i];

@@ -37,3 +37,17 @@ def test_tiles(rows, cols, classes, x, w, dw, forward, backward):
     torch.cuda.synchronize()
     for a, b in zip(first, c.outputs()):
         assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("rows,cols,classes,x", [((1 << 20) - 5, 67, 9001, "bf16"), (1 << 20, 64, 8200, "f32"), (131000, 4090, 50001, "bf16")], ids=str)
+def test_pairs_joined_several_times(rows, cols, classes, x):
+    """More rows and classes than the pairs have room for at a time.  Rows have nothing to do with each other, so 700 of them
+    are compared, the first and last ones among them."""
+    c = Case([rows], cols, classes, TYPES[x], TYPES[x], bias=True, out=0.1, seed=32)
+    c.forward()
+    torch.cuda.synchronize()
+    some = torch.cat([torch.arange(64, device="cuda"), torch.randint(0, rows, (572,), device="cuda", generator=torch.Generator("cuda").manual_seed(1)),
+                      torch.arange(rows - 64, rows, device="cuda")])
+    c.rows = [len(some)]
+    c.x, c.label, c.loss, c.lse = [[t[0][some]] for t in (c.x, c.label, c.loss, c.lse)]
+    check_forward(c)
