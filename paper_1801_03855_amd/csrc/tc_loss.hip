@@ -1065,9 +1065,11 @@ Plan plan_of(int K, const int64_t* rows, int64_t cols, int64_t classes, int dtyp
     p.planes_x = dtype == TC_BF16 ? 1 : 2;
     p.planes_w = w_dtype == TC_BF16 ? 1 : 2;
     p.planes_g = dtype == TC_BF16 ? 1 : 2;
-    p.planes_wt = dtype == TC_BF16 || w_dtype == TC_BF16 ? 1 : 2;
+    // (an operand has its 22 bits whatever the result is rounded to: where the sums
+    // cancel, the weight's common part in dx, its lower half is all that is left)
+    p.planes_wt = p.planes_w;
     p.planes_gt = dw_dtype == TC_BF16 ? 1 : 2;
-    p.planes_xt = dtype == TC_BF16 || dw_dtype == TC_BF16 ? 1 : 2;
+    p.planes_xt = p.planes_x;
     for (int k = 0; k < K; ++k) p.rows = std::max(p.rows, rows[k]);
     p.rows_p = round_up(p.rows, 256);
     p.cols_p = round_up(cols, 256);
