@@ -23,8 +23,8 @@
 // bits (cut off, not rounded, so that the largest value does not overflow; for
 // the logits each of the others is scaled to the first one's size and has sums of
 // its own, or the smallest values' pieces would be under bfloat16's).  Of
-// the pieces' products those under 2^-24 of a term are left out; of g, whose
-// results are rounded to bfloat16, two pieces are taken.
+// the pieces' products those under 2^-24 of a term are left out; of g, where the
+// result is rounded to bfloat16, two pieces are taken (16 bits next to 1).
 //
 // A matrix instruction sums over 32 elements, of which a lane has eight.  For
 // the logits they are neighbours in a row.  For the other two products the sum
@@ -604,7 +604,7 @@ __device__ __forceinline__ void side_gradient(const SumArgs& a, int k, int t, in
 template <bool SB, int MT, bool ROWS, int PG>
 __global__ void __launch_bounds__(256) few_sum_kernel(const SumArgs a) {
     using Col = Columns<SB, SB && MT < 4 ? 8 : 4>;  // (with more the sums would not fit the registers)
-    constexpr int kT = MT * 16, kB = Col::kBlock, kPS = SB ? 1 : PG;
+    constexpr int kT = MT * 16, kB = Col::kBlock, kPS = SB ? 1 : 3;
     __shared__ __attribute__((aligned(16))) float lds[2][kT][kB + 4];
     const int k = blockIdx.z, tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const int64_t rows = a.rows[k], n_s = ROWS ? rows : a.classes;
@@ -760,7 +760,7 @@ struct OuterArgs {
 template <bool TB, int KS, bool ROWS, int PG>
 __global__ void __launch_bounds__(256) few_outer_kernel(const OuterArgs a) {
     using Col = Columns<TB>;
-    constexpr int kPT = TB ? 1 : PG;
+    constexpr int kPT = TB ? 1 : 3;
     const int k = blockIdx.z, lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
     const int64_t rows = a.rows[k], n_s = ROWS ? rows : a.classes;
     const int n_t = static_cast<int>(ROWS ? a.classes : rows);
