@@ -230,8 +230,8 @@ struct FewArgs {
     int64_t stride;            // of the workspace, from worker to worker
     int64_t at_pairs, at_own;  // forward, stream of classes: (largest, sum) [row][workgroup]; the label's logit
     int64_t at_side;           // the side as operands: [32 columns][16 rows][piece][lane]
-    int64_t at_g;              // backward: g as operands: [32 rows of the stream][16 of the side][piece][lane]
-    int64_t at_fg;             // f g: [16 rows of the stream][32 of the side][piece][lane]
+    int64_t at_g;              // backward, g and f g as operands, one: [32 rows of the stream][16 of the side][piece][lane]
+    int64_t at_fg;             // the other: [16 rows of the stream][32 of the side][piece][lane]
     int64_t at_f;              // stream of rows: their factors
     int64_t at_db;             // and partial sums of dbias [workgroup][class]
     int64_t at_z;              // sums over a part of the columns [part][workgroup][row of the side][of the stream]
@@ -341,9 +341,9 @@ __device__ __forceinline__ void few_results(const FewArgs& a, int k, int64_t s0,
             if (counts && label >= s0 && label < s0 + kS) reinterpret_cast<float*>(work + a.at_own)[row] = get(static_cast<int>(label - s0));
         }
     } else {
-        // g, stored for the side's gradient (with the factor if its sum runs over
-        // the rows), and f g for the stream's: two elements at a time, as pieces
-        // 1,024 bytes from each other
+        // g with its factor for the gradient that is a sum over the rows, and without
+        // for the other one: two elements at a time, as pieces 1,024 bytes from each
+        // other
         auto store = [&](char* to, int pieces, float g0, float g1) {
             for (int n = 0; n < pieces; ++n) {
                 *reinterpret_cast<uint32_t*>(to + n * 1024) = high_halves(__float_as_uint(g0), __float_as_uint(g1));
@@ -363,13 +363,13 @@ __device__ __forceinline__ void few_results(const FewArgs& a, int k, int64_t s0,
                     const float p = __builtin_amdgcn_exp2f((at_z(t, s + e) - a.lse[k][row]) * kLog2e);
                     g[e] = a.label[k][row] == v ? p - 1.0f : p;
                 }
-                at_z(t, s + e) = g[e] * f;
+                at_z(t, s + e) = ROWS ? g[e] : g[e] * f;
                 if (ROWS) g[e] *= f;
             }
             const int64_t at = s0 + s;
             store(work + a.at_g + (at / 32 * MT + t / 16) * a.pieces_g * 1024 + ((at % 32 / 8) * 16 + t % 16) * 16 + at % 8 * 2, a.pieces_g, g[0], g[1]);
         }
-        if (ROWS && tid < kS && s0 + tid < rows) reinterpret_cast<float*>(work + a.at_f)[s0 + tid] = factors[tid];
+        if (ROWS && tid < kS) reinterpret_cast<float*>(work + a.at_f)[s0 + tid] = factors[tid];
         __syncthreads();
         constexpr int kKs = MT > 2 ? 2 : 1, kSide = kKs * 32;  // rows of the side in f g, with zeros
         for (int n = tid; n < kS * kSide / 2; n += kThreads) {
@@ -383,7 +383,7 @@ __device__ __forceinline__ void few_results(const FewArgs& a, int k, int64_t s0,
         if constexpr (ROWS) {
             if (tid < kT) {
                 float sum = 0.0f;
-                for (int s = 0; s < kS; ++s) sum += at_z(tid, s);
+                for (int s = 0; s < kS; ++s) sum += at_z(tid, s) * factors[s];
                 reinterpret_cast<float*>(work + a.at_db)[static_cast<int64_t>(blockIdx.x) * kShort + tid] = sum;
             }
         } else if (tid < kS && s0 + tid < a.classes) {
@@ -746,7 +746,7 @@ struct OuterArgs {
     void* out[kWorkers];
     int64_t rows[kWorkers];
     char* work;
-    int64_t stride, at_fg;
+    int64_t stride, at_fg, at_f;
     int64_t ld, out_ld;  // elements
     int64_t classes;
     int32_t cols, out_bf, has_dloss, chunk;  // rows of the stream of a workgroup
@@ -796,14 +796,17 @@ __global__ void __launch_bounds__(256) few_outer_kernel(const OuterArgs a) {
     }
     const char* fg = a.work + k * a.stride + a.at_fg + lane * 16;
     const int64_t first = static_cast<int64_t>(blockIdx.y) * a.chunk, end = std::min<int64_t>(first + a.chunk, n_s);
-    struct Factors {
+    const char* f0 = a.work + k * a.stride + a.at_f + lane / 16 * 16;
+    struct Operands {
         Pieces<PG> b[KS];
+        f32x4 f;  // of the lane's rows of a stream of rows
     } now, next;
-    auto fetch = [&](Factors& f, int64_t s) {
+    auto fetch = [&](Operands& f, int64_t s) {
 #pragma unroll
         for (int h = 0; h < KS; ++h)
 #pragma unroll
             for (int p = 0; p < PG; ++p) f.b[h].p[p] = *reinterpret_cast<const u32x4*>(fg + ((s / 16 * KS + h) * PG + p) * 1024);
+        if (ROWS) f.f = *reinterpret_cast<const f32x4*>(f0 + s * 4);
         loads_first();
     };
     if (first >= end) return;
@@ -816,6 +819,7 @@ __global__ void __launch_bounds__(256) few_outer_kernel(const OuterArgs a) {
         for (int q = 0; q < Col::kTiles; ++q)
 #pragma unroll
             for (int h = 0; h < KS; ++h) d[q] = multiply(now.b[h], x[h][q], d[q]);
+        const f32x4 f = now.f;
         now = next;
         // lane: rows lane / 16 * 4 + e of the stream, its columns of the side
 #pragma unroll
@@ -826,7 +830,7 @@ __global__ void __launch_bounds__(256) few_outer_kernel(const OuterArgs a) {
             const int at = c;
             float v[8] = {};
 #pragma unroll
-            for (int q = 0; q < Col::kTiles; ++q) v[q] = d[q][e] * a.scale;
+            for (int q = 0; q < Col::kTiles; ++q) v[q] = !ROWS ? d[q][e] * a.scale : f[e] == 0.0f ? 0.0f : d[q][e] * (f[e] * a.scale);
             if (a.out_bf) {
                 if constexpr (TB) {
                     store_vec<__bf16, true, true>(out, at / 8, cols, v);
@@ -1059,7 +1063,7 @@ hipError_t launch_few(const LossCall& c, const int* list, int count, hipStream_t
         a.at_side = p.at_side;
         a.at_g = m.at_g = p.at_g;
         a.at_fg = o.at_fg = p.at_fg;
-        a.at_f = m.at_f = p.at_f;
+        a.at_f = m.at_f = o.at_f = p.at_f;
         a.at_db = m.at_db = p.at_db;
         a.x_ld = c.x_ld;
         a.classes = m.classes = o.classes = c.classes;
