@@ -26,6 +26,11 @@
 // the pieces' products those under 2^-24 of a term are left out; of g, where the
 // result is rounded to bfloat16, two pieces are taken (16 bits next to 1).
 //
+// The gradients' pieces share one sum, for which the registers are enough: there
+// an operand whose values are all far under one is taken times a power of two
+// (the stream's as long as a wave has seen no larger one, so others' calls do not
+// pay for it), and so are factors.
+//
 // A matrix instruction sums over 32 elements, of which a lane has eight.  For
 // the logits they are neighbours in a row.  For the other two products the sum
 // runs over rows: a lane takes 16 bytes of the same columns of eight rows, and
@@ -160,6 +165,13 @@ __device__ __forceinline__ Pieces<KIND == kF32 ? 3 : 1> pieces(const Eight<KIND>
     }
 }
 
+// Operands of the gradients' products with no value of kSmall or more are taken
+// times kLift, factors with none of kSmallFactor times kLiftFactor: their last
+// pieces would be under bfloat16's values (2^-133) otherwise.
+constexpr float kSmall = 0x1p-90f, kLift = 0x1p100f, kSmallFactor = 0x1p-60f, kLiftFactor = 0x1p64f;
+
+__device__ __forceinline__ bool in_any_lane(bool b) { return __builtin_amdgcn_ballot_w64(b) != 0; }
+
 // The operands of one block of columns from eight rows: one for each of the
 // TILES columns that a lane has, 16 bytes of a row (8 of bfloat16, 4 of
 // binary32) or 8 (4 of bfloat16).  As right operands: the results' rows are the
@@ -191,6 +203,21 @@ struct Columns {
         for (int j = 0; j < 8; ++j)
 #pragma unroll
             for (int i = 0; i < kWords; ++i) v[j][i] = rows >> j & 1 ? v[j][i] : 0u;
+    }
+    // binary32: the lane's largest value; all of them times kLift
+    __device__ __forceinline__ float largest() const {
+        float top = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) top = fmaxf(top, fabsf(__uint_as_float(v[j][i])));
+        return top;
+    }
+    __device__ __forceinline__ void lift() {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) v[j][i] = __float_as_uint(__uint_as_float(v[j][i]) * kLift);
     }
     // column t of the lane's, over the eight rows
     template <int P>
@@ -290,17 +317,28 @@ __global__ void __launch_bounds__(256) few_side_kernel(const FewArgs a, int mt) 
 
 constexpr int kLogitThreads = 512;
 
-// The factors of the rows that a workgroup has (backward).
+// The factors of the rows that a workgroup has (backward), and what f g is held
+// times: of the worker's rows, or of each 32 of a stream of rows, for which the
+// sum over them finds it from the factors alone.
+struct Factors {
+    float f[64], lift[2];
+};
 template <int kS, int MT, bool ROWS>
-__device__ __forceinline__ void few_factors(const FewArgs& a, int k, int64_t s0, float* factors) {
+__device__ __forceinline__ void few_factors(const FewArgs& a, int k, int64_t s0, Factors& factors) {
     constexpr int kT = MT * 16;
     const int tid = threadIdx.x;
     const int64_t rows = a.rows[k];
     const float* dloss = a.has_dloss ? a.dloss[k] : nullptr;
-    if (a.backward && tid < (ROWS ? kS : kT)) {
-        const int64_t row = ROWS ? s0 + tid : tid;
-        factors[tid] = row < rows ? factor_of(a.label[k], dloss, row, a.classes) : 0.0f;
+    if (!a.backward || tid >= 64) return;
+    auto of = [&](int64_t row) { return row < rows ? factor_of(a.label[k], dloss, row, a.classes) : 0.0f; };
+    if (tid < (ROWS ? kS : kT)) factors.f[tid] = of(ROWS ? s0 + tid : tid);
+    float top = 1.0f;
+    if (dloss) {
+        top = fabsf(of(ROWS ? s0 / 32 * 32 + tid : tid));
+#pragma unroll
+        for (int m = ROWS ? 16 : 32; m > 0; m >>= 1) top = fmaxf(top, __shfl_xor(top, m, 64));
     }
+    if (tid % 32 == 0) factors.lift[tid / 32] = top < kSmallFactor ? kLiftFactor : 1.0f;
 }
 
 // A class's bias; classes that are none have -infinity.
@@ -310,7 +348,7 @@ __device__ __forceinline__ float few_bias(const FewArgs& a, int k, int64_t v) {
 
 // What comes of the logits z [row of the side][of the stream].
 template <int kS, int MT, bool ROWS>
-__device__ __forceinline__ void few_results(const FewArgs& a, int k, int64_t s0, float* z, const float* factors) {
+__device__ __forceinline__ void few_results(const FewArgs& a, int k, int64_t s0, float* z, const Factors& factors) {
     constexpr int kThreads = kLogitThreads, kT = MT * 16, kPitch = kS + 4;
     const int tid = threadIdx.x;
     const int64_t rows = a.rows[k];
@@ -357,33 +395,34 @@ __device__ __forceinline__ void few_results(const FewArgs& a, int k, int64_t s0,
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 const int64_t row = ROWS ? s0 + s + e : t, v = ROWS ? t : s0 + s + e;
-                const float f = factors[ROWS ? s + e : t];
+                const float f = factors.f[ROWS ? s + e : t];
                 g[e] = 0.0f;
                 if (f != 0.0f && v < a.classes) {
                     const float p = __builtin_amdgcn_exp2f((at_z(t, s + e) - a.lse[k][row]) * kLog2e);
                     g[e] = a.label[k][row] == v ? p - 1.0f : p;
                 }
                 at_z(t, s + e) = ROWS ? g[e] : g[e] * f;
-                if (ROWS) g[e] *= f;
+                if (ROWS) g[e] *= f * factors.lift[(s0 % 32 + s) / 32];
             }
             const int64_t at = s0 + s;
             store(work + a.at_g + (at / 32 * MT + t / 16) * a.pieces_g * 1024 + ((at % 32 / 8) * 16 + t % 16) * 16 + at % 8 * 2, a.pieces_g, g[0], g[1]);
         }
-        if (ROWS && tid < kS) reinterpret_cast<float*>(work + a.at_f)[s0 + tid] = factors[tid];
+        if (ROWS && tid < kS) reinterpret_cast<float*>(work + a.at_f)[s0 + tid] = factors.f[tid];
         __syncthreads();
         constexpr int kKs = MT > 2 ? 2 : 1, kSide = kKs * 32;  // rows of the side in f g, with zeros
         for (int n = tid; n < kS * kSide / 2; n += kThreads) {
             const int s = n / (kSide / 2), t = n % (kSide / 2) * 2;
             const bool in = t < kT;
+            const float lift = ROWS ? 1.0f : factors.lift[0];
             store(work + a.at_fg + ((s0 + s) / 16 * kKs + t / 32) * a.pieces_fg * 1024 + ((t % 32 / 8) * 16 + s % 16) * 16 + t % 8 * 2,
-                  a.pieces_fg, in ? at_z(in ? t : 0, s) : 0.0f, in ? at_z(in ? t + 1 : 0, s) : 0.0f);
+                  a.pieces_fg, in ? at_z(in ? t : 0, s) * lift : 0.0f, in ? at_z(in ? t + 1 : 0, s) * lift : 0.0f);
         }
         // dbias: sums over the rows
         if (!a.db[k]) return;
         if constexpr (ROWS) {
             if (tid < kT) {
                 float sum = 0.0f;
-                for (int s = 0; s < kS; ++s) sum += at_z(tid, s) * factors[s];
+                for (int s = 0; s < kS; ++s) sum += at_z(tid, s) * factors.f[s];
                 reinterpret_cast<float*>(work + a.at_db)[static_cast<int64_t>(blockIdx.x) * kShort + tid] = sum;
             }
         } else if (tid < kS && s0 + tid < a.classes) {
@@ -404,7 +443,7 @@ __global__ void __launch_bounds__(kLogitThreads) few_logit_kernel(const FewArgs 
     constexpr int kS = CT * 16 * (8 / W), kT = MT * 16;  // rows of the stream and the side
     constexpr int kPitch = kS + 4, PT = TB ? 1 : 3;
     __shared__ __attribute__((aligned(16))) float z[W * kT * kPitch];
-    __shared__ float factors[ROWS ? kS : kT];
+    __shared__ Factors factors;
     const int k = blockIdx.y, tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const int64_t rows = a.rows[k];
     const int64_t n_s = ROWS ? rows : a.classes;
@@ -535,7 +574,7 @@ template <int kS, int MT, bool ROWS>
 __global__ void __launch_bounds__(kLogitThreads) few_rest_kernel(const FewArgs a) {
     constexpr int kT = MT * 16, kPitch = kS + 4;
     __shared__ __attribute__((aligned(16))) float z[kT * kPitch];
-    __shared__ float factors[ROWS ? kS : kT];
+    __shared__ Factors factors;
     const int k = blockIdx.y;
     const int64_t n_s = ROWS ? a.rows[k] : a.classes, s0 = static_cast<int64_t>(blockIdx.x) * kS;
     if (s0 >= (n_s + 63) / 64 * 64) return;
@@ -621,6 +660,7 @@ __global__ void __launch_bounds__(256) few_sum_kernel(const SumArgs a) {
         Col x;
         Pieces<PG> g[MT];
         uint32_t there;
+        float top;  // of the lane's rows' factors
     } st[2];
     const bool whole = c0 + kB <= cols;
     auto fetch = [&](Step& q, int64_t step) {
@@ -637,8 +677,13 @@ __global__ void __launch_bounds__(256) few_sum_kernel(const SumArgs a) {
         if (ROWS) {
             // rows that are left out (g is zero there, and the rows may hold anything)
             q.there = 0;
+            q.top = 0.0f;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) q.there |= f0[std::min(s + j, n_s - 1)] != 0.0f ? 1u << j : 0u;
+            for (int j = 0; j < 8; ++j) {
+                const float f = f0[std::min(s + j, n_s - 1)];
+                q.there |= f != 0.0f ? 1u << j : 0u;
+                q.top = fmaxf(q.top, fabsf(f));
+            }
         }
 #pragma unroll
         for (int m = 0; m < MT; ++m)
@@ -648,14 +693,53 @@ __global__ void __launch_bounds__(256) few_sum_kernel(const SumArgs a) {
         loads_first();
     };
     f32x4 acc[Col::kTiles][MT] = {};
-    auto use = [&](Step& q) {
-        if (ROWS) q.x.keep(q.there);
+    auto times = [&](f32x4 (&v)[Col::kTiles][MT], float by) {
+#pragma unroll
+        for (int t = 0; t < Col::kTiles; ++t)
+#pragma unroll
+            for (int m = 0; m < MT; ++m) v[t][m] *= by;
+    };
+    auto add = [&](const Step& q, f32x4 (&v)[Col::kTiles][MT]) {
 #pragma unroll
         for (int t = 0; t < Col::kTiles; ++t) {
             const Pieces<kPS> x = q.x.template get<kPS>(t);
 #pragma unroll
-            for (int m = 0; m < MT; ++m) acc[t][m] = multiply(q.g[m], x, acc[t][m]);
+            for (int m = 0; m < MT; ++m) v[t][m] = multiply(q.g[m], x, v[t][m]);
         }
+    };
+    // What the sums are times kLift, or kLiftFactor: until a larger value, or a
+    // larger factor, comes.
+    bool small = !SB, small_factors = ROWS && a.has_dloss;
+    auto use = [&](Step& q) {
+        if (ROWS) q.x.keep(q.there);
+        if constexpr (!SB)
+            if (small) {
+                if (in_any_lane(q.x.largest() >= kSmall)) {
+                    small = false;
+                    times(acc, 1.0f / kLift);
+                } else {
+                    q.x.lift();
+                }
+            }
+        if constexpr (ROWS)
+            if (a.has_dloss && in_any_lane(q.there != 0)) {
+                const bool lifted = !in_any_lane(q.top >= kSmallFactor);
+                if (lifted && !small_factors) {
+                    f32x4 own[Col::kTiles][MT] = {};
+                    add(q, own);
+                    times(own, 1.0f / kLiftFactor);
+#pragma unroll
+                    for (int t = 0; t < Col::kTiles; ++t)
+#pragma unroll
+                        for (int m = 0; m < MT; ++m) acc[t][m] += own[t][m];
+                    return;
+                }
+                if (small_factors && !lifted) {
+                    small_factors = false;
+                    times(acc, 1.0f / kLiftFactor);
+                }
+            }
+        add(q, acc);
     };
     // (past the last step it is loaded again: were the loads left out, the counts
     // of loads under way would differ, and all would be waited for)
@@ -673,6 +757,8 @@ __global__ void __launch_bounds__(256) few_sum_kernel(const SumArgs a) {
             at += 8;
         }
     }
+    if (small) times(acc, 1.0f / kLift);
+    if (small_factors) times(acc, 1.0f / kLiftFactor);
     // the four waves' sums, two at a time
     auto place = [&](int half, int m, int e) -> float* { return &lds[half][m * 16 + lane / 16 * 4 + e][lane % 16 * Col::kTiles]; };
 #pragma unroll
@@ -770,9 +856,11 @@ __global__ void __launch_bounds__(256) few_outer_kernel(const OuterArgs a) {
     const uintptr_t side = reinterpret_cast<uintptr_t>(a.side[k]);
     const int64_t t_ld = a.ld * (TB ? 2 : 4);
     Pieces<kPT> x[KS][Col::kTiles];
+    Col block[KS];
+    float top = 0.0f;  // of the factors
 #pragma unroll
     for (int h = 0; h < KS; ++h) {
-        Col v;
+        Col& v = block[h];
         auto fetch = [&](auto whole) {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
@@ -787,13 +875,29 @@ __global__ void __launch_bounds__(256) few_outer_kernel(const OuterArgs a) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int r = h * 32 + lane / 16 * 8 + j;
-                if (r < n_t && factor_of(a.label[k], a.has_dloss ? a.dloss[k] : nullptr, r, a.classes) != 0.0f) there |= 1u << j;
+                const float f = r < n_t ? factor_of(a.label[k], a.has_dloss ? a.dloss[k] : nullptr, r, a.classes) : 0.0f;
+                if (f != 0.0f) there |= 1u << j;
+                top = fmaxf(top, fabsf(f));
             }
             v.keep(there);
         }
-#pragma unroll
-        for (int q = 0; q < Col::kTiles; ++q) x[h][q] = v.template get<kPT>(q);
     }
+    // what the results are times
+    bool small = false;
+    if constexpr (!TB) {
+        float largest = 0.0f;
+#pragma unroll
+        for (int h = 0; h < KS; ++h) largest = fmaxf(largest, block[h].largest());
+        small = !in_any_lane(largest >= kSmall);
+        if (small)
+#pragma unroll
+            for (int h = 0; h < KS; ++h) block[h].lift();
+    }
+    const bool small_factors = !ROWS && a.has_dloss && !in_any_lane(top >= kSmallFactor);
+#pragma unroll
+    for (int h = 0; h < KS; ++h)
+#pragma unroll
+        for (int q = 0; q < Col::kTiles; ++q) x[h][q] = block[h].template get<kPT>(q);
     const char* fg = a.work + k * a.stride + a.at_fg + lane * 16;
     const int64_t first = static_cast<int64_t>(blockIdx.y) * a.chunk, end = std::min<int64_t>(first + a.chunk, n_s);
     const char* f0 = a.work + k * a.stride + a.at_f + lane / 16 * 16;
@@ -819,6 +923,9 @@ __global__ void __launch_bounds__(256) few_outer_kernel(const OuterArgs a) {
         for (int q = 0; q < Col::kTiles; ++q)
 #pragma unroll
             for (int h = 0; h < KS; ++h) d[q] = multiply(now.b[h], x[h][q], d[q]);
+        if (small || small_factors)
+#pragma unroll
+            for (int q = 0; q < Col::kTiles; ++q) d[q] = d[q] * (small ? 1.0f / kLift : 1.0f) * (small_factors ? 1.0f / kLiftFactor : 1.0f);
         const f32x4 f = now.f;
         now = next;
         // lane: rows lane / 16 * 4 + e of the stream, its columns of the side
