@@ -751,17 +751,22 @@ int32_t check_vectors(int32_t K, const int64_t* rows, const void* const* p, int 
 
 // The rows' memory belongs to the current device, whose stream the call's work
 // goes to (calls without a group have no device of their own to compare).
-int32_t check_row_device(int32_t K, const int64_t* rows, const void* const* p, const char* name) {
+// dweight: what is written of workers without rows, if anything is.
+int32_t check_row_device(int32_t K, const int64_t* rows, const void* const* p, const char* name,
+                         const void* const* dweight = nullptr) {
     int dev = -1;
     if (hipError_t e = hipGetDevice(&dev)) return hip_fail(e, "hipGetDevice");
-    for (int32_t k = 0; k < K; ++k) {
-        if (rows[k] == 0) continue;
-        hipPointerAttribute_t at{};
-        if (hipPointerGetAttributes(&at, p[k]) != hipSuccess) {
-            (void)hipGetLastError();  // not the runtime's memory: nothing is known of it
-        } else if (at.type == hipMemoryTypeDevice && at.device != dev) {
-            set_error("%s[%d] is on device %d but device %d is current", name, k, at.device, dev);
-            return TC_EINVAL;
+    for (const bool with : {true, false}) {
+        const void* const* at_k = with ? p : dweight;
+        for (int32_t k = 0; k < K && at_k; ++k) {
+            if ((rows[k] > 0) != with) continue;
+            hipPointerAttribute_t at{};
+            if (hipPointerGetAttributes(&at, at_k[k]) != hipSuccess) {
+                (void)hipGetLastError();  // not the runtime's memory: nothing is known of it
+            } else if (at.type == hipMemoryTypeDevice && at.device != dev) {
+                set_error("%s[%d] is on device %d but device %d is current", with ? name : "dweight", k, at.device, dev);
+                return TC_EINVAL;
+            }
         }
     }
     return TC_OK;
@@ -860,7 +865,7 @@ TC_API int32_t tc_layernorm_backward(int32_t K, const int64_t* rows, int64_t col
     }
     spans.add(workspace, need, "workspace", 0, true);
     if (int32_t r = spans.check()) return r;
-    if (int32_t r = check_row_device(K, rows, x, "x")) return r;
+    if (int32_t r = check_row_device(K, rows, x, "x", const_cast<const void* const*>(dweight))) return r;
     hipError_t e = launch_layernorm_backward(K, rows, cols, dy, dy_ld, x, x_ld, dtype, weight, mean, rstd, dx, dx_ld,
                                              dweight, dbias, w_dtype, workspace, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, "tc_layernorm_backward launch");
@@ -990,7 +995,7 @@ int32_t run_loss(LossCall& c, int64_t workspace_bytes, void* stream, const char*
     }
     spans.add(c.workspace, need, "workspace", 0, true);
     if (int32_t r = spans.check()) return r;
-    if (int32_t r = check_row_device(K, rows, c.x, "x")) return r;
+    if (int32_t r = check_row_device(K, rows, c.x, "x", const_cast<const void* const*>(c.dweight))) return r;
     hipError_t e = launch_cross_entropy(c, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return hip_fail(e, name);
     return TC_OK;
