@@ -58,7 +58,7 @@ for call in json.load(sys.stdin):
     rows, cols, K = call["rows"], call["cols"], len(call["rows"])
     counts = (ctypes.c_int64 * K)(*rows)
     at = iter(range(1, 1 << 20))
-    each = lambda: (ctypes.c_void_p * K)(*[next(at) << 40 for _ in rows])
+    each = lambda: (ctypes.c_void_p * K)(*[next(at) << (52 if call["op"] == "dropout" else 40) for _ in rows])
     types = ("f32", "bf16")
     x, w, dw = [i(types.index(call[n])) for n in ("x", "w", "dw")]
     if call["op"] in ("ce", "ce_grad"):
@@ -76,7 +76,7 @@ for call in json.load(sys.stdin):
     else:
         need = 0
         residual = each() if call["residual"] else None
-        ld = l((cols + 15) // 16 * 16)
+        ld = l(cols + call["pad"])
         args = (i(K), counts, l(cols), each(), ld, x, residual, ld, each(), ld, f(0.5), p(1 << 60), l(0), None)
         status = lambda: L.tc_dropout(*args)
     runtime.start()
@@ -96,9 +96,9 @@ class Launch:
         return all(0 < g and g * t < 1 << 32 for g, t in zip(self.grid, self.block)) and max(self.grid[1:]) <= 65535
 
 
-def call(op, rows, cols, classes=0, x="f32", w="f32", dw="f32", bias=True, weighted=False, residual=False):
+def call(op, rows, cols, classes=0, x="f32", w="f32", dw="f32", bias=True, weighted=False, residual=False, pad=0):
     return {"op": op, "rows": list(rows), "cols": cols, "classes": classes, "x": x, "w": w, "dw": dw, "bias": bias, "weighted": weighted,
-            "residual": residual}
+            "residual": residual, "pad": pad}
 
 
 def launches(tmp_path, calls):
