@@ -485,7 +485,8 @@ int32_t tc_dropout_backward(int32_t K, const int64_t* rows, int64_t cols, const 
  * integers.  loss, lse: K device pointers to rows[k] binary32 values that
  * receive the rows' losses and logs of sums (the backward pass needs them).
  * Binary32 operands are taken with 22 bits or more next to the operand's
- * largest value, products are summed and exponentials taken in binary32.  The
+ * largest value, products are summed and exponentials taken in binary32 (a
+ * logit is finite if the sizes of its terms add up to less than 2^125).  The
  * same inputs give the same bits.  loss, lse and the workspace share no byte
  * with each other or with what is read.  A worker without rows needs no
  * pointers.  The rows are on the current device.  cols in [1, TC_MAX_CE_COLS],
@@ -526,10 +527,12 @@ int64_t tc_cross_entropy_backward_workspace(int32_t K, const int64_t* rows, int6
  * dx: rows of dtype every dx_ld elements; dx[k] may be x[k] itself (with the
  * same stride).  dweight (classes x cols), dbias: K device pointers to values
  * of dw_dtype, at any alignment of the type (pieces of a flat gradient buffer);
- * dbias NULL: not wanted.  Sums are kept in binary32, g is held with 11 bits
- * next to 1 (22 where the result it goes to is binary32) or more, for dweight
- * f g next to the worker's largest |f|, and results are rounded once.  The same
- * inputs give the same bits.  workspace: at least
+ * dbias NULL: not wanted.  Operands are held as above, whatever the results'
+ * type, and sums are kept in binary32.  g is held with 11 bits next to 1 (22
+ * where the result it goes to is binary32) or more, in steps of at most 2^-37;
+ * for dweight f g alike next to the worker's largest |f| (dweight of a class
+ * that all rows give less than 2^-38 may be zero).  Results are rounded once.
+ * The same inputs give the same bits.  workspace: at least
  * tc_cross_entropy_backward_workspace bytes, 256-byte aligned, that nothing
  * else uses until the call's work is done.  dx apart from the above, dweight,
  * dbias and the workspace share no byte with each other or with what is

@@ -10,8 +10,8 @@
 //
 // Bound by memory: x (and the residual) read once, y written once.  A counter's
 // 20 products of 32 bits go to the vector units while the loads are under way.
-// Eight workers' 4,096 x 4,096 bfloat16: 82 us, 6.5 TB/s, what the library's own
-// copy reaches; with the residual 143 us, 5.6 TB/s.
+// Eight workers' 4,096 x 4,096 bfloat16: 82 to 96 us from run to run, 6.5 to 5.6
+// TB/s (the library's own copy reaches 6.5); with the residual 143 us, 5.6 TB/s.
 #include "tc_lane.h"
 
 namespace tc {
@@ -181,8 +181,8 @@ hipError_t launch_dropout(int K, const int64_t* rows, int64_t cols, const void* 
         }
         if (a.wg[a.K] == 0) continue;
         // What the last-level cache (256 MB) does not hold passes it by, if rows
-        // are whole 16 bytes: 8 x 4,096 x 4,096 bfloat16 100 -> 82 us, with the
-        // residual 147 -> 143; at other addresses it takes longer (30,000 x 4,003
+        // are whole 16 bytes (in turn, 8 x 4,096 x 4,096 bfloat16 100 -> 83 us, with
+        // the residual 147 -> 143); at other addresses it takes longer (30,000 x 4,003
         // float 182 -> 187).
         bool nt = total * 8 * es * (r ? 3 : 2) > int64_t{256} << 20 && (a.x_ld | a.y_ld | a.r_ld) % 16 == 0;
         for (int k = 0; k < a.K; ++k)

@@ -49,7 +49,12 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kWorkers = 16;  // of one launch
 constexpr int kShort = 64;    // rows of the short side
-constexpr int kTurn = 5;      // steps from one workgroup's beginning to the next one's
+// Steps from one workgroup's beginning to the next one's: odd, so that neighbours
+// are at different halves of 64 columns too, and far enough for the memory's
+// channels (8 rows of 4,096 over 131,072 classes in bfloat16 with 0, 1, 2, 5, 8,
+// 32 steps: 261, 221, 312, 218, 257, 262 us; 16 of 8,192 over 32,000 155, 120, 118,
+// 116, 191, 155; 5 of 4,096 over 32,000 in binary32 119, 111, 154, 102, 105, 119).
+constexpr int kTurn = 5;
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 // --------------------------------------------------------------------- operands
