@@ -6,6 +6,7 @@ GPU, that these sizes take these kernels."""
 import pytest
 import torch
 
+import paper_1801_03855_amd as tc
 from tests.loss_tiles import TILES
 from tests.test_gpu_loss import Case, check_backward, check_forward
 
@@ -51,3 +52,68 @@ def test_pairs_joined_several_times(rows, cols, classes, x):
     c.rows = [len(some)]
     c.x, c.label, c.loss, c.lse = [[t[0][some]] for t in (c.x, c.label, c.loss, c.lse)]
     check_forward(c)
+
+
+LARGE = [([2100, 700], 1701, 8201, "bf16", "f32", "f32"), ([2050], 3301, 8193, "bf16", "bf16", "bf16"), ([2100], 1700, 8200, "f32", "f32", "f32")]
+
+
+@pytest.mark.parametrize("rows,cols,classes,x,w,dw", LARGE, ids=str)
+def test_what_is_left_out_may_hold_anything(rows, cols, classes, x, w, dw):
+    results = []
+    for bad in (0.0, float("nan"), float("inf"), 3e38):
+        c = Case(rows, cols, classes, TYPES[x], TYPES[w], TYPES[dw], bias=True, weighted=True, seed=33)
+        for t, label, dloss in zip(c.x, c.label, c.dloss):
+            label[1], label[300], dloss[257] = -1, classes, 0.0
+            dloss[1] = float("nan")
+            for r in (1, 257, 300):
+                t[r] = bad
+        c.forward()
+        c.backward()
+        torch.cuda.synchronize()
+        out = [r for r in range(rows[0]) if r not in (1, 257, 300)]
+        for k in range(len(rows)):
+            assert not c.dx[k][[1, 257, 300]].any()
+        results.append([c.loss[0][out], c.lse[0][out]] + c.dx + c.dw + c.db)
+    for other in results[1:]:
+        for a, b in zip(results[0], other):
+            assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("rows,cols,classes,x,w,dw", LARGE + [([4000], 3301, 40001, "f32", "f32", "f32")], ids=str)
+def test_dx_in_the_place_of_x(rows, cols, classes, x, w, dw):
+    c = Case(rows, cols, classes, TYPES[x], TYPES[w], TYPES[dw], bias=True, seed=34)
+    c.forward()
+    c.backward()
+    torch.cuda.synchronize()
+    want = [t.clone() for t in c.dx + c.dw + c.db]
+    c.dx = c.x
+    c.backward()
+    torch.cuda.synchronize()
+    for a, b in zip(want, c.x + c.dw + c.db):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("rows,cols,classes,x,w,dw", LARGE + [([4096, 17], 4100, 33201, "bf16", "bf16", "bf16"), ([70000], 67, 70001, "bf16", "f32", "bf16")], ids=str)
+def test_replayed_graphs(rows, cols, classes, x, w, dw):
+    """Replays over a workspace that the program has written in between."""
+    c = Case(rows, cols, classes, TYPES[x], TYPES[w], TYPES[dw], bias=True, weighted=True, seed=35)
+    types = TYPES[x], TYPES[w]
+    need = max(tc.cross_entropy_workspace(rows, cols, classes, *types), tc.cross_entropy_backward_workspace(rows, cols, classes, *types, TYPES[dw]))
+    ws = torch.full((need,), 255, dtype=torch.uint8, device="cuda")
+    c.forward(workspace=ws)
+    c.backward(workspace=ws)
+    torch.cuda.synchronize()
+    want = [t.clone() for t in c.outputs()]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c.forward(workspace=ws)
+        c.backward(workspace=ws)
+    for _ in range(3):
+        for t in c.outputs():
+            t.fill_(7.0)
+        ws.random_(0, 255)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(want, c.outputs()):
+            assert torch.equal(a, b)
